@@ -10,8 +10,10 @@ there is no fallback.
 
 from __future__ import annotations
 
+import contextlib
 import ctypes
 import os
+from typing import NamedTuple
 
 PKG = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(PKG, "libreshard.so")
@@ -28,7 +30,8 @@ RESHARD_NO_GATHER = 0x100
 RESHARD_MAX_BUFFERS = 496
 
 _DTYPES = {"uint8": 0, "int8": 1, "float16": 2, "bfloat16": 3, "float32": 4, "int32": 5,
-           "float64": 6, "int64": 7, "uint16": 8, "int16": 9, "uint32": 10, "uint64": 11}
+           "float64": 6, "int64": 7, "uint16": 8, "int16": 9, "uint32": 10, "uint64": 11,
+           "float8_e4m3fn": 12, "float8_e8m0fnu": 13}
 
 _STATUS = {RESHARD_EINVAL: "EINVAL", RESHARD_EUNSUPPORTED: "EUNSUPPORTED",
            RESHARD_ENOMEM: "ENOMEM", RESHARD_EHIP: "EHIP"}
@@ -116,6 +119,8 @@ def load(path=None):
                                               ctypes.c_double, ctypes.c_double, ctypes.c_double, ctypes.c_int32,
                                               ctypes.POINTER(ctypes.c_double), ctypes.POINTER(ctypes.c_int32)]
     lib.reshard_pipeline_simulate.restype = ctypes.c_int
+    if hasattr(lib, "reshard_matmul"):  # the planner built by itself, without GPU code, lacks the operators
+        _declare_operators(lib)
     lib.reshard_last_error.argtypes = []
     lib.reshard_last_error.restype = ctypes.c_char_p
     lib.reshard_version.argtypes = []
@@ -123,6 +128,23 @@ def load(path=None):
     if path == LIB_PATH:
         _lib = lib
     return lib
+
+
+def _declare_operators(lib):
+    i64, vp, ci, fp = ctypes.c_int64, ctypes.c_void_p, ctypes.c_int, ctypes.c_void_p
+    lib.reshard_layer_norm.argtypes = [i64, i64, vp, i64, ci, vp, vp, ci, ctypes.c_double, vp, i64, fp, fp, vp]
+    lib.reshard_layer_norm_backward_workspace.argtypes = [i64, i64]
+    lib.reshard_layer_norm_backward_workspace.restype = i64
+    lib.reshard_layer_norm_backward.argtypes = [i64, i64, vp, i64, vp, i64, ci, vp, ci, fp, fp, vp, i64, fp, fp, ci,
+                                                vp, i64, vp]
+    lib.reshard_quantize.argtypes = [i64, i64, vp, i64, ci, ci, ci, vp, i64, vp, i64, vp, i64, vp, i64, vp]
+    lib.reshard_dequantize.argtypes = [i64, i64, vp, i64, ci, vp, i64, ci, vp, i64, ci, vp]
+    lib.reshard_matmul_workspace.argtypes = [i64, i64, i64]
+    lib.reshard_matmul_workspace.restype = i64
+    lib.reshard_matmul.argtypes = [i64, i64, i64, vp, i64, ci, vp, i64, vp, i64, ci, vp, i64, ci, vp, i64, ci, ci,
+                                   vp, i64, vp]
+    for f in ("layer_norm", "layer_norm_backward", "quantize", "dequantize", "matmul"):
+        getattr(lib, "reshard_" + f).restype = ctypes.c_int
 
 
 def _check(status):
@@ -364,6 +386,217 @@ def reshard_pipeline_simulate(stages, microbatches, eager, t_fwd, t_bwd, t_comm_
                                             float(t_comm_fwd if t_comm_bwd is None else t_comm_bwd),
                                             int(bool(serial_links)), ctypes.byref(lat), peak))
     return lat.value, list(peak[:int(stages)])
+
+
+# ------------------------------------------- operators at a stage's edge
+
+class Blocked(NamedTuple):
+    """A matrix in 8 bits with a scale per block of 128 columns.
+
+    data: float8_e4m3fn [..., cols]; scales: float8_e8m0fnu or float32
+    [ceil(rows / block_rows), ceil(cols / 128)]; block_rows: 1 or 128.  Both
+    tensors reshard like any other (a plan on each)."""
+    data: object
+    scales: object
+    block_rows: int = 1
+
+
+def _matrix(name, t):
+    """(rows, cols, pitch) of a tensor whose leading dimensions step evenly and whose last is dense."""
+    shape, strides = t.shape, t.stride()
+    if not shape:
+        raise ValueError(f"{name} needs at least one dimension")
+    cols = shape[-1]
+    if cols > 1 and strides[-1] != 1:
+        raise ValueError(f"{name}: the last dimension must be dense, its stride is {strides[-1]}")
+    if len(shape) == 2:
+        return shape[0], cols, strides[0]
+    rows, pitch = 1, None
+    for n, s in zip(reversed(shape[:-1]), reversed(strides[:-1])):
+        if n != 1:
+            if pitch is None:
+                pitch = s
+            elif s != rows * pitch:
+                raise ValueError(f"{name}: the leading dimensions do not step evenly from row to row")
+        rows *= n
+    return rows, cols, cols if pitch is None else pitch
+
+
+def _like(name, t, shape, dtype, device):
+    """A caller's output or statistic: the shape, type and device it must have."""
+    if tuple(t.shape) != tuple(shape) or t.dtype != dtype or t.device != device:
+        raise ValueError(f"{name} must be {dtype} {tuple(shape)} on {device}, "
+                         f"got {t.dtype} {tuple(t.shape)} on {t.device}")
+    return t
+
+
+def _dense(name, t, shape, device, dtype=None):
+    _like(name, t, shape, dtype or t.dtype, device)
+    if not t.is_contiguous():
+        raise ValueError(f"{name} must be dense")
+    return t
+
+
+def _on(stream):
+    """Memory that a call takes comes from the pool of the stream it runs on."""
+    if stream is None:
+        return contextlib.nullcontext()
+    import torch
+    return torch.cuda.stream(torch.cuda.ExternalStream(stream) if isinstance(stream, int) else stream)
+
+
+def _ptr(t):
+    return None if t is None else t.data_ptr()
+
+
+def reshard_layer_norm(x, weight=None, bias=None, eps=1e-5, out=None, stream=None):
+    """(y, mean, rstd): layer norm over x's last dimension; mean and rstd (float32) are for the backward pass."""
+    import torch
+    lib = _lib or load()
+    rows, cols, pitch = _matrix("x", x)
+    wdt = (weight if weight is not None else bias if bias is not None else x).dtype
+    for name, w in (("weight", weight), ("bias", bias)):
+        if w is not None:
+            _dense(name, w, (cols,), x.device, wdt)
+    with _on(stream):
+        y = torch.empty(x.shape, dtype=x.dtype, device=x.device) if out is None else \
+            _like("out", out, x.shape, x.dtype, x.device)
+        stats = torch.empty((2, *x.shape[:-1]), dtype=torch.float32, device=x.device)
+    mean, rstd = stats.unbind(0)
+    _check(lib.reshard_layer_norm(rows, cols, x.data_ptr(), pitch, _dtype_code(x.dtype), _ptr(weight), _ptr(bias),
+                                  _dtype_code(wdt), eps, y.data_ptr(), _matrix("out", y)[2], mean.data_ptr(),
+                                  rstd.data_ptr(), _stream_handle(stream)))
+    return y, mean, rstd
+
+
+def reshard_layer_norm_backward(dy, x, weight, mean, rstd, dweight=None, dbias=None, accumulate=False, out=None,
+                                stream=None):
+    """(dx, dweight, dbias) of reshard_layer_norm.  dweight and dbias are
+    float32; given ones are overwritten, or added to with accumulate."""
+    import torch
+    lib = _lib or load()
+    rows, cols, pitch = _matrix("x", x)
+    _like("dy", dy, x.shape, x.dtype, x.device)
+    if weight is not None:
+        _dense("weight", weight, (cols,), x.device)
+    for name, s in (("mean", mean), ("rstd", rstd)):
+        _dense(name, s, x.shape[:-1], x.device, torch.float32)
+    if accumulate and (dweight is None or dbias is None):
+        raise ValueError("accumulate needs the dweight and dbias to add to")
+    need = lib.reshard_layer_norm_backward_workspace(rows, cols)
+    with _on(stream):
+        dx = torch.empty(x.shape, dtype=x.dtype, device=x.device) if out is None else \
+            _like("out", out, x.shape, x.dtype, x.device)
+        if dweight is None:
+            dweight = torch.empty(cols, dtype=torch.float32, device=x.device)
+        if dbias is None:
+            dbias = torch.empty(cols, dtype=torch.float32, device=x.device)
+        work = torch.empty(max(0, need), dtype=torch.uint8, device=x.device)
+    for name, d in (("dweight", dweight), ("dbias", dbias)):
+        _dense(name, d, (cols,), x.device, torch.float32)
+    _check(lib.reshard_layer_norm_backward(
+        rows, cols, dy.data_ptr(), _matrix("dy", dy)[2], x.data_ptr(), pitch, _dtype_code(x.dtype), _ptr(weight),
+        _dtype_code(x.dtype if weight is None else weight.dtype), mean.data_ptr(), rstd.data_ptr(), dx.data_ptr(),
+        _matrix("out", dx)[2], dweight.data_ptr(), dbias.data_ptr(), int(accumulate), work.data_ptr(), need,
+        _stream_handle(stream)))
+    return dx, dweight, dbias
+
+
+_E4M3, _BLOCK = "float8_e4m3fn", 128
+
+
+def _empty_blocked(rows, cols, block_rows, scale_dtype, device):
+    """Codes whose rows are padded to whole blocks, so that each starts on a 16-byte boundary."""
+    import torch
+    across = -(-cols // _BLOCK)
+    data = torch.empty((rows, across * _BLOCK), dtype=torch.float8_e4m3fn, device=device)[:, :cols]
+    scales = torch.empty((-(-rows // block_rows), across), dtype=scale_dtype, device=device)
+    return Blocked(data, scales, block_rows)
+
+
+def _blocked(name, b):
+    """(rows, cols, pitch, scales' pitch) of a Blocked."""
+    rows, cols, pitch = _matrix(f"{name}.data", b.data)
+    if str(b.data.dtype) != "torch." + _E4M3:
+        raise ValueError(f"{name}.data must be {_E4M3}, got {b.data.dtype}")
+    if b.block_rows not in (1, _BLOCK):
+        raise ValueError(f"{name}.block_rows must be 1 or {_BLOCK}, got {b.block_rows}")
+    srows, scols, spitch = _matrix(f"{name}.scales", b.scales)
+    if (srows, scols) != (-(-rows // b.block_rows), -(-cols // _BLOCK)):
+        raise ValueError(f"{name}.scales must be {(-(-rows // b.block_rows), -(-cols // _BLOCK))}, "
+                         f"got {(srows, scols)}")
+    if b.scales.device != b.data.device:
+        raise ValueError(f"{name}.scales are on {b.scales.device}, its data on {b.data.device}")
+    return rows, cols, pitch, spitch
+
+
+def reshard_quantize(x, block_rows=1, transposed=False, scale_dtype=None, stream=None):
+    """x in 8 bits with a power-of-two scale per block (Blocked, rows of x's
+    leading dimensions together).  transposed=True: of x transposed, blocks
+    along x's rows; "both": the pair, from one reading of x.  scale_dtype:
+    torch.float8_e8m0fnu (default) or torch.float32."""
+    import torch
+    lib = _lib or load()
+    rows, cols, pitch = _matrix("x", x)
+    if transposed not in (False, True, "both"):
+        raise ValueError(f'transposed must be False, True or "both", got {transposed!r}')
+    if block_rows not in (1, _BLOCK):
+        raise ValueError(f"block_rows must be 1 or {_BLOCK}, got {block_rows}")
+    if scale_dtype is None:
+        scale_dtype = torch.float8_e8m0fnu
+    with _on(stream):
+        q = None if transposed is True else _empty_blocked(rows, cols, block_rows, scale_dtype, x.device)
+        t = None if transposed is False else _empty_blocked(cols, rows, block_rows, scale_dtype, x.device)
+    args = []
+    for b in (q, t):
+        args += [None, 0, None, 0] if b is None else [b.data.data_ptr(), b.data.stride(0), b.scales.data_ptr(),
+                                                      b.scales.stride(0)]
+    _check(lib.reshard_quantize(rows, cols, x.data_ptr(), pitch, _dtype_code(x.dtype), block_rows,
+                                _dtype_code(scale_dtype), *args, _stream_handle(stream)))
+    return (q, t) if transposed == "both" else q if t is None else t
+
+
+def reshard_dequantize(b, dtype, out=None, stream=None):
+    """The values of a Blocked, rounded once to dtype (torch.float16, bfloat16 or float32)."""
+    import torch
+    lib = _lib or load()
+    rows, cols, pitch, spitch = _blocked("b", b)
+    with _on(stream):
+        y = torch.empty(b.data.shape, dtype=dtype, device=b.data.device) if out is None else \
+            _like("out", out, b.data.shape, dtype, b.data.device)
+    _check(lib.reshard_dequantize(rows, cols, b.data.data_ptr(), pitch, b.block_rows, b.scales.data_ptr(), spitch,
+                                  _dtype_code(b.scales.dtype), y.data_ptr(), _matrix("out", y)[2],
+                                  _dtype_code(dtype), _stream_handle(stream)))
+    return y
+
+
+def reshard_matmul(a, b, out_dtype=None, out=None, accumulate=False, stream=None):
+    """a [..., k] times b [n, k] transposed, both Blocked with scales of one
+    type; [..., n] of out_dtype (default torch.bfloat16), or into `out`, added
+    to what is there with accumulate."""
+    import torch
+    lib = _lib or load()
+    m, k, a_pitch, a_spitch = _blocked("a", a)
+    n, kb, b_pitch, b_spitch = _blocked("b", b)
+    if k != kb:
+        raise ValueError(f"a has {k} columns and b {kb}")
+    if a.scales.dtype != b.scales.dtype:
+        raise ValueError(f"a's scales are {a.scales.dtype}, b's {b.scales.dtype}")
+    if a.data.device != b.data.device:
+        raise ValueError(f"a is on {a.data.device}, b on {b.data.device}")
+    if accumulate and out is None:
+        raise ValueError("accumulate needs the out to add to")
+    shape = (*a.data.shape[:-1], n)
+    need = lib.reshard_matmul_workspace(m, n, k)
+    with _on(stream):
+        y = torch.empty(shape, dtype=out_dtype or torch.bfloat16, device=a.data.device) if out is None else \
+            _like("out", out, shape, out_dtype or out.dtype, a.data.device)
+        work = torch.empty(need, dtype=torch.uint8, device=a.data.device) if need > 0 else None
+    _check(lib.reshard_matmul(m, n, k, a.data.data_ptr(), a_pitch, a.block_rows, a.scales.data_ptr(), a_spitch,
+                              b.data.data_ptr(), b_pitch, b.block_rows, b.scales.data_ptr(), b_spitch,
+                              _dtype_code(a.scales.dtype), y.data_ptr(), _matrix("out", y)[2], _dtype_code(y.dtype),
+                              int(accumulate), _ptr(work), max(0, need), _stream_handle(stream)))
+    return y
 
 
 def reshard_last_error():

@@ -25,7 +25,7 @@ COMMON = ["-O3", "-fPIC", "-std=c++17", "-Wall", "-Wextra", "-Wno-unused-paramet
 # packed-fp32 instructions are disabled for all device code
 HIP_FLAGS = [f"--offload-arch={ARCH}", "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops"]
 HOST_SOURCES = ["planner.cpp", "capi.cpp", "schedule.cpp", "pipeline.cpp"]
-HIP_SOURCES = ["execute.hip"]
+HIP_SOURCES = ["execute.hip", "norm.hip", "quantize.hip", "matmul.hip"]
 
 
 def _run(cmd, verbose):

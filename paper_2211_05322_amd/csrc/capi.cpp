@@ -41,7 +41,7 @@ namespace {
 
 int64_t elem_size(reshard_dtype_t dt) {
     switch (dt) {
-        case RESHARD_U8: case RESHARD_I8: return 1;
+        case RESHARD_U8: case RESHARD_I8: case RESHARD_E4M3: case RESHARD_E8M0: return 1;
         case RESHARD_F16: case RESHARD_BF16: case RESHARD_U16: case RESHARD_I16: return 2;
         case RESHARD_F32: case RESHARD_I32: case RESHARD_U32: return 4;
         case RESHARD_F64: case RESHARD_I64: case RESHARD_U64: return 8;

@@ -1,0 +1,475 @@
+// norm.hip -- layer norm of rows and its gradients.
+//
+//   mean = sum_c x / C      rstd = 1 / sqrt(sum_c (x - mean)^2 / C + eps)
+//   xhat = (x - mean) rstd  y = xhat w + b
+//   g = dy w                dx = rstd (g - mean_c(g) - xhat mean_c(g xhat))
+//   dw = sum_r dy xhat      db = sum_r dy
+//
+// Both are bound by memory: the forward pass reads and writes each element
+// once, the backward pass reads two and writes one.  A row's elements stay in
+// registers between the reductions and the result, so the second moment is
+// taken about the mean (no cancellation) without a second read.
+#include <algorithm>
+
+#include "operators.hpp"
+
+namespace rs {
+namespace {
+
+// Sum of N values over the THREADS threads that share a row: a wave by
+// shuffles; more waves through `part`, which every call site owns a part of.
+template <int THREADS, int N>
+__device__ inline void row_sum(float (&v)[N], float *part) {
+#pragma unroll
+    for (int i = 0; i < N; ++i) v[i] = wave_sum(v[i]);
+    if constexpr (THREADS > kWave) {
+        constexpr int W = THREADS / kWave;
+        const int wave = threadIdx.x / kWave;
+        if (threadIdx.x % kWave == 0) {
+#pragma unroll
+            for (int i = 0; i < N; ++i) part[i * W + wave] = v[i];
+        }
+        __syncthreads();
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+            float s = 0;
+#pragma unroll
+            for (int w = 0; w < W; ++w) s += part[i * W + w];
+            v[i] = s;
+        }
+    }
+}
+
+struct NormArgs {
+    const void *x, *weight, *bias;
+    void *y;
+    float *mean, *rstd;
+    int64_t rows, cols, x_pitch, y_pitch;
+    float eps;
+    int weight_dtype;
+};
+
+// THREADS threads hold a row, NV vectors each; 256 / THREADS rows a workgroup
+// where a wave holds one.
+template <typename T, int THREADS, int NV>
+__global__ __launch_bounds__(THREADS < 256 ? 256 : THREADS) void norm_kernel(NormArgs a) {
+    constexpr int ROWS = THREADS < 256 ? 256 / THREADS : 1;
+    constexpr int V = kVec<T>;
+    __shared__ float part[2][THREADS / kWave];
+    const int t = threadIdx.x % THREADS;
+    const float cols = float(a.cols);
+    for (int64_t row = int64_t(blockIdx.x) * ROWS + threadIdx.x / THREADS; row < a.rows;
+         row += int64_t(gridDim.x) * ROWS) {
+        const T *x = static_cast<const T *>(a.x) + row * a.x_pitch;
+        Pack<T> p[NV];
+        float s[1] = {0};
+#pragma unroll
+        for (int k = 0; k < NV; ++k) {
+            const int64_t c = int64_t(k * THREADS + t) * V;
+            p[k] = load_pack(x + c, a.cols - c);
+        }
+#pragma unroll
+        for (int k = 0; k < NV; ++k)
+#pragma unroll
+            for (int i = 0; i < V; ++i) s[0] += float(p[k].e[i]);
+        row_sum<THREADS>(s, part[0]);
+        const float mean = s[0] / cols;
+        float q[1] = {0};
+#pragma unroll
+        for (int k = 0; k < NV; ++k) {
+            const int64_t c = int64_t(k * THREADS + t) * V;
+#pragma unroll
+            for (int i = 0; i < V; ++i) {
+                const float d = float(p[k].e[i]) - mean;
+                q[0] += c + i < a.cols ? d * d : 0.0f;
+            }
+        }
+        row_sum<THREADS>(q, part[1]);
+        const float rstd = 1.0f / sqrtf(q[0] / cols + a.eps);
+        if (t == 0) {
+            if (a.mean) a.mean[row] = mean;
+            if (a.rstd) a.rstd[row] = rstd;
+        }
+        T *y = static_cast<T *>(a.y) + row * a.y_pitch;
+#pragma unroll
+        for (int k = 0; k < NV; ++k) {
+            const int64_t c = int64_t(k * THREADS + t) * V;
+            if (c < a.cols) {
+                float w[V], b[V];
+                load_as_float<V>(a.weight, a.weight_dtype, c, a.cols, 1.0f, w);
+                load_as_float<V>(a.bias, a.weight_dtype, c, a.cols, 0.0f, b);
+                Pack<T> r;
+#pragma unroll
+                for (int i = 0; i < V; ++i) r.e[i] = T((float(p[k].e[i]) - mean) * rstd * w[i] + b[i]);
+                store_pack(y + c, r, a.cols - c);
+            }
+        }
+    }
+}
+
+// Rows too long for registers: read once for each moment and once for the result.
+template <typename T>
+__global__ __launch_bounds__(1024) void norm_long_kernel(NormArgs a) {
+    constexpr int V = kVec<T>;
+    __shared__ float part[2][1024 / kWave];
+    const float cols = float(a.cols);
+    for (int64_t row = blockIdx.x; row < a.rows; row += gridDim.x) {
+        const T *x = static_cast<const T *>(a.x) + row * a.x_pitch;
+        T *y = static_cast<T *>(a.y) + row * a.y_pitch;
+        float s[1] = {0}, q[1] = {0};
+        for (int64_t c = int64_t(threadIdx.x) * V; c < a.cols; c += 1024 * V) {
+            const Pack<T> p = load_pack(x + c, a.cols - c);
+#pragma unroll
+            for (int i = 0; i < V; ++i) s[0] += float(p.e[i]);
+        }
+        row_sum<1024>(s, part[0]);
+        const float mean = s[0] / cols;
+        for (int64_t c = int64_t(threadIdx.x) * V; c < a.cols; c += 1024 * V) {
+            const Pack<T> p = load_pack(x + c, a.cols - c);
+#pragma unroll
+            for (int i = 0; i < V; ++i) {
+                const float d = float(p.e[i]) - mean;
+                q[0] += c + i < a.cols ? d * d : 0.0f;
+            }
+        }
+        row_sum<1024>(q, part[1]);
+        const float rstd = 1.0f / sqrtf(q[0] / cols + a.eps);
+        if (threadIdx.x == 0) {
+            if (a.mean) a.mean[row] = mean;
+            if (a.rstd) a.rstd[row] = rstd;
+        }
+        for (int64_t c = int64_t(threadIdx.x) * V; c < a.cols; c += 1024 * V) {
+            const Pack<T> p = load_pack(x + c, a.cols - c);
+            float w[V], b[V];
+            load_as_float<V>(a.weight, a.weight_dtype, c, a.cols, 1.0f, w);
+            load_as_float<V>(a.bias, a.weight_dtype, c, a.cols, 0.0f, b);
+            Pack<T> r;
+#pragma unroll
+            for (int i = 0; i < V; ++i) r.e[i] = T((float(p.e[i]) - mean) * rstd * w[i] + b[i]);
+            store_pack(y + c, r, a.cols - c);
+        }
+    }
+}
+
+struct NormGradArgs {
+    const void *dy, *x, *weight;
+    const float *mean, *rstd;
+    void *dx;
+    float *partial;  // [groups][2][cols]: sums of dy xhat, then of dy, over the rows of one group
+    int64_t rows, cols, dy_pitch, x_pitch, dx_pitch;
+    int weight_dtype;
+};
+
+// Each group of THREADS threads takes every groups-th row and keeps its
+// columns' sums in registers over all of them; no atomics, so the gradients
+// of the weights are the same in every run.
+template <typename T, int THREADS, int NV>
+__global__ __launch_bounds__(THREADS < 256 ? 256 : THREADS) void norm_grad_kernel(NormGradArgs a) {
+    constexpr int ROWS = THREADS < 256 ? 256 / THREADS : 1;
+    constexpr int V = kVec<T>;
+    __shared__ float part[2][2 * (THREADS / kWave)];
+    const int t = threadIdx.x % THREADS;
+    const int64_t group = int64_t(blockIdx.x) * ROWS + threadIdx.x / THREADS;
+    const int64_t groups = int64_t(gridDim.x) * ROWS;
+    const float cols = float(a.cols);
+    float dw[NV][V], db[NV][V];
+#pragma unroll
+    for (int k = 0; k < NV; ++k)
+#pragma unroll
+        for (int i = 0; i < V; ++i) dw[k][i] = db[k][i] = 0;
+    int turn = 0;  // rows in turn use the two halves of `part`: one barrier a row
+    for (int64_t row = group; row < a.rows; row += groups, turn ^= 1) {
+        const T *x = static_cast<const T *>(a.x) + row * a.x_pitch;
+        const T *dy = static_cast<const T *>(a.dy) + row * a.dy_pitch;
+        const float mean = a.mean[row], rstd = a.rstd[row];
+        Pack<T> px[NV], pg[NV];
+#pragma unroll
+        for (int k = 0; k < NV; ++k) {
+            const int64_t c = int64_t(k * THREADS + t) * V;
+            px[k] = load_pack(x + c, a.cols - c);
+            pg[k] = load_pack(dy + c, a.cols - c);
+        }
+        float s[2] = {0, 0};
+#pragma unroll
+        for (int k = 0; k < NV; ++k) {
+            const int64_t c = int64_t(k * THREADS + t) * V;
+            if (c < a.cols) {
+                float w[V];
+                load_as_float<V>(a.weight, a.weight_dtype, c, a.cols, 1.0f, w);
+#pragma unroll
+                for (int i = 0; i < V; ++i) {
+                    const float d = float(pg[k].e[i]);  // 0 past the row's end
+                    const float h = (float(px[k].e[i]) - mean) * rstd;
+                    dw[k][i] += d * h;
+                    db[k][i] += d;
+                    s[0] += d * w[i];
+                    s[1] += d * w[i] * h;
+                }
+            }
+        }
+        row_sum<THREADS>(s, part[turn]);
+        const float c0 = s[0] / cols, c1 = s[1] / cols;
+        T *dx = static_cast<T *>(a.dx) + row * a.dx_pitch;
+        if (a.dx) {
+#pragma unroll
+            for (int k = 0; k < NV; ++k) {
+                const int64_t c = int64_t(k * THREADS + t) * V;
+                if (c < a.cols) {
+                    float w[V];
+                    load_as_float<V>(a.weight, a.weight_dtype, c, a.cols, 1.0f, w);
+                    Pack<T> r;
+#pragma unroll
+                    for (int i = 0; i < V; ++i) {
+                        const float h = (float(px[k].e[i]) - mean) * rstd;
+                        r.e[i] = T(rstd * (float(pg[k].e[i]) * w[i] - c0 - h * c1));
+                    }
+                    store_pack(dx + c, r, a.cols - c);
+                }
+            }
+        }
+    }
+    if (a.partial && group < a.rows) {
+        float *out = a.partial + group * 2 * a.cols;
+#pragma unroll
+        for (int k = 0; k < NV; ++k) {
+            const int64_t c = int64_t(k * THREADS + t) * V;
+#pragma unroll
+            for (int i = 0; i < V; ++i) {
+                if (c + i < a.cols) {
+                    out[c + i] = dw[k][i];
+                    out[a.cols + c + i] = db[k][i];
+                }
+            }
+        }
+    }
+}
+
+// Rows too long for registers: dx, reading the row twice.
+template <typename T>
+__global__ __launch_bounds__(1024) void norm_grad_long_kernel(NormGradArgs a) {
+    constexpr int V = kVec<T>;
+    __shared__ float part[2][2 * (1024 / kWave)];
+    const float cols = float(a.cols);
+    int turn = 0;
+    for (int64_t row = blockIdx.x; row < a.rows; row += gridDim.x, turn ^= 1) {
+        const T *x = static_cast<const T *>(a.x) + row * a.x_pitch;
+        const T *dy = static_cast<const T *>(a.dy) + row * a.dy_pitch;
+        T *dx = static_cast<T *>(a.dx) + row * a.dx_pitch;
+        const float mean = a.mean[row], rstd = a.rstd[row];
+        float s[2] = {0, 0};
+        for (int64_t c = int64_t(threadIdx.x) * V; c < a.cols; c += 1024 * V) {
+            const Pack<T> px = load_pack(x + c, a.cols - c), pg = load_pack(dy + c, a.cols - c);
+            float w[V];
+            load_as_float<V>(a.weight, a.weight_dtype, c, a.cols, 1.0f, w);
+#pragma unroll
+            for (int i = 0; i < V; ++i) {
+                const float g = float(pg.e[i]) * w[i];
+                s[0] += g;
+                s[1] += g * ((float(px.e[i]) - mean) * rstd);
+            }
+        }
+        row_sum<1024>(s, part[turn]);
+        const float c0 = s[0] / cols, c1 = s[1] / cols;
+        for (int64_t c = int64_t(threadIdx.x) * V; c < a.cols; c += 1024 * V) {
+            const Pack<T> px = load_pack(x + c, a.cols - c), pg = load_pack(dy + c, a.cols - c);
+            float w[V];
+            load_as_float<V>(a.weight, a.weight_dtype, c, a.cols, 1.0f, w);
+            Pack<T> r;
+#pragma unroll
+            for (int i = 0; i < V; ++i) {
+                const float h = (float(px.e[i]) - mean) * rstd;
+                r.e[i] = T(rstd * (float(pg.e[i]) * w[i] - c0 - h * c1));
+            }
+            store_pack(dx + c, r, a.cols - c);
+        }
+    }
+}
+
+// The columns' sums for such rows: a thread holds one vector's columns over
+// the rows of its group.
+template <typename T>
+__global__ __launch_bounds__(256) void norm_columns_kernel(NormGradArgs a) {
+    constexpr int V = kVec<T>;
+    const int64_t c = (int64_t(blockIdx.x) * 256 + threadIdx.x) * V;
+    if (c >= a.cols) return;
+    float dw[V], db[V];
+#pragma unroll
+    for (int i = 0; i < V; ++i) dw[i] = db[i] = 0;
+    for (int64_t row = blockIdx.y; row < a.rows; row += gridDim.y) {
+        const Pack<T> px = load_pack(static_cast<const T *>(a.x) + row * a.x_pitch + c, a.cols - c);
+        const Pack<T> pg = load_pack(static_cast<const T *>(a.dy) + row * a.dy_pitch + c, a.cols - c);
+        const float mean = a.mean[row], rstd = a.rstd[row];
+#pragma unroll
+        for (int i = 0; i < V; ++i) {
+            const float d = float(pg.e[i]);
+            dw[i] += d * ((float(px.e[i]) - mean) * rstd);
+            db[i] += d;
+        }
+    }
+    float *out = a.partial + int64_t(blockIdx.y) * 2 * a.cols + c;
+#pragma unroll
+    for (int i = 0; i < V; ++i) {
+        if (c + i < a.cols) {
+            out[i] = dw[i];
+            out[a.cols + i] = db[i];
+        }
+    }
+}
+
+// Joins the groups' sums: 64 columns a workgroup, the groups dealt to its 16
+// waves, whose sums are then added in a fixed order.
+__global__ __launch_bounds__(1024) void norm_join_kernel(const float *partial, int64_t groups, int64_t cols, float *dw,
+                                                         float *db, int accumulate) {
+    __shared__ float part[16][kWave];
+    const int lane = threadIdx.x % kWave, wave = threadIdx.x / kWave;
+    const int64_t j = int64_t(blockIdx.x) * kWave + lane;
+    float s = 0;
+    if (j < 2 * cols) {
+#pragma unroll 8
+        for (int64_t g = wave; g < groups; g += 16) s += partial[g * 2 * cols + j];
+    }
+    part[wave][lane] = s;
+    __syncthreads();
+    if (wave == 0 && j < 2 * cols) {
+        s = 0;
+#pragma unroll
+        for (int w = 0; w < 16; ++w) s += part[w][lane];
+        float *out = j < cols ? dw : db;
+        const int64_t c = j < cols ? j : j - cols;
+        if (out) out[c] = accumulate ? out[c] + s : s;
+    }
+}
+
+constexpr int64_t kMaxGrid = int64_t(1) << 21;  // workgroups; rows beyond are taken in turn
+
+reshard_status_t check_norm(int64_t rows, int64_t cols, reshard_dtype_t dtype, reshard_dtype_t weight_dtype,
+                            bool weights) {
+    reshard_status_t st = check_extent("rows", rows);
+    if (st == RESHARD_OK) st = check_extent("cols", cols);
+    if (st != RESHARD_OK) return st;
+    if (cols == 0) return fail(RESHARD_EINVAL, "cols must be >= 1: a row without elements has no mean");
+    if (cols > int64_t(1) << 24) return fail(RESHARD_EUNSUPPORTED, "cols is above 2^24");
+    if (!is_float_type(dtype)) return fail(RESHARD_EINVAL, "dtype must be F16, BF16 or F32");
+    if (weights && !is_float_type(weight_dtype))
+        return fail(RESHARD_EINVAL, "weight_dtype must be F16, BF16 or F32");
+    return RESHARD_OK;
+}
+
+template <typename T>
+void launch_norm(const NormArgs &a, hipStream_t s) {
+    const int64_t nv = ceil_div(a.cols, kVec<T>);
+    auto grid = [&](int64_t rows_per_wg) { return dim3(unsigned(std::min(ceil_div(a.rows, rows_per_wg), kMaxGrid))); };
+    if (nv <= 64) norm_kernel<T, 64, 1><<<grid(4), 256, 0, s>>>(a);
+    else if (nv <= 128) norm_kernel<T, 64, 2><<<grid(4), 256, 0, s>>>(a);
+    else if (nv <= 256) norm_kernel<T, 64, 4><<<grid(4), 256, 0, s>>>(a);
+    else if (nv <= 512) norm_kernel<T, 256, 2><<<grid(1), 256, 0, s>>>(a);
+    else if (nv <= 1024) norm_kernel<T, 256, 4><<<grid(1), 256, 0, s>>>(a);
+    else if (nv <= 2048) norm_kernel<T, 512, 4><<<grid(1), 512, 0, s>>>(a);
+    else if (nv <= 4096) norm_kernel<T, 1024, 4><<<grid(1), 1024, 0, s>>>(a);
+    else norm_long_kernel<T><<<grid(1), 1024, 0, s>>>(a);
+}
+
+// Groups of rows whose column sums are kept apart until the join.
+int64_t norm_groups(int64_t rows) { return std::min<int64_t>(rows, 512); }
+
+template <typename T>
+void launch_norm_grad(const NormGradArgs &a, int64_t groups, hipStream_t s) {
+    const int64_t nv = ceil_div(a.cols, kVec<T>);
+    const dim3 four(unsigned(ceil_div(groups, 4))), one{unsigned(groups)};
+    if (nv <= 64) norm_grad_kernel<T, 64, 1><<<four, 256, 0, s>>>(a);
+    else if (nv <= 128) norm_grad_kernel<T, 64, 2><<<four, 256, 0, s>>>(a);
+    else if (nv <= 256) norm_grad_kernel<T, 64, 4><<<four, 256, 0, s>>>(a);
+    else if (nv <= 512) norm_grad_kernel<T, 256, 2><<<one, 256, 0, s>>>(a);
+    else if (nv <= 1024) norm_grad_kernel<T, 512, 2><<<one, 512, 0, s>>>(a);
+    else if (nv <= 2048) norm_grad_kernel<T, 1024, 2><<<one, 1024, 0, s>>>(a);
+    else {
+        // the sums first: dx may take dy's place
+        if (a.partial)
+            norm_columns_kernel<T><<<dim3(unsigned(ceil_div(nv, 256)), unsigned(groups)), 256, 0, s>>>(a);
+        if (a.dx) norm_grad_long_kernel<T><<<dim3(unsigned(std::min(a.rows, kMaxGrid))), 1024, 0, s>>>(a);
+    }
+}
+
+}  // namespace
+}  // namespace rs
+
+using rs::fail;
+
+extern "C" reshard_status_t reshard_layer_norm(int64_t rows, int64_t cols, const void *x, int64_t x_pitch,
+                                               reshard_dtype_t dtype, const void *weight, const void *bias,
+                                               reshard_dtype_t weight_dtype, double eps, void *y, int64_t y_pitch,
+                                               float *mean, float *rstd, void *stream) {
+    return rs::guarded([&]() -> reshard_status_t {
+        using namespace rs;
+        reshard_status_t st = check_norm(rows, cols, dtype, weight_dtype, weight || bias);
+        const int64_t es = dtype == RESHARD_F32 ? 4 : 2, ws = weight_dtype == RESHARD_F32 ? 4 : 2;
+        if (st == RESHARD_OK && !(eps >= 0)) st = fail(RESHARD_EINVAL, "eps must be >= 0");
+        if (st == RESHARD_OK) st = check_matrix("x", x, rows, cols, x_pitch, es);
+        if (st == RESHARD_OK) st = check_matrix("y", y, rows, cols, y_pitch, es);
+        if (st == RESHARD_OK && weight) st = check_matrix("weight", weight, 1, cols, cols, ws);
+        if (st == RESHARD_OK && bias) st = check_matrix("bias", bias, 1, cols, cols, ws);
+        if (st == RESHARD_OK && mean) st = check_matrix("mean", mean, 1, rows, rows, 4);
+        if (st == RESHARD_OK && rstd) st = check_matrix("rstd", rstd, 1, rows, rows, 4);
+        if (st != RESHARD_OK || rows == 0) return st;
+        const NormArgs a{x, weight, bias, y, mean, rstd, rows, cols, x_pitch, y_pitch, float(eps), int(weight_dtype)};
+        const hipStream_t s = static_cast<hipStream_t>(stream);
+        if (dtype == RESHARD_F32) launch_norm<float>(a, s);
+        else if (dtype == RESHARD_BF16) launch_norm<bf16>(a, s);
+        else launch_norm<f16>(a, s);
+        return launched("layer norm launch");
+    });
+}
+
+extern "C" int64_t reshard_layer_norm_backward_workspace(int64_t rows, int64_t cols) {
+    if (rows < 0 || cols < 1 || cols > int64_t(1) << 24) return -1;
+    return rs::norm_groups(rows) * 2 * cols * int64_t(sizeof(float));
+}
+
+extern "C" reshard_status_t reshard_layer_norm_backward(int64_t rows, int64_t cols, const void *dy, int64_t dy_pitch,
+                                                        const void *x, int64_t x_pitch, reshard_dtype_t dtype,
+                                                        const void *weight, reshard_dtype_t weight_dtype,
+                                                        const float *mean, const float *rstd, void *dx,
+                                                        int64_t dx_pitch, float *dweight, float *dbias, int accumulate,
+                                                        void *workspace, int64_t workspace_bytes, void *stream) {
+    return rs::guarded([&]() -> reshard_status_t {
+        using namespace rs;
+        reshard_status_t st = check_norm(rows, cols, dtype, weight_dtype, weight != nullptr);
+        const int64_t es = dtype == RESHARD_F32 ? 4 : 2, ws = weight_dtype == RESHARD_F32 ? 4 : 2;
+        if (st == RESHARD_OK) st = check_matrix("dy", dy, rows, cols, dy_pitch, es);
+        if (st == RESHARD_OK) st = check_matrix("x", x, rows, cols, x_pitch, es);
+        if (st == RESHARD_OK && weight) st = check_matrix("weight", weight, 1, cols, cols, ws);
+        if (st == RESHARD_OK) st = check_matrix("mean", mean, 1, rows, rows, 4);
+        if (st == RESHARD_OK) st = check_matrix("rstd", rstd, 1, rows, rows, 4);
+        if (st == RESHARD_OK && dx) st = check_matrix("dx", dx, rows, cols, dx_pitch, es);
+        if (st == RESHARD_OK && dweight) st = check_matrix("dweight", dweight, 1, cols, cols, 4);
+        if (st == RESHARD_OK && dbias) st = check_matrix("dbias", dbias, 1, cols, cols, 4);
+        if (st == RESHARD_OK && (accumulate & ~1)) st = fail(RESHARD_EINVAL, "accumulate must be 0 or 1");
+        if (st != RESHARD_OK) return st;
+        const bool sums = dweight || dbias;
+        const int64_t need = reshard_layer_norm_backward_workspace(rows, cols);
+        if (sums && rows > 0) {
+            if (!workspace || workspace_bytes < need)
+                return fail(RESHARD_EINVAL, "the gradients of the weights need a workspace of " +
+                                                std::to_string(need) + " bytes, got " +
+                                                std::to_string(workspace ? workspace_bytes : 0));
+            if (reinterpret_cast<uintptr_t>(workspace) % 16)
+                return fail(RESHARD_EINVAL, "workspace is not aligned to 16 bytes");
+        }
+        const hipStream_t s = static_cast<hipStream_t>(stream);
+        const int64_t groups = norm_groups(rows);
+        if (rows > 0 && (dx || sums)) {
+            const NormGradArgs a{dy,   x,    weight,   mean,    rstd,     dx, sums ? static_cast<float *>(workspace) : nullptr,
+                                 rows, cols, dy_pitch, x_pitch, dx_pitch, int(weight_dtype)};
+            if (dtype == RESHARD_F32) launch_norm_grad<float>(a, groups, s);
+            else if (dtype == RESHARD_BF16) launch_norm_grad<bf16>(a, groups, s);
+            else launch_norm_grad<f16>(a, groups, s);
+            st = launched("layer norm gradient launch");
+            if (st != RESHARD_OK) return st;
+        }
+        if (!sums || (rows == 0 && accumulate)) return RESHARD_OK;
+        // no rows: the sums are zeros (0 groups to join)
+        norm_join_kernel<<<dim3(unsigned(ceil_div(2 * cols, kWave))), 1024, 0, s>>>(
+            static_cast<const float *>(workspace), groups, cols, dweight, dbias, accumulate);
+        return launched("layer norm gradient join launch");
+    });
+}
