@@ -139,7 +139,7 @@ def _declare_operators(lib):
                                                 vp, i64, vp]
     lib.reshard_quantize.argtypes = [i64, i64, vp, i64, ci, ci, ci, vp, i64, vp, i64, vp, i64, vp, i64, vp]
     lib.reshard_dequantize.argtypes = [i64, i64, vp, i64, ci, vp, i64, ci, vp, i64, ci, vp]
-    lib.reshard_matmul_workspace.argtypes = [i64, i64, i64]
+    lib.reshard_matmul_workspace.argtypes = [i64, i64, i64, ci, ci]
     lib.reshard_matmul_workspace.restype = i64
     lib.reshard_matmul.argtypes = [i64, i64, i64, vp, i64, ci, vp, i64, vp, i64, ci, vp, i64, ci, vp, i64, ci, ci,
                                    vp, i64, vp]
@@ -587,15 +587,16 @@ def reshard_matmul(a, b, out_dtype=None, out=None, accumulate=False, stream=None
     if accumulate and out is None:
         raise ValueError("accumulate needs the out to add to")
     shape = (*a.data.shape[:-1], n)
-    need = lib.reshard_matmul_workspace(m, n, k)
+    out_dtype = out_dtype or (torch.bfloat16 if out is None else out.dtype)
+    sdt, odt = _dtype_code(a.scales.dtype), _dtype_code(out_dtype)
+    need = lib.reshard_matmul_workspace(m, n, k, sdt, odt)
     with _on(stream):
-        y = torch.empty(shape, dtype=out_dtype or torch.bfloat16, device=a.data.device) if out is None else \
-            _like("out", out, shape, out_dtype or out.dtype, a.data.device)
+        y = torch.empty(shape, dtype=out_dtype, device=a.data.device) if out is None else \
+            _like("out", out, shape, out_dtype, a.data.device)
         work = torch.empty(need, dtype=torch.uint8, device=a.data.device) if need > 0 else None
     _check(lib.reshard_matmul(m, n, k, a.data.data_ptr(), a_pitch, a.block_rows, a.scales.data_ptr(), a_spitch,
                               b.data.data_ptr(), b_pitch, b.block_rows, b.scales.data_ptr(), b_spitch,
-                              _dtype_code(a.scales.dtype), y.data_ptr(), _matrix("out", y)[2], _dtype_code(y.dtype),
-                              int(accumulate), _ptr(work), max(0, need), _stream_handle(stream)))
+                              sdt, y.data_ptr(), _matrix("out", y)[2], odt, int(accumulate), _ptr(work), max(0, need), _stream_handle(stream)))
     return y
 
 

@@ -27,6 +27,7 @@ namespace {
 typedef int i32x8 __attribute__((ext_vector_type(8)));
 typedef int i32x4 __attribute__((ext_vector_type(4)));
 typedef float f32x4 __attribute__((ext_vector_type(4)));
+typedef float f32x16 __attribute__((ext_vector_type(16)));
 typedef bf16 bf16x2 __attribute__((ext_vector_type(2)));
 typedef bf16 bf16x8 __attribute__((ext_vector_type(8)));
 
@@ -79,12 +80,33 @@ struct Operand {
 struct MatmulArgs {
     Operand a, b;
     void *out;
+    float *parts;  // [parts of the reduction][m][n], where it is split
     int64_t k, out_pitch;
     int out_dtype, accumulate, e8m0;
 };
 
 __device__ inline int scale_code(const Operand &o, int64_t row, int64_t block) {
     return static_cast<const uint8_t *>(o.scales)[(row >> o.row_shift) * o.scales_pitch + block];
+}
+
+__device__ inline f32x16 zeros() {
+    f32x16 z;
+#pragma unroll
+    for (int e = 0; e < 16; ++e) z[e] = 0;
+    return z;
+}
+
+// The same for half a block and tiles of 32 x 32, added to p.
+template <Sum SUM>
+__device__ inline f32x16 block_product(const Codes &b, const Codes &a, f32x16 p) {
+    if constexpr (SUM == kExact) {
+        const Wide wb(b), wa(a);
+#pragma unroll
+        for (int s = 0; s < 4; ++s) p = __builtin_amdgcn_mfma_f32_32x32x16_bf16(wb.v[s], wa.v[s], p, 0, 0, 0);
+        return p;
+    } else {
+        return __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(b.v, a.v, p, 0, 0, 0, 0, 0, 0);
+    }
 }
 
 __device__ inline float scale_value(const Operand &o, int e8m0, int64_t row, int64_t block) {
@@ -214,6 +236,530 @@ __global__ __launch_bounds__(256) void matmul_kernel(MatmulArgs g, uint32_t tile
     }
 }
 
+// Eight neighbouring results.
+template <typename T>
+__device__ inline void store_eight(const MatmulArgs &g, int64_t i, int64_t j, f32x4 lo, f32x4 hi) {
+    T *p = static_cast<T *>(g.out) + i * g.out_pitch + j;
+    const int64_t n = g.b.rows - j;
+    typedef T T8 __attribute__((ext_vector_type(8)));
+    float v[8] = {lo[0], lo[1], lo[2], lo[3], hi[0], hi[1], hi[2], hi[3]};
+    if (n >= 8) {
+        T8 r;
+        if (g.accumulate) r = load_any<T8>(p);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) r[e] = T(g.accumulate ? float(r[e]) + v[e] : v[e]);
+        store_any(p, r);
+    } else {
+#pragma unroll
+        for (int e = 0; e < 8; ++e)
+            if (e < n) p[e] = T(g.accumulate ? float(p[e]) + v[e] : v[e]);
+    }
+}
+
+__device__ inline void store_run(const MatmulArgs &g, int64_t i, int64_t j, f32x4 lo, f32x4 hi) {
+    if (g.out_dtype == RESHARD_F32) store_eight<float>(g, i, j, lo, hi);
+    else if (g.out_dtype == RESHARD_BF16) store_eight<bf16>(g, i, j, lo, hi);
+    else store_eight<f16>(g, i, j, lo, hi);
+}
+
+// A descriptor for `bytes` bytes from p, the same in every lane.  Loads past
+// the end give zeros, the wave's offset counted in.
+__device__ inline __amdgpu_buffer_rsrc_t bytes_from(const uint8_t *p, int64_t bytes) {
+    const uint64_t a = reinterpret_cast<uint64_t>(p);
+    const uint64_t lo = uint32_t(__builtin_amdgcn_readfirstlane(int(a)));
+    const uint64_t hi = uint32_t(__builtin_amdgcn_readfirstlane(int(a >> 32)));
+    const int n = __builtin_amdgcn_readfirstlane(int(bytes < 0xffffffff ? uint32_t(bytes) : 0xffffffffu));
+    return __builtin_amdgcn_make_buffer_rsrc(reinterpret_cast<void *>(hi << 32 | lo), 0, n, 0x00020000);
+}
+
+// 16 bytes of a lane's straight into LDS, from `base` + its offset + the
+// wave's offset; lane l's go to `to` + 16 l, `to` being the wave's.
+__device__ inline void load_to_lds(__amdgpu_buffer_rsrc_t base, uint32_t offset, uint32_t wave_offset, uint4 *to) {
+    __builtin_amdgcn_raw_ptr_buffer_load_lds(base, (__attribute__((address_space(3))) void *)to, 16, offset,
+                                             wave_offset, 0, 0);
+}
+
+// Before a barrier behind which other waves read what this one loaded into
+// LDS: the barrier itself waits for LDS accesses, not for such loads.
+__device__ inline void loads_done() { __builtin_amdgcn_s_waitcnt(0x0f70); }  // vmcnt(0)
+
+struct Tile {
+    uint32_t i, j;
+};
+
+// Workgroups start on the 8 XCDs in turn.  Each XCD takes a contiguous run of
+// the tiles, ordered in bands of kBand rows of tiles, column by column, so
+// that the tiles in flight there share rows of A and of B in its L2.
+constexpr uint32_t kBand = 8;
+__device__ inline Tile tile_of(uint32_t wg, uint32_t tiles, uint32_t tiles_n) {
+    const uint32_t xcd = wg % 8, each = tiles / 8, more = tiles % 8;
+    const uint32_t p = xcd * each + min(xcd, more) + wg / 8;
+    const uint32_t band = p / (kBand * tiles_n), r = p - band * (kBand * tiles_n);
+    const uint32_t rows = min(kBand, tiles / tiles_n - band * kBand), j = r / rows;
+    return Tile{uint32_t(__builtin_amdgcn_readfirstlane(band * kBand + (r - j * rows))),
+                uint32_t(__builtin_amdgcn_readfirstlane(j))};
+}
+
+template <typename F, int... I>
+__device__ inline void each(F &&f, std::integer_sequence<int, I...>) {
+    (f(std::integral_constant<int, I>{}), ...);
+}
+
+// f(0), f(1), ..., f(N - 1) with constants.
+template <int N, typename F>
+__device__ inline void unrolled(F &&f) {
+    each(f, std::make_integer_sequence<int, N>{});
+}
+
+// The large products: a WM x WN grid of waves, each TM x TN instruction tiles
+// of 32 x 32.  A block of both operands' rows goes from memory into LDS
+// without passing through registers, while the block before it is multiplied
+// (two LDS buffers).
+//
+// An instruction takes half a block, so a step has two phases.  While one is
+// multiplied, row of tiles by row of tiles, the fragments of the next are
+// read: B's and the last rows' of A beside those in use, the first rows' of A
+// in place of them once they are done.  The step's one barrier lies between
+// its phases: there a wave holds the rest of its block in registers, so that
+// the block two steps ahead can be loaded over it, and the next block, loaded
+// since the last barrier, can be read.
+//
+// LDS rows are 128 bytes, eight 16-byte words, word w of row r in slot
+// w ^ (r / 2 % 8): lanes that read at once fall on different banks.  The loads
+// write LDS in order, so the order of words is set by the addresses they read.
+template <int ROWS>
+struct Stage {
+    uint4 words[ROWS * 8];
+};
+
+template <Sum SUM, bool E8M0, int TM, int TN, int WM, int WN>
+__global__ __launch_bounds__(WM *WN *kWave, WM *WN / 4) void matmul_tile_kernel(MatmulArgs g, uint32_t tiles_n, int32_t blocks) {
+    constexpr int THREADS = WM * WN * kWave, BM = WM * TM * 32, BN = WN * TN * 32;
+    constexpr int LA = BM * 8 / THREADS, LB = BN * 8 / THREADS;  // 16-byte loads a thread and step
+    constexpr int ROWS_AT_ONCE = THREADS / 8;
+    constexpr int SROWS = (BM + BN) / THREADS;  // scales a thread and step
+    using Given = typename std::conditional<E8M0, uint8_t, float>::type;
+    using Scale = typename std::conditional<SUM == kScaled, uint8_t, float>::type;  // in LDS
+    __shared__ Stage<BM> a_lds0, a_lds1;
+    __shared__ Stage<BN> b_lds0, b_lds1;
+    __shared__ __align__(16) Scale s_lds[3][BM + BN];  // three: a step's may be read while those two ahead are written
+
+    const Tile at = tile_of(blockIdx.x, gridDim.x, tiles_n);
+    const int64_t i0 = int64_t(at.i) * BM, j0 = int64_t(at.j) * BN;
+    const int t = threadIdx.x, lane = t % kWave, wave = __builtin_amdgcn_readfirstlane(t / kWave);
+    const int r32 = lane % 32, half = lane / 32, wi = wave / WN, wj = wave % WN;
+    if (gridDim.y > 1) {  // this workgroup's part of the reduction, to a place of its own
+        const int64_t first = int64_t(blockIdx.y) * blocks;
+        g.a.q += first * kBlock;
+        g.b.q += first * kBlock;
+        g.a.scales = static_cast<const Given *>(g.a.scales) + first;
+        g.b.scales = static_cast<const Given *>(g.b.scales) + first;
+        g.k = min(g.k - first * kBlock, int64_t(blocks) * kBlock);
+        g.out = g.parts + int64_t(blockIdx.y) * g.a.rows * g.b.rows;
+        g.out_pitch = g.b.rows;
+        g.out_dtype = RESHARD_F32;
+        g.accumulate = 0;
+    }
+    const int32_t steps = int32_t(ceil_div(g.k, kBlock));
+    const int32_t paired = int32_t(g.k / (2 * kBlock)) * 2;  // whole blocks, two at a time
+
+    // rows past a matrix's end are read as zeros
+    const int lrow = t / 8, lword = (t % 8) ^ ((lrow / 2) % 8);
+    const uint32_t a_off = lrow * uint32_t(g.a.pitch) + lword * 16, b_off = lrow * uint32_t(g.b.pitch) + lword * 16;
+    const uint32_t a_next_rows = ROWS_AT_ONCE * uint32_t(g.a.pitch), b_next_rows = ROWS_AT_ONCE * uint32_t(g.b.pitch);
+    const __amdgpu_buffer_rsrc_t a_base =
+        bytes_from(g.a.q + i0 * g.a.pitch, (g.a.rows - 1 - i0) * g.a.pitch + g.k);
+    const __amdgpu_buffer_rsrc_t b_base =
+        bytes_from(g.b.q + j0 * g.b.pitch, (g.b.rows - 1 - j0) * g.b.pitch + g.k);
+    auto stage_one = [&](int32_t s, auto &a_lds, auto &b_lds, auto u_) {
+        constexpr int u = decltype(u_)::value;
+        if constexpr (u < LA)
+            load_to_lds(a_base, a_off, u * a_next_rows + s * kBlock, &a_lds.words[u * THREADS + wave * kWave]);
+        else
+            load_to_lds(b_base, b_off, (u - LA) * b_next_rows + s * kBlock,
+                        &b_lds.words[(u - LA) * THREADS + wave * kWave]);
+    };
+    auto stage = [&](int32_t s, auto &a_lds, auto &b_lds) {
+        unrolled<LA + LB>([&](auto u) { stage_one(s, a_lds, b_lds, u); });
+    };
+
+    // A row's scales lie a row apart from the next row's, so each load of them
+    // touches as many cache lines as it has lanes: two steps' at once.
+    using Two = typename std::conditional<E8M0, uint16_t, uint64_t>::type;
+    const Given *s_at[SROWS];
+    int s_to[SROWS];
+    Two s_held[SROWS], s_next[SROWS];
+#pragma unroll
+    for (int u = 0; u < SROWS; ++u) {
+        const int r = t + u * THREADS;
+        const bool is_a = r < BM;
+        const Operand &o = is_a ? g.a : g.b;
+        const int rr = is_a ? r : r - BM, T = is_a ? TM : TN;
+        const int64_t row = min((is_a ? i0 : j0) + rr, o.rows - 1);
+        s_at[u] = static_cast<const Given *>(o.scales) + (row >> o.row_shift) * o.scales_pitch;
+        // [wave's row][r32][tile]: a lane's scales of all tiles lie together
+        s_to[u] = is_a || SUM == kScaled ? (is_a ? 0 : BM) + rr / (T * 32) * (T * 32) + rr % 32 * T + rr / 32 % T : r;
+    }
+    // Of blocks s and s + 1; past the last, any.  Nothing is computed from
+    // what is loaded before it is put into LDS, so that nothing waits for it.
+    auto load_scales = [&](int32_t s, Two (&to)[SROWS]) {
+#pragma unroll
+        for (int u = 0; u < SROWS; ++u) to[u] = load_any<Two>(s_at[u] + min(s, steps - 2));
+    };
+    auto in_lds = [](Two w) -> Scale {
+        if constexpr (SUM == kScaled) return uint8_t(w);
+        else if constexpr (E8M0) return e8m0_value(uint8_t(w));
+        else return __uint_as_float(uint32_t(w));
+    };
+    auto put_scales = [&](int buf, int32_t s, int32_t block) {  // block's, from those loaded for s and s + 1
+        const int shift = block > min(s, steps - 2) ? 4 * int(sizeof(Two)) : 0;
+#pragma unroll
+        for (int u = 0; u < SROWS; ++u) {
+            s_lds[buf][s_to[u]] = in_lds(Two(s_held[u] >> shift));
+        }
+    };
+
+    // A lane's share of 32 rows' half block: words half and half + 2 of a row,
+    // or half + 4 and half + 6.  Which element of the block is which of the
+    // instruction's does not matter, as long as A and B agree.  One address a
+    // word and operand, with the tile and the buffer in the instruction's
+    // offset: left to itself, the compiler keeps a register for each.
+    uint32_t a_word[4], b_word[4];
+#pragma unroll
+    for (int p = 0; p < 4; ++p) {
+        const uint32_t word = r32 * 8 + ((half + 2 * p) ^ ((r32 / 2) % 8));
+        a_word[p] = wi * TM * 256 + word;
+        b_word[p] = wj * TN * 256 + word;
+        asm("" : "+v"(a_word[p]), "+v"(b_word[p]));
+    }
+    auto read = [&](auto &lds, const uint32_t (&word)[4], int part, int tile) {
+        Codes c;
+        c.h[0] = lds.words[word[2 * part] + tile * 256];
+        c.h[1] = lds.words[word[2 * part + 1] + tile * 256];
+        return c;
+    };
+
+    f32x16 acc[TM][TN], sum[TM][TN];  // sum: of the block at hand, where its scales are applied to it
+    unrolled<TM>([&](auto x) { unrolled<TN>([&](auto y) { acc[x][y] = zeros(); }); });
+    constexpr int TWO = TM / 2;  // rows of tiles from here on have two sets of registers
+    Codes fa[TM], fa_odd[TM - TWO], fb[2][TN];
+    auto frag_a = [&](auto part, auto x) -> Codes & {
+        if constexpr (decltype(part)::value == 1 && decltype(x)::value >= TWO) return fa_odd[decltype(x)::value - TWO];
+        else return fa[decltype(x)::value];
+    };
+    int ka[2], kb[2];  // kScaled: the tiles' exponents, a byte each
+    float kf[2][TM];   // else: A's scales
+    auto read_scales = [&](const Scale *sc, int into) {
+        if constexpr (SUM == kScaled) {
+            using Bytes_m = typename std::conditional<TM == 4, uint32_t, uint16_t>::type;
+            using Bytes_n = typename std::conditional<TN == 4, uint32_t, uint16_t>::type;
+            ka[into] = *reinterpret_cast<const Bytes_m *>(&sc[wi * TM * 32 + r32 * TM]);
+            kb[into] = *reinterpret_cast<const Bytes_n *>(&sc[BM + wj * TN * 32 + r32 * TN]);
+        } else {
+#pragma unroll
+            for (int x = 0; x < TM; ++x) kf[into][x] = sc[wi * TM * 32 + r32 * TM + x];
+        }
+    };
+
+    constexpr std::integral_constant<int, 0> low{};
+    constexpr std::integral_constant<int, 1> high{};
+    int sbuf = 0;  // the step's scales, of three
+    auto product = [&](auto cur_, auto part, auto x_, auto y_) {
+        constexpr int cur = decltype(cur_)::value, x = decltype(x_)::value, y = decltype(y_)::value;
+        const Codes &a = frag_a(part, x_), &b = fb[part][y];
+        if constexpr (SUM == kScaled) {
+            acc[x][y] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(b.v, a.v, acc[x][y], 0, 0, y, kb[cur], x, ka[cur]);
+        } else {
+            sum[x][y] = block_product<SUM>(b, a, decltype(part)::value ? sum[x][y] : zeros());
+        }
+    };
+    // A row of tiles' sums over the block, scaled, to the results.
+    auto scale_row = [&](auto cur_, auto x_) {
+        constexpr int cur = decltype(cur_)::value, x = decltype(x_)::value;
+        unrolled<TN>([&](auto y) {
+            unrolled<4>([&](auto q_) {
+                constexpr int q = decltype(q_)::value;
+                const f32x4 sb =
+                    *reinterpret_cast<const f32x4 *>(&s_lds[sbuf][BM + (wj * TN + y) * 32 + q * 8 + half * 4]);
+#pragma unroll
+                for (int e = 0; e < 4; ++e)
+                    acc[x][y][q * 4 + e] = fmaf(sum[x][y][q * 4 + e], kf[cur][x] * sb[e], acc[x][y][q * 4 + e]);
+            });
+        });
+    };
+    // One phase: a_from and b_from are the buffers that the other part's
+    // fragments are read from, and load(x) what else is done beside a row.
+    auto phase = [&](auto cur, auto part, auto &a_from, auto &b_from, auto &&load) {
+        constexpr std::integral_constant<int, decltype(part)::value ^ 1> other{};
+        unrolled<TM>([&](auto x_) {
+            constexpr int x = decltype(x_)::value;
+            if constexpr (x == 0) {
+                unrolled<TN>([&](auto y) { fb[other][y] = read(b_from, b_word, other, y); });
+            }
+            if constexpr (x > 0 && x <= TWO) {
+                frag_a(other, std::integral_constant<int, x - 1>{}) = read(a_from, a_word, other, x - 1);
+            }
+            if constexpr (x < TM - TWO) {
+                frag_a(other, std::integral_constant<int, TWO + x>{}) = read(a_from, a_word, other, TWO + x);
+            }
+            load(x_);
+            unrolled<TN>([&](auto y) { product(cur, part, x_, y); });
+            // the row before this one, whose products are done by now
+            if constexpr (SUM != kScaled && decltype(part)::value == 1 && x > 0)
+                scale_row(cur, std::integral_constant<int, x - 1>{});
+            __builtin_amdgcn_sched_barrier(0);
+        });
+        if constexpr (SUM != kScaled && decltype(part)::value == 1) scale_row(cur, std::integral_constant<int, TM - 1>{});
+    };
+    auto step = [&](auto cur_, int32_t s, auto &a_cur, auto &b_cur, auto &a_next, auto &b_next) {
+        constexpr int cur = decltype(cur_)::value, EACH = (LA + LB + TM - 1) / TM;
+        const int snext = sbuf == 2 ? 0 : sbuf + 1;
+        const int32_t ahead = min(s + 2, paired - 1);
+        phase(cur_, low, a_cur, b_cur, [](auto) {});
+        // the last step's reads ahead find an older block, which is not used
+        put_scales(snext, s + 1 - cur, s + 1);
+        loads_done();
+        __syncthreads();
+        __builtin_amdgcn_sched_barrier(0);
+        read_scales(s_lds[snext], cur ^ 1);
+        if constexpr (cur == 1) {  // those of s + 2 and s + 3 were loaded two steps ago
+#pragma unroll
+            for (int u = 0; u < SROWS; ++u) s_held[u] = s_next[u];
+            load_scales(s + 4, s_next);
+        }
+        phase(cur_, high, a_next, b_next, [&](auto x) {
+            unrolled<EACH>([&](auto e) {
+                constexpr int u = decltype(x)::value * EACH + decltype(e)::value;
+                if constexpr (u < LA + LB) stage_one(ahead, a_cur, b_cur, std::integral_constant<int, u>{});
+            });
+        });
+        sbuf = snext;
+    };
+
+    if (paired > 0) {
+        load_scales(0, s_held);
+        stage(0, a_lds0, b_lds0);
+        put_scales(0, 0, 0);
+        load_scales(1, s_held);
+        load_scales(3, s_next);
+        loads_done();
+        stage(1, a_lds1, b_lds1);
+        __syncthreads();
+        read_scales(s_lds[0], 0);
+        unrolled<TM>([&](auto x) { fa[x] = read(a_lds0, a_word, 0, x); });
+        unrolled<TN>([&](auto y) { fb[0][y] = read(b_lds0, b_word, 0, y); });
+        for (int32_t s = 0; s < paired; s += 2) {
+            step(low, s, a_lds0, b_lds0, a_lds1, b_lds1);
+            step(high, s + 1, a_lds1, b_lds1, a_lds0, b_lds0);
+        }
+        loads_done();
+        __syncthreads();
+    }
+#pragma unroll 1
+    for (int32_t s = paired; s < steps; ++s) {  // an odd block and a short one, whose missing codes are zeros
+        const int64_t l = int64_t(s) * kBlock + lword * 16;
+#pragma unroll 1
+        for (int u = 0; u < LA; ++u)
+            a_lds0.words[u * THREADS + t] = load_codes(g.a, i0 + lrow + u * ROWS_AT_ONCE, l, g.k);
+#pragma unroll 1
+        for (int u = 0; u < LB; ++u)
+            b_lds0.words[u * THREADS + t] = load_codes(g.b, j0 + lrow + u * ROWS_AT_ONCE, l, g.k);
+#pragma unroll
+        for (int u = 0; u < SROWS; ++u) {
+            if constexpr (E8M0) s_lds[0][s_to[u]] = in_lds(s_at[u][s]);
+            else s_lds[0][s_to[u]] = s_at[u][s];
+        }
+        sbuf = 0;
+        __syncthreads();
+        read_scales(s_lds[0], 0);
+        unrolled<TM>([&](auto x) { fa[x] = read(a_lds0, a_word, 0, x); });
+        unrolled<TN>([&](auto y) { fb[0][y] = read(b_lds0, b_word, 0, y); });
+        phase(low, low, a_lds0, b_lds0, [](auto) {});
+        phase(low, high, a_lds0, b_lds0, [](auto) {});
+        __syncthreads();
+    }
+
+    // Each wave turns its results, 32 rows of one column of tiles at a time,
+    // through its part of LDS (float32, 16-byte word w of row r in slot
+    // w ^ (r % 8)), so that lanes store runs of a row.
+    f32x4 *turn = reinterpret_cast<f32x4 *>(a_lds0.words) + wave * 256;
+    static_assert(WM * WN * 256 <= BM * 16, "LDS for the results");
+    unrolled<TM>([&](auto x) {
+        unrolled<TN>([&](auto y) {
+            unrolled<4>([&](auto q_) {
+                constexpr int q = decltype(q_)::value;
+                turn[r32 * 8 + ((q * 2 + half) ^ (r32 % 8))] =
+                    f32x4{acc[x][y][q * 4], acc[x][y][q * 4 + 1], acc[x][y][q * 4 + 2], acc[x][y][q * 4 + 3]};
+            });
+#pragma unroll 1
+            for (int r = lane / 4; r < 32; r += 16) {
+                const int w = lane % 4 * 2;
+                const f32x4 lo = turn[r * 8 + (w ^ (r % 8))], hi = turn[r * 8 + ((w + 1) ^ (r % 8))];
+                const int64_t i = i0 + (wi * TM + x) * 32 + r, j = j0 + (wj * TN + y) * 32 + w * 4;
+                if (i < g.a.rows) store_run(g, i, j, lo, hi);
+            }
+        });
+    });
+}
+
+// Adds the parts of a split reduction, in order.
+__global__ __launch_bounds__(256) void matmul_join_kernel(MatmulArgs g, int parts) {
+    const int64_t across = ceil_div(g.b.rows, 8), total = g.a.rows * across;
+    for (int64_t at = int64_t(blockIdx.x) * 256 + threadIdx.x; at < total; at += int64_t(gridDim.x) * 256) {
+        const int64_t i = at / across, j = (at - i * across) * 8;
+        const float *p = g.parts + i * g.b.rows + j;
+        f32x4 lo{0, 0, 0, 0}, hi{0, 0, 0, 0};
+        for (int s = 0; s < parts; ++s, p += g.a.rows * g.b.rows) {
+            const Pack<float> x = load_pack(p, g.b.rows - j), y = load_pack(p + 4, g.b.rows - j - 4);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                lo[e] += x.e[e];
+                hi[e] += y.e[e];
+            }
+        }
+        store_run(g, i, j, lo, hi);
+    }
+}
+
+// Few rows of A: the weights' bytes are the work.  A workgroup takes 16 NT
+// rows of B and all of A's; its waves deal the blocks of the reduction among
+// them, load their fragments straight into registers, and add their sums
+// through LDS.  Nothing is loaded twice but A, which the caches hold.
+template <Sum SUM, int MT, int NT, int WAVES>
+__global__ __launch_bounds__(WAVES *kWave) void matmul_few_kernel(MatmulArgs g) {
+    constexpr int DEPTH = MT * NT > 4 ? 1 : 2;  // blocks loaded together
+    __shared__ f32x4 part[WAVES][MT * NT][kWave];
+    const int lane = threadIdx.x % kWave, wave = threadIdx.x / kWave, r16 = lane % 16, quad = lane / 16;
+    const int64_t j0 = int64_t(blockIdx.x) * 16 * NT;
+    const int32_t steps = int32_t(ceil_div(g.k, kBlock));
+    f32x4 acc[MT][NT];
+#pragma unroll
+    for (int x = 0; x < MT; ++x)
+#pragma unroll
+        for (int y = 0; y < NT; ++y) acc[x][y] = f32x4{0, 0, 0, 0};
+
+    auto blocks = [&](int32_t s0, auto depth_) {
+        constexpr int D = decltype(depth_)::value;
+        Codes fa[D][MT], fb[D][NT];
+        float ka[D][MT], kb[D][NT][4];
+        int ea[D][MT], eb[D][NT];
+#pragma unroll
+        for (int d = 0; d < D; ++d) {
+            const int64_t s = s0 + d * WAVES, l = s * kBlock + quad * 16;
+#pragma unroll
+            for (int y = 0; y < NT; ++y) {
+                const int64_t j = j0 + y * 16 + r16;
+                fb[d][y].h[0] = load_codes(g.b, j, l, g.k);
+                fb[d][y].h[1] = load_codes(g.b, j, l + 64, g.k);
+            }
+#pragma unroll
+            for (int x = 0; x < MT; ++x) {
+                fa[d][x].h[0] = load_codes(g.a, x * 16 + r16, l, g.k);
+                fa[d][x].h[1] = load_codes(g.a, x * 16 + r16, l + 64, g.k);
+            }
+            if constexpr (SUM == kScaled) {
+#pragma unroll
+                for (int y = 0; y < NT; ++y) eb[d][y] = scale_code(g.b, min(j0 + y * 16 + r16, g.b.rows - 1), s);
+#pragma unroll
+                for (int x = 0; x < MT; ++x) ea[d][x] = scale_code(g.a, min(int64_t(x * 16 + r16), g.a.rows - 1), s);
+            } else {
+#pragma unroll
+                for (int y = 0; y < NT; ++y)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e)
+                        kb[d][y][e] = scale_value(g.b, g.e8m0, min(j0 + y * 16 + quad * 4 + e, g.b.rows - 1), s);
+#pragma unroll
+                for (int x = 0; x < MT; ++x)
+                    ka[d][x] = scale_value(g.a, g.e8m0, min(int64_t(x * 16 + r16), g.a.rows - 1), s);
+            }
+        }
+#pragma unroll
+        for (int d = 0; d < D; ++d)
+#pragma unroll
+            for (int y = 0; y < NT; ++y) {
+                const typename std::conditional<SUM == kExact, Wide, Codes>::type b(fb[d][y]);
+#pragma unroll
+                for (int x = 0; x < MT; ++x) {
+                    if constexpr (SUM == kScaled) {
+                        acc[x][y] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(b.v, fa[d][x].v, acc[x][y], 0, 0, 0,
+                                                                                     eb[d][y], 0, ea[d][x]);
+                    } else {
+                        const typename std::conditional<SUM == kExact, Wide, Codes>::type a(fa[d][x]);
+                        const f32x4 p = block_product(b, a);
+#pragma unroll
+                        for (int e = 0; e < 4; ++e)
+                            acc[x][y][e] = fmaf(p[e], ka[d][x] * kb[d][y][e], acc[x][y][e]);
+                    }
+                }
+            }
+    };
+    int32_t s = wave;
+    for (; s + (DEPTH - 1) * WAVES < steps; s += DEPTH * WAVES) blocks(s, std::integral_constant<int, DEPTH>{});
+    if constexpr (DEPTH > 1) {
+        for (; s < steps; s += WAVES) blocks(s, std::integral_constant<int, 1>{});
+    }
+
+#pragma unroll
+    for (int x = 0; x < MT; ++x)
+#pragma unroll
+        for (int y = 0; y < NT; ++y) part[wave][x * NT + y][lane] = acc[x][y];
+    __syncthreads();
+    for (int at = threadIdx.x; at < MT * NT * kWave; at += WAVES * kWave) {
+        const int tile = at / kWave, l = at % kWave;
+        f32x4 v = part[0][tile][l];
+#pragma unroll
+        for (int w = 1; w < WAVES; ++w) {
+            const f32x4 o = part[w][tile][l];
+#pragma unroll
+            for (int e = 0; e < 4; ++e) v[e] += o[e];
+        }
+        const int64_t i = tile / NT * 16 + l % 16, j = j0 + tile % NT * 16 + l / 16 * 4;
+        if (i < g.a.rows && j < g.b.rows) store_any_type(g, i, j, v);
+    }
+}
+
+// How a product is launched: with few rows of A by its weights' rows alone;
+// otherwise in tiles of 256 x 256 (16-bit results of E8M0 operands) or
+// 128 x 128, and where those are too few for the 256 CUs, the reduction
+// split into parts that are joined.
+struct Plan {
+    bool few, large;
+    int64_t tile, tiles_m, tiles_n;
+    int32_t parts, blocks;  // parts of the reduction, and the blocks of each
+};
+
+Plan plan_matmul(int64_t m, int64_t n, int64_t k, bool scaled) {
+    Plan p{};
+    p.few = m <= 64;
+    const int64_t steps = ceil_div(k, kBlock);
+    auto tiles = [&](int64_t side) { return ceil_div(m, side) * ceil_div(n, side); };
+    p.large = scaled && tiles(256) >= 192;
+    p.tile = p.large ? 256 : 128;
+    p.tiles_m = ceil_div(m, p.tile);
+    p.tiles_n = ceil_div(n, p.tile);
+    p.parts = 1;
+    if (!p.few && tiles(128) <= 256) {
+        const int64_t most = std::min<int64_t>(std::max<int64_t>(1, steps / 8), 32);
+        p.parts = int32_t(std::min(most, std::max<int64_t>(1, 512 / tiles(128))));
+    }
+    p.blocks = int32_t(ceil_div(ceil_div(std::max<int64_t>(steps, 1), p.parts), 2) * 2);
+    p.parts = int32_t(ceil_div(std::max<int64_t>(steps, 1), p.blocks));
+    return p;
+}
+
+template <Sum SUM>
+void launch_few(const MatmulArgs &g, hipStream_t s) {
+    const int64_t m = g.a.rows, n = g.b.rows;
+    if (m <= 16) {
+        if (ceil_div(n, 16) >= 256) matmul_few_kernel<SUM, 1, 1, 4><<<dim3(unsigned(ceil_div(n, 16))), 256, 0, s>>>(g);
+        else matmul_few_kernel<SUM, 1, 1, 16><<<dim3(unsigned(ceil_div(n, 16))), 1024, 0, s>>>(g);
+    } else if (m <= 32) {
+        matmul_few_kernel<SUM, 2, 1, 8><<<dim3(unsigned(ceil_div(n, 16))), 512, 0, s>>>(g);
+    } else {
+        matmul_few_kernel<SUM, 4, 2, 8><<<dim3(unsigned(ceil_div(n, 32))), 512, 0, s>>>(g);
+    }
+}
+
 reshard_status_t check_operand(const char *name, const char *scales_name, const void *q, int64_t rows, int64_t k,
                                int64_t pitch, int block_rows, const void *scales, int64_t scales_pitch,
                                reshard_dtype_t scale_dtype) {
@@ -230,9 +776,12 @@ reshard_status_t check_operand(const char *name, const char *scales_name, const 
 
 using rs::fail;
 
-extern "C" int64_t reshard_matmul_workspace(int64_t m, int64_t n, int64_t k) {
-    if (m < 0 || n < 0 || k < 0) return -1;
-    return 0;
+extern "C" int64_t reshard_matmul_workspace(int64_t m, int64_t n, int64_t k, reshard_dtype_t scale_dtype,
+                                            reshard_dtype_t out_dtype) {
+    if (m < 0 || n < 0 || k < 0 || m > int64_t(1) << 40 || n > int64_t(1) << 40 || k > int64_t(1) << 36) return -1;
+    if (m == 0 || n == 0) return 0;
+    const rs::Plan p = rs::plan_matmul(m, n, k, scale_dtype == RESHARD_E8M0 && out_dtype != RESHARD_F32);
+    return p.parts > 1 ? int64_t(p.parts) * m * n * int64_t(sizeof(float)) : 0;
 }
 
 extern "C" reshard_status_t reshard_matmul(int64_t m, int64_t n, int64_t k, const void *a, int64_t a_pitch,
@@ -257,9 +806,9 @@ extern "C" reshard_status_t reshard_matmul(int64_t m, int64_t n, int64_t k, cons
         if (st == RESHARD_OK)
             st = check_matrix("out", out, m, n, out_pitch, out_dtype == RESHARD_F32 ? 4 : 2);
         if (st != RESHARD_OK || m == 0 || n == 0) return st;
-        const int64_t tiles_m = ceil_div(m, 128), tiles_n = ceil_div(n, 128);
-        if (tiles_n > (int64_t(1) << 23) / tiles_m)
-            return fail(RESHARD_EUNSUPPORTED, "out has more than 2^23 tiles of 128 x 128");
+        if (ceil_div(n, 128) > (int64_t(1) << 22) / ceil_div(m, 128))
+            return fail(RESHARD_EUNSUPPORTED, "out has more than 2^22 tiles of 128 x 128");
+        if (k > int64_t(1) << 36) return fail(RESHARD_EUNSUPPORTED, "k is above 2^36");
         MatmulArgs g{};
         g.a = Operand{static_cast<const uint8_t *>(a), a_scales, m, a_pitch, a_scales_pitch, a_block_rows == 1 ? 0 : 7};
         g.b = Operand{static_cast<const uint8_t *>(b), b_scales, n, b_pitch, b_scales_pitch, b_block_rows == 1 ? 0 : 7};
@@ -270,10 +819,47 @@ extern "C" reshard_status_t reshard_matmul(int64_t m, int64_t n, int64_t k, cons
         g.accumulate = accumulate;
         g.e8m0 = scale_dtype == RESHARD_E8M0;
         const hipStream_t s = static_cast<hipStream_t>(stream);
-        const dim3 grid(unsigned(tiles_m * tiles_n));
-        if (out_dtype == RESHARD_F32) matmul_kernel<kExact><<<grid, 256, 0, s>>>(g, uint32_t(tiles_n));
-        else if (g.e8m0) matmul_kernel<kScaled><<<grid, 256, 0, s>>>(g, uint32_t(tiles_n));
-        else matmul_kernel<kFloat><<<grid, 256, 0, s>>>(g, uint32_t(tiles_n));
+        const Sum sum = out_dtype == RESHARD_F32 ? kExact : g.e8m0 ? kScaled : kFloat;
+        const Plan p = plan_matmul(m, n, k, sum == kScaled);
+        if (p.few) {
+            if (sum == kExact) launch_few<kExact>(g, s);
+            else if (sum == kScaled) launch_few<kScaled>(g, s);
+            else launch_few<kFloat>(g, s);
+            return launched("matmul launch");
+        }
+        // the tile kernel's loads into LDS: whole 16-byte words, 32-bit offsets within a tile's rows
+        const bool aligned = (reinterpret_cast<uintptr_t>(a) | reinterpret_cast<uintptr_t>(b) | uintptr_t(a_pitch) |
+                              uintptr_t(b_pitch)) % 16 == 0 && a_pitch <= 1 << 22 && b_pitch <= 1 << 22;
+        if (!aligned) {
+            const dim3 grid(unsigned(ceil_div(m, 128) * ceil_div(n, 128)));
+            const uint32_t tiles_n = uint32_t(ceil_div(n, 128));
+            if (sum == kExact) matmul_kernel<kExact><<<grid, 256, 0, s>>>(g, tiles_n);
+            else if (sum == kScaled) matmul_kernel<kScaled><<<grid, 256, 0, s>>>(g, tiles_n);
+            else matmul_kernel<kFloat><<<grid, 256, 0, s>>>(g, tiles_n);
+            return launched("matmul launch");
+        }
+        if (p.parts > 1) {
+            const int64_t need = int64_t(p.parts) * m * n * int64_t(sizeof(float));
+            if (!workspace || workspace_bytes < need)
+                return fail(RESHARD_EINVAL, "the product needs a workspace of " + std::to_string(need) +
+                                                " bytes, got " + std::to_string(workspace ? workspace_bytes : 0));
+            if (reinterpret_cast<uintptr_t>(workspace) % 16)
+                return fail(RESHARD_EINVAL, "workspace is not aligned to 16 bytes");
+            g.parts = static_cast<float *>(workspace);
+        }
+        const dim3 grid(unsigned(p.tiles_m * p.tiles_n), unsigned(p.parts));
+        const uint32_t tn = uint32_t(p.tiles_n);
+        if (sum == kExact && g.e8m0) matmul_tile_kernel<kExact, true, 2, 2, 2, 2><<<grid, 256, 0, s>>>(g, tn, p.blocks);
+        else if (sum == kExact) matmul_tile_kernel<kExact, false, 2, 2, 2, 2><<<grid, 256, 0, s>>>(g, tn, p.blocks);
+        else if (sum == kFloat) matmul_tile_kernel<kFloat, false, 2, 2, 2, 2><<<grid, 256, 0, s>>>(g, tn, p.blocks);
+        else if (p.large) matmul_tile_kernel<kScaled, true, 4, 2, 2, 4><<<grid, 512, 0, s>>>(g, tn, p.blocks);
+        else matmul_tile_kernel<kScaled, true, 2, 2, 2, 2><<<grid, 256, 0, s>>>(g, tn, p.blocks);
+        if (p.parts > 1) {
+            const reshard_status_t started = launched("matmul launch");
+            if (started != RESHARD_OK) return started;
+            const int64_t wgs = std::min<int64_t>(ceil_div(m * ceil_div(n, 8), 256), 4096);
+            matmul_join_kernel<<<dim3(unsigned(wgs)), 256, 0, s>>>(g, p.parts);
+        }
         return launched("matmul launch");
     });
 }

@@ -431,6 +431,33 @@ def test_matmul(a_rows, b_rows, scale_dtype, m, n, k, gpu_lib):
         assert torch.equal(first, second), "another run, other bits"
 
 
+# the reduction in parts (few tiles, a long reduction: whole, odd and short blocks at the parts' ends), and tiles of 256 x 256
+@gpu
+@pytest.mark.parametrize("m,n,k", [(65, 130, 2048), (130, 260, 4098), (100, 70, 9000), (300, 129, 5130), (257, 1000, 8191),
+                                   (3080, 4100, 390), (4097, 3300, 640)])
+@pytest.mark.parametrize("scale_dtype", [E8M0, torch.float32], ids=["e8m0", "fp32"])
+def test_matmul_long_and_large(scale_dtype, m, n, k, gpu_lib):
+    g = _seed("long", str(scale_dtype), m, n, k)
+    a, a64 = _operand(g, m, k, 1, scale_dtype, (-k) % 16)
+    b, b64 = _operand(g, n, k, 128, scale_dtype, (-k) % 16 + 16)
+    want, size = a64 @ b64.t(), a64.abs() @ b64.abs().t()
+    within = (128 + 4 + math.ceil(k / 128) + 64) * F32 * size
+    start = _randn(g, m, n).float()
+    for dt, cut in ((torch.float32, within), (torch.bfloat16, within + 2.0 ** -10 * size)):
+        out, untouched = _guarded((m, n), dt)
+        got = B.reshard_matmul(a, b, dt, out=out)
+        torch.cuda.synchronize()
+        _near(got, want, cut + HALVES[dt] * (want.abs() + cut), f"{dt}")
+        assert untouched()
+        assert torch.equal(B.reshard_matmul(a, b, dt), got), "another run, other bits"
+        held = start.to(dt).cuda()
+        B.reshard_matmul(a, b, out=held, accumulate=True)
+        more = start.to(dt).double()
+        _near(held, want + more, cut + F32 * (want.abs() + more.abs()) + HALVES[dt] * (want.abs() + cut + more.abs()), "+=")
+    need = gpu_lib.reshard_matmul_workspace(m, n, k, 13 if scale_dtype == E8M0 else 4, 4)
+    assert (need > 0) == (k >= 2048), "the sizes no longer reach the path that they are for"
+
+
 @gpu
 def test_matmul_special_values(gpu_lib):
     """NaN codes and scales reach their rows and columns alone; without a reduction the product is zeros."""
@@ -620,7 +647,15 @@ def test_matmul_refusals():
             (mul(ot=6), EI, "out_dtype"), (mul(acc=-1), EI, "accumulate"), (mul(out=P + 1), EI, "aligned"),
             (mul(m=1 << 30, n=1 << 30, op=1 << 30), EU, "out")):
         _refused(call, status, text)
-    assert lib.reshard_matmul_workspace(-1, 1, 1) == -1
+    assert lib.reshard_matmul_workspace(-1, 1, 1, 13, 3) == -1
+    need = lib.reshard_matmul_workspace(128, 128, 8192, 13, 3)  # a reduction in parts
+    assert need > 0
+
+    def split(work, nbytes):
+        return _answer(lib.reshard_matmul(128, 128, 8192, P, 8192, 1, P, 64, P, 8192, 128, P, 64, 13, P, 128, 3, 0, work, nbytes,
+                                          None))
+    for answer in (split(None, need), split(P, need - 1), split(P + 4, need)):
+        _refused(answer, EI, "workspace")
 
 
 def test_binding_refusals():
