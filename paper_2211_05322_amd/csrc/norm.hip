@@ -10,6 +10,7 @@
 // registers between the reductions and the result, so the second moment is
 // taken about the mean (no cancellation) without a second read.
 #include <algorithm>
+#include <type_traits>
 
 #include "operators.hpp"
 
@@ -40,6 +41,36 @@ __device__ inline void row_sum(float (&v)[N], float *part) {
     }
 }
 
+// A thread's columns of a row: NV vectors, the k-th the (k * THREADS + t)-th
+// of the row.  NV is the fewest that cover the row, so only the last can pass
+// the row's end; it is moved back to end there, and its first `skip` elements
+// are another vector's.  Both compute the same values for those.
+template <typename T, int THREADS, int NV>
+struct Columns {
+    static constexpr int V = kVec<T>;
+    int64_t last;
+    int first, skip;
+
+    __device__ Columns(int64_t cols, int t) {
+        const int64_t c = int64_t((NV - 1) * THREADS + t) * V;
+        last = min(c, cols - V);
+        skip = int(min(c - last, int64_t(V)));
+        first = t * V;
+    }
+    __device__ int64_t at(int k) const { return k == NV - 1 ? last : int64_t(k) * (THREADS * V) + first; }
+    __device__ bool mine(int k, int i) const { return k < NV - 1 || i >= skip; }
+    __device__ bool any(int k) const { return k < NV - 1 || skip < V; }
+};
+
+// Between a reduction and the next use of a row: elements are converted again
+// there.  Without it the compiler keeps both forms of them in registers
+// across the barrier, and spills.
+template <typename T, int NV>
+__device__ inline void packed(Pack<T> (&p)[NV]) {
+#pragma unroll
+    for (int k = 0; k < NV; ++k) asm("" : "+v"(p[k].v.x), "+v"(p[k].v.y), "+v"(p[k].v.z), "+v"(p[k].v.w));
+}
+
 struct NormArgs {
     const void *x, *weight, *bias;
     void *y;
@@ -49,42 +80,57 @@ struct NormArgs {
     int weight_dtype;
 };
 
-// THREADS threads hold a row, NV vectors each; 256 / THREADS rows a workgroup
-// where a wave holds one.
+// THREADS threads hold a row, 256 / THREADS rows a workgroup where a wave
+// holds one.  A workgroup keeps its columns' weights in registers over the
+// rows that it takes in turn, and loads each row while the one before is
+// reduced.
 template <typename T, int THREADS, int NV>
 __global__ __launch_bounds__(THREADS < 256 ? 256 : THREADS) void norm_kernel(NormArgs a) {
     constexpr int ROWS = THREADS < 256 ? 256 / THREADS : 1;
     constexpr int V = kVec<T>;
+    constexpr bool AHEAD = THREADS * NV < 4096;  // registers for two rows
     __shared__ float part[2][THREADS / kWave];
     const int t = threadIdx.x % THREADS;
+    const Columns<T, THREADS, NV> my(a.cols, t);
     const float cols = float(a.cols);
-    for (int64_t row = int64_t(blockIdx.x) * ROWS + threadIdx.x / THREADS; row < a.rows;
-         row += int64_t(gridDim.x) * ROWS) {
-        const T *x = static_cast<const T *>(a.x) + row * a.x_pitch;
-        Pack<T> p[NV];
-        float s[1] = {0};
+    float w[NV][V], b[NV][V];
 #pragma unroll
-        for (int k = 0; k < NV; ++k) {
-            const int64_t c = int64_t(k * THREADS + t) * V;
-            p[k] = load_pack(x + c, a.cols - c);
-        }
+    for (int k = 0; k < NV; ++k) {
+        load_as_float<V>(a.weight, a.weight_dtype, my.at(k), a.cols, 1.0f, w[k]);
+        load_as_float<V>(a.bias, a.weight_dtype, my.at(k), a.cols, 0.0f, b[k]);
+    }
+    const int64_t stride = int64_t(gridDim.x) * ROWS;
+    int64_t row = int64_t(blockIdx.x) * ROWS + threadIdx.x / THREADS;
+    Pack<T> next[NV];
+    auto load = [&](int64_t r) {
+        const T *x = static_cast<const T *>(a.x) + min(r, a.rows - 1) * a.x_pitch;
+#pragma unroll
+        for (int k = 0; k < NV; ++k) next[k].v = load_any<uint4>(x + my.at(k));
+    };
+    if (AHEAD) load(row);
+    for (; row < a.rows; row += stride) {
+        if (!AHEAD) load(row);
+        Pack<T> p[NV];
+#pragma unroll
+        for (int k = 0; k < NV; ++k) p[k] = next[k];
+        if (AHEAD) load(row + stride);
+        float s[1] = {0}, q[1] = {0};
 #pragma unroll
         for (int k = 0; k < NV; ++k)
 #pragma unroll
-            for (int i = 0; i < V; ++i) s[0] += float(p[k].e[i]);
+            for (int i = 0; i < V; ++i) s[0] += my.mine(k, i) ? float(p[k].e[i]) : 0.0f;
         row_sum<THREADS>(s, part[0]);
+        packed(p);
         const float mean = s[0] / cols;
-        float q[1] = {0};
 #pragma unroll
-        for (int k = 0; k < NV; ++k) {
-            const int64_t c = int64_t(k * THREADS + t) * V;
+        for (int k = 0; k < NV; ++k)
 #pragma unroll
             for (int i = 0; i < V; ++i) {
                 const float d = float(p[k].e[i]) - mean;
-                q[0] += c + i < a.cols ? d * d : 0.0f;
+                q[0] += my.mine(k, i) ? d * d : 0.0f;
             }
-        }
         row_sum<THREADS>(q, part[1]);
+        packed(p);
         const float rstd = 1.0f / sqrtf(q[0] / cols + a.eps);
         if (t == 0) {
             if (a.mean) a.mean[row] = mean;
@@ -93,21 +139,16 @@ __global__ __launch_bounds__(THREADS < 256 ? 256 : THREADS) void norm_kernel(Nor
         T *y = static_cast<T *>(a.y) + row * a.y_pitch;
 #pragma unroll
         for (int k = 0; k < NV; ++k) {
-            const int64_t c = int64_t(k * THREADS + t) * V;
-            if (c < a.cols) {
-                float w[V], b[V];
-                load_as_float<V>(a.weight, a.weight_dtype, c, a.cols, 1.0f, w);
-                load_as_float<V>(a.bias, a.weight_dtype, c, a.cols, 0.0f, b);
-                Pack<T> r;
+            Pack<T> r;
 #pragma unroll
-                for (int i = 0; i < V; ++i) r.e[i] = T((float(p[k].e[i]) - mean) * rstd * w[i] + b[i]);
-                store_pack(y + c, r, a.cols - c);
-            }
+            for (int i = 0; i < V; ++i) r.e[i] = T((float(p[k].e[i]) - mean) * rstd * w[k][i] + b[k][i]);
+            if (my.any(k)) store_any(y + my.at(k), r.v);
         }
     }
 }
 
-// Rows too long for registers: read once for each moment and once for the result.
+// Rows too long for registers, or shorter than one vector: read once for each
+// moment and once for the result.
 template <typename T>
 __global__ __launch_bounds__(1024) void norm_long_kernel(NormArgs a) {
     constexpr int V = kVec<T>;
@@ -161,70 +202,88 @@ struct NormGradArgs {
 };
 
 // Each group of THREADS threads takes every groups-th row and keeps its
-// columns' sums in registers over all of them; no atomics, so the gradients
-// of the weights are the same in every run.
+// columns' sums in registers over all of them, loading each row while the one
+// before is reduced; no atomics, so the gradients of the weights are the same
+// in every run.  The weights, as float32, lie in LDS: with them the registers
+// would not hold two rows and the sums.
 template <typename T, int THREADS, int NV>
 __global__ __launch_bounds__(THREADS < 256 ? 256 : THREADS) void norm_grad_kernel(NormGradArgs a) {
     constexpr int ROWS = THREADS < 256 ? 256 / THREADS : 1;
     constexpr int V = kVec<T>;
+    constexpr bool AHEAD = THREADS < 1024;
     __shared__ float part[2][2 * (THREADS / kWave)];
+    extern __shared__ float weights[];  // cols, a whole number of vectors
     const int t = threadIdx.x % THREADS;
+    const Columns<T, THREADS, NV> my(a.cols, t);
     const int64_t group = int64_t(blockIdx.x) * ROWS + threadIdx.x / THREADS;
     const int64_t groups = int64_t(gridDim.x) * ROWS;
     const float cols = float(a.cols);
+    for (int64_t c = threadIdx.x * V; c < a.cols; c += blockDim.x * V) {
+        float w[V];
+        load_as_float<V>(a.weight, a.weight_dtype, c, a.cols, 1.0f, w);
+#pragma unroll
+        for (int i = 0; i < V; ++i) weights[c + i] = w[i];
+    }
+    __syncthreads();
     float dw[NV][V], db[NV][V];
 #pragma unroll
     for (int k = 0; k < NV; ++k)
 #pragma unroll
         for (int i = 0; i < V; ++i) dw[k][i] = db[k][i] = 0;
+    Pack<T> next_x[NV], next_g[NV];
+    float next_mean, next_rstd;
+    auto load = [&](int64_t r) {
+        r = min(r, a.rows - 1);
+        const T *x = static_cast<const T *>(a.x) + r * a.x_pitch, *dy = static_cast<const T *>(a.dy) + r * a.dy_pitch;
+#pragma unroll
+        for (int k = 0; k < NV; ++k) {
+            next_x[k].v = load_any<uint4>(x + my.at(k));
+            next_g[k].v = load_any<uint4>(dy + my.at(k));
+        }
+        next_mean = a.mean[r];
+        next_rstd = a.rstd[r];
+    };
+    if (AHEAD) load(group);
     int turn = 0;  // rows in turn use the two halves of `part`: one barrier a row
     for (int64_t row = group; row < a.rows; row += groups, turn ^= 1) {
-        const T *x = static_cast<const T *>(a.x) + row * a.x_pitch;
-        const T *dy = static_cast<const T *>(a.dy) + row * a.dy_pitch;
-        const float mean = a.mean[row], rstd = a.rstd[row];
+        if (!AHEAD) load(row);
         Pack<T> px[NV], pg[NV];
 #pragma unroll
         for (int k = 0; k < NV; ++k) {
-            const int64_t c = int64_t(k * THREADS + t) * V;
-            px[k] = load_pack(x + c, a.cols - c);
-            pg[k] = load_pack(dy + c, a.cols - c);
+            px[k] = next_x[k];
+            pg[k] = next_g[k];
         }
+        const float mean = next_mean, rstd = next_rstd;
+        if (AHEAD) load(row + groups);
         float s[2] = {0, 0};
 #pragma unroll
         for (int k = 0; k < NV; ++k) {
-            const int64_t c = int64_t(k * THREADS + t) * V;
-            if (c < a.cols) {
-                float w[V];
-                load_as_float<V>(a.weight, a.weight_dtype, c, a.cols, 1.0f, w);
+            const float *w = weights + my.at(k);
 #pragma unroll
-                for (int i = 0; i < V; ++i) {
-                    const float d = float(pg[k].e[i]);  // 0 past the row's end
-                    const float h = (float(px[k].e[i]) - mean) * rstd;
-                    dw[k][i] += d * h;
-                    db[k][i] += d;
-                    s[0] += d * w[i];
-                    s[1] += d * w[i] * h;
-                }
+            for (int i = 0; i < V; ++i) {
+                const float d = float(pg[k].e[i]), h = (float(px[k].e[i]) - mean) * rstd;
+                dw[k][i] += d * h;
+                db[k][i] += d;
+                s[0] += my.mine(k, i) ? d * w[i] : 0.0f;
+                s[1] += my.mine(k, i) ? d * w[i] * h : 0.0f;
             }
         }
         row_sum<THREADS>(s, part[turn]);
-        const float c0 = s[0] / cols, c1 = s[1] / cols;
-        T *dx = static_cast<T *>(a.dx) + row * a.dx_pitch;
+        packed(px);
+        packed(pg);
         if (a.dx) {
+            const float c0 = s[0] / cols, c1 = s[1] / cols;
+            T *dx = static_cast<T *>(a.dx) + row * a.dx_pitch;
 #pragma unroll
             for (int k = 0; k < NV; ++k) {
-                const int64_t c = int64_t(k * THREADS + t) * V;
-                if (c < a.cols) {
-                    float w[V];
-                    load_as_float<V>(a.weight, a.weight_dtype, c, a.cols, 1.0f, w);
-                    Pack<T> r;
+                const float *w = weights + my.at(k);
+                Pack<T> r;
 #pragma unroll
-                    for (int i = 0; i < V; ++i) {
-                        const float h = (float(px[k].e[i]) - mean) * rstd;
-                        r.e[i] = T(rstd * (float(pg[k].e[i]) * w[i] - c0 - h * c1));
-                    }
-                    store_pack(dx + c, r, a.cols - c);
+                for (int i = 0; i < V; ++i) {
+                    const float h = (float(px[k].e[i]) - mean) * rstd;
+                    r.e[i] = T(rstd * (float(pg[k].e[i]) * w[i] - c0 - h * c1));
                 }
+                if (my.any(k)) store_any(dx + my.at(k), r.v);
             }
         }
     }
@@ -232,19 +291,19 @@ __global__ __launch_bounds__(THREADS < 256 ? 256 : THREADS) void norm_grad_kerne
         float *out = a.partial + group * 2 * a.cols;
 #pragma unroll
         for (int k = 0; k < NV; ++k) {
-            const int64_t c = int64_t(k * THREADS + t) * V;
+            if (my.any(k)) {
 #pragma unroll
-            for (int i = 0; i < V; ++i) {
-                if (c + i < a.cols) {
-                    out[c + i] = dw[k][i];
-                    out[a.cols + c + i] = db[k][i];
+                for (int i = 0; i < V; i += 4) {  // elements that are another's have the same sums
+                    store_any(out + my.at(k) + i, make_float4(dw[k][i], dw[k][i + 1], dw[k][i + 2], dw[k][i + 3]));
+                    store_any(out + a.cols + my.at(k) + i, make_float4(db[k][i], db[k][i + 1], db[k][i + 2], db[k][i + 3]));
                 }
             }
         }
     }
 }
 
-// Rows too long for registers: dx, reading the row twice.
+// Rows too long for registers, or shorter than one vector: dx, reading the
+// row twice.
 template <typename T>
 __global__ __launch_bounds__(1024) void norm_grad_long_kernel(NormGradArgs a) {
     constexpr int V = kVec<T>;
@@ -355,39 +414,71 @@ reshard_status_t check_norm(int64_t rows, int64_t cols, reshard_dtype_t dtype, r
     return RESHARD_OK;
 }
 
+// Calls f(THREADS, NV), as constants, for rows of nv vectors; false where no
+// registers hold such rows.  A wave a row up to 2 vectors a lane; then as many
+// waves as keep a thread at `each` vectors at most.
+template <int V, int EACH, int MOST, typename F>
+bool with_columns(int64_t cols, F &&f) {
+    const int64_t nv = ceil_div(cols, V);
+    if (cols < V || nv > MOST) return false;
+    bool done = false;
+    auto offer = [&](auto threads, auto n) {
+        constexpr int THREADS = decltype(threads)::value, NV = decltype(n)::value;
+        if constexpr (THREADS * NV <= MOST && NV <= (THREADS == 512 ? EACH : 4)) {
+            if (!done && nv <= THREADS * NV) {
+                f(threads, n);
+                done = true;
+            }
+        }
+    };
+    using std::integral_constant;
+    constexpr integral_constant<int, 1> n1{};
+    constexpr integral_constant<int, 2> n2{};
+    constexpr integral_constant<int, 3> n3{};
+    constexpr integral_constant<int, 4> n4{};
+    offer(integral_constant<int, 64>{}, n1);
+    offer(integral_constant<int, 64>{}, n2);
+    offer(integral_constant<int, 256>{}, n1);
+    offer(integral_constant<int, 256>{}, n2);
+    offer(integral_constant<int, 256>{}, n3);
+    offer(integral_constant<int, 512>{}, n2);
+    offer(integral_constant<int, 512>{}, n3);
+    offer(integral_constant<int, 512>{}, n4);
+    offer(integral_constant<int, 1024>{}, n2);
+    offer(integral_constant<int, 1024>{}, n3);
+    offer(integral_constant<int, 1024>{}, n4);
+    return done;
+}
+
 template <typename T>
 void launch_norm(const NormArgs &a, hipStream_t s) {
-    const int64_t nv = ceil_div(a.cols, kVec<T>);
-    auto grid = [&](int64_t rows_per_wg) { return dim3(unsigned(std::min(ceil_div(a.rows, rows_per_wg), kMaxGrid))); };
-    if (nv <= 64) norm_kernel<T, 64, 1><<<grid(4), 256, 0, s>>>(a);
-    else if (nv <= 128) norm_kernel<T, 64, 2><<<grid(4), 256, 0, s>>>(a);
-    else if (nv <= 256) norm_kernel<T, 64, 4><<<grid(4), 256, 0, s>>>(a);
-    else if (nv <= 512) norm_kernel<T, 256, 2><<<grid(1), 256, 0, s>>>(a);
-    else if (nv <= 1024) norm_kernel<T, 256, 4><<<grid(1), 256, 0, s>>>(a);
-    else if (nv <= 2048) norm_kernel<T, 512, 4><<<grid(1), 512, 0, s>>>(a);
-    else if (nv <= 4096) norm_kernel<T, 1024, 4><<<grid(1), 1024, 0, s>>>(a);
-    else norm_long_kernel<T><<<grid(1), 1024, 0, s>>>(a);
+    const bool done = with_columns<kVec<T>, 3, 4096>(a.cols, [&](auto threads, auto n) {
+        constexpr int THREADS = decltype(threads)::value, ROWS = THREADS < 256 ? 256 / THREADS : 1;
+        const int64_t most = 256 * 2048 / (THREADS < 256 ? 256 : THREADS);  // what the CUs hold at once
+        const dim3 grid(unsigned(std::min(ceil_div(a.rows, ROWS), most)));
+        norm_kernel<T, THREADS, decltype(n)::value><<<grid, THREADS < 256 ? 256 : THREADS, 0, s>>>(a);
+    });
+    if (!done) norm_long_kernel<T><<<dim3(unsigned(std::min(a.rows, kMaxGrid))), 1024, 0, s>>>(a);
 }
 
 // Groups of rows whose column sums are kept apart until the join.
-int64_t norm_groups(int64_t rows) { return std::min<int64_t>(rows, 512); }
+int64_t norm_groups(int64_t rows, int64_t cols) { return std::min<int64_t>(rows, cols > 8192 ? 256 : 512); }
 
 template <typename T>
 void launch_norm_grad(const NormGradArgs &a, int64_t groups, hipStream_t s) {
-    const int64_t nv = ceil_div(a.cols, kVec<T>);
-    const dim3 four(unsigned(ceil_div(groups, 4))), one{unsigned(groups)};
-    if (nv <= 64) norm_grad_kernel<T, 64, 1><<<four, 256, 0, s>>>(a);
-    else if (nv <= 128) norm_grad_kernel<T, 64, 2><<<four, 256, 0, s>>>(a);
-    else if (nv <= 256) norm_grad_kernel<T, 64, 4><<<four, 256, 0, s>>>(a);
-    else if (nv <= 512) norm_grad_kernel<T, 256, 2><<<one, 256, 0, s>>>(a);
-    else if (nv <= 1024) norm_grad_kernel<T, 512, 2><<<one, 512, 0, s>>>(a);
-    else if (nv <= 2048) norm_grad_kernel<T, 1024, 2><<<one, 1024, 0, s>>>(a);
-    else {
-        // the sums first: dx may take dy's place
-        if (a.partial)
-            norm_columns_kernel<T><<<dim3(unsigned(ceil_div(nv, 256)), unsigned(groups)), 256, 0, s>>>(a);
-        if (a.dx) norm_grad_long_kernel<T><<<dim3(unsigned(std::min(a.rows, kMaxGrid))), 1024, 0, s>>>(a);
-    }
+    // 16384 columns: the sums of more do not fit
+    const bool done = with_columns<kVec<T>, 4, 16384 / kVec<T>>(a.cols, [&](auto threads, auto n) {
+        constexpr int THREADS = decltype(threads)::value, ROWS = THREADS < 256 ? 256 / THREADS : 1;
+        const dim3 grid(unsigned(ceil_div(groups, ROWS)));
+        const size_t lds = size_t(ceil_div(a.cols, kVec<T>)) * kVec<T> * sizeof(float);
+        norm_grad_kernel<T, THREADS, decltype(n)::value><<<grid, THREADS < 256 ? 256 : THREADS, lds, s>>>(a);
+    });
+    if (done) return;
+    // the sums first: dx may take dy's place
+    if (a.partial)
+        norm_columns_kernel<T>
+            <<<dim3(unsigned(ceil_div(ceil_div(a.cols, kVec<T>), 256)), unsigned(groups)), 256, 0, s>>>(a);
+    if (a.dx) norm_grad_long_kernel<T><<<dim3(unsigned(std::min(a.rows, kMaxGrid))), 1024, 0, s>>>(a);
 }
 
 }  // namespace
@@ -422,7 +513,7 @@ extern "C" reshard_status_t reshard_layer_norm(int64_t rows, int64_t cols, const
 
 extern "C" int64_t reshard_layer_norm_backward_workspace(int64_t rows, int64_t cols) {
     if (rows < 0 || cols < 1 || cols > int64_t(1) << 24) return -1;
-    return rs::norm_groups(rows) * 2 * cols * int64_t(sizeof(float));
+    return rs::norm_groups(rows, cols) * 2 * cols * int64_t(sizeof(float));
 }
 
 extern "C" reshard_status_t reshard_layer_norm_backward(int64_t rows, int64_t cols, const void *dy, int64_t dy_pitch,
@@ -456,7 +547,7 @@ extern "C" reshard_status_t reshard_layer_norm_backward(int64_t rows, int64_t co
                 return fail(RESHARD_EINVAL, "workspace is not aligned to 16 bytes");
         }
         const hipStream_t s = static_cast<hipStream_t>(stream);
-        const int64_t groups = norm_groups(rows);
+        const int64_t groups = norm_groups(rows, cols);
         if (rows > 0 && (dx || sums)) {
             const NormGradArgs a{dy,   x,    weight,   mean,    rstd,     dx, sums ? static_cast<float *>(workspace) : nullptr,
                                  rows, cols, dy_pitch, x_pitch, dx_pitch, int(weight_dtype)};
