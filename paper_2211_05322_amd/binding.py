@@ -157,7 +157,17 @@ def _i64(vals):
     return (ctypes.c_int64 * max(1, len(vals)))(*vals)
 
 
+_CODES = {}  # what _dtype_code has answered, by the dtype itself
+
+
 def _dtype_code(dtype):
+    code = _CODES.get(dtype)
+    if code is None:
+        code = _CODES[dtype] = _find_dtype_code(dtype)
+    return code
+
+
+def _find_dtype_code(dtype):
     name = str(dtype).replace("torch.", "")
     if name not in _DTYPES:
         raise ValueError(f"unsupported dtype {dtype}")
@@ -404,6 +414,8 @@ class Blocked(NamedTuple):
 def _matrix(name, t):
     """(rows, cols, pitch) of a tensor whose leading dimensions step evenly and whose last is dense."""
     shape, strides = t.shape, t.stride()
+    if len(shape) == 2 and strides[1] == 1:
+        return shape[0], shape[1], strides[0]
     if not shape:
         raise ValueError(f"{name} needs at least one dimension")
     cols = shape[-1]
@@ -424,23 +436,26 @@ def _matrix(name, t):
 
 def _like(name, t, shape, dtype, device):
     """A caller's output or statistic: the shape, type and device it must have."""
-    if tuple(t.shape) != tuple(shape) or t.dtype != dtype or t.device != device:
+    if t.shape != tuple(shape) or t.dtype != dtype or t.device != device:
         raise ValueError(f"{name} must be {dtype} {tuple(shape)} on {device}, "
                          f"got {t.dtype} {tuple(t.shape)} on {t.device}")
     return t
 
 
-def _dense(name, t, shape, device, dtype=None):
-    _like(name, t, shape, dtype or t.dtype, device)
-    if not t.is_contiguous():
-        raise ValueError(f"{name} must be dense")
+def _dense(name, t, shape, device, dtype):
+    if t.shape != shape or t.dtype != dtype or t.device != device or not t.is_contiguous():
+        raise ValueError(f"{name} must be dense, {dtype} {tuple(shape)} on {device}, "
+                         f"got {t.dtype} {tuple(t.shape)}, strides {t.stride()}, on {t.device}")
     return t
+
+
+_HERE = contextlib.nullcontext()
 
 
 def _on(stream):
     """Memory that a call takes comes from the pool of the stream it runs on."""
     if stream is None:
-        return contextlib.nullcontext()
+        return _HERE
     import torch
     return torch.cuda.stream(torch.cuda.ExternalStream(stream) if isinstance(stream, int) else stream)
 
@@ -449,23 +464,33 @@ def _ptr(t):
     return None if t is None else t.data_ptr()
 
 
+def _result(out, like):
+    """(tensor, pitch) of a result of like's shape and type: the caller's, or a dense one."""
+    if out is not None:
+        return _like("out", out, like.shape, like.dtype, like.device), _matrix("out", out)[2]
+    import torch
+    y = torch.empty_like(like) if like.is_contiguous() else like.new_empty(like.shape)
+    return y, like.shape[-1]
+
+
 def reshard_layer_norm(x, weight=None, bias=None, eps=1e-5, out=None, stream=None):
     """(y, mean, rstd): layer norm over x's last dimension; mean and rstd (float32) are for the backward pass."""
     import torch
     lib = _lib or load()
     rows, cols, pitch = _matrix("x", x)
     wdt = (weight if weight is not None else bias if bias is not None else x).dtype
-    for name, w in (("weight", weight), ("bias", bias)):
-        if w is not None:
-            _dense(name, w, (cols,), x.device, wdt)
+    if weight is not None:
+        _dense("weight", weight, (cols,), x.device, wdt)
+    if bias is not None:
+        _dense("bias", bias, (cols,), x.device, wdt)
     with _on(stream):
-        y = torch.empty(x.shape, dtype=x.dtype, device=x.device) if out is None else \
-            _like("out", out, x.shape, x.dtype, x.device)
-        stats = torch.empty((2, *x.shape[:-1]), dtype=torch.float32, device=x.device)
-    mean, rstd = stats.unbind(0)
-    _check(lib.reshard_layer_norm(rows, cols, x.data_ptr(), pitch, _dtype_code(x.dtype), _ptr(weight), _ptr(bias),
-                                  _dtype_code(wdt), eps, y.data_ptr(), _matrix("out", y)[2], mean.data_ptr(),
-                                  rstd.data_ptr(), _stream_handle(stream)))
+        y, y_pitch = _result(out, x)
+        mean, rstd = x.new_empty((2, *x.shape[:-1]), dtype=torch.float32).unbind()
+    status = lib.reshard_layer_norm(rows, cols, x.data_ptr(), pitch, _dtype_code(x.dtype), _ptr(weight), _ptr(bias),
+                                    _dtype_code(wdt), eps, y.data_ptr(), y_pitch, mean.data_ptr(), rstd.data_ptr(),
+                                    _stream_handle(stream))
+    if status != RESHARD_OK:
+        _check(status)
     return y, mean, rstd
 
 
@@ -478,51 +503,56 @@ def reshard_layer_norm_backward(dy, x, weight, mean, rstd, dweight=None, dbias=N
     rows, cols, pitch = _matrix("x", x)
     _like("dy", dy, x.shape, x.dtype, x.device)
     if weight is not None:
-        _dense("weight", weight, (cols,), x.device)
-    for name, s in (("mean", mean), ("rstd", rstd)):
-        _dense(name, s, x.shape[:-1], x.device, torch.float32)
+        _dense("weight", weight, (cols,), x.device, weight.dtype)
+    _dense("mean", mean, x.shape[:-1], x.device, torch.float32)
+    _dense("rstd", rstd, x.shape[:-1], x.device, torch.float32)
     if accumulate and (dweight is None or dbias is None):
         raise ValueError("accumulate needs the dweight and dbias to add to")
     need = lib.reshard_layer_norm_backward_workspace(rows, cols)
     with _on(stream):
-        dx = torch.empty(x.shape, dtype=x.dtype, device=x.device) if out is None else \
-            _like("out", out, x.shape, x.dtype, x.device)
-        if dweight is None:
-            dweight = torch.empty(cols, dtype=torch.float32, device=x.device)
-        if dbias is None:
-            dbias = torch.empty(cols, dtype=torch.float32, device=x.device)
-        work = torch.empty(max(0, need), dtype=torch.uint8, device=x.device)
-    for name, d in (("dweight", dweight), ("dbias", dbias)):
-        _dense(name, d, (cols,), x.device, torch.float32)
-    _check(lib.reshard_layer_norm_backward(
+        dx, dx_pitch = _result(out, x)
+        if dweight is None and dbias is None:
+            dweight, dbias = x.new_empty((2, cols), dtype=torch.float32).unbind()
+        elif dweight is None:
+            dweight = x.new_empty(cols, dtype=torch.float32)
+        elif dbias is None:
+            dbias = x.new_empty(cols, dtype=torch.float32)
+        work = x.new_empty(max(0, need), dtype=torch.uint8)
+    _dense("dweight", dweight, (cols,), x.device, torch.float32)
+    _dense("dbias", dbias, (cols,), x.device, torch.float32)
+    status = lib.reshard_layer_norm_backward(
         rows, cols, dy.data_ptr(), _matrix("dy", dy)[2], x.data_ptr(), pitch, _dtype_code(x.dtype), _ptr(weight),
         _dtype_code(x.dtype if weight is None else weight.dtype), mean.data_ptr(), rstd.data_ptr(), dx.data_ptr(),
-        _matrix("out", dx)[2], dweight.data_ptr(), dbias.data_ptr(), int(accumulate), work.data_ptr(), need,
-        _stream_handle(stream)))
+        dx_pitch, dweight.data_ptr(), dbias.data_ptr(), int(accumulate), work.data_ptr(), need, _stream_handle(stream))
+    if status != RESHARD_OK:
+        _check(status)
     return dx, dweight, dbias
 
 
 _E4M3, _BLOCK = "float8_e4m3fn", 128
 
 
-def _empty_blocked(rows, cols, block_rows, scale_dtype, device):
-    """Codes whose rows are padded to whole blocks, so that each starts on a 16-byte boundary."""
+def _empty_blocked(x, rows, cols, block_rows, scale_dtype):
+    """(Blocked, codes' pitch, scales' pitch) beside x.  Rows of codes are padded to whole blocks, so that each
+    starts on a 16-byte boundary."""
     import torch
     across = -(-cols // _BLOCK)
-    data = torch.empty((rows, across * _BLOCK), dtype=torch.float8_e4m3fn, device=device)[:, :cols]
-    scales = torch.empty((-(-rows // block_rows), across), dtype=scale_dtype, device=device)
-    return Blocked(data, scales, block_rows)
+    data = x.new_empty((rows, across * _BLOCK), dtype=torch.float8_e4m3fn)
+    scales = x.new_empty((rows if block_rows == 1 else -(-rows // block_rows), across), dtype=scale_dtype)
+    if cols != across * _BLOCK:
+        data = data[:, :cols]
+    return Blocked(data, scales, block_rows), across * _BLOCK, across
 
 
 def _blocked(name, b):
     """(rows, cols, pitch, scales' pitch) of a Blocked."""
-    rows, cols, pitch = _matrix(f"{name}.data", b.data)
-    if str(b.data.dtype) != "torch." + _E4M3:
+    rows, cols, pitch = _matrix("data", b.data)
+    if _dtype_code(b.data.dtype) != _DTYPES[_E4M3]:
         raise ValueError(f"{name}.data must be {_E4M3}, got {b.data.dtype}")
     if b.block_rows not in (1, _BLOCK):
         raise ValueError(f"{name}.block_rows must be 1 or {_BLOCK}, got {b.block_rows}")
-    srows, scols, spitch = _matrix(f"{name}.scales", b.scales)
-    if (srows, scols) != (-(-rows // b.block_rows), -(-cols // _BLOCK)):
+    srows, scols, spitch = _matrix("scales", b.scales)
+    if srows != -(-rows // b.block_rows) or scols != -(-cols // _BLOCK):
         raise ValueError(f"{name}.scales must be {(-(-rows // b.block_rows), -(-cols // _BLOCK))}, "
                          f"got {(srows, scols)}")
     if b.scales.device != b.data.device:
@@ -544,29 +574,36 @@ def reshard_quantize(x, block_rows=1, transposed=False, scale_dtype=None, stream
         raise ValueError(f"block_rows must be 1 or {_BLOCK}, got {block_rows}")
     if scale_dtype is None:
         scale_dtype = torch.float8_e8m0fnu
+    q = t = None
+    args = [None, 0, None, 0, None, 0, None, 0]
     with _on(stream):
-        q = None if transposed is True else _empty_blocked(rows, cols, block_rows, scale_dtype, x.device)
-        t = None if transposed is False else _empty_blocked(cols, rows, block_rows, scale_dtype, x.device)
-    args = []
-    for b in (q, t):
-        args += [None, 0, None, 0] if b is None else [b.data.data_ptr(), b.data.stride(0), b.scales.data_ptr(),
-                                                      b.scales.stride(0)]
-    _check(lib.reshard_quantize(rows, cols, x.data_ptr(), pitch, _dtype_code(x.dtype), block_rows,
-                                _dtype_code(scale_dtype), *args, _stream_handle(stream)))
+        if transposed is not True:
+            q, pitch_q, pitch_s = _empty_blocked(x, rows, cols, block_rows, scale_dtype)
+            args[:4] = q.data.data_ptr(), pitch_q, q.scales.data_ptr(), pitch_s
+        if transposed is not False:
+            t, pitch_q, pitch_s = _empty_blocked(x, cols, rows, block_rows, scale_dtype)
+            args[4:] = t.data.data_ptr(), pitch_q, t.scales.data_ptr(), pitch_s
+    status = lib.reshard_quantize(rows, cols, x.data_ptr(), pitch, _dtype_code(x.dtype), block_rows,
+                                  _dtype_code(scale_dtype), *args, _stream_handle(stream))
+    if status != RESHARD_OK:
+        _check(status)
     return (q, t) if transposed == "both" else q if t is None else t
 
 
 def reshard_dequantize(b, dtype, out=None, stream=None):
     """The values of a Blocked, rounded once to dtype (torch.float16, bfloat16 or float32)."""
-    import torch
     lib = _lib or load()
     rows, cols, pitch, spitch = _blocked("b", b)
     with _on(stream):
-        y = torch.empty(b.data.shape, dtype=dtype, device=b.data.device) if out is None else \
-            _like("out", out, b.data.shape, dtype, b.data.device)
-    _check(lib.reshard_dequantize(rows, cols, b.data.data_ptr(), pitch, b.block_rows, b.scales.data_ptr(), spitch,
-                                  _dtype_code(b.scales.dtype), y.data_ptr(), _matrix("out", y)[2],
-                                  _dtype_code(dtype), _stream_handle(stream)))
+        if out is None:
+            y, y_pitch = b.data.new_empty(b.data.shape, dtype=dtype), cols
+        else:
+            y, y_pitch = _like("out", out, b.data.shape, dtype, b.data.device), _matrix("out", out)[2]
+    status = lib.reshard_dequantize(rows, cols, b.data.data_ptr(), pitch, b.block_rows, b.scales.data_ptr(), spitch,
+                                    _dtype_code(b.scales.dtype), y.data_ptr(), y_pitch, _dtype_code(dtype),
+                                    _stream_handle(stream))
+    if status != RESHARD_OK:
+        _check(status)
     return y
 
 
@@ -590,13 +627,20 @@ def reshard_matmul(a, b, out_dtype=None, out=None, accumulate=False, stream=None
     out_dtype = out_dtype or (torch.bfloat16 if out is None else out.dtype)
     sdt, odt = _dtype_code(a.scales.dtype), _dtype_code(out_dtype)
     need = lib.reshard_matmul_workspace(m, n, k, sdt, odt)
+    work = None
     with _on(stream):
-        y = torch.empty(shape, dtype=out_dtype, device=a.data.device) if out is None else \
-            _like("out", out, shape, out_dtype, a.data.device)
-        work = torch.empty(need, dtype=torch.uint8, device=a.data.device) if need > 0 else None
-    _check(lib.reshard_matmul(m, n, k, a.data.data_ptr(), a_pitch, a.block_rows, a.scales.data_ptr(), a_spitch,
-                              b.data.data_ptr(), b_pitch, b.block_rows, b.scales.data_ptr(), b_spitch,
-                              sdt, y.data_ptr(), _matrix("out", y)[2], odt, int(accumulate), _ptr(work), max(0, need), _stream_handle(stream)))
+        if out is None:
+            y, y_pitch = a.data.new_empty(shape, dtype=out_dtype), n
+        else:
+            y, y_pitch = _like("out", out, shape, out_dtype, a.data.device), _matrix("out", out)[2]
+        if need > 0:
+            work = a.data.new_empty(need, dtype=torch.uint8)
+    status = lib.reshard_matmul(m, n, k, a.data.data_ptr(), a_pitch, a.block_rows, a.scales.data_ptr(), a_spitch,
+                                b.data.data_ptr(), b_pitch, b.block_rows, b.scales.data_ptr(), b_spitch, sdt,
+                                y.data_ptr(), y_pitch, odt, int(accumulate), _ptr(work), max(0, need),
+                                _stream_handle(stream))
+    if status != RESHARD_OK:
+        _check(status)
     return y
 
 

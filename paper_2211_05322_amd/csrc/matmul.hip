@@ -33,9 +33,11 @@ typedef bf16 bf16x8 __attribute__((ext_vector_type(8)));
 
 // How a block's products are summed.
 enum Sum {
-    kScaled,  // 8-bit instruction with E8M0 scales
-    kFloat,   // 8-bit instruction, scales applied to its result
-    kExact    // bf16 instruction, scales applied to its result
+    kScaled,   // 8-bit instruction with E8M0 scales
+    kFloat,    // 8-bit instruction, scales applied to its result
+    kUniform,  // the same where all of a wave's rows of B share a scale
+    kExact,    // bf16 instruction, scales applied to its result
+    kWide      // bf16 instruction, E8M0 scales applied as codes are converted
 };
 
 // 32 codes of a row: a lane's share of a block, for the 8-bit instruction as
@@ -50,11 +52,12 @@ struct Wide {
         bf16x8 v[4];
         bf16x2 p[16];
     };
-    __device__ explicit Wide(const Codes &c) {
+    // times a power of two (its exponent 0 stands for 2^-127, 255 gives NaN, as in E8M0)
+    __device__ explicit Wide(const Codes &c, float scale = 1.0f) {
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
-            p[2 * i] = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(c.w[i], 1.0f, false);
-            p[2 * i + 1] = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(c.w[i], 1.0f, true);
+            p[2 * i] = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(c.w[i], scale, false);
+            p[2 * i + 1] = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(c.w[i], scale, true);
         }
     }
 };
@@ -98,15 +101,15 @@ __device__ inline f32x16 zeros() {
 
 // The same for half a block and tiles of 32 x 32, added to p.
 template <Sum SUM>
-__device__ inline f32x16 block_product(const Codes &b, const Codes &a, f32x16 p) {
-    if constexpr (SUM == kExact) {
-        const Wide wb(b), wa(a);
+__device__ inline f32x16 block_product(const Wide &b, const Wide &a, f32x16 p) {
 #pragma unroll
-        for (int s = 0; s < 4; ++s) p = __builtin_amdgcn_mfma_f32_32x32x16_bf16(wb.v[s], wa.v[s], p, 0, 0, 0);
-        return p;
-    } else {
-        return __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(b.v, a.v, p, 0, 0, 0, 0, 0, 0);
-    }
+    for (int s = 0; s < 4; ++s) p = __builtin_amdgcn_mfma_f32_32x32x16_bf16(b.v[s], a.v[s], p, 0, 0, 0);
+    return p;
+}
+
+template <Sum SUM>
+__device__ inline f32x16 block_product(const Codes &b, const Codes &a, f32x16 p) {
+    return __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(b.v, a.v, p, 0, 0, 0, 0, 0, 0);
 }
 
 __device__ inline float scale_value(const Operand &o, int e8m0, int64_t row, int64_t block) {
@@ -332,14 +335,14 @@ struct Stage {
     uint4 words[ROWS * 8];
 };
 
-template <Sum SUM, bool E8M0, int TM, int TN, int WM, int WN>
-__global__ __launch_bounds__(WM *WN *kWave, WM *WN / 4) void matmul_tile_kernel(MatmulArgs g, uint32_t tiles_n, int32_t blocks) {
+template <Sum SUM, int TM, int TN, int WM, int WN>
+__global__ __launch_bounds__(WM *WN *kWave, 2) void matmul_tile_kernel(MatmulArgs g, uint32_t tiles_n, int32_t blocks) {
     constexpr int THREADS = WM * WN * kWave, BM = WM * TM * 32, BN = WN * TN * 32;
     constexpr int LA = BM * 8 / THREADS, LB = BN * 8 / THREADS;  // 16-byte loads a thread and step
     constexpr int ROWS_AT_ONCE = THREADS / 8;
     constexpr int SROWS = (BM + BN) / THREADS;  // scales a thread and step
-    using Given = typename std::conditional<E8M0, uint8_t, float>::type;
-    using Scale = typename std::conditional<SUM == kScaled, uint8_t, float>::type;  // in LDS
+    constexpr bool E8M0 = SUM == kScaled || SUM == kWide;  // else the block's sum is scaled
+    using Scale = typename std::conditional<E8M0, uint8_t, float>::type;
     __shared__ Stage<BM> a_lds0, a_lds1;
     __shared__ Stage<BN> b_lds0, b_lds1;
     __shared__ __align__(16) Scale s_lds[3][BM + BN];  // three: a step's may be read while those two ahead are written
@@ -352,8 +355,8 @@ __global__ __launch_bounds__(WM *WN *kWave, WM *WN / 4) void matmul_tile_kernel(
         const int64_t first = int64_t(blockIdx.y) * blocks;
         g.a.q += first * kBlock;
         g.b.q += first * kBlock;
-        g.a.scales = static_cast<const Given *>(g.a.scales) + first;
-        g.b.scales = static_cast<const Given *>(g.b.scales) + first;
+        g.a.scales = static_cast<const Scale *>(g.a.scales) + first;
+        g.b.scales = static_cast<const Scale *>(g.b.scales) + first;
         g.k = min(g.k - first * kBlock, int64_t(blocks) * kBlock);
         g.out = g.parts + int64_t(blockIdx.y) * g.a.rows * g.b.rows;
         g.out_pitch = g.b.rows;
@@ -386,7 +389,7 @@ __global__ __launch_bounds__(WM *WN *kWave, WM *WN / 4) void matmul_tile_kernel(
     // A row's scales lie a row apart from the next row's, so each load of them
     // touches as many cache lines as it has lanes: two steps' at once.
     using Two = typename std::conditional<E8M0, uint16_t, uint64_t>::type;
-    const Given *s_at[SROWS];
+    const Scale *s_at[SROWS];
     int s_to[SROWS];
     Two s_held[SROWS], s_next[SROWS];
 #pragma unroll
@@ -396,9 +399,9 @@ __global__ __launch_bounds__(WM *WN *kWave, WM *WN / 4) void matmul_tile_kernel(
         const Operand &o = is_a ? g.a : g.b;
         const int rr = is_a ? r : r - BM, T = is_a ? TM : TN;
         const int64_t row = min((is_a ? i0 : j0) + rr, o.rows - 1);
-        s_at[u] = static_cast<const Given *>(o.scales) + (row >> o.row_shift) * o.scales_pitch;
+        s_at[u] = static_cast<const Scale *>(o.scales) + (row >> o.row_shift) * o.scales_pitch;
         // [wave's row][r32][tile]: a lane's scales of all tiles lie together
-        s_to[u] = is_a || SUM == kScaled ? (is_a ? 0 : BM) + rr / (T * 32) * (T * 32) + rr % 32 * T + rr / 32 % T : r;
+        s_to[u] = is_a || E8M0 ? (is_a ? 0 : BM) + rr / (T * 32) * (T * 32) + rr % 32 * T + rr / 32 % T : r;
     }
     // Of blocks s and s + 1; past the last, any.  Nothing is computed from
     // what is loaded before it is put into LDS, so that nothing waits for it.
@@ -406,16 +409,12 @@ __global__ __launch_bounds__(WM *WN *kWave, WM *WN / 4) void matmul_tile_kernel(
 #pragma unroll
         for (int u = 0; u < SROWS; ++u) to[u] = load_any<Two>(s_at[u] + min(s, steps - 2));
     };
-    auto in_lds = [](Two w) -> Scale {
-        if constexpr (SUM == kScaled) return uint8_t(w);
-        else if constexpr (E8M0) return e8m0_value(uint8_t(w));
-        else return __uint_as_float(uint32_t(w));
-    };
     auto put_scales = [&](int buf, int32_t s, int32_t block) {  // block's, from those loaded for s and s + 1
         const int shift = block > min(s, steps - 2) ? 4 * int(sizeof(Two)) : 0;
 #pragma unroll
         for (int u = 0; u < SROWS; ++u) {
-            s_lds[buf][s_to[u]] = in_lds(Two(s_held[u] >> shift));
+            const Two w = Two(s_held[u] >> shift);
+            __builtin_memcpy(&s_lds[buf][s_to[u]], &w, sizeof(Scale));
         }
     };
 
@@ -447,17 +446,20 @@ __global__ __launch_bounds__(WM *WN *kWave, WM *WN / 4) void matmul_tile_kernel(
         if constexpr (decltype(part)::value == 1 && decltype(x)::value >= TWO) return fa_odd[decltype(x)::value - TWO];
         else return fa[decltype(x)::value];
     };
-    int ka[2], kb[2];  // kScaled: the tiles' exponents, a byte each
-    float kf[2][TM];   // else: A's scales
+    int ka[2], kb[2];  // E8M0: the tiles' exponents, a byte each
+    float kf[2][TM];   // else: A's scales (kUniform: times B's)
     auto read_scales = [&](const Scale *sc, int into) {
-        if constexpr (SUM == kScaled) {
+        if constexpr (E8M0) {
             using Bytes_m = typename std::conditional<TM == 4, uint32_t, uint16_t>::type;
             using Bytes_n = typename std::conditional<TN == 4, uint32_t, uint16_t>::type;
             ka[into] = *reinterpret_cast<const Bytes_m *>(&sc[wi * TM * 32 + r32 * TM]);
             kb[into] = *reinterpret_cast<const Bytes_n *>(&sc[BM + wj * TN * 32 + r32 * TN]);
         } else {
 #pragma unroll
-            for (int x = 0; x < TM; ++x) kf[into][x] = sc[wi * TM * 32 + r32 * TM + x];
+            for (int x = 0; x < TM; ++x) {
+                kf[into][x] = sc[wi * TM * 32 + r32 * TM + x];
+                if constexpr (SUM == kUniform) kf[into][x] *= sc[BM + wj * TN * 32];
+            }
         }
     };
 
@@ -469,8 +471,13 @@ __global__ __launch_bounds__(WM *WN *kWave, WM *WN / 4) void matmul_tile_kernel(
         const Codes &a = frag_a(part, x_), &b = fb[part][y];
         if constexpr (SUM == kScaled) {
             acc[x][y] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(b.v, a.v, acc[x][y], 0, 0, y, kb[cur], x, ka[cur]);
+        } else if constexpr (SUM == kWide) {
+            auto scale = [](int codes, int i) { return __uint_as_float((uint32_t(codes) >> (8 * i) & 255) << 23); };
+            acc[x][y] = block_product<SUM>(Wide(b, scale(kb[cur], y)), Wide(a, scale(ka[cur], x)), acc[x][y]);
         } else {
-            sum[x][y] = block_product<SUM>(b, a, decltype(part)::value ? sum[x][y] : zeros());
+            const f32x16 before = decltype(part)::value ? sum[x][y] : zeros();
+            if constexpr (SUM == kExact) sum[x][y] = block_product<SUM>(Wide(b), Wide(a), before);
+            else sum[x][y] = block_product<SUM>(b, a, before);
         }
     };
     // A row of tiles' sums over the block, scaled, to the results.
@@ -479,11 +486,12 @@ __global__ __launch_bounds__(WM *WN *kWave, WM *WN / 4) void matmul_tile_kernel(
         unrolled<TN>([&](auto y) {
             unrolled<4>([&](auto q_) {
                 constexpr int q = decltype(q_)::value;
-                const f32x4 sb =
-                    *reinterpret_cast<const f32x4 *>(&s_lds[sbuf][BM + (wj * TN + y) * 32 + q * 8 + half * 4]);
+                f32x4 k{kf[cur][x], kf[cur][x], kf[cur][x], kf[cur][x]};
+                if constexpr (SUM != kUniform)
+                    k *= *reinterpret_cast<const f32x4 *>(&s_lds[sbuf][BM + (wj * TN + y) * 32 + q * 8 + half * 4]);
 #pragma unroll
                 for (int e = 0; e < 4; ++e)
-                    acc[x][y][q * 4 + e] = fmaf(sum[x][y][q * 4 + e], kf[cur][x] * sb[e], acc[x][y][q * 4 + e]);
+                    acc[x][y][q * 4 + e] = fmaf(sum[x][y][q * 4 + e], k[e], acc[x][y][q * 4 + e]);
             });
         });
     };
@@ -505,11 +513,11 @@ __global__ __launch_bounds__(WM *WN *kWave, WM *WN / 4) void matmul_tile_kernel(
             load(x_);
             unrolled<TN>([&](auto y) { product(cur, part, x_, y); });
             // the row before this one, whose products are done by now
-            if constexpr (SUM != kScaled && decltype(part)::value == 1 && x > 0)
+            if constexpr (!E8M0 && decltype(part)::value == 1 && x > 0)
                 scale_row(cur, std::integral_constant<int, x - 1>{});
             __builtin_amdgcn_sched_barrier(0);
         });
-        if constexpr (SUM != kScaled && decltype(part)::value == 1) scale_row(cur, std::integral_constant<int, TM - 1>{});
+        if constexpr (!E8M0 && decltype(part)::value == 1) scale_row(cur, std::integral_constant<int, TM - 1>{});
     };
     auto step = [&](auto cur_, int32_t s, auto &a_cur, auto &b_cur, auto &a_next, auto &b_next) {
         constexpr int cur = decltype(cur_)::value, EACH = (LA + LB + TM - 1) / TM;
@@ -565,10 +573,7 @@ __global__ __launch_bounds__(WM *WN *kWave, WM *WN / 4) void matmul_tile_kernel(
         for (int u = 0; u < LB; ++u)
             b_lds0.words[u * THREADS + t] = load_codes(g.b, j0 + lrow + u * ROWS_AT_ONCE, l, g.k);
 #pragma unroll
-        for (int u = 0; u < SROWS; ++u) {
-            if constexpr (E8M0) s_lds[0][s_to[u]] = in_lds(s_at[u][s]);
-            else s_lds[0][s_to[u]] = s_at[u][s];
-        }
+        for (int u = 0; u < SROWS; ++u) s_lds[0][s_to[u]] = s_at[u][s];
         sbuf = 0;
         __syncthreads();
         read_scales(s_lds[0], 0);
@@ -849,11 +854,13 @@ extern "C" reshard_status_t reshard_matmul(int64_t m, int64_t n, int64_t k, cons
         }
         const dim3 grid(unsigned(p.tiles_m * p.tiles_n), unsigned(p.parts));
         const uint32_t tn = uint32_t(p.tiles_n);
-        if (sum == kExact && g.e8m0) matmul_tile_kernel<kExact, true, 2, 2, 2, 2><<<grid, 256, 0, s>>>(g, tn, p.blocks);
-        else if (sum == kExact) matmul_tile_kernel<kExact, false, 2, 2, 2, 2><<<grid, 256, 0, s>>>(g, tn, p.blocks);
-        else if (sum == kFloat) matmul_tile_kernel<kFloat, false, 2, 2, 2, 2><<<grid, 256, 0, s>>>(g, tn, p.blocks);
-        else if (p.large) matmul_tile_kernel<kScaled, true, 4, 2, 2, 4><<<grid, 512, 0, s>>>(g, tn, p.blocks);
-        else matmul_tile_kernel<kScaled, true, 2, 2, 2, 2><<<grid, 256, 0, s>>>(g, tn, p.blocks);
+        auto launch = [&](auto kernel, int threads) { kernel<<<grid, threads, 0, s>>>(g, tn, p.blocks); };
+        if (sum == kExact && g.e8m0) launch(matmul_tile_kernel<kWide, 2, 2, 2, 2>, 256);
+        else if (sum == kExact) launch(matmul_tile_kernel<kExact, 2, 2, 2, 2>, 256);
+        else if (sum == kFloat && b_block_rows == kBlock) launch(matmul_tile_kernel<kUniform, 2, 2, 2, 2>, 256);
+        else if (sum == kFloat) launch(matmul_tile_kernel<kFloat, 2, 2, 2, 2>, 256);
+        else if (p.large) launch(matmul_tile_kernel<kScaled, 4, 2, 2, 4>, 512);
+        else launch(matmul_tile_kernel<kScaled, 2, 2, 2, 2>, 256);
         if (p.parts > 1) {
             const reshard_status_t started = launched("matmul launch");
             if (started != RESHARD_OK) return started;
