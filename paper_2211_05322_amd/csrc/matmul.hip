@@ -626,119 +626,98 @@ __global__ __launch_bounds__(256) void matmul_join_kernel(MatmulArgs g, int part
     }
 }
 
-// Few rows of A: the weights' bytes are the work.  A workgroup takes 16 NT
-// rows of B and all of A's; its waves deal the blocks of the reduction among
-// them, load their fragments straight into registers, and add their sums
-// through LDS.  Nothing is loaded twice but A, which the caches hold.
-template <Sum SUM, int MT, int NT, int WAVES>
+// Few rows of A: the weights' bytes are the work.  A workgroup takes 16 rows
+// of B and all of A's (at most 16); its waves deal the blocks of the reduction
+// among them, load DEPTH blocks' fragments at once straight into registers,
+// and add their sums through LDS.
+template <Sum SUM, int WAVES, int DEPTH>
 __global__ __launch_bounds__(WAVES *kWave) void matmul_few_kernel(MatmulArgs g) {
-    constexpr int DEPTH = MT * NT > 4 ? 1 : 2;  // blocks loaded together
-    __shared__ f32x4 part[WAVES][MT * NT][kWave];
+    __shared__ f32x4 part[WAVES][kWave];
     const int lane = threadIdx.x % kWave, wave = threadIdx.x / kWave, r16 = lane % 16, quad = lane / 16;
-    const int64_t j0 = int64_t(blockIdx.x) * 16 * NT;
-    const int32_t steps = int32_t(ceil_div(g.k, kBlock));
-    f32x4 acc[MT][NT];
-#pragma unroll
-    for (int x = 0; x < MT; ++x)
-#pragma unroll
-        for (int y = 0; y < NT; ++y) acc[x][y] = f32x4{0, 0, 0, 0};
+    const int64_t j0 = int64_t(blockIdx.x) * 16;
+    const int32_t steps = int32_t(ceil_div(g.k, kBlock)), full = int32_t(g.k / kBlock);
+    // rows past a matrix's end repeat its last, whose results are not stored
+    const int64_t i = min(int64_t(r16), g.a.rows - 1), j = min(j0 + r16, g.b.rows - 1);
+    const uint8_t *a_at = g.a.q + i * g.a.pitch + quad * 16, *b_at = g.b.q + j * g.b.pitch + quad * 16;
+    f32x4 acc{0, 0, 0, 0};
 
-    auto blocks = [&](int32_t s0, auto depth_) {
-        constexpr int D = decltype(depth_)::value;
-        Codes fa[D][MT], fb[D][NT];
-        float ka[D][MT], kb[D][NT][4];
-        int ea[D][MT], eb[D][NT];
+    // blocks s0, s0 + WAVES, ..., `depth` of them; `whole`: none is the short one at the end
+    auto blocks = [&](int32_t s0, auto depth, auto whole) {
+        constexpr int D = decltype(depth)::value;
+        Codes fa[D], fb[D];
+        float ka[D], kb[D][4];
+        int ea[D], eb[D];
+        auto load = [&](const Operand &o, const uint8_t *at, int64_t row, int64_t s) {
+            Codes c;
+            if constexpr (decltype(whole)::value) {
+                c.h[0] = load_any<uint4>(at + s * kBlock);
+                c.h[1] = load_any<uint4>(at + s * kBlock + 64);
+            } else {
+                c.h[0] = load_codes(o, row, s * kBlock + quad * 16, g.k);
+                c.h[1] = load_codes(o, row, s * kBlock + quad * 16 + 64, g.k);
+            }
+            return c;
+        };
 #pragma unroll
         for (int d = 0; d < D; ++d) {
-            const int64_t s = s0 + d * WAVES, l = s * kBlock + quad * 16;
-#pragma unroll
-            for (int y = 0; y < NT; ++y) {
-                const int64_t j = j0 + y * 16 + r16;
-                fb[d][y].h[0] = load_codes(g.b, j, l, g.k);
-                fb[d][y].h[1] = load_codes(g.b, j, l + 64, g.k);
-            }
-#pragma unroll
-            for (int x = 0; x < MT; ++x) {
-                fa[d][x].h[0] = load_codes(g.a, x * 16 + r16, l, g.k);
-                fa[d][x].h[1] = load_codes(g.a, x * 16 + r16, l + 64, g.k);
-            }
+            const int64_t s = s0 + d * WAVES;
+            fb[d] = load(g.b, b_at, j, s);
+            fa[d] = load(g.a, a_at, i, s);
             if constexpr (SUM == kScaled) {
-#pragma unroll
-                for (int y = 0; y < NT; ++y) eb[d][y] = scale_code(g.b, min(j0 + y * 16 + r16, g.b.rows - 1), s);
-#pragma unroll
-                for (int x = 0; x < MT; ++x) ea[d][x] = scale_code(g.a, min(int64_t(x * 16 + r16), g.a.rows - 1), s);
+                eb[d] = scale_code(g.b, j, s);
+                ea[d] = scale_code(g.a, i, s);
             } else {
 #pragma unroll
-                for (int y = 0; y < NT; ++y)
-#pragma unroll
-                    for (int e = 0; e < 4; ++e)
-                        kb[d][y][e] = scale_value(g.b, g.e8m0, min(j0 + y * 16 + quad * 4 + e, g.b.rows - 1), s);
-#pragma unroll
-                for (int x = 0; x < MT; ++x)
-                    ka[d][x] = scale_value(g.a, g.e8m0, min(int64_t(x * 16 + r16), g.a.rows - 1), s);
+                for (int e = 0; e < 4; ++e)
+                    kb[d][e] = scale_value(g.b, 0, min(j0 + quad * 4 + e, g.b.rows - 1), s);
+                ka[d] = scale_value(g.a, 0, i, s);
             }
         }
 #pragma unroll
-        for (int d = 0; d < D; ++d)
+        for (int d = 0; d < D; ++d) {
+            if constexpr (SUM == kScaled) {
+                acc = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(fb[d].v, fa[d].v, acc, 0, 0, 0, eb[d], 0, ea[d]);
+            } else {
+                const f32x4 p = block_product(fb[d], fa[d]);
 #pragma unroll
-            for (int y = 0; y < NT; ++y) {
-                const typename std::conditional<SUM == kExact, Wide, Codes>::type b(fb[d][y]);
-#pragma unroll
-                for (int x = 0; x < MT; ++x) {
-                    if constexpr (SUM == kScaled) {
-                        acc[x][y] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(b.v, fa[d][x].v, acc[x][y], 0, 0, 0,
-                                                                                     eb[d][y], 0, ea[d][x]);
-                    } else {
-                        const typename std::conditional<SUM == kExact, Wide, Codes>::type a(fa[d][x]);
-                        const f32x4 p = block_product(b, a);
-#pragma unroll
-                        for (int e = 0; e < 4; ++e)
-                            acc[x][y][e] = fmaf(p[e], ka[d][x] * kb[d][y][e], acc[x][y][e]);
-                    }
-                }
+                for (int e = 0; e < 4; ++e) acc[e] = fmaf(p[e], ka[d] * kb[d][e], acc[e]);
             }
+        }
     };
+    constexpr std::integral_constant<int, 1> one{};
+    constexpr std::integral_constant<bool, true> whole{};
     int32_t s = wave;
-    for (; s + (DEPTH - 1) * WAVES < steps; s += DEPTH * WAVES) blocks(s, std::integral_constant<int, DEPTH>{});
-    if constexpr (DEPTH > 1) {
-        for (; s < steps; s += WAVES) blocks(s, std::integral_constant<int, 1>{});
-    }
+    for (; s + (DEPTH - 1) * WAVES < full; s += DEPTH * WAVES) blocks(s, std::integral_constant<int, DEPTH>{}, whole);
+    for (; s < full; s += WAVES) blocks(s, one, whole);
+    if (s < steps) blocks(s, one, std::integral_constant<bool, false>{});
 
-#pragma unroll
-    for (int x = 0; x < MT; ++x)
-#pragma unroll
-        for (int y = 0; y < NT; ++y) part[wave][x * NT + y][lane] = acc[x][y];
+    part[wave][lane] = acc;
     __syncthreads();
-    for (int at = threadIdx.x; at < MT * NT * kWave; at += WAVES * kWave) {
-        const int tile = at / kWave, l = at % kWave;
-        f32x4 v = part[0][tile][l];
+    if (wave == 0) {
 #pragma unroll
-        for (int w = 1; w < WAVES; ++w) {
-            const f32x4 o = part[w][tile][l];
-#pragma unroll
-            for (int e = 0; e < 4; ++e) v[e] += o[e];
-        }
-        const int64_t i = tile / NT * 16 + l % 16, j = j0 + tile % NT * 16 + l / 16 * 4;
-        if (i < g.a.rows && j < g.b.rows) store_any_type(g, i, j, v);
+        for (int w = 1; w < WAVES; ++w) acc += part[w][lane];
+        if (r16 < g.a.rows && j0 + quad * 4 < g.b.rows) store_any_type(g, r16, j0 + quad * 4, acc);
     }
 }
 
-// How a product is launched: with few rows of A by its weights' rows alone;
-// otherwise in tiles of 256 x 256 (16-bit results of E8M0 operands) or
-// 128 x 128, and where those are too few for the 256 CUs, the reduction
-// split into parts that are joined.
+// How a product is launched: up to 8 rows of A into 16-bit results by its
+// weights' rows alone (1 x 12288 x 12288: 31 us against 37 in tiles; 8 x 5120 x
+// 5120: 11 against 15; but 16 x 15360 x 5120: 29 against 23); otherwise in tiles
+// of 256 x 256 (16-bit results of E8M0 operands, where there are enough of
+// them) or 128 x 128, and where those are too few for the 256 CUs, the
+// reduction split into parts that are joined.
 struct Plan {
     bool few, large;
     int64_t tile, tiles_m, tiles_n;
     int32_t parts, blocks;  // parts of the reduction, and the blocks of each
 };
 
-Plan plan_matmul(int64_t m, int64_t n, int64_t k, bool scaled) {
+Plan plan_matmul(int64_t m, int64_t n, int64_t k, Sum sum) {
     Plan p{};
-    p.few = m <= 64;
+    p.few = m <= 8 && sum != kExact;
     const int64_t steps = ceil_div(k, kBlock);
     auto tiles = [&](int64_t side) { return ceil_div(m, side) * ceil_div(n, side); };
-    p.large = scaled && tiles(256) >= 192;
+    p.large = sum == kScaled && tiles(256) >= 192;
     p.tile = p.large ? 256 : 128;
     p.tiles_m = ceil_div(m, p.tile);
     p.tiles_n = ceil_div(n, p.tile);
@@ -752,17 +731,15 @@ Plan plan_matmul(int64_t m, int64_t n, int64_t k, bool scaled) {
     return p;
 }
 
+Sum sum_for(reshard_dtype_t scale_dtype, reshard_dtype_t out_dtype) {
+    return out_dtype == RESHARD_F32 ? kExact : scale_dtype == RESHARD_E8M0 ? kScaled : kFloat;
+}
+
 template <Sum SUM>
 void launch_few(const MatmulArgs &g, hipStream_t s) {
-    const int64_t m = g.a.rows, n = g.b.rows;
-    if (m <= 16) {
-        if (ceil_div(n, 16) >= 256) matmul_few_kernel<SUM, 1, 1, 4><<<dim3(unsigned(ceil_div(n, 16))), 256, 0, s>>>(g);
-        else matmul_few_kernel<SUM, 1, 1, 16><<<dim3(unsigned(ceil_div(n, 16))), 1024, 0, s>>>(g);
-    } else if (m <= 32) {
-        matmul_few_kernel<SUM, 2, 1, 8><<<dim3(unsigned(ceil_div(n, 16))), 512, 0, s>>>(g);
-    } else {
-        matmul_few_kernel<SUM, 4, 2, 8><<<dim3(unsigned(ceil_div(n, 32))), 512, 0, s>>>(g);
-    }
+    const dim3 grid(unsigned(ceil_div(g.b.rows, 16)));
+    if (grid.x >= 256) matmul_few_kernel<SUM, 4, 8><<<grid, 4 * kWave, 0, s>>>(g);
+    else matmul_few_kernel<SUM, 16, 2><<<grid, 16 * kWave, 0, s>>>(g);  // more waves a row where rows are few
 }
 
 reshard_status_t check_operand(const char *name, const char *scales_name, const void *q, int64_t rows, int64_t k,
@@ -785,7 +762,7 @@ extern "C" int64_t reshard_matmul_workspace(int64_t m, int64_t n, int64_t k, res
                                             reshard_dtype_t out_dtype) {
     if (m < 0 || n < 0 || k < 0 || m > int64_t(1) << 40 || n > int64_t(1) << 40 || k > int64_t(1) << 36) return -1;
     if (m == 0 || n == 0) return 0;
-    const rs::Plan p = rs::plan_matmul(m, n, k, scale_dtype == RESHARD_E8M0 && out_dtype != RESHARD_F32);
+    const rs::Plan p = rs::plan_matmul(m, n, k, rs::sum_for(scale_dtype, out_dtype));
     return p.parts > 1 ? int64_t(p.parts) * m * n * int64_t(sizeof(float)) : 0;
 }
 
@@ -824,11 +801,10 @@ extern "C" reshard_status_t reshard_matmul(int64_t m, int64_t n, int64_t k, cons
         g.accumulate = accumulate;
         g.e8m0 = scale_dtype == RESHARD_E8M0;
         const hipStream_t s = static_cast<hipStream_t>(stream);
-        const Sum sum = out_dtype == RESHARD_F32 ? kExact : g.e8m0 ? kScaled : kFloat;
-        const Plan p = plan_matmul(m, n, k, sum == kScaled);
+        const Sum sum = sum_for(scale_dtype, out_dtype);
+        const Plan p = plan_matmul(m, n, k, sum);
         if (p.few) {
-            if (sum == kExact) launch_few<kExact>(g, s);
-            else if (sum == kScaled) launch_few<kScaled>(g, s);
+            if (sum == kScaled) launch_few<kScaled>(g, s);
             else launch_few<kFloat>(g, s);
             return launched("matmul launch");
         }
