@@ -460,6 +460,11 @@ def _on(stream):
     return torch.cuda.stream(torch.cuda.ExternalStream(stream) if isinstance(stream, int) else stream)
 
 
+def _on_gpu(name, t):
+    if not t.is_cuda:
+        raise ValueError(f"{name} must be on the GPU, got {t.device}")
+
+
 def _ptr(t):
     return None if t is None else t.data_ptr()
 
@@ -483,6 +488,9 @@ def reshard_layer_norm(x, weight=None, bias=None, eps=1e-5, out=None, stream=Non
         _dense("weight", weight, (cols,), x.device, wdt)
     if bias is not None:
         _dense("bias", bias, (cols,), x.device, wdt)
+    if out is not None:
+        _like("out", out, x.shape, x.dtype, x.device)
+    _on_gpu("x", x)
     with _on(stream):
         y, y_pitch = _result(out, x)
         mean, rstd = x.new_empty((2, *x.shape[:-1]), dtype=torch.float32).unbind()
@@ -508,6 +516,7 @@ def reshard_layer_norm_backward(dy, x, weight, mean, rstd, dweight=None, dbias=N
     _dense("rstd", rstd, x.shape[:-1], x.device, torch.float32)
     if accumulate and (dweight is None or dbias is None):
         raise ValueError("accumulate needs the dweight and dbias to add to")
+    _on_gpu("x", x)
     need = lib.reshard_layer_norm_backward_workspace(rows, cols)
     with _on(stream):
         dx, dx_pitch = _result(out, x)
@@ -574,6 +583,7 @@ def reshard_quantize(x, block_rows=1, transposed=False, scale_dtype=None, stream
         raise ValueError(f"block_rows must be 1 or {_BLOCK}, got {block_rows}")
     if scale_dtype is None:
         scale_dtype = torch.float8_e8m0fnu
+    _on_gpu("x", x)
     q = t = None
     args = [None, 0, None, 0, None, 0, None, 0]
     with _on(stream):
@@ -594,6 +604,7 @@ def reshard_dequantize(b, dtype, out=None, stream=None):
     """The values of a Blocked, rounded once to dtype (torch.float16, bfloat16 or float32)."""
     lib = _lib or load()
     rows, cols, pitch, spitch = _blocked("b", b)
+    _on_gpu("b", b.data)
     with _on(stream):
         if out is None:
             y, y_pitch = b.data.new_empty(b.data.shape, dtype=dtype), cols
@@ -623,6 +634,9 @@ def reshard_matmul(a, b, out_dtype=None, out=None, accumulate=False, stream=None
         raise ValueError(f"a is on {a.data.device}, b on {b.data.device}")
     if accumulate and out is None:
         raise ValueError("accumulate needs the out to add to")
+    if out is not None:
+        _like("out", out, (*a.data.shape[:-1], n), out_dtype or out.dtype, a.data.device)
+    _on_gpu("a", a.data)
     shape = (*a.data.shape[:-1], n)
     out_dtype = out_dtype or (torch.bfloat16 if out is None else out.dtype)
     sdt, odt = _dtype_code(a.scales.dtype), _dtype_code(out_dtype)

@@ -363,8 +363,7 @@ __global__ __launch_bounds__(WM *WN *kWave, 2) void matmul_tile_kernel(MatmulArg
         g.out_dtype = RESHARD_F32;
         g.accumulate = 0;
     }
-    const int32_t steps = int32_t(ceil_div(g.k, kBlock));
-    const int32_t paired = int32_t(g.k / (2 * kBlock)) * 2;  // whole blocks, two at a time
+    const int32_t steps = int32_t(ceil_div(g.k, kBlock)), whole = int32_t(g.k / kBlock);
 
     // rows past a matrix's end are read as zeros
     const int lrow = t / 8, lword = (t % 8) ^ ((lrow / 2) % 8);
@@ -522,7 +521,7 @@ __global__ __launch_bounds__(WM *WN *kWave, 2) void matmul_tile_kernel(MatmulArg
     auto step = [&](auto cur_, int32_t s, auto &a_cur, auto &b_cur, auto &a_next, auto &b_next) {
         constexpr int cur = decltype(cur_)::value, EACH = (LA + LB + TM - 1) / TM;
         const int snext = sbuf == 2 ? 0 : sbuf + 1;
-        const int32_t ahead = min(s + 2, paired - 1);
+        const int32_t ahead = min(s + 2, whole - 1);
         phase(cur_, low, a_cur, b_cur, [](auto) {});
         // the last step's reads ahead find an older block, which is not used
         put_scales(snext, s + 1 - cur, s + 1);
@@ -544,7 +543,7 @@ __global__ __launch_bounds__(WM *WN *kWave, 2) void matmul_tile_kernel(MatmulArg
         sbuf = snext;
     };
 
-    if (paired > 0) {
+    if (whole > 1) {
         load_scales(0, s_held);
         stage(0, a_lds0, b_lds0);
         put_scales(0, 0, 0);
@@ -556,15 +555,16 @@ __global__ __launch_bounds__(WM *WN *kWave, 2) void matmul_tile_kernel(MatmulArg
         read_scales(s_lds[0], 0);
         unrolled<TM>([&](auto x) { fa[x] = read(a_lds0, a_word, 0, x); });
         unrolled<TN>([&](auto y) { fb[0][y] = read(b_lds0, b_word, 0, y); });
-        for (int32_t s = 0; s < paired; s += 2) {
+        for (int32_t s = 0; s + 1 < whole; s += 2) {
             step(low, s, a_lds0, b_lds0, a_lds1, b_lds1);
             step(high, s + 1, a_lds1, b_lds1, a_lds0, b_lds0);
         }
+        if (whole & 1) step(low, whole - 1, a_lds0, b_lds0, a_lds1, b_lds1);
         loads_done();
         __syncthreads();
     }
 #pragma unroll 1
-    for (int32_t s = paired; s < steps; ++s) {  // an odd block and a short one, whose missing codes are zeros
+    for (int32_t s = whole > 1 ? whole : 0; s < steps; ++s) {  // the short block, whose missing codes are zeros
         const int64_t l = int64_t(s) * kBlock + lword * 16;
 #pragma unroll 1
         for (int u = 0; u < LA; ++u)
@@ -717,7 +717,8 @@ Plan plan_matmul(int64_t m, int64_t n, int64_t k, Sum sum) {
     p.few = m <= 8 && sum != kExact;
     const int64_t steps = ceil_div(k, kBlock);
     auto tiles = [&](int64_t side) { return ceil_div(m, side) * ceil_div(n, side); };
-    p.large = sum == kScaled && tiles(256) >= 192;
+    // rounds of tiles over the CUs: one of 256 x 256 each, or two of 128 x 128 in 2/3 of its time (not 1/2)
+    p.large = sum == kScaled && ceil_div(tiles(256), 256) * 3 <= ceil_div(tiles(128), 512) * 2;
     p.tile = p.large ? 256 : 128;
     p.tiles_m = ceil_div(m, p.tile);
     p.tiles_n = ceil_div(n, p.tile);

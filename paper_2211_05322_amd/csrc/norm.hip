@@ -196,7 +196,7 @@ struct NormGradArgs {
     const void *dy, *x, *weight;
     const float *mean, *rstd;
     void *dx;
-    float *partial;  // [groups][2][cols]: sums of dy xhat, then of dy, over the rows of one group
+    float *partial;  // [workgroups][2][cols]: sums of dy xhat, then of dy, over a workgroup's rows
     int64_t rows, cols, dy_pitch, x_pitch, dx_pitch;
     int weight_dtype;
 };
@@ -287,16 +287,34 @@ __global__ __launch_bounds__(THREADS < 256 ? 256 : THREADS) void norm_grad_kerne
             }
         }
     }
-    if (a.partial && group < a.rows) {
-        float *out = a.partial + group * 2 * a.cols;
+    if (!a.partial) return;
+    float *out = a.partial + int64_t(blockIdx.x) * 2 * a.cols;
+    if constexpr (ROWS > 1) {  // the waves of a workgroup add up in LDS, one after the other
+        float *sums = weights + ceil_div(a.cols, V) * V;
+        for (int r = 0; r < ROWS; ++r) {
+            __syncthreads();
+            if (threadIdx.x / THREADS != r) continue;
 #pragma unroll
-        for (int k = 0; k < NV; ++k) {
-            if (my.any(k)) {
+            for (int k = 0; k < NV; ++k)
 #pragma unroll
-                for (int i = 0; i < V; i += 4) {  // elements that are another's have the same sums
-                    store_any(out + my.at(k) + i, make_float4(dw[k][i], dw[k][i + 1], dw[k][i + 2], dw[k][i + 3]));
-                    store_any(out + a.cols + my.at(k) + i, make_float4(db[k][i], db[k][i + 1], db[k][i + 2], db[k][i + 3]));
+                for (int i = 0; i < V; ++i) {
+                    if (!my.mine(k, i)) continue;
+                    float *w = sums + my.at(k) + i, *b = w + a.cols;
+                    *w = r ? *w + dw[k][i] : dw[k][i];
+                    *b = r ? *b + db[k][i] : db[k][i];
                 }
+        }
+        __syncthreads();
+        for (int64_t c = threadIdx.x; c < 2 * a.cols; c += blockDim.x) out[c] = sums[c];
+        return;
+    }
+#pragma unroll
+    for (int k = 0; k < NV; ++k) {
+        if (my.any(k)) {
+#pragma unroll
+            for (int i = 0; i < V; i += 4) {  // elements that are another's have the same sums
+                store_any(out + my.at(k) + i, make_float4(dw[k][i], dw[k][i + 1], dw[k][i + 2], dw[k][i + 3]));
+                store_any(out + a.cols + my.at(k) + i, make_float4(db[k][i], db[k][i + 1], db[k][i + 2], db[k][i + 3]));
             }
         }
     }
@@ -461,7 +479,8 @@ void launch_norm(const NormArgs &a, hipStream_t s) {
     if (!done) norm_long_kernel<T><<<dim3(unsigned(std::min(a.rows, kMaxGrid))), 1024, 0, s>>>(a);
 }
 
-// Groups of rows whose column sums are kept apart until the join.
+// Workgroups of the backward pass, whose column sums are kept apart until the
+// join: two a CU; one where rows are long and their sums cost the most.
 int64_t norm_groups(int64_t rows, int64_t cols) { return std::min<int64_t>(rows, cols > 8192 ? 256 : 512); }
 
 template <typename T>
@@ -469,8 +488,9 @@ void launch_norm_grad(const NormGradArgs &a, int64_t groups, hipStream_t s) {
     // 16384 columns: the sums of more do not fit
     const bool done = with_columns<kVec<T>, 4, 16384 / kVec<T>>(a.cols, [&](auto threads, auto n) {
         constexpr int THREADS = decltype(threads)::value, ROWS = THREADS < 256 ? 256 / THREADS : 1;
-        const dim3 grid(unsigned(ceil_div(groups, ROWS)));
-        const size_t lds = size_t(ceil_div(a.cols, kVec<T>)) * kVec<T> * sizeof(float);
+        const dim3 grid{unsigned(groups)};
+        const size_t padded = size_t(ceil_div(a.cols, kVec<T>)) * kVec<T>;
+        const size_t lds = (padded + (ROWS > 1 ? 2 * a.cols : 0)) * sizeof(float);
         norm_grad_kernel<T, THREADS, decltype(n)::value><<<grid, THREADS < 256 ? 256 : THREADS, lds, s>>>(a);
     });
     if (done) return;

@@ -674,6 +674,9 @@ def test_binding_refusals():
             (lambda: B.reshard_dequantize(B.Blocked(codes, ones, 128), torch.float32), "scales must be"),
             (lambda: B.reshard_matmul(b, B.Blocked(codes[:, :299], ones)), "columns"),
             (lambda: B.reshard_matmul(b, B.Blocked(codes, ones.to(E8M0))), "scales"),
+            (lambda: B.reshard_layer_norm(x), "on the GPU"), (lambda: B.reshard_quantize(x), "on the GPU"),
+            (lambda: B.reshard_layer_norm_backward(x, x, None, x[:, 0].clone(), x[:, 0].clone()), "on the GPU"),
+            (lambda: B.reshard_dequantize(b, torch.float32), "on the GPU"), (lambda: B.reshard_matmul(b, b), "on the GPU"),
             (lambda: B.reshard_matmul(b, b, accumulate=True), "accumulate"),
             (lambda: B.reshard_matmul(b, b, torch.float32, out=torch.empty(4, 5)), "out")):
         with pytest.raises(ValueError, match=text):
