@@ -570,9 +570,9 @@ def _blocked(name, b):
 
 
 def reshard_quantize(x, block_rows=1, transposed=False, scale_dtype=None, stream=None):
-    """x in 8 bits with a power-of-two scale per block (Blocked, rows of x's
-    leading dimensions together).  transposed=True: of x transposed, blocks
-    along x's rows; "both": the pair, from one reading of x.  scale_dtype:
+    """x in 8 bits with a power-of-two scale per block (Blocked; x's leading
+    dimensions are kept, and count as rows).  transposed=True: of x as a matrix
+    of rows, transposed, with blocks along x's rows; "both": the pair, from one reading of x.  scale_dtype:
     torch.float8_e8m0fnu (default) or torch.float32."""
     import torch
     lib = _lib or load()
@@ -597,6 +597,9 @@ def reshard_quantize(x, block_rows=1, transposed=False, scale_dtype=None, stream
                                   _dtype_code(scale_dtype), *args, _stream_handle(stream))
     if status != RESHARD_OK:
         _check(status)
+    if q is not None and x.dim() > 2:
+        scales = q.scales.unflatten(0, x.shape[:-1]) if block_rows == 1 else q.scales
+        q = Blocked(q.data.unflatten(0, x.shape[:-1]), scales, block_rows)
     return (q, t) if transposed == "both" else q if t is None else t
 
 
