@@ -78,6 +78,7 @@ struct NormArgs {
     int64_t rows, cols, x_pitch, y_pitch;
     float eps;
     int weight_dtype;
+    bool past_cache;  // y is larger than the last-level cache
 };
 
 // THREADS threads hold a row, 256 / THREADS rows a workgroup where a wave
@@ -142,7 +143,9 @@ __global__ __launch_bounds__(THREADS < 256 ? 256 : THREADS) void norm_kernel(Nor
             Pack<T> r;
 #pragma unroll
             for (int i = 0; i < V; ++i) r.e[i] = T((float(p[k].e[i]) - mean) * rstd * w[k][i] + b[k][i]);
-            if (my.any(k)) store_any(y + my.at(k), r.v);
+            if (!my.any(k)) continue;
+            if (a.past_cache) store_past(y + my.at(k), r.v);
+            else store_any(y + my.at(k), r.v);
         }
     }
 }
@@ -254,6 +257,8 @@ __global__ __launch_bounds__(THREADS < 256 ? 256 : THREADS) void norm_grad_kerne
             pg[k] = next_g[k];
         }
         const float mean = next_mean, rstd = next_rstd;
+        // xhat; x * rstd - mean * rstd would save an operation and lose digits where x is near the mean
+        auto normal = [&](T x) { return (float(x) - mean) * rstd; };
         if (AHEAD) load(row + groups);
         float s[2] = {0, 0};
 #pragma unroll
@@ -261,28 +266,27 @@ __global__ __launch_bounds__(THREADS < 256 ? 256 : THREADS) void norm_grad_kerne
             const float *w = weights + my.at(k);
 #pragma unroll
             for (int i = 0; i < V; ++i) {
-                const float d = float(pg[k].e[i]), h = (float(px[k].e[i]) - mean) * rstd;
-                dw[k][i] += d * h;
+                const float d = float(pg[k].e[i]), h = normal(px[k].e[i]);
+                const float g = my.mine(k, i) ? d * w[i] : 0.0f;
+                dw[k][i] = fmaf(d, h, dw[k][i]);
                 db[k][i] += d;
-                s[0] += my.mine(k, i) ? d * w[i] : 0.0f;
-                s[1] += my.mine(k, i) ? d * w[i] * h : 0.0f;
+                s[0] += g;
+                s[1] = fmaf(g, h, s[1]);
             }
         }
         row_sum<THREADS>(s, part[turn]);
         packed(px);
         packed(pg);
         if (a.dx) {
-            const float c0 = s[0] / cols, c1 = s[1] / cols;
+            const float c0 = -rstd * (s[0] / cols), c1 = -rstd * (s[1] / cols);
             T *dx = static_cast<T *>(a.dx) + row * a.dx_pitch;
 #pragma unroll
             for (int k = 0; k < NV; ++k) {
                 const float *w = weights + my.at(k);
                 Pack<T> r;
 #pragma unroll
-                for (int i = 0; i < V; ++i) {
-                    const float h = (float(px[k].e[i]) - mean) * rstd;
-                    r.e[i] = T(rstd * (float(pg[k].e[i]) * w[i] - c0 - h * c1));
-                }
+                for (int i = 0; i < V; ++i)
+                    r.e[i] = T(fmaf(normal(px[k].e[i]), c1, fmaf(float(pg[k].e[i]) * w[i], rstd, c0)));
                 if (my.any(k)) store_any(dx + my.at(k), r.v);
             }
         }
@@ -480,8 +484,12 @@ void launch_norm(const NormArgs &a, hipStream_t s) {
 }
 
 // Workgroups of the backward pass, whose column sums are kept apart until the
-// join: two a CU; one where rows are long and their sums cost the most.
-int64_t norm_groups(int64_t rows, int64_t cols) { return std::min<int64_t>(rows, cols > 8192 ? 256 : 512); }
+// join: two a CU; one where a row takes 512 threads, of which a CU holds one
+// workgroup (8192 x 8192 bf16: 97 us against 103), or rows are few and the sums
+// weigh more (1024 x 4096: 19 against 22; but 8192 x 4096: 62 against 51).
+int64_t norm_groups(int64_t rows, int64_t cols) {
+    return std::min<int64_t>(rows, cols > 6144 || rows < 4096 ? 256 : 512);
+}
 
 template <typename T>
 void launch_norm_grad(const NormGradArgs &a, int64_t groups, hipStream_t s) {
@@ -522,7 +530,8 @@ extern "C" reshard_status_t reshard_layer_norm(int64_t rows, int64_t cols, const
         if (st == RESHARD_OK && mean) st = check_matrix("mean", mean, 1, rows, rows, 4);
         if (st == RESHARD_OK && rstd) st = check_matrix("rstd", rstd, 1, rows, rows, 4);
         if (st != RESHARD_OK || rows == 0) return st;
-        const NormArgs a{x, weight, bias, y, mean, rstd, rows, cols, x_pitch, y_pitch, float(eps), int(weight_dtype)};
+        const NormArgs a{x, weight, bias, y, mean, rstd, rows, cols, x_pitch, y_pitch, float(eps), int(weight_dtype),
+                         rows * cols * es >= int64_t(256) << 20};
         const hipStream_t s = static_cast<hipStream_t>(stream);
         if (dtype == RESHARD_F32) launch_norm<float>(a, s);
         else if (dtype == RESHARD_BF16) launch_norm<bf16>(a, s);

@@ -7,6 +7,7 @@
 
 #include <cstdint>
 #include <string>
+#include <type_traits>
 
 #include "../../include/reshard.h"
 #include "status.hpp"
@@ -31,6 +32,13 @@ __device__ inline V load_any(const void *p) {
 template <typename V>
 __device__ inline void store_any(void *p, V v) {
     __builtin_memcpy(p, &v, sizeof(V));
+}
+
+// A store that is not kept in the caches: for outputs that they could not hold
+// until their reader comes.
+__device__ inline void store_past(void *p, uint4 v) {
+    typedef uint32_t words __attribute__((ext_vector_type(4), aligned(2), may_alias));
+    __builtin_nontemporal_store(words{v.x, v.y, v.z, v.w}, static_cast<words *>(p));
 }
 
 template <typename T>
@@ -96,10 +104,23 @@ __device__ inline void load_as_float(const void *base, int dtype, int64_t c, int
     }
 }
 
+// The wave's sum, in every lane.  Within rows of 16 lanes and then from row to
+// row by data-parallel moves, which cost an addition each; shuffles go through
+// LDS and would be most of a short row's time.
 __device__ inline float wave_sum(float x) {
-#pragma unroll
-    for (int o = kWave / 2; o > 0; o >>= 1) x += __shfl_xor(x, o, kWave);
-    return x;
+    auto moved = [&](auto ctrl, auto rows) {
+        return __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(x), decltype(ctrl)::value,
+                                                          decltype(rows)::value, 0xf, true));
+    };
+    using std::integral_constant;
+    constexpr integral_constant<int, 0xf> all{};
+    x += moved(integral_constant<int, 0x111>{}, all);  // right by 1, 2, 4 and 8: lane 15 has its row's sum
+    x += moved(integral_constant<int, 0x112>{}, all);
+    x += moved(integral_constant<int, 0x114>{}, all);
+    x += moved(integral_constant<int, 0x118>{}, all);
+    x += moved(integral_constant<int, 0x142>{}, integral_constant<int, 0xa>{});  // lane 15 to the next row
+    x += moved(integral_constant<int, 0x143>{}, integral_constant<int, 0xc>{});  // lane 31 to rows 2 and 3
+    return __int_as_float(__builtin_amdgcn_readlane(__float_as_int(x), kWave - 1));
 }
 
 __device__ inline float e8m0_value(uint8_t code) {
