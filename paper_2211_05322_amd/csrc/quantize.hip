@@ -32,7 +32,9 @@ __device__ inline float max16(float x) {
     return x;
 }
 
-// |x| where x is finite, else 0: NaN and infinities do not widen their block's scale.
+// |x| where x is finite, else 0: NaN and infinities do not widen their block's
+// scale.  The maximum leaves NaN out by itself, so this is needed only where
+// a block's comes out infinite.
 __device__ inline float finite_abs(float x) {
     const float a = fabsf(x);
     return a < kInf ? a : 0.0f;
@@ -47,11 +49,11 @@ __device__ inline int scale_code(float amax) {
 
 __device__ inline float inverse_of(int code) { return __int_as_float((254 - code) << 23); }
 
-// Four codes of x / s; e4m3 has no infinity: one becomes NaN and so is not lost.
+// Four codes of x / s.  e4m3 has no infinity: the conversion makes NaN of one,
+// which so is not lost.
 __device__ inline uint32_t to_codes(float a, float b, float c, float d, float inv) {
-    auto scaled = [&](float x) { return fabsf(x) < kInf ? x * inv : __builtin_nanf(""); };
-    int r = __builtin_amdgcn_cvt_pk_fp8_f32(scaled(a), scaled(b), 0, false);
-    return uint32_t(__builtin_amdgcn_cvt_pk_fp8_f32(scaled(c), scaled(d), r, true));
+    const int r = __builtin_amdgcn_cvt_pk_fp8_f32(a * inv, b * inv, 0, false);
+    return uint32_t(__builtin_amdgcn_cvt_pk_fp8_f32(c * inv, d * inv, r, true));
 }
 
 __device__ inline void store_scale(void *scales, int64_t at, int code, bool e8m0) {
@@ -59,16 +61,17 @@ __device__ inline void store_scale(void *scales, int64_t at, int code, bool e8m0
     else static_cast<float *>(scales)[at] = __int_as_float(code << 23);
 }
 
-// Eight elements as float32, zeros past the n that exist.
+// Eight elements, zeros past the n that exist.
 template <typename T>
-__device__ inline void load8(const T *p, int64_t n, float (&v)[8]) {
+struct Eight {
+    Pack<T> p[8 / kVec<T>];
+
+    __device__ void load(const T *at, int64_t n) {
 #pragma unroll
-    for (int h = 0; h < 8; h += kVec<T>) {
-        const Pack<T> x = load_pack(p + h, n - h);
-#pragma unroll
-        for (int i = 0; i < kVec<T>; ++i) v[h + i] = float(x.e[i]);
+        for (int h = 0; h < 8 / kVec<T>; ++h) p[h] = load_pack(at + h * kVec<T>, n - h * kVec<T>);
     }
-}
+    __device__ float operator[](int i) const { return float(p[i / kVec<T>].e[i % kVec<T>]); }
+};
 
 __device__ inline void store_codes(uint8_t *p, uint2 c, int64_t n) {
     if (n >= 8) {
@@ -97,7 +100,7 @@ __global__ __launch_bounds__(256) void quantize_rows_kernel(QuantArgs a, uint32_
     const int64_t row0 = first / per_row;
     const uint32_t b0 = uint32_t(first - row0 * per_row);
     const int lane = threadIdx.x % 16;
-    float v[kUnits][8];
+    Eight<T> v[kUnits];
     int64_t row[kUnits], col[kUnits];
 #pragma unroll
     for (int u = 0; u < kUnits; ++u) {
@@ -105,13 +108,18 @@ __global__ __launch_bounds__(256) void quantize_rows_kernel(QuantArgs a, uint32_
         row[u] = row0 + b / per_row;
         col[u] = int64_t(b % per_row) * kBlock + lane * 8;
         const int64_t n = row[u] < a.rows ? a.cols - col[u] : 0;
-        load8(static_cast<const T *>(a.x) + row[u] * a.x_pitch + col[u], n, v[u]);
+        v[u].load(static_cast<const T *>(a.x) + row[u] * a.x_pitch + col[u], n);
     }
 #pragma unroll
     for (int u = 0; u < kUnits; ++u) {
         float m = 0;
 #pragma unroll
-        for (int i = 0; i < 8; ++i) m = fmaxf(m, finite_abs(v[u][i]));
+        for (int i = 0; i < 8; ++i) m = fmaxf(m, fabsf(v[u][i]));
+        if (__any(m == kInf)) {
+            m = 0;
+#pragma unroll
+            for (int i = 0; i < 8; ++i) m = fmaxf(m, finite_abs(v[u][i]));
+        }
         const int code = scale_code(max16(m));
         if (row[u] >= a.rows) continue;
         const float inv = inverse_of(code);
@@ -136,22 +144,34 @@ __global__ __launch_bounds__(256) void quantize_tile_kernel(QuantArgs a, uint32_
     const int64_t tr = blockIdx.x / tiles_across, tc = blockIdx.x % tiles_across;
     const int g = threadIdx.x / 16, lane = threadIdx.x % 16, wave = threadIdx.x / kWave;
     const int64_t r0 = tr * kBlock + g * 8, c0 = tc * kBlock + lane * 8;
+    Eight<T> raw[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i)
+        raw[i].load(static_cast<const T *>(a.x) + (r0 + i) * a.x_pitch + c0, r0 + i < a.rows ? a.cols - c0 : 0);
     float v[8][8];
 #pragma unroll
     for (int i = 0; i < 8; ++i)
-        load8(static_cast<const T *>(a.x) + (r0 + i) * a.x_pitch + c0, r0 + i < a.rows ? a.cols - c0 : 0, v[i]);
+#pragma unroll
+        for (int j = 0; j < 8; ++j) v[i][j] = raw[i][j];
 
     float rmax[8], cmax[8];
+    auto largest = [&](auto magnitude) {
 #pragma unroll
-    for (int i = 0; i < 8; ++i) rmax[i] = cmax[i] = 0;
+        for (int i = 0; i < 8; ++i) rmax[i] = cmax[i] = 0;
 #pragma unroll
-    for (int i = 0; i < 8; ++i)
+        for (int i = 0; i < 8; ++i)
 #pragma unroll
-        for (int j = 0; j < 8; ++j) {
-            const float m = finite_abs(v[i][j]);
-            rmax[i] = fmaxf(rmax[i], m);
-            cmax[j] = fmaxf(cmax[j], m);
-        }
+            for (int j = 0; j < 8; ++j) {
+                const float m = magnitude(v[i][j]);
+                rmax[i] = fmaxf(rmax[i], m);
+                cmax[j] = fmaxf(cmax[j], m);
+            }
+    };
+    largest([](float x) { return fabsf(x); });
+    float any = 0;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) any = fmaxf(any, rmax[i]);
+    if (__any(any == kInf)) largest([](float x) { return finite_abs(x); });
     if constexpr (TILE) {
         float m = 0;
 #pragma unroll
@@ -220,6 +240,7 @@ struct DequantArgs {
     void *y;
     int64_t rows, cols, q_pitch, scales_pitch, y_pitch;
     int e8m0, row_shift;  // rows that share a scale: 1 << row_shift
+    bool past_cache;      // y is larger than the last-level cache
 };
 
 template <typename T>
@@ -273,7 +294,8 @@ __global__ __launch_bounds__(256) void dequantize_kernel(DequantArgs a, uint32_t
             Pack<T> r;
 #pragma unroll
             for (int i = 0; i < kVec<T>; ++i) r.e[i] = T(v[h + i]);
-            if (n[u] > h) store_pack(y + h, r, n[u] - h);
+            if (a.past_cache && n[u] >= h + kVec<T>) store_past(y + h, r.v);
+            else if (n[u] > h) store_pack(y + h, r, n[u] - h);
         }
     }
 }
@@ -359,7 +381,8 @@ extern "C" reshard_status_t reshard_dequantize(int64_t rows, int64_t cols, const
         if (st == RESHARD_OK) st = check_matrix("y", y, rows, cols, y_pitch, dtype == RESHARD_F32 ? 4 : 2);
         if (st != RESHARD_OK || rows == 0 || cols == 0) return st;
         const DequantArgs a{static_cast<const uint8_t *>(q), scales, y, rows, cols, q_pitch, scales_pitch, y_pitch,
-                            scale_dtype == RESHARD_E8M0, block_rows == 1 ? 0 : 7};
+                            scale_dtype == RESHARD_E8M0, block_rows == 1 ? 0 : 7,
+                            rows * cols * (dtype == RESHARD_F32 ? 4 : 2) >= int64_t(256) << 20};
         const hipStream_t s = static_cast<hipStream_t>(stream);
         const dim3 grid(unsigned(ceil_div(rows * across, 16 * kUnits)));
         if (dtype == RESHARD_F32) dequantize_kernel<float><<<grid, 256, 0, s>>>(a, uint32_t(across));
