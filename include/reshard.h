@@ -525,8 +525,8 @@ reshard_status_t reshard_dequantize(int64_t rows, int64_t cols, const void *q, i
  * neighbouring ones are cut 13 bits below the largest of the eight before they
  * are summed, as the 8-bit matrix instruction does: at most 2^-10 of it in
  * all, typically 1e-5 to 2e-4 of the sum.  With k = 0 the product is zeros.  Rows of codes and scales may have any pitch and start at
- * any byte; rows of codes at 16-byte boundaries, at most 4 MiB apart, load
- * fastest.  k is at most 2^36, out at most 2^22 tiles of 128 x 128.  Bytes of a row past k
+ * any byte; rows of codes at 16-byte boundaries, at most 4 MiB apart and long,
+ * load fastest.  k is at most 2^36, out at most 2^20 tiles of 128 x 128.  Bytes of a row past k
  * are not read into the result, whatever they hold.
  */
 int64_t reshard_matmul_workspace(int64_t m, int64_t n, int64_t k, reshard_dtype_t scale_dtype,

@@ -18,6 +18,7 @@
 // results are then neighbours in a row of `out`, and they share A's scale.
 #include <algorithm>
 #include <type_traits>
+#include <utility>
 
 #include "operators.hpp"
 
@@ -25,7 +26,6 @@ namespace rs {
 namespace {
 
 typedef int i32x8 __attribute__((ext_vector_type(8)));
-typedef int i32x4 __attribute__((ext_vector_type(4)));
 typedef float f32x4 __attribute__((ext_vector_type(4)));
 typedef float f32x16 __attribute__((ext_vector_type(16)));
 typedef bf16 bf16x2 __attribute__((ext_vector_type(2)));
@@ -158,11 +158,18 @@ __device__ inline void store_any_type(const MatmulArgs &g, int64_t i, int64_t j,
     else store_out<f16>(g, i, j, v);
 }
 
-// 128 x 128 of `out` a workgroup, 64 x 64 a wave.  A row of the LDS tiles is
-// one block, eight 16-byte words; word w of row r lies in slot w ^ (r % 8).
+// Operands whose rows start anywhere, or lie too far apart for the tile
+// kernel's 32-bit offsets: codes go through registers, a step ahead, 128 x 128
+// of `out` a workgroup, 64 x 64 a wave.  Bound by those loads, which straddle
+// cache lines, and two barriers a step: 8192 x 8192 x 4096 with rows 4097 apart
+// takes 690 us (246 in tiles on 16-byte boundaries), 800 into float32 (466).
+// A row of the LDS tiles is one block, eight 16-byte words; word w of row r
+// lies in slot w ^ (r % 8).
 template <Sum SUM>
-__global__ __launch_bounds__(256) void matmul_kernel(MatmulArgs g, uint32_t tiles_n) {
+__global__ __launch_bounds__(256, 2) void matmul_kernel(MatmulArgs g, uint32_t tiles_n) {
+    using Scale = typename std::conditional<SUM == kScaled, int, float>::type;
     __shared__ uint4 sa[128][8], sb[128][8];
+    __shared__ __align__(16) Scale sk[256];  // of A's rows, then of B's
     const int64_t i0 = int64_t(blockIdx.x / tiles_n) * 128, j0 = int64_t(blockIdx.x % tiles_n) * 128;
     const int lane = threadIdx.x % kWave, wave = threadIdx.x / kWave;
     const int wi = (wave / 2) * 64, wj = (wave % 2) * 64, r16 = lane % 16, quad = lane / 16;
@@ -171,15 +178,41 @@ __global__ __launch_bounds__(256) void matmul_kernel(MatmulArgs g, uint32_t tile
     for (int x = 0; x < 4; ++x)
 #pragma unroll
         for (int y = 0; y < 4; ++y) acc[x][y] = f32x4{0, 0, 0, 0};
-    const int64_t steps = ceil_div(g.k, kBlock);
+    const int64_t steps = ceil_div(g.k, kBlock), whole = g.k / kBlock;
+    // A thread's words of a block, loaded while the block before is multiplied;
+    // rows past a matrix's end repeat its last, whose results are not stored.
+    const int row0 = threadIdx.x / 8, word = threadIdx.x % 8;
+    uint4 a_next[4], b_next[4];
+    Scale k_next;
+    const Operand &mine = threadIdx.x < 128 ? g.a : g.b;
+    const int64_t k_row = min((threadIdx.x < 128 ? i0 : j0 - 128) + threadIdx.x, mine.rows - 1);
+    auto load = [&](int64_t s) {
+        const int64_t l = s * kBlock + word * 16;
+        if constexpr (SUM == kScaled) k_next = scale_code(mine, k_row, s);
+        else k_next = scale_value(mine, g.e8m0, k_row, s);
+#pragma unroll
+        for (int u = 0; u < 4; ++u) {
+            const int64_t i = min(i0 + row0 + u * 32, g.a.rows - 1), j = min(j0 + row0 + u * 32, g.b.rows - 1);
+            if (s < whole) {
+                a_next[u] = load_any<uint4>(g.a.q + i * g.a.pitch + l);
+                b_next[u] = load_any<uint4>(g.b.q + j * g.b.pitch + l);
+            } else {
+                a_next[u] = load_codes(g.a, i, l, g.k);
+                b_next[u] = load_codes(g.b, j, l, g.k);
+            }
+        }
+    };
+    if (steps > 0) load(0);
     for (int64_t s = 0; s < steps; ++s) {
 #pragma unroll
         for (int u = 0; u < 4; ++u) {
-            const int w = u * 256 + threadIdx.x, r = w / 8, c = w % 8;
-            sa[r][c ^ (r & 7)] = load_codes(g.a, i0 + r, s * kBlock + c * 16, g.k);
-            sb[r][c ^ (r & 7)] = load_codes(g.b, j0 + r, s * kBlock + c * 16, g.k);
+            const int r = row0 + u * 32;
+            sa[r][word ^ (r & 7)] = a_next[u];
+            sb[r][word ^ (r & 7)] = b_next[u];
         }
+        sk[threadIdx.x] = k_next;
         __syncthreads();
+        if (s + 1 < steps) load(s + 1);
         Codes fa[4], fb[4];
 #pragma unroll
         for (int x = 0; x < 4; ++x) {
@@ -194,9 +227,8 @@ __global__ __launch_bounds__(256) void matmul_kernel(MatmulArgs g, uint32_t tile
             int ka[4], kb[4];
 #pragma unroll
             for (int x = 0; x < 4; ++x) {
-                const int64_t i = i0 + wi + x * 16 + r16, j = j0 + wj + x * 16 + r16;
-                ka[x] = i < g.a.rows ? scale_code(g.a, i, s) : 127;
-                kb[x] = j < g.b.rows ? scale_code(g.b, j, s) : 127;
+                ka[x] = sk[wi + x * 16 + r16];
+                kb[x] = sk[128 + wj + x * 16 + r16];
             }
 #pragma unroll
             for (int x = 0; x < 4; ++x)
@@ -205,26 +237,17 @@ __global__ __launch_bounds__(256) void matmul_kernel(MatmulArgs g, uint32_t tile
                     acc[x][y] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(fb[y].v, fa[x].v, acc[x][y], 0, 0, 0,
                                                                                  kb[y], 0, ka[x]);
         } else {
-            float ka[4], kb[4][4];
-#pragma unroll
-            for (int x = 0; x < 4; ++x) {
-                const int64_t i = i0 + wi + x * 16 + r16;
-                ka[x] = i < g.a.rows ? scale_value(g.a, g.e8m0, i, s) : 0.0f;
-#pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    const int64_t j = j0 + wj + x * 16 + quad * 4 + e;
-                    kb[x][e] = j < g.b.rows ? scale_value(g.b, g.e8m0, j, s) : 0.0f;
-                }
-            }
 #pragma unroll
             for (int y = 0; y < 4; ++y) {
                 const typename std::conditional<SUM == kExact, Wide, Codes>::type b(fb[y]);
+                const f32x4 kb = *reinterpret_cast<const f32x4 *>(&sk[128 + wj + y * 16 + quad * 4]);
 #pragma unroll
                 for (int x = 0; x < 4; ++x) {
                     const typename std::conditional<SUM == kExact, Wide, Codes>::type a(fa[x]);
                     const f32x4 p = block_product(b, a);
+                    const float ka = sk[wi + x * 16 + r16];
 #pragma unroll
-                    for (int e = 0; e < 4; ++e) acc[x][y][e] = fmaf(p[e], ka[x] * kb[y][e], acc[x][y][e]);
+                    for (int e = 0; e < 4; ++e) acc[x][y][e] = fmaf(p[e], ka * kb[e], acc[x][y][e]);
                 }
             }
         }
@@ -330,6 +353,16 @@ __device__ inline void unrolled(F &&f) {
 // LDS rows are 128 bytes, eight 16-byte words, word w of row r in slot
 // w ^ (r / 2 % 8): lanes that read at once fall on different banks.  The loads
 // write LDS in order, so the order of words is set by the addresses they read.
+//
+// Bound by the matrix instructions and the power they take: 16384 x 12288 x
+// 12288 in 256 x 256 tiles with E8M0 scales runs at 2540 TFLOP/s, the
+// instruction busy 74 % of the cycles at a clock of 1.65 GHz (on zeros, which
+// take less power, the same code reaches 3430).  Waves of 128 x 128, which read
+// a third less from LDS, measured the same.  Float scales cost an operation
+// an element and block beside the matrix instruction (1590 TFLOP/s with a
+// scale per tile of B, 1320 per row), float32 results the conversion and the
+// bf16 instruction's half rate (1250 TFLOP/s with E8M0 scales, 990 with float
+// ones).
 template <int ROWS>
 struct Stage {
     uint4 words[ROWS * 8];
@@ -629,7 +662,8 @@ __global__ __launch_bounds__(256) void matmul_join_kernel(MatmulArgs g, int part
 // Few rows of A: the weights' bytes are the work.  A workgroup takes 16 rows
 // of B and all of A's (at most 16); its waves deal the blocks of the reduction
 // among them, load DEPTH blocks' fragments at once straight into registers,
-// and add their sums through LDS.
+// and add their sums through LDS.  Bound by memory: 1 x 12288 x 12288 in 30 us,
+// 5.0 TB/s of weights.
 template <Sum SUM, int WAVES, int DEPTH>
 __global__ __launch_bounds__(WAVES *kWave) void matmul_few_kernel(MatmulArgs g) {
     __shared__ f32x4 part[WAVES][kWave];
@@ -706,14 +740,14 @@ __global__ __launch_bounds__(WAVES *kWave) void matmul_few_kernel(MatmulArgs g) 
 // of 256 x 256 (16-bit results of E8M0 operands, where there are enough of
 // them) or 128 x 128, and where those are too few for the 256 CUs, the
 // reduction split into parts that are joined.
-struct Plan {
+struct Launch {
     bool few, large;
     int64_t tile, tiles_m, tiles_n;
     int32_t parts, blocks;  // parts of the reduction, and the blocks of each
 };
 
-Plan plan_matmul(int64_t m, int64_t n, int64_t k, Sum sum) {
-    Plan p{};
+Launch launch_of(int64_t m, int64_t n, int64_t k, Sum sum) {
+    Launch p{};
     p.few = m <= 8 && sum != kExact;
     const int64_t steps = ceil_div(k, kBlock);
     auto tiles = [&](int64_t side) { return ceil_div(m, side) * ceil_div(n, side); };
@@ -763,7 +797,7 @@ extern "C" int64_t reshard_matmul_workspace(int64_t m, int64_t n, int64_t k, res
                                             reshard_dtype_t out_dtype) {
     if (m < 0 || n < 0 || k < 0 || m > int64_t(1) << 40 || n > int64_t(1) << 40 || k > int64_t(1) << 36) return -1;
     if (m == 0 || n == 0) return 0;
-    const rs::Plan p = rs::plan_matmul(m, n, k, rs::sum_for(scale_dtype, out_dtype));
+    const rs::Launch p = rs::launch_of(m, n, k, rs::sum_for(scale_dtype, out_dtype));
     return p.parts > 1 ? int64_t(p.parts) * m * n * int64_t(sizeof(float)) : 0;
 }
 
@@ -789,8 +823,8 @@ extern "C" reshard_status_t reshard_matmul(int64_t m, int64_t n, int64_t k, cons
         if (st == RESHARD_OK)
             st = check_matrix("out", out, m, n, out_pitch, out_dtype == RESHARD_F32 ? 4 : 2);
         if (st != RESHARD_OK || m == 0 || n == 0) return st;
-        if (ceil_div(n, 128) > (int64_t(1) << 22) / ceil_div(m, 128))
-            return fail(RESHARD_EUNSUPPORTED, "out has more than 2^22 tiles of 128 x 128");
+        if (ceil_div(n, 128) > (int64_t(1) << 20) / ceil_div(m, 128))
+            return fail(RESHARD_EUNSUPPORTED, "out has more than 2^20 tiles of 128 x 128");
         if (k > int64_t(1) << 36) return fail(RESHARD_EUNSUPPORTED, "k is above 2^36");
         MatmulArgs g{};
         g.a = Operand{static_cast<const uint8_t *>(a), a_scales, m, a_pitch, a_scales_pitch, a_block_rows == 1 ? 0 : 7};
@@ -803,7 +837,7 @@ extern "C" reshard_status_t reshard_matmul(int64_t m, int64_t n, int64_t k, cons
         g.e8m0 = scale_dtype == RESHARD_E8M0;
         const hipStream_t s = static_cast<hipStream_t>(stream);
         const Sum sum = sum_for(scale_dtype, out_dtype);
-        const Plan p = plan_matmul(m, n, k, sum);
+        const Launch p = launch_of(m, n, k, sum);
         if (p.few) {
             if (sum == kScaled) launch_few<kScaled>(g, s);
             else launch_few<kFloat>(g, s);
@@ -811,7 +845,8 @@ extern "C" reshard_status_t reshard_matmul(int64_t m, int64_t n, int64_t k, cons
         }
         // the tile kernel's loads into LDS: whole 16-byte words, 32-bit offsets within a tile's rows
         const bool aligned = (reinterpret_cast<uintptr_t>(a) | reinterpret_cast<uintptr_t>(b) | uintptr_t(a_pitch) |
-                              uintptr_t(b_pitch)) % 16 == 0 && a_pitch <= 1 << 22 && b_pitch <= 1 << 22;
+                              uintptr_t(b_pitch)) % 16 == 0 &&
+                             a_pitch <= 1 << 22 && b_pitch <= 1 << 22 && k <= 1 << 22;
         if (!aligned) {
             const dim3 grid(unsigned(ceil_div(m, 128) * ceil_div(n, 128)));
             const uint32_t tiles_n = uint32_t(ceil_div(n, 128));
