@@ -14,8 +14,9 @@
  *
  * On one GPU every mesh "device" is a separate buffer in the GPU's memory.
  *
- * Conventions shared by all calls
- * -------------------------------
+ * Conventions shared by the calls on plans (those of the operators at a
+ * stage's edge stand with them, at the end)
+ * ------------------------------------------------------------------------
  *  - Meshes are n-dimensional (1..8 axes).  Devices are numbered row-major
  *    over mesh coordinates: the (2,2) mesh is [[0,1],[2,3]] (Section 2.2,
  *    "Device mesh").  Pointer arrays are indexed by that number.

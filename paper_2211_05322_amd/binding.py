@@ -49,7 +49,7 @@ class reshard_tuning_t(ctypes.Structure):
                 ("reserved", ctypes.c_int32 * 3)]
 
 
-_lib = None
+_lib = _torch = None
 _I64P = ctypes.POINTER(ctypes.c_int64)
 _VPP = ctypes.POINTER(ctypes.c_void_p)
 
@@ -67,7 +67,9 @@ def load(path=None):
     # libamdhip64.so.7.  Opened the other way round, the process would map
     # the system runtime for the library and torch's for its tensors and
     # streams -- two HIP runtimes, with kernels registered in only one.
-    import torch  # noqa: F401
+    global _torch
+    import torch
+    _torch = torch
     lib = ctypes.CDLL(path)
     plan_args = [ctypes.c_int, _I64P, ctypes.c_int, ctypes.c_int, _I64P, ctypes.c_char_p,
                  ctypes.c_int, _I64P, ctypes.c_char_p, ctypes.c_uint]
@@ -442,9 +444,9 @@ def _like(name, t, shape, dtype, device):
     return t
 
 
-def _dense(name, t, shape, device, dtype):
-    if t.shape != shape or t.dtype != dtype or t.device != device or not t.is_contiguous():
-        raise ValueError(f"{name} must be dense, {dtype} {tuple(shape)} on {device}, "
+def _dense(name, t, shape, beside, dtype):
+    if t.shape != shape or t.dtype != dtype or t.get_device() != beside.get_device() or not t.is_contiguous():
+        raise ValueError(f"{name} must be dense, {dtype} {tuple(shape)} on {beside.device}, "
                          f"got {t.dtype} {tuple(t.shape)}, strides {t.stride()}, on {t.device}")
     return t
 
@@ -456,8 +458,7 @@ def _on(stream):
     """Memory that a call takes comes from the pool of the stream it runs on."""
     if stream is None:
         return _HERE
-    import torch
-    return torch.cuda.stream(torch.cuda.ExternalStream(stream) if isinstance(stream, int) else stream)
+    return _torch.cuda.stream(_torch.cuda.ExternalStream(stream) if isinstance(stream, int) else stream)
 
 
 def _on_gpu(name, t):
@@ -473,27 +474,25 @@ def _result(out, like):
     """(tensor, pitch) of a result of like's shape and type: the caller's, or a dense one."""
     if out is not None:
         return _like("out", out, like.shape, like.dtype, like.device), _matrix("out", out)[2]
-    import torch
-    y = torch.empty_like(like) if like.is_contiguous() else like.new_empty(like.shape)
+    y = _torch.empty_like(like) if like.is_contiguous() else like.new_empty(like.shape)
     return y, like.shape[-1]
 
 
 def reshard_layer_norm(x, weight=None, bias=None, eps=1e-5, out=None, stream=None):
     """(y, mean, rstd): layer norm over x's last dimension; mean and rstd (float32) are for the backward pass."""
-    import torch
     lib = _lib or load()
     rows, cols, pitch = _matrix("x", x)
     wdt = (weight if weight is not None else bias if bias is not None else x).dtype
     if weight is not None:
-        _dense("weight", weight, (cols,), x.device, wdt)
+        _dense("weight", weight, (cols,), x, wdt)
     if bias is not None:
-        _dense("bias", bias, (cols,), x.device, wdt)
+        _dense("bias", bias, (cols,), x, wdt)
     if out is not None:
         _like("out", out, x.shape, x.dtype, x.device)
     _on_gpu("x", x)
     with _on(stream):
         y, y_pitch = _result(out, x)
-        mean, rstd = x.new_empty((2, *x.shape[:-1]), dtype=torch.float32).unbind()
+        mean, rstd = x.new_empty((2, *x.shape[:-1]), dtype=_torch.float32).unbind()
     status = lib.reshard_layer_norm(rows, cols, x.data_ptr(), pitch, _dtype_code(x.dtype), _ptr(weight), _ptr(bias),
                                     _dtype_code(wdt), eps, y.data_ptr(), y_pitch, mean.data_ptr(), rstd.data_ptr(),
                                     _stream_handle(stream))
@@ -506,14 +505,13 @@ def reshard_layer_norm_backward(dy, x, weight, mean, rstd, dweight=None, dbias=N
                                 stream=None):
     """(dx, dweight, dbias) of reshard_layer_norm.  dweight and dbias are
     float32; given ones are overwritten, or added to with accumulate."""
-    import torch
     lib = _lib or load()
     rows, cols, pitch = _matrix("x", x)
     _like("dy", dy, x.shape, x.dtype, x.device)
     if weight is not None:
-        _dense("weight", weight, (cols,), x.device, weight.dtype)
-    _dense("mean", mean, x.shape[:-1], x.device, torch.float32)
-    _dense("rstd", rstd, x.shape[:-1], x.device, torch.float32)
+        _dense("weight", weight, (cols,), x, weight.dtype)
+    _dense("mean", mean, x.shape[:-1], x, _torch.float32)
+    _dense("rstd", rstd, x.shape[:-1], x, _torch.float32)
     if accumulate and (dweight is None or dbias is None):
         raise ValueError("accumulate needs the dweight and dbias to add to")
     _on_gpu("x", x)
@@ -521,14 +519,14 @@ def reshard_layer_norm_backward(dy, x, weight, mean, rstd, dweight=None, dbias=N
     with _on(stream):
         dx, dx_pitch = _result(out, x)
         if dweight is None and dbias is None:
-            dweight, dbias = x.new_empty((2, cols), dtype=torch.float32).unbind()
+            dweight, dbias = x.new_empty((2, cols), dtype=_torch.float32).unbind()
         elif dweight is None:
-            dweight = x.new_empty(cols, dtype=torch.float32)
+            dweight = x.new_empty(cols, dtype=_torch.float32)
         elif dbias is None:
-            dbias = x.new_empty(cols, dtype=torch.float32)
-        work = x.new_empty(max(0, need), dtype=torch.uint8)
-    _dense("dweight", dweight, (cols,), x.device, torch.float32)
-    _dense("dbias", dbias, (cols,), x.device, torch.float32)
+            dbias = x.new_empty(cols, dtype=_torch.float32)
+        work = x.new_empty(max(0, need), dtype=_torch.uint8)
+    _dense("dweight", dweight, (cols,), x, _torch.float32)
+    _dense("dbias", dbias, (cols,), x, _torch.float32)
     status = lib.reshard_layer_norm_backward(
         rows, cols, dy.data_ptr(), _matrix("dy", dy)[2], x.data_ptr(), pitch, _dtype_code(x.dtype), _ptr(weight),
         _dtype_code(x.dtype if weight is None else weight.dtype), mean.data_ptr(), rstd.data_ptr(), dx.data_ptr(),
@@ -544,9 +542,8 @@ _E4M3, _BLOCK = "float8_e4m3fn", 128
 def _empty_blocked(x, rows, cols, block_rows, scale_dtype):
     """(Blocked, codes' pitch, scales' pitch) beside x.  Rows of codes are padded to whole blocks, so that each
     starts on a 16-byte boundary."""
-    import torch
     across = -(-cols // _BLOCK)
-    data = x.new_empty((rows, across * _BLOCK), dtype=torch.float8_e4m3fn)
+    data = x.new_empty((rows, across * _BLOCK), dtype=_torch.float8_e4m3fn)
     scales = x.new_empty((rows if block_rows == 1 else -(-rows // block_rows), across), dtype=scale_dtype)
     if cols != across * _BLOCK:
         data = data[:, :cols]
@@ -555,16 +552,17 @@ def _empty_blocked(x, rows, cols, block_rows, scale_dtype):
 
 def _blocked(name, b):
     """(rows, cols, pitch, scales' pitch) of a Blocked."""
-    rows, cols, pitch = _matrix("data", b.data)
-    if _dtype_code(b.data.dtype) != _DTYPES[_E4M3]:
-        raise ValueError(f"{name}.data must be {_E4M3}, got {b.data.dtype}")
-    if b.block_rows not in (1, _BLOCK):
-        raise ValueError(f"{name}.block_rows must be 1 or {_BLOCK}, got {b.block_rows}")
-    srows, scols, spitch = _matrix("scales", b.scales)
-    if srows != -(-rows // b.block_rows) or scols != -(-cols // _BLOCK):
+    data, scales, block_rows = b
+    rows, cols, pitch = _matrix("data", data)
+    if _dtype_code(data.dtype) != _DTYPES[_E4M3]:
+        raise ValueError(f"{name}.data must be {_E4M3}, got {data.dtype}")
+    if block_rows not in (1, _BLOCK):
+        raise ValueError(f"{name}.block_rows must be 1 or {_BLOCK}, got {block_rows}")
+    srows, scols, spitch = _matrix("scales", scales)
+    if srows != -(-rows // block_rows) or scols != -(-cols // _BLOCK):
         raise ValueError(f"{name}.scales must be {(-(-rows // b.block_rows), -(-cols // _BLOCK))}, "
                          f"got {(srows, scols)}")
-    if b.scales.device != b.data.device:
+    if scales.get_device() != data.get_device():
         raise ValueError(f"{name}.scales are on {b.scales.device}, its data on {b.data.device}")
     return rows, cols, pitch, spitch
 
@@ -574,7 +572,6 @@ def reshard_quantize(x, block_rows=1, transposed=False, scale_dtype=None, stream
     dimensions are kept, and count as rows).  transposed=True: of x as a matrix
     of rows, transposed, with blocks along x's rows; "both": the pair, from one reading of x.  scale_dtype:
     torch.float8_e8m0fnu (default) or torch.float32."""
-    import torch
     lib = _lib or load()
     rows, cols, pitch = _matrix("x", x)
     if transposed not in (False, True, "both"):
@@ -582,7 +579,7 @@ def reshard_quantize(x, block_rows=1, transposed=False, scale_dtype=None, stream
     if block_rows not in (1, _BLOCK):
         raise ValueError(f"block_rows must be 1 or {_BLOCK}, got {block_rows}")
     if scale_dtype is None:
-        scale_dtype = torch.float8_e8m0fnu
+        scale_dtype = _torch.float8_e8m0fnu
     _on_gpu("x", x)
     q = t = None
     args = [None, 0, None, 0, None, 0, None, 0]
@@ -625,7 +622,6 @@ def reshard_matmul(a, b, out_dtype=None, out=None, accumulate=False, stream=None
     """a [..., k] times b [n, k] transposed, both Blocked with scales of one
     type; [..., n] of out_dtype (default torch.bfloat16), or into `out`, added
     to what is there with accumulate."""
-    import torch
     lib = _lib or load()
     m, k, a_pitch, a_spitch = _blocked("a", a)
     n, kb, b_pitch, b_spitch = _blocked("b", b)
@@ -633,7 +629,7 @@ def reshard_matmul(a, b, out_dtype=None, out=None, accumulate=False, stream=None
         raise ValueError(f"a has {k} columns and b {kb}")
     if a.scales.dtype != b.scales.dtype:
         raise ValueError(f"a's scales are {a.scales.dtype}, b's {b.scales.dtype}")
-    if a.data.device != b.data.device:
+    if a.data.get_device() != b.data.get_device():
         raise ValueError(f"a is on {a.data.device}, b on {b.data.device}")
     if accumulate and out is None:
         raise ValueError("accumulate needs the out to add to")
@@ -641,7 +637,7 @@ def reshard_matmul(a, b, out_dtype=None, out=None, accumulate=False, stream=None
         _like("out", out, (*a.data.shape[:-1], n), out_dtype or out.dtype, a.data.device)
     _on_gpu("a", a.data)
     shape = (*a.data.shape[:-1], n)
-    out_dtype = out_dtype or (torch.bfloat16 if out is None else out.dtype)
+    out_dtype = out_dtype or (_torch.bfloat16 if out is None else out.dtype)
     sdt, odt = _dtype_code(a.scales.dtype), _dtype_code(out_dtype)
     need = lib.reshard_matmul_workspace(m, n, k, sdt, odt)
     work = None
@@ -651,7 +647,7 @@ def reshard_matmul(a, b, out_dtype=None, out=None, accumulate=False, stream=None
         else:
             y, y_pitch = _like("out", out, shape, out_dtype, a.data.device), _matrix("out", out)[2]
         if need > 0:
-            work = a.data.new_empty(need, dtype=torch.uint8)
+            work = a.data.new_empty(need, dtype=_torch.uint8)
     status = lib.reshard_matmul(m, n, k, a.data.data_ptr(), a_pitch, a.block_rows, a.scales.data_ptr(), a_spitch,
                                 b.data.data_ptr(), b_pitch, b.block_rows, b.scales.data_ptr(), b_spitch, sdt,
                                 y.data_ptr(), y_pitch, odt, int(accumulate), _ptr(work), max(0, need),

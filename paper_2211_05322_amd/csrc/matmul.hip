@@ -642,9 +642,9 @@ __global__ __launch_bounds__(WM *WN *kWave, 2) void matmul_tile_kernel(MatmulArg
 
 // Adds the parts of a split reduction, in order.
 __global__ __launch_bounds__(256) void matmul_join_kernel(MatmulArgs g, int parts) {
-    const int64_t across = ceil_div(g.b.rows, 8), total = g.a.rows * across;
-    for (int64_t at = int64_t(blockIdx.x) * 256 + threadIdx.x; at < total; at += int64_t(gridDim.x) * 256) {
-        const int64_t i = at / across, j = (at - i * across) * 8;
+    const uint32_t across = uint32_t(ceil_div(g.b.rows, 8)), total = uint32_t(g.a.rows) * across;  // at most 2^31
+    for (uint32_t at = blockIdx.x * 256 + threadIdx.x; at < total; at += gridDim.x * 256) {
+        const int64_t i = at / across, j = int64_t(at % across) * 8;
         const float *p = g.parts + i * g.b.rows + j;
         f32x4 lo{0, 0, 0, 0}, hi{0, 0, 0, 0};
         for (int s = 0; s < parts; ++s, p += g.a.rows * g.b.rows) {

@@ -94,12 +94,6 @@ __global__ __launch_bounds__(THREADS < 256 ? 256 : THREADS) void norm_kernel(Nor
     const int t = threadIdx.x % THREADS;
     const Columns<T, THREADS, NV> my(a.cols, t);
     const float cols = float(a.cols);
-    float w[NV][V], b[NV][V];
-#pragma unroll
-    for (int k = 0; k < NV; ++k) {
-        load_as_float<V>(a.weight, a.weight_dtype, my.at(k), a.cols, 1.0f, w[k]);
-        load_as_float<V>(a.bias, a.weight_dtype, my.at(k), a.cols, 0.0f, b[k]);
-    }
     const int64_t stride = int64_t(gridDim.x) * ROWS;
     int64_t row = int64_t(blockIdx.x) * ROWS + threadIdx.x / THREADS;
     Pack<T> next[NV];
@@ -108,7 +102,13 @@ __global__ __launch_bounds__(THREADS < 256 ? 256 : THREADS) void norm_kernel(Nor
 #pragma unroll
         for (int k = 0; k < NV; ++k) next[k].v = load_any<uint4>(x + my.at(k));
     };
-    if (AHEAD) load(row);
+    if (AHEAD) load(row);  // before the weights, which few rows would wait for too
+    float w[NV][V], b[NV][V];
+#pragma unroll
+    for (int k = 0; k < NV; ++k) {
+        load_as_float<V>(a.weight, a.weight_dtype, my.at(k), a.cols, 1.0f, w[k]);
+        load_as_float<V>(a.bias, a.weight_dtype, my.at(k), a.cols, 0.0f, b[k]);
+    }
     for (; row < a.rows; row += stride) {
         if (!AHEAD) load(row);
         Pack<T> p[NV];
@@ -221,13 +221,6 @@ __global__ __launch_bounds__(THREADS < 256 ? 256 : THREADS) void norm_grad_kerne
     const int64_t group = int64_t(blockIdx.x) * ROWS + threadIdx.x / THREADS;
     const int64_t groups = int64_t(gridDim.x) * ROWS;
     const float cols = float(a.cols);
-    for (int64_t c = threadIdx.x * V; c < a.cols; c += blockDim.x * V) {
-        float w[V];
-        load_as_float<V>(a.weight, a.weight_dtype, c, a.cols, 1.0f, w);
-#pragma unroll
-        for (int i = 0; i < V; ++i) weights[c + i] = w[i];
-    }
-    __syncthreads();
     float dw[NV][V], db[NV][V];
 #pragma unroll
     for (int k = 0; k < NV; ++k)
@@ -247,6 +240,13 @@ __global__ __launch_bounds__(THREADS < 256 ? 256 : THREADS) void norm_grad_kerne
         next_rstd = a.rstd[r];
     };
     if (AHEAD) load(group);
+    for (int64_t c = threadIdx.x * V; c < a.cols; c += blockDim.x * V) {
+        float w[V];
+        load_as_float<V>(a.weight, a.weight_dtype, c, a.cols, 1.0f, w);
+#pragma unroll
+        for (int i = 0; i < V; ++i) weights[c + i] = w[i];
+    }
+    __syncthreads();
     int turn = 0;  // rows in turn use the two halves of `part`: one barrier a row
     for (int64_t row = group; row < a.rows; row += groups, turn ^= 1) {
         if (!AHEAD) load(row);

@@ -96,16 +96,14 @@ constexpr int kUnits = 4;  // blocks of 128 that 16 lanes take, loaded before th
 // Blocks of one row: 16 lanes hold a block, eight elements each.
 template <typename T>
 __global__ __launch_bounds__(256) void quantize_rows_kernel(QuantArgs a, uint32_t per_row) {
-    const int64_t first = int64_t(blockIdx.x) * (16 * kUnits);
-    const int64_t row0 = first / per_row;
-    const uint32_t b0 = uint32_t(first - row0 * per_row);
+    const uint32_t first = blockIdx.x * (16 * kUnits), row0 = first / per_row, b0 = first - row0 * per_row;
     const int lane = threadIdx.x % 16;
     Eight<T> v[kUnits];
     int64_t row[kUnits], col[kUnits];
 #pragma unroll
     for (int u = 0; u < kUnits; ++u) {
         const uint32_t b = b0 + u * 16 + threadIdx.x / 16;
-        row[u] = row0 + b / per_row;
+        row[u] = row0 + b / per_row;  // at most 2^29 blocks: 32-bit divisions, a tenth of 64-bit ones
         col[u] = int64_t(b % per_row) * kBlock + lane * 8;
         const int64_t n = row[u] < a.rows ? a.cols - col[u] : 0;
         v[u].load(static_cast<const T *>(a.x) + row[u] * a.x_pitch + col[u], n);
@@ -141,7 +139,8 @@ template <typename T, bool TILE>
 __global__ __launch_bounds__(256) void quantize_tile_kernel(QuantArgs a, uint32_t tiles_across) {
     __shared__ uint2 words[kBlock][16];
     __shared__ float part[4][kBlock];
-    const int64_t tr = blockIdx.x / tiles_across, tc = blockIdx.x % tiles_across;
+    const uint32_t down = blockIdx.x / tiles_across;
+    const int64_t tr = down, tc = blockIdx.x - down * tiles_across;
     const int g = threadIdx.x / 16, lane = threadIdx.x % 16, wave = threadIdx.x / kWave;
     const int64_t r0 = tr * kBlock + g * 8, c0 = tc * kBlock + lane * 8;
     Eight<T> raw[8];
@@ -245,9 +244,7 @@ struct DequantArgs {
 
 template <typename T>
 __global__ __launch_bounds__(256) void dequantize_kernel(DequantArgs a, uint32_t per_row) {
-    const int64_t first = int64_t(blockIdx.x) * (16 * kUnits);
-    const int64_t row0 = first / per_row;
-    const uint32_t b0 = uint32_t(first - row0 * per_row);
+    const uint32_t first = blockIdx.x * (16 * kUnits), row0 = first / per_row, b0 = first - row0 * per_row;
     const int lane = threadIdx.x % 16;
     uint2 c[kUnits];
     float s[kUnits];
