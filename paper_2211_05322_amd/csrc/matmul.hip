@@ -361,7 +361,7 @@ __device__ inline void unrolled(F &&f) {
 // a third less from LDS, measured the same.  Float scales cost an operation
 // an element and block beside the matrix instruction (1590 TFLOP/s with a
 // scale per tile of B, 1320 per row), float32 results the conversion and the
-// bf16 instruction's half rate (1250 TFLOP/s with E8M0 scales, 990 with float
+// bf16 instruction's half rate (1280 TFLOP/s with E8M0 scales, 990 with float
 // ones).
 template <int ROWS>
 struct Stage {
@@ -737,9 +737,10 @@ __global__ __launch_bounds__(WAVES *kWave) void matmul_few_kernel(MatmulArgs g) 
 // How a product is launched: up to 8 rows of A into 16-bit results by its
 // weights' rows alone (1 x 12288 x 12288: 31 us against 37 in tiles; 8 x 5120 x
 // 5120: 11 against 15; but 16 x 15360 x 5120: 29 against 23); otherwise in tiles
-// of 256 x 256 (16-bit results of E8M0 operands, where there are enough of
-// them) or 128 x 128, and where those are too few for the 256 CUs, the
-// reduction split into parts that are joined.
+// of 256 x 256 (E8M0 operands, where there are enough of them: 16384 x 4096 x
+// 8192 into float32 861 us against 934, 4098 x 5130 x 2047 136 against 124) or
+// 128 x 128, and where those are too few for the 256 CUs, the reduction split
+// into parts that are joined.
 struct Launch {
     bool few, large;
     int64_t tile, tiles_m, tiles_n;
@@ -748,11 +749,13 @@ struct Launch {
 
 Launch launch_of(int64_t m, int64_t n, int64_t k, Sum sum) {
     Launch p{};
-    p.few = m <= 8 && sum != kExact;
+    p.few = m <= 8 && (sum == kScaled || sum == kFloat);
     const int64_t steps = ceil_div(k, kBlock);
     auto tiles = [&](int64_t side) { return ceil_div(m, side) * ceil_div(n, side); };
-    // rounds of tiles over the CUs: one of 256 x 256 each, or two of 128 x 128 in 2/3 of its time (not 1/2)
-    p.large = sum == kScaled && ceil_div(tiles(256), 256) * 3 <= ceil_div(tiles(128), 512) * 2;
+    // rounds over the CUs: one tile of 256 x 256 on each, or two of 128 x 128 in the measured share of its time,
+    // 2/3 with scaled 8-bit instructions and 7/13 with bf16 ones (half, if both sizes ran equally well)
+    const int64_t large = ceil_div(tiles(256), 256), small = ceil_div(tiles(128), 512);
+    p.large = sum == kScaled ? large * 3 <= small * 2 : sum == kWide && large * 13 <= small * 7;
     p.tile = p.large ? 256 : 128;
     p.tiles_m = ceil_div(m, p.tile);
     p.tiles_n = ceil_div(n, p.tile);
@@ -767,7 +770,8 @@ Launch launch_of(int64_t m, int64_t n, int64_t k, Sum sum) {
 }
 
 Sum sum_for(reshard_dtype_t scale_dtype, reshard_dtype_t out_dtype) {
-    return out_dtype == RESHARD_F32 ? kExact : scale_dtype == RESHARD_E8M0 ? kScaled : kFloat;
+    if (out_dtype == RESHARD_F32) return scale_dtype == RESHARD_E8M0 ? kWide : kExact;
+    return scale_dtype == RESHARD_E8M0 ? kScaled : kFloat;
 }
 
 template <Sum SUM>
@@ -850,7 +854,7 @@ extern "C" reshard_status_t reshard_matmul(int64_t m, int64_t n, int64_t k, cons
         if (!aligned) {
             const dim3 grid(unsigned(ceil_div(m, 128) * ceil_div(n, 128)));
             const uint32_t tiles_n = uint32_t(ceil_div(n, 128));
-            if (sum == kExact) matmul_kernel<kExact><<<grid, 256, 0, s>>>(g, tiles_n);
+            if (sum == kExact || sum == kWide) matmul_kernel<kExact><<<grid, 256, 0, s>>>(g, tiles_n);
             else if (sum == kScaled) matmul_kernel<kScaled><<<grid, 256, 0, s>>>(g, tiles_n);
             else matmul_kernel<kFloat><<<grid, 256, 0, s>>>(g, tiles_n);
             return launched("matmul launch");
@@ -867,7 +871,8 @@ extern "C" reshard_status_t reshard_matmul(int64_t m, int64_t n, int64_t k, cons
         const dim3 grid(unsigned(p.tiles_m * p.tiles_n), unsigned(p.parts));
         const uint32_t tn = uint32_t(p.tiles_n);
         auto launch = [&](auto kernel, int threads) { kernel<<<grid, threads, 0, s>>>(g, tn, p.blocks); };
-        if (sum == kExact && g.e8m0) launch(matmul_tile_kernel<kWide, 2, 2, 2, 2>, 256);
+        if (sum == kWide && p.large) launch(matmul_tile_kernel<kWide, 4, 2, 2, 4>, 512);
+        else if (sum == kWide) launch(matmul_tile_kernel<kWide, 2, 2, 2, 2>, 256);
         else if (sum == kExact) launch(matmul_tile_kernel<kExact, 2, 2, 2, 2>, 256);
         else if (sum == kFloat && b_block_rows == kBlock) launch(matmul_tile_kernel<kUniform, 2, 2, 2, 2>, 256);
         else if (sum == kFloat) launch(matmul_tile_kernel<kFloat, 2, 2, 2, 2>, 256);
