@@ -355,12 +355,12 @@ __device__ inline void unrolled(F &&f) {
 // write LDS in order, so the order of words is set by the addresses they read.
 //
 // Bound by the matrix instructions and the power they take: 16384 x 12288 x
-// 12288 in 256 x 256 tiles with E8M0 scales runs at 2540 TFLOP/s, the
+// 12288 in 256 x 256 tiles with E8M0 scales runs at 2380 to 2560 TFLOP/s, the
 // instruction busy 74 % of the cycles at a clock of 1.65 GHz (on zeros, which
 // take less power, the same code reaches 3430).  Waves of 128 x 128, which read
 // a third less from LDS, measured the same.  Float scales cost an operation
-// an element and block beside the matrix instruction (1590 TFLOP/s with a
-// scale per tile of B, 1320 per row), float32 results the conversion and the
+// an element and block beside the matrix instruction (1450 to 1590 TFLOP/s with
+// a scale per tile of B, 1320 per row), float32 results the conversion and the
 // bf16 instruction's half rate (1280 TFLOP/s with E8M0 scales, 990 with float
 // ones).
 template <int ROWS>
@@ -396,7 +396,8 @@ __global__ __launch_bounds__(WM *WN *kWave, 2) void matmul_tile_kernel(MatmulArg
         g.out_dtype = RESHARD_F32;
         g.accumulate = 0;
     }
-    const int32_t steps = int32_t(ceil_div(g.k, kBlock)), whole = int32_t(g.k / kBlock);
+    const int32_t steps = int32_t(ceil_div(g.k, kBlock));
+    const int32_t paired = int32_t(g.k / (2 * kBlock)) * 2;  // whole blocks, two at a time
 
     // rows past a matrix's end are read as zeros
     const int lrow = t / 8, lword = (t % 8) ^ ((lrow / 2) % 8);
@@ -554,7 +555,7 @@ __global__ __launch_bounds__(WM *WN *kWave, 2) void matmul_tile_kernel(MatmulArg
     auto step = [&](auto cur_, int32_t s, auto &a_cur, auto &b_cur, auto &a_next, auto &b_next) {
         constexpr int cur = decltype(cur_)::value, EACH = (LA + LB + TM - 1) / TM;
         const int snext = sbuf == 2 ? 0 : sbuf + 1;
-        const int32_t ahead = min(s + 2, whole - 1);
+        const int32_t ahead = min(s + 2, paired - 1);
         phase(cur_, low, a_cur, b_cur, [](auto) {});
         // the last step's reads ahead find an older block, which is not used
         put_scales(snext, s + 1 - cur, s + 1);
@@ -576,7 +577,7 @@ __global__ __launch_bounds__(WM *WN *kWave, 2) void matmul_tile_kernel(MatmulArg
         sbuf = snext;
     };
 
-    if (whole > 1) {
+    if (paired > 0) {
         load_scales(0, s_held);
         stage(0, a_lds0, b_lds0);
         put_scales(0, 0, 0);
@@ -588,16 +589,17 @@ __global__ __launch_bounds__(WM *WN *kWave, 2) void matmul_tile_kernel(MatmulArg
         read_scales(s_lds[0], 0);
         unrolled<TM>([&](auto x) { fa[x] = read(a_lds0, a_word, 0, x); });
         unrolled<TN>([&](auto y) { fb[0][y] = read(b_lds0, b_word, 0, y); });
-        for (int32_t s = 0; s + 1 < whole; s += 2) {
+        for (int32_t s = 0; s < paired; s += 2) {
             step(low, s, a_lds0, b_lds0, a_lds1, b_lds1);
             step(high, s + 1, a_lds1, b_lds1, a_lds0, b_lds0);
         }
-        if (whole & 1) step(low, whole - 1, a_lds0, b_lds0, a_lds1, b_lds1);
         loads_done();
         __syncthreads();
     }
+    // An odd block, and a short one, whose missing codes are zeros.  (An odd one in the pipeline above would save 3 %
+    // where there are 15 and cost all others 1 %, in spilled registers.)
 #pragma unroll 1
-    for (int32_t s = whole > 1 ? whole : 0; s < steps; ++s) {  // the short block, whose missing codes are zeros
+    for (int32_t s = paired; s < steps; ++s) {
         const int64_t l = int64_t(s) * kBlock + lword * 16;
 #pragma unroll 1
         for (int u = 0; u < LA; ++u)

@@ -127,6 +127,24 @@ def test_layer_norm_without_weights_in_place_and_no_rows(gpu_lib):
 
 
 @gpu
+@pytest.mark.parametrize("cols", [3, 130, 777, 4098])
+@pytest.mark.parametrize("dtype,wt", [(torch.float32, torch.float16), (torch.float32, torch.bfloat16),
+                                      (torch.bfloat16, torch.float16), (torch.float16, torch.bfloat16)], ids=str)
+def test_layer_norm_weights_of_another_type(dtype, wt, cols, gpu_lib):
+    """Weights of one 16-bit type equal the same weights in float32, bit for bit, in both passes; either may be left out."""
+    g = _seed("types", dtype, wt, cols)
+    x, dy = _randn(g, 6, cols).to(dtype).cuda(), _randn(g, 6, cols).to(dtype).cuda()
+    w, b = (_randn(g, cols).to(wt).cuda() for _ in range(2))
+    for weight, bias in ((w, b), (w, None), (None, b)):
+        got = B.reshard_layer_norm(x, weight, bias)
+        want = B.reshard_layer_norm(x, *(None if v is None else v.float() for v in (weight, bias)))
+        assert all(torch.equal(p, q) for p, q in zip(got, want))
+    got = B.reshard_layer_norm_backward(dy, x, w, *got[1:])
+    want = B.reshard_layer_norm_backward(dy, x, w.float(), *want[1:])
+    assert all(torch.equal(p, q) for p, q in zip(got, want))
+
+
+@gpu
 def test_layer_norm_special_rows(gpu_lib):
     """A constant row, the type's largest values, and rows with NaN or an infinity, beside ordinary ones."""
     cols = 777
