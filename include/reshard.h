@@ -421,8 +421,9 @@ reshard_status_t reshard_pipeline_simulate(int32_t stages, int32_t microbatches,
  * What a pipeline stage does with an activation or gradient right before it
  * leaves and right after it arrives: layer norm and its gradients, the 8-bit
  * form in which it crosses in half the bytes (the codes and the scales are
- * tensors that a plan moves like any other, types E4M3 and E8M0), and the
- * product that takes that form.
+ * tensors that a plan moves like any other, types E4M3 and E8M0; a plan's
+ * buffers are dense, so rows of codes that it moves have a pitch of cols), and
+ * the product that takes that form.
  *
  * Conventions shared by these calls:
  *  - Matrices are row-major: element (r, c) lies at base + (r * pitch + c)

@@ -176,17 +176,35 @@ def _find_dtype_code(dtype):
     return _DTYPES[name]
 
 
+def _gapless(shape, strides):
+    """Whether elements fill one run of memory, the dimensions in any order (a buffer's need not be the tensor's)."""
+    run = 1
+    for step, n in sorted((s, n) for n, s in zip(shape, strides) if n != 1):
+        if step != run:
+            return False
+        run *= n
+    return True
+
+
+def _refuse_gaps(shape, strides):
+    if 0 not in shape and not _gapless(shape, strides):
+        raise ValueError(f"a plan's buffers are dense, got shape {tuple(shape)} with strides {tuple(strides)}")
+
+
 def _addr(b):
     if b is None or isinstance(b, int):
         return b
-    return b.data_ptr() if b.numel() > 0 else None
+    if not b.is_contiguous():
+        _refuse_gaps(b.shape, b.stride())
+    return b.data_ptr() or None  # NULL for an empty tensor
 
 
 def pointer_array(bufs):
     """The `void *const *` array reshard_execute takes, built once.
 
     `bufs` holds tensors (an empty one passes NULL), integer addresses or
-    None.  A caller that reshards the same buffers repeatedly can build the
+    None.  A tensor with gaps between its elements is refused: the plan would
+    move what lies in them.  A caller that reshards the same buffers repeatedly can build the
     two arrays once and pass them to every reshard_execute, which then skips
     the per-buffer marshalling.  The array holds addresses only: the tensors
     must stay alive (and unmoved) while it is in use.
@@ -308,8 +326,9 @@ def reshard_debug_execute_host(plan, src_bufs, dst_bufs):
         if b is None:
             return None
         if hasattr(b, "ctypes"):
+            _refuse_gaps(b.shape, [s // b.itemsize for s in b.strides])
             return b.ctypes.data if b.size > 0 else None
-        return b.data_ptr() if b.numel() > 0 else None
+        return _addr(b)
     if len(src_bufs) != plan.n_src or len(dst_bufs) != plan.n_dst:
         raise ValueError(f"need {plan.n_src} source and {plan.n_dst} destination buffers")
     _check(load().reshard_debug_execute_host(plan.handle, _ptrs([ptr(b) for b in src_bufs]),
@@ -407,7 +426,9 @@ class Blocked(NamedTuple):
 
     data: float8_e4m3fn [..., cols]; scales: float8_e8m0fnu or float32
     [ceil(rows / block_rows), ceil(cols / 128)]; block_rows: 1 or 128.  Both
-    tensors reshard like any other (a plan on each)."""
+    tensors reshard like any other (a plan on each) where they are dense, as
+    plans take all buffers: codes made with dense=True, or of a width that 128
+    divides."""
     data: object
     scales: object
     block_rows: int = 1
@@ -539,15 +560,16 @@ def reshard_layer_norm_backward(dy, x, weight, mean, rstd, dweight=None, dbias=N
 _E4M3, _BLOCK = "float8_e4m3fn", 128
 
 
-def _empty_blocked(x, rows, cols, block_rows, scale_dtype):
-    """(Blocked, codes' pitch, scales' pitch) beside x.  Rows of codes are padded to whole blocks, so that each
-    starts on a 16-byte boundary."""
+def _empty_blocked(x, rows, cols, block_rows, scale_dtype, dense):
+    """(Blocked, codes' pitch, scales' pitch) beside x.  Rows of codes are dense, or padded to whole blocks, so that
+    each starts on a 16-byte boundary."""
     across = -(-cols // _BLOCK)
-    data = x.new_empty((rows, across * _BLOCK), dtype=_torch.float8_e4m3fn)
+    pitch = cols if dense else across * _BLOCK
+    data = x.new_empty((rows, pitch), dtype=_torch.float8_e4m3fn)
     scales = x.new_empty((rows if block_rows == 1 else -(-rows // block_rows), across), dtype=scale_dtype)
-    if cols != across * _BLOCK:
+    if cols != pitch:
         data = data[:, :cols]
-    return Blocked(data, scales, block_rows), across * _BLOCK, across
+    return Blocked(data, scales, block_rows), pitch, across
 
 
 def _blocked(name, b):
@@ -567,11 +589,14 @@ def _blocked(name, b):
     return rows, cols, pitch, spitch
 
 
-def reshard_quantize(x, block_rows=1, transposed=False, scale_dtype=None, stream=None):
+def reshard_quantize(x, block_rows=1, transposed=False, scale_dtype=None, stream=None, dense=False):
     """x in 8 bits with a power-of-two scale per block (Blocked; x's leading
     dimensions are kept, and count as rows).  transposed=True: of x as a matrix
     of rows, transposed, with blocks along x's rows; "both": the pair, from one reading of x.  scale_dtype:
-    torch.float8_e8m0fnu (default) or torch.float32."""
+    torch.float8_e8m0fnu (default) or torch.float32.  Rows of codes start on
+    16-byte boundaries, with room between them where 128 does not divide the
+    width: so a product reads them fastest.  dense=True: they follow each
+    other, as a plan's buffers do."""
     lib = _lib or load()
     rows, cols, pitch = _matrix("x", x)
     if transposed not in (False, True, "both"):
@@ -585,10 +610,10 @@ def reshard_quantize(x, block_rows=1, transposed=False, scale_dtype=None, stream
     args = [None, 0, None, 0, None, 0, None, 0]
     with _on(stream):
         if transposed is not True:
-            q, pitch_q, pitch_s = _empty_blocked(x, rows, cols, block_rows, scale_dtype)
+            q, pitch_q, pitch_s = _empty_blocked(x, rows, cols, block_rows, scale_dtype, dense)
             args[:4] = q.data.data_ptr(), pitch_q, q.scales.data_ptr(), pitch_s
         if transposed is not False:
-            t, pitch_q, pitch_s = _empty_blocked(x, cols, rows, block_rows, scale_dtype)
+            t, pitch_q, pitch_s = _empty_blocked(x, cols, rows, block_rows, scale_dtype, dense)
             args[4:] = t.data.data_ptr(), pitch_q, t.scales.data_ptr(), pitch_s
     status = lib.reshard_quantize(rows, cols, x.data_ptr(), pitch, _dtype_code(x.dtype), block_rows,
                                   _dtype_code(scale_dtype), *args, _stream_handle(stream))

@@ -49,7 +49,7 @@ class Boundary:
 
     def move(self, way, shards):
         """16-bit shards across the boundary in 8 bits."""
-        sent = [B.reshard_quantize(x) for x in shards]
+        sent = [B.reshard_quantize(x, dense=True) for x in shards]
         codes, scales = self.plans[way]
         arrived = [B.empty_shards(codes, 1), B.empty_shards(scales, 1)]
         B.reshard_execute(codes, [b.data for b in sent], arrived[0])

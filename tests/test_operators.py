@@ -711,3 +711,52 @@ def test_blocked_types_reshard():
         B.reshard_debug_execute_host(plan, src, dst)
         for d, want in zip(dst, (codes[:, :4], codes[:, 4:])):
             assert torch.equal(d.view(torch.uint8), want)
+
+
+def test_plans_refuse_buffers_with_gaps():
+    """Codes whose rows are padded are no plan's buffer: moved as if they were dense, the padding would arrive as codes."""
+    x = torch.zeros(128, 390)
+    padded = B._empty_blocked(x, 128, 390, 1, E8M0, False)[0].data
+    dense = B._empty_blocked(x, 128, 390, 1, E8M0, True)[0].data
+    assert padded.stride() == (512, 1) and dense.stride() == (390, 1)
+    plan = B.reshard_plan((128, 390), E4M3, (1,), "R R", (1,), "R R")
+    for src, dst in ((padded, dense), (dense, padded)):
+        for move in (B.reshard_debug_execute_host, B.reshard_execute, B.reshard_execute_noalloc):
+            with pytest.raises(ValueError, match="dense"):
+                move(plan, [src], [dst])
+    with pytest.raises(ValueError, match="dense"):
+        B.reshard_debug_execute_host(plan, [padded.view(torch.uint8).numpy()], [dense])
+    # elements without gaps, in another order of dimensions: a permuted plan's buffer seen as the tensor it holds
+    turned = torch.zeros(3, 1, 5, 4).permute(2, 0, 3, 1)
+    assert B.pointer_array([turned, padded[:1], padded[:0]])[:] == [turned.data_ptr(), padded.data_ptr(), None]
+
+
+def test_dense_codes_reshard_at_an_odd_width():
+    codes = torch.randint(0, 256, (128, 390), generator=_seed("move")).to(torch.uint8)
+    plan = B.reshard_plan((128, 390), E4M3, (2,), "S^0 R", (3,), "R S^0")
+    src = [B._empty_blocked(codes, 64, 390, 1, E8M0, True)[0].data for _ in range(2)]
+    for i, t in enumerate(src):
+        t.view(torch.uint8).copy_(codes[64 * i:64 * i + 64])
+    dst = B.empty_shards(plan, 1, device="cpu")
+    B.reshard_debug_execute_host(plan, src, dst)
+    for i, t in enumerate(dst):
+        assert torch.equal(t.view(torch.uint8), codes[:, 130 * i:130 * i + 130])
+
+
+@gpu
+@pytest.mark.parametrize("cols", [390, 512, 7])
+def test_quantized_shards_through_plans(cols, gpu_lib):
+    """Each sender's rows to 8 bits, codes and scales through plans, and back on every receiver: the values of the
+    whole tensor's 8-bit form, bit for bit."""
+    x = (_randn(_seed("through", cols), 6, 64, cols) * 3).to(torch.bfloat16).cuda()
+    want = B.reshard_dequantize(B.reshard_quantize(x), x.dtype)
+    blocks = -(-cols // 128)
+    for scale_dtype in (E8M0, torch.float32):
+        sent = [B.reshard_quantize(s, scale_dtype=scale_dtype, dense=True) for s in x.split(3)]
+        arrived = []
+        for part, width, dtype in ((0, cols, E4M3), (1, blocks, scale_dtype)):
+            plan = B.reshard_plan((6, 64, width), dtype, (2,), "S^0 R R", (4,), "R S^0 R")
+            arrived.append(B.empty_shards(plan, 1))
+            B.reshard_execute(plan, [b[part] for b in sent], arrived[-1])
+        for q, s, w in zip(*arrived, want.split(16, 1)):
+            assert torch.equal(B.reshard_dequantize(B.Blocked(q, s), x.dtype), w)
