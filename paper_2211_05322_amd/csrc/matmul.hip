@@ -288,8 +288,8 @@ __device__ inline void store_run(const MatmulArgs &g, int64_t i, int64_t j, f32x
     else store_eight<f16>(g, i, j, lo, hi);
 }
 
-// A descriptor for `bytes` bytes from p, the same in every lane.  Loads past
-// the end give zeros, the wave's offset counted in.
+// A descriptor for `bytes` bytes from p, the same in every lane.  Loads from an
+// offset past the end give zeros.
 __device__ inline __amdgpu_buffer_rsrc_t bytes_from(const uint8_t *p, int64_t bytes) {
     const uint64_t a = reinterpret_cast<uint64_t>(p);
     const uint64_t lo = uint32_t(__builtin_amdgcn_readfirstlane(int(a)));
@@ -298,11 +298,12 @@ __device__ inline __amdgpu_buffer_rsrc_t bytes_from(const uint8_t *p, int64_t by
     return __builtin_amdgcn_make_buffer_rsrc(reinterpret_cast<void *>(hi << 32 | lo), 0, n, 0x00020000);
 }
 
-// 16 bytes of a lane's straight into LDS, from `base` + its offset + the
-// wave's offset; lane l's go to `to` + 16 l, `to` being the wave's.
-__device__ inline void load_to_lds(__amdgpu_buffer_rsrc_t base, uint32_t offset, uint32_t wave_offset, uint4 *to) {
-    __builtin_amdgcn_raw_ptr_buffer_load_lds(base, (__attribute__((address_space(3))) void *)to, 16, offset,
-                                             wave_offset, 0, 0);
+// 16 bytes of a lane's straight into LDS, from `base` + its offset; lane l's
+// go to `to` + 16 l, `to` being the wave's.  The whole offset is the lane's:
+// the instruction's scalar offset is subtracted from the descriptor's size in
+// the range check, which past a matrix's last rows would be below zero.
+__device__ inline void load_to_lds(__amdgpu_buffer_rsrc_t base, uint32_t offset, uint4 *to) {
+    __builtin_amdgcn_raw_ptr_buffer_load_lds(base, (__attribute__((address_space(3))) void *)to, 16, offset, 0, 0, 0);
 }
 
 // Before a barrier behind which other waves read what this one loaded into
@@ -410,9 +411,9 @@ __global__ __launch_bounds__(WM *WN *kWave, 2) void matmul_tile_kernel(MatmulArg
     auto stage_one = [&](int32_t s, auto &a_lds, auto &b_lds, auto u_) {
         constexpr int u = decltype(u_)::value;
         if constexpr (u < LA)
-            load_to_lds(a_base, a_off, u * a_next_rows + s * kBlock, &a_lds.words[u * THREADS + wave * kWave]);
+            load_to_lds(a_base, a_off + (u * a_next_rows + s * kBlock), &a_lds.words[u * THREADS + wave * kWave]);
         else
-            load_to_lds(b_base, b_off, (u - LA) * b_next_rows + s * kBlock,
+            load_to_lds(b_base, b_off + ((u - LA) * b_next_rows + s * kBlock),
                         &b_lds.words[(u - LA) * THREADS + wave * kWave]);
     };
     auto stage = [&](int32_t s, auto &a_lds, auto &b_lds) {

@@ -760,3 +760,30 @@ def test_quantized_shards_through_plans(cols, gpu_lib):
             B.reshard_execute(plan, [b[part] for b in sent], arrived[-1])
         for q, s, w in zip(*arrived, want.split(16, 1)):
             assert torch.equal(B.reshard_dequantize(B.Blocked(q, s), x.dtype), w)
+
+
+def _whole_numbers(g, rows, cols, block_rows, scale_dtype, at_end=False):
+    """A Blocked of whole numbers from -8 to 8, all scales 1, and its values: eight neighbouring products span 7 bits
+    at most, so that any kernel's sums are exact.  at_end: as the last bytes of an allocation of its own."""
+    x = torch.randint(-8, 9, (rows, cols), generator=g).float()
+    pitch = -(-cols // 16) * 16
+    whole = -(-rows * pitch // (2 << 20)) * (2 << 20) + (20 << 20)  # above what an allocator shares
+    store = torch.full((whole,), 0x7F, dtype=torch.uint8, device="cuda")
+    end = (rows - 1) * pitch + cols
+    data = store[(whole - end) // 16 * 16 if at_end else 0:].as_strided((rows, cols), (pitch, 1))
+    data.copy_(x.cuda().to(E4M3).view(torch.uint8))
+    scales = torch.ones(-(-rows // block_rows), -(-cols // 128), device="cuda").to(scale_dtype)
+    return B.Blocked(data.view(E4M3), scales, block_rows), x.double()
+
+
+# last tiles of a few rows, where most of a tile's rows lie past the end of the matrix, in both tile sizes
+@gpu
+@pytest.mark.parametrize("m,n,k", [(9, 1, 256), (65, 129, 512), (130, 257, 1024), (129, 130, 4096), (3080, 4100, 512)])
+@pytest.mark.parametrize("scale_dtype", [E8M0, torch.float32], ids=["e8m0", "fp32"])
+def test_matmul_at_the_end_of_its_memory(scale_dtype, m, n, k, gpu_lib):
+    g = _seed("end", str(scale_dtype), m, n, k)
+    a, a64 = _whole_numbers(g, m, k, 1, scale_dtype, at_end=True)
+    b, b64 = _whole_numbers(g, n, k, 128, scale_dtype, at_end=True)
+    want = (a64.float().cuda() @ b64.float().cuda().t())  # below 2^24: exact
+    for dt in HALVES:
+        assert torch.equal(B.reshard_matmul(a, b, dt), want.to(dt)), dt
