@@ -532,7 +532,7 @@ reshard_status_t reshard_dequantize(int64_t rows, int64_t cols, const void *q, i
  * are not read into the result, whatever they hold.
  */
 int64_t reshard_matmul_workspace(int64_t m, int64_t n, int64_t k, reshard_dtype_t scale_dtype,
-                                 reshard_dtype_t out_dtype); /* bytes, 0: none needed; -1: bad extents */
+                                 reshard_dtype_t out_dtype); /* bytes, 0: none needed; -1: bad extents, or too many tiles */
 reshard_status_t reshard_matmul(int64_t m, int64_t n, int64_t k, const void *a, int64_t a_pitch, int a_block_rows,
                                 const void *a_scales, int64_t a_scales_pitch, const void *b, int64_t b_pitch,
                                 int b_block_rows, const void *b_scales, int64_t b_scales_pitch,

@@ -751,6 +751,10 @@ struct Launch {
     int32_t parts, blocks;  // parts of the reduction, and the blocks of each
 };
 
+// At most 2^20 tiles of 128 x 128 in `out`.  Extents up to 2^40 have as many
+// tiles as 64 bits do not count, so this comes before launch_of.
+bool too_many_tiles(int64_t m, int64_t n) { return ceil_div(n, 128) > (int64_t(1) << 20) / ceil_div(m, 128); }
+
 Launch launch_of(int64_t m, int64_t n, int64_t k, Sum sum) {
     Launch p{};
     p.few = m <= 8 && (sum == kScaled || sum == kFloat);
@@ -805,6 +809,7 @@ extern "C" int64_t reshard_matmul_workspace(int64_t m, int64_t n, int64_t k, res
                                             reshard_dtype_t out_dtype) {
     if (m < 0 || n < 0 || k < 0 || m > int64_t(1) << 40 || n > int64_t(1) << 40 || k > int64_t(1) << 36) return -1;
     if (m == 0 || n == 0) return 0;
+    if (rs::too_many_tiles(m, n)) return -1;
     const rs::Launch p = rs::launch_of(m, n, k, rs::sum_for(scale_dtype, out_dtype));
     return p.parts > 1 ? int64_t(p.parts) * m * n * int64_t(sizeof(float)) : 0;
 }
@@ -831,7 +836,7 @@ extern "C" reshard_status_t reshard_matmul(int64_t m, int64_t n, int64_t k, cons
         if (st == RESHARD_OK)
             st = check_matrix("out", out, m, n, out_pitch, out_dtype == RESHARD_F32 ? 4 : 2);
         if (st != RESHARD_OK || m == 0 || n == 0) return st;
-        if (ceil_div(n, 128) > (int64_t(1) << 20) / ceil_div(m, 128))
+        if (too_many_tiles(m, n))
             return fail(RESHARD_EUNSUPPORTED, "out has more than 2^20 tiles of 128 x 128");
         if (k > int64_t(1) << 36) return fail(RESHARD_EUNSUPPORTED, "k is above 2^36");
         MatmulArgs g{};

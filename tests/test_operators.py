@@ -787,3 +787,14 @@ def test_matmul_at_the_end_of_its_memory(scale_dtype, m, n, k, gpu_lib):
     want = (a64.float().cuda() @ b64.float().cuda().t())  # below 2^24: exact
     for dt in HALVES:
         assert torch.equal(B.reshard_matmul(a, b, dt), want.to(dt)), dt
+
+
+@pytest.mark.parametrize("m,n", [(1 << 40, 1 << 40), (1 << 40, 1 << 39), (1 << 33, 1 << 38), ((1 << 40) - 127, (1 << 38) + 1),
+                                 (1 << 27, 129), (129, 1 << 27)])
+def test_workspace_of_more_tiles_than_a_product_has(m, n):
+    """Refused by the query as by the product, also where the tiles' number leaves 64 bits; to the limit it answers."""
+    lib = B.load()
+    for scales in (4, 13):
+        for out in (2, 3, 4):
+            assert lib.reshard_matmul_workspace(m, n, 128, scales, out) == -1
+            assert lib.reshard_matmul_workspace(1 << 20, 1 << 14, 1 << 20, scales, out) == 0
