@@ -798,3 +798,43 @@ def test_workspace_of_more_tiles_than_a_product_has(m, n):
         for out in (2, 3, 4):
             assert lib.reshard_matmul_workspace(m, n, 128, scales, out) == -1
             assert lib.reshard_matmul_workspace(1 << 20, 1 << 14, 1 << 20, scales, out) == 0
+
+
+def _round_once(v, dtype):
+    """Doubles to the nearest of dtype's values, ties to even, from its precision and smallest exponent alone."""
+    digits, least = {torch.float16: (11, -14), torch.bfloat16: (8, -126)}[dtype]
+    _, e = torch.frexp(v)
+    step = torch.exp2((e - 1).clamp(min=least).double() - (digits - 1))
+    r = torch.round(v / step) * step
+    return torch.where(r.abs() > torch.finfo(dtype).max, torch.copysign(torch.tensor(math.inf, dtype=torch.float64), r), r)
+
+
+@gpu
+@pytest.mark.parametrize("dtype", [torch.float16, torch.bfloat16], ids=str)
+def test_dequantize_rounds_once(dtype, gpu_lib):
+    """Products that lie nearer to the midpoint of two 16-bit values than float32 tells, of every code with scales of
+    every size: those of the type's subnormals, of float32's, and past the largest value."""
+    g = _seed("once", dtype)
+    codes = torch.arange(256, dtype=torch.uint8).repeat(4, 1).t().reshape(8, 128)  # four of each code in a row
+    digits = 11 if dtype == torch.float16 else 8
+    rows = []
+    for e in list(range(-149, 121, 3)) + list(range(-40, 20)):
+        code = codes.view(E4M3).double()[torch.randint(0, 8, (1,), generator=g), torch.randint(0, 128, (16,), generator=g)]
+        code = code[torch.isfinite(code) & (code != 0)].abs()
+        middle = 1 + (2 * torch.randint(0, 1 << (digits - 1), code.shape, generator=g) + 1).double() * 2.0 ** -digits
+        near = (middle / code * 2.0 ** e).float()  # a scale that takes this code to a midpoint, or as near as float32 comes
+        rows += [near, torch.nextafter(near, torch.tensor(math.inf))]
+    scales = torch.cat(rows)
+    scales = torch.cat([scales, torch.tensor([0.0, -0.0, 1e-45, -1.7, math.inf, -math.inf, math.nan, float.fromhex("0x1.3caaaap-2")])])
+    x = codes.repeat_interleave(len(scales), 0)
+    s = scales.repeat(8)[:, None]
+    got = B.reshard_dequantize(B.Blocked(x.cuda().view(E4M3), s.cuda()), dtype).cpu()
+    exact = x.view(E4M3).double() * s.double()
+    want = _round_once(exact, dtype)
+    want = torch.where(torch.isfinite(exact), want, exact)
+    _same(got.double(), want, dtype)
+    assert (want != exact.float().to(dtype).double()).nan_to_num().any(), "no product here that two roundings get wrong"
+    one = B.Blocked(torch.tensor([[0x03]], dtype=torch.uint8, device="cuda").view(E4M3),
+                    torch.tensor([[float.fromhex("0x1.3caaaap-2")]], device="cuda"))
+    if dtype == torch.bfloat16:
+        assert B.reshard_dequantize(one, dtype).item() == 0.00180816650390625
