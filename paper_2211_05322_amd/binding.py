@@ -446,6 +446,8 @@ def _matrix(name, t):
         raise ValueError(f"{name}: the last dimension must be dense, its stride is {strides[-1]}")
     if len(shape) == 2:
         return shape[0], cols, strides[0]
+    if 0 in shape[:-1]:
+        return 0, cols, cols
     rows, pitch = 1, None
     for n, s in zip(reversed(shape[:-1]), reversed(strides[:-1])):
         if n != 1:

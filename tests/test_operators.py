@@ -838,3 +838,29 @@ def test_dequantize_rounds_once(dtype, gpu_lib):
                     torch.tensor([[float.fromhex("0x1.3caaaap-2")]], device="cuda"))
     if dtype == torch.bfloat16:
         assert B.reshard_dequantize(one, dtype).item() == 0.00180816650390625
+
+
+def test_matrix_of_empty_leading_dimensions():
+    for shape in ((4, 0, 130), (0, 4, 130), (4, 3, 0, 5), (2, 0, 0, 7), (0, 0)):
+        rows, cols, _ = B._matrix("x", torch.zeros(shape))
+        assert rows == 0 and cols == shape[-1]
+    assert B._matrix("x", torch.zeros(4, 3, 0))[:2] == (12, 0)
+    with pytest.raises(ValueError, match="step evenly"):
+        B._matrix("x", torch.zeros(4, 6, 5)[:, ::2][:, :2])
+
+
+@gpu
+@pytest.mark.parametrize("shape", [(4, 0, 130), (0, 3, 130), (2, 0, 0, 256)])
+def test_empty_batches(shape, gpu_lib):
+    """A batch without rows, as a device has that a dimension's split leaves nothing: empty results, no gradient."""
+    x = torch.empty(shape, device="cuda")
+    y, mean, rstd = B.reshard_layer_norm(x)
+    assert y.shape == x.shape and mean.shape == rstd.shape == x.shape[:-1]
+    dx, dw, db = B.reshard_layer_norm_backward(y, x, None, mean, rstd)
+    assert dx.shape == x.shape and (dw == 0).all() and (db == 0).all()
+    q, t = B.reshard_quantize(x, transposed="both")
+    assert q.data.shape == x.shape and t.data.shape == (shape[-1], 0)
+    assert B.reshard_dequantize(q, torch.float16).shape == x.shape
+    w = B.reshard_quantize(torch.randn(9, shape[-1], device="cuda"), 128)
+    assert B.reshard_matmul(q, w).shape == (*shape[:-1], 9)
+    assert (B.reshard_matmul(t, t, torch.float32) == 0).all()  # a reduction over no rows

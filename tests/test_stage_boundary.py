@@ -61,3 +61,18 @@ def test_boundary_refuses_blocks_across_devices(gpu_lib):
     w = torch.zeros(8, 300, device="cuda")
     with pytest.raises(ValueError, match="multiple of 512"):
         S.Boundary(2, 8, 300, w, w[0], w[0])
+
+
+def test_boundary_with_devices_that_hold_nothing(gpu_lib):
+    """Fewer rows than devices: their shards are empty, and the others' results those of the whole tensors."""
+    batch, seq, hidden, out = 1, 2, 512, 130
+    edge, x, dz = S.example(batch, seq, hidden, out, seed=5)
+    outs, kept = edge.forward(S.scatter(x, S.SENDER))
+    assert sorted(z.numel() // out for z in outs) == [0] * 6 + [1, 1]
+    back = edge.backward(S.scatter(dz, S.RECEIVER), kept)
+    whole_x, y, mean, rstd = _whole(edge, x, dz)
+    assert torch.equal(S.gather([k[0] for k in kept], x.shape, S.RECEIVER), whole_x)
+    assert torch.equal(S.gather(outs, dz.shape, S.RECEIVER), B.reshard_matmul(B.reshard_quantize(y), edge.weight, x.dtype))
+    dy = B.reshard_matmul(B.reshard_quantize(dz), edge.weight_t, dz.dtype)
+    dx, _, _ = B.reshard_layer_norm_backward(dy, whole_x, edge.gamma, mean, rstd)
+    assert torch.equal(S.gather(back, x.shape, S.SENDER), B.reshard_dequantize(B.reshard_quantize(dx), dx.dtype))
