@@ -621,9 +621,10 @@ def reshard_quantize(x, block_rows=1, transposed=False, scale_dtype=None, stream
                                   _dtype_code(scale_dtype), *args, _stream_handle(stream))
     if status != RESHARD_OK:
         _check(status)
-    if q is not None and x.dim() > 2:
-        scales = q.scales.unflatten(0, x.shape[:-1]) if block_rows == 1 else q.scales
-        q = Blocked(q.data.unflatten(0, x.shape[:-1]), scales, block_rows)
+    if q is not None and x.dim() != 2:
+        def lead(t):
+            return t.unflatten(0, x.shape[:-1]) if x.dim() > 2 else t[0]
+        q = Blocked(lead(q.data), lead(q.scales) if block_rows == 1 else q.scales, block_rows)
     return (q, t) if transposed == "both" else q if t is None else t
 
 

@@ -864,3 +864,35 @@ def test_empty_batches(shape, gpu_lib):
     w = B.reshard_quantize(torch.randn(9, shape[-1], device="cuda"), 128)
     assert B.reshard_matmul(q, w).shape == (*shape[:-1], 9)
     assert (B.reshard_matmul(t, t, torch.float32) == 0).all()  # a reduction over no rows
+
+
+@gpu
+@pytest.mark.parametrize("cols", [1, 300, 512])
+def test_operators_on_a_single_row(cols, gpu_lib):
+    """A tensor of one dimension is one row, and so are its results."""
+    x = torch.randn(cols, device="cuda")
+    for block_rows in (1, 128):
+        q, q2 = B.reshard_quantize(x, block_rows), B.reshard_quantize(x[None], block_rows)
+        assert q.data.shape == x.shape and torch.equal(q.data.view(torch.uint8), q2.data[0].view(torch.uint8))
+        assert q.scales.shape == ((-(-cols // 128),) if block_rows == 1 else q2.scales.shape)
+        back = B.reshard_dequantize(q, torch.float32)
+        assert back.shape == x.shape and torch.equal(back, B.reshard_dequantize(q2, torch.float32)[0])
+        w = B.reshard_quantize(torch.randn(9, cols, device="cuda"))
+        assert torch.equal(B.reshard_matmul(q, w), B.reshard_matmul(q2, w)[0])
+        t = B.reshard_quantize(x, block_rows, transposed=True)
+        assert t.data.shape == (cols, 1)
+    y, mean, rstd = B.reshard_layer_norm(x)
+    assert y.shape == x.shape and mean.shape == rstd.shape == ()
+    dx, dw, _ = B.reshard_layer_norm_backward(y, x, None, mean, rstd)
+    assert dx.shape == dw.shape == x.shape
+
+
+@gpu
+def test_operators_keep_leading_dimensions(gpu_lib):
+    x = torch.randn(2, 3, 50, 300, device="cuda")
+    flat = x.view(300, 300)
+    for block_rows in (1, 128):
+        q, want = B.reshard_quantize(x, block_rows), B.reshard_quantize(flat, block_rows)
+        assert q.data.shape == x.shape and q.scales.shape == ((2, 3, 50, 3) if block_rows == 1 else (3, 3))
+        assert torch.equal(B.reshard_dequantize(q, x.dtype).view(300, 300), B.reshard_dequantize(want, x.dtype))
+        assert torch.equal(B.reshard_matmul(q, want).view(300, 300), B.reshard_matmul(want, want))
