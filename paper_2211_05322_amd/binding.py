@@ -603,6 +603,8 @@ def reshard_quantize(x, block_rows=1, transposed=False, scale_dtype=None, stream
     rows, cols, pitch = _matrix("x", x)
     if transposed not in (False, True, "both"):
         raise ValueError(f'transposed must be False, True or "both", got {transposed!r}')
+    if transposed != "both":
+        transposed = bool(transposed)  # 0 and numpy's False equal False and are not it
     if block_rows not in (1, _BLOCK):
         raise ValueError(f"block_rows must be 1 or {_BLOCK}, got {block_rows}")
     if scale_dtype is None:

@@ -15,6 +15,7 @@ import itertools
 import math
 import zlib
 
+import numpy as np
 import pytest
 import torch
 
@@ -896,3 +897,11 @@ def test_operators_keep_leading_dimensions(gpu_lib):
         assert q.data.shape == x.shape and q.scales.shape == ((2, 3, 50, 3) if block_rows == 1 else (3, 3))
         assert torch.equal(B.reshard_dequantize(q, x.dtype).view(300, 300), B.reshard_dequantize(want, x.dtype))
         assert torch.equal(B.reshard_matmul(q, want).view(300, 300), B.reshard_matmul(want, want))
+
+
+@gpu
+def test_quantize_takes_truth_values_of_any_type(gpu_lib):
+    x = torch.randn(5, 300, device="cuda")
+    for no, yes in ((0, 1), (np.False_, np.True_)):
+        assert B.reshard_quantize(x, transposed=no).data.shape == (5, 300)
+        assert B.reshard_quantize(x, transposed=yes).data.shape == (300, 5)
