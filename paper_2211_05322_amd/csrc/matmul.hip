@@ -624,7 +624,7 @@ __global__ __launch_bounds__(WM *WN *kWave, 2) void matmul_tile_kernel(MatmulArg
     // through its part of LDS (float32, 16-byte word w of row r in slot
     // w ^ (r % 8)), so that lanes store runs of a row.
     f32x4 *turn = reinterpret_cast<f32x4 *>(a_lds0.words) + wave * 256;
-    static_assert(WM * WN * 256 <= BM * 16, "LDS for the results");
+    static_assert(WM * WN * 256 * sizeof(f32x4) <= sizeof(a_lds0.words), "LDS for the results");
     unrolled<TM>([&](auto x) {
         unrolled<TN>([&](auto y) {
             unrolled<4>([&](auto q_) {
