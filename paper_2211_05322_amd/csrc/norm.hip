@@ -453,7 +453,9 @@ bool with_columns(int64_t cols, F &&f) {
     bool done = false;
     auto offer = [&](auto threads, auto n) {
         constexpr int THREADS = decltype(threads)::value, NV = decltype(n)::value;
-        if constexpr (THREADS * NV <= MOST && NV <= (THREADS == 512 ? EACH : 4)) {
+        // 1024 threads only for rows that 512 do not hold
+        if constexpr (THREADS * NV <= MOST && NV <= (THREADS == 512 ? EACH : 4) &&
+                      (THREADS < 1024 || THREADS * NV > 512 * EACH)) {
             if (!done && nv <= THREADS * NV) {
                 f(threads, n);
                 done = true;
