@@ -454,7 +454,9 @@ reshard_status_t reshard_pipeline_simulate(int32_t stages, int32_t microbatches,
  * elements of weight_dtype (one of the three, whatever dtype is) and may be
  * NULL for 1 and 0.  mean and rstd (rows floats each, may be NULL) are what
  * the backward pass reads.  y may be x itself with the same pitch.  cols >= 1,
- * eps >= 0; rows may be 0; at most 2^24 columns.
+ * eps >= 0; rows may be 0; at most 2^24 columns.  A row whose squared distances
+ * from its mean sum to more than float32 holds has rstd 0, and y = bias; one
+ * whose elements do, an infinite mean and NaN in y.
  */
 reshard_status_t reshard_layer_norm(int64_t rows, int64_t cols, const void *x, int64_t x_pitch,
                                     reshard_dtype_t dtype, const void *weight, const void *bias,

@@ -905,3 +905,149 @@ def test_quantize_takes_truth_values_of_any_type(gpu_lib):
     for no, yes in ((0, 1), (np.False_, np.True_)):
         assert B.reshard_quantize(x, transposed=no).data.shape == (5, 300)
         assert B.reshard_quantize(x, transposed=yes).data.shape == (300, 5)
+
+
+def _check_norm(x, y, mean, rstd, w, b, what):
+    """Bounds of test_layer_norm, on the GPU."""
+    x64, w64, b64 = x.double(), w.double(), b.double()
+    want, m64, r64 = _norm64(x64, w64, b64, 1e-5)
+    d = _chain(x.shape[1])
+    dm = (d + 2) * F32 * x64.abs().mean(1, keepdim=True)
+    spread = (x64 - m64).abs()
+    dv = (d + 6) * F32 * (spread ** 2).mean(1, keepdim=True) + 2 * dm * spread.mean(1, keepdim=True) + dm ** 2
+    dr = r64 * (0.5 * dv * r64 ** 2 + 4 * F32)
+    within = w64.abs() * (spread * dr + dm * r64) * 1.01 + 6 * F32 * ((spread * r64 * w64).abs() + b64.abs())
+    for got, ref, bound, name in ((mean[:, None], m64, dm, "mean"), (rstd[:, None], r64, dr + r64 * (dv * r64 ** 2) ** 2, "rstd"),
+                                  (y, want, within + HALVES[x.dtype] * (want.abs() + within) + TINY[x.dtype], "y")):
+        assert bool(((got.double() - ref).abs() <= bound).all()), f"{what}: {name}"
+
+
+# more rows than the workgroups that run at once take in one turn, by a few: 64, 256, 512 and 1024 threads a row, rows
+# loaded ahead and not (32768 16-bit columns, 16384 of float32)
+@gpu
+@pytest.mark.parametrize("rows,cols", [(8203, 390), (2055, 2047), (1030, 8200), (520, 16384), (520, 32768), (8195, 1000)])
+@pytest.mark.parametrize("dtype", list(HALVES), ids=str)
+def test_layer_norm_of_many_rows(dtype, rows, cols, gpu_lib):
+    g = torch.Generator(device="cuda").manual_seed(rows)
+    x = (torch.randn(rows, cols, generator=g, device="cuda") + torch.randn(rows, 1, generator=g, device="cuda")).to(dtype)
+    w, b = (1 + 0.3 * torch.randn(cols, generator=g, device="cuda")), torch.randn(cols, generator=g, device="cuda")
+    out, untouched = _guarded((rows, cols), dtype, 3)
+    y, mean, rstd = B.reshard_layer_norm(x, w, b, 1e-5, out=out)
+    _check_norm(x, y, mean, rstd, w, b, (rows, cols))
+    assert untouched()
+    # rows are computed apart from each other: the last ones by themselves have the same bits
+    tail = B.reshard_layer_norm(x[-9:], w, b, 1e-5)
+    assert all(torch.equal(p[-9:], q) for p, q in zip((y, mean, rstd), tail))
+    assert torch.equal(B.reshard_layer_norm(x, w, b, 1e-5, out=x)[0], y)  # in place
+
+
+@gpu
+@pytest.mark.parametrize("rows,cols", [(300, 16384), (300, 12000), (600, 2047), (523, 8200), (4100, 4097), (2100, 1000)])
+@pytest.mark.parametrize("dtype", list(HALVES), ids=str)
+def test_layer_norm_backward_of_many_rows(dtype, rows, cols, gpu_lib):
+    """Bounds of test_layer_norm_backward where each group of threads takes several rows in turn."""
+    g = torch.Generator(device="cuda").manual_seed(rows)
+    x = (torch.randn(rows, cols, generator=g, device="cuda") + 0.5).to(dtype)
+    dy = (torch.randn(rows, cols, generator=g, device="cuda") * 0.1).to(dtype)
+    w = 1 + 0.3 * torch.randn(cols, generator=g, device="cuda")
+    _, mean, rstd = B.reshard_layer_norm(x)
+    dx, dw, db = B.reshard_layer_norm_backward(dy, x, w, mean, rstd)
+    dy64, rstd64 = dy.double(), rstd.double()[:, None]
+    wdx, wdw, wdb, xh = _norm_grad64(dy64, x.double(), w.double(), mean.double()[:, None], rstd64)
+    gw = dy64 * w.double()
+    size = gw.abs() + gw.abs().mean(1, keepdim=True) + xh.abs() * (gw * xh).abs().mean(1, keepdim=True)
+    within = (2 * _chain(cols) + 12) * F32 * rstd64 * size
+    assert bool(((dx.double() - wdx).abs() <= within + HALVES[dtype] * (wdx.abs() + within) + TINY[dtype]).all())
+    chain = math.ceil(rows / 256) + 32 + 16 + 8  # rows of one group of 256, and as in test_layer_norm_backward
+    assert bool(((dw.double() - wdw).abs() <= chain * F32 * (dy64 * xh).abs().sum(0) + 1e-30).all())
+    assert bool(((db.double() - wdb).abs() <= chain * F32 * dy64.abs().sum(0) + 1e-30).all())
+    assert torch.equal(B.reshard_layer_norm_backward(dy, x, w, mean, rstd, out=dy)[0], dx)  # in place
+
+
+@gpu
+@pytest.mark.parametrize("dtype,rows", [(torch.bfloat16, 16400), (torch.float16, 16400), (torch.float32, 8200)], ids=str)
+def test_outputs_larger_than_the_cache(dtype, rows, gpu_lib):
+    """From 256 MiB on results are stored past the caches: the same bits as of a few rows at a time, none beside them."""
+    cols = 8191
+    assert rows * cols * dtype.itemsize >= 256 << 20
+    x = torch.randn(rows, cols, device="cuda", generator=torch.Generator(device="cuda").manual_seed(7)).to(dtype)
+    w, b = torch.randn(cols, device="cuda"), torch.randn(cols, device="cuda")
+    out, untouched = _guarded((rows, cols), dtype, 3)
+    y, mean, rstd = B.reshard_layer_norm(x, w, b, out=out)
+    assert untouched()
+    for lo in range(0, rows, 1000):
+        part = B.reshard_layer_norm(x[lo:lo + 1000], w, b)
+        assert all(torch.equal(p[lo:lo + 1000], q) for p, q in zip((y, mean, rstd), part))
+    for scale_dtype in (E8M0, torch.float32):
+        q = B.reshard_quantize(x, scale_dtype=scale_dtype)
+        back = B.reshard_dequantize(q, dtype, out=out)
+        assert untouched()
+        for lo in range(0, rows, 1000):
+            some = B.Blocked(q.data[lo:lo + 1000], q.scales[lo:lo + 1000])
+            assert torch.equal(back[lo:lo + 1000], B.reshard_dequantize(some, dtype))
+
+
+@gpu
+@pytest.mark.parametrize("cols", [6, 130, 4096, 40000])
+def test_layer_norm_beyond_float32(cols, gpu_lib):
+    """Squares whose sum leaves float32's range: rstd is 0 and y the bias; elements whose sum does: NaN.  Rows beside
+    them are as ever."""
+    x = _randn(_seed("beyond", cols), 4, cols).float()
+    x[1] = 1e30 * torch.tensor([1.0, -1.0]).repeat(cols // 2)
+    x[2] = 3e38
+    b = _randn(_seed("bias", cols), cols).float()
+    y, mean, rstd = (t.cpu() for t in B.reshard_layer_norm(x.cuda(), None, b.cuda()))
+    assert rstd[1] == 0 and torch.equal(y[1], b)
+    assert torch.isinf(mean[2]) and rstd[2] == 0 and torch.isnan(y[2]).all()
+    alone = B.reshard_layer_norm(x[[0, 3]].cuda(), None, b.cuda())
+    assert all(torch.equal(p[[0, 3]], q.cpu()) for p, q in zip((y, mean, rstd), alone))
+
+
+@gpu
+@pytest.mark.parametrize("m,n,k", SIZES + [(65, 130, 2048), (130, 260, 4098), (2047, 300, 5130), (3080, 4100, 390)])
+@pytest.mark.parametrize("scale_dtype", [E8M0, torch.float32], ids=["e8m0", "fp32"])
+@pytest.mark.parametrize("a_rows,b_rows", [(1, 128), (1, 1), (128, 128)])
+def test_matmul_of_whole_numbers(a_rows, b_rows, scale_dtype, m, n, k, gpu_lib):
+    """Every product counts, into every type: codes are whole numbers from -8 to 8 and scales 1/4 to 4, so that no bit is
+    cut within the 8-bit instruction's eight, and sums of a few hundred thousand sixteenths are exact."""
+    g = _seed("whole", a_rows, b_rows, str(scale_dtype), m, n, k)
+    for extra in ((-k) % 16, (-k) % 16 + 5):
+        sides = []
+        for rows, block_rows in ((m, a_rows), (n, b_rows)):
+            x = torch.randint(-8, 9, (rows, k), generator=g).float()
+            s = torch.exp2(torch.randint(-2, 3, (-(-rows // block_rows), -(-k // 128)), generator=g).float())
+            data, _ = _pitched(x.to(E4M3).view(torch.uint8), extra, 0x7F)
+            b = B.Blocked(data.view(E4M3), s.cuda().to(scale_dtype), block_rows)
+            spread = s.repeat_interleave(block_rows, 0)[:rows].repeat_interleave(128, 1)[:, :k]
+            sides.append((b, (x * spread).double()))
+        (a, a64), (b, b64) = sides
+        want = (a64 @ b64.t()).float()
+        for dt in HALVES:
+            out, untouched = _guarded((m, n), dt)
+            assert torch.equal(B.reshard_matmul(a, b, dt, out=out).cpu(), want.to(dt)), (dt, extra)
+            assert untouched()
+        held = torch.full((m, n), 2.0, dtype=torch.bfloat16, device="cuda")
+        B.reshard_matmul(a, b, out=held, accumulate=True)
+        assert torch.equal(held.cpu(), (want + 2).to(torch.bfloat16))
+
+
+@gpu
+@pytest.mark.parametrize("m,n", [(5, 90), (70, 90), (3080, 4100)])
+@pytest.mark.parametrize("scale_dtype", [E8M0, torch.float32], ids=["e8m0", "fp32"])
+@pytest.mark.parametrize("extra", [4, 9])
+def test_matmul_nan_into_every_type(extra, scale_dtype, m, n, gpu_lib):
+    """A NaN code or scale reaches its row or column alone, whatever the kernel; in a whole and in the short last block."""
+    k = 300
+    g = _seed("nan", str(scale_dtype), m, n, extra)
+    a, _ = _operand(g, m, k, 1, scale_dtype, extra)
+    b, _ = _operand(g, n, k, 1, scale_dtype, extra)
+    nan = torch.zeros(m, n, dtype=torch.bool)
+    a.data.view(torch.uint8)[1, 299] = 0x7F
+    a.data.view(torch.uint8)[2, 17] = 0xFF
+    b.data.view(torch.uint8)[7, 0] = 0xFF
+    held = [t.view(torch.uint8) if scale_dtype == E8M0 else t for t in (a.scales, b.scales)]
+    for t, at in ((held[0], (3, 2)), (held[0], (4, 0)), (held[1], (n - 1, 1))):
+        t[at] = 255 if scale_dtype == E8M0 else math.nan
+    nan[1:5], nan[:, 7], nan[:, n - 1] = True, True, True
+    for dt in HALVES:
+        assert torch.equal(torch.isnan(B.reshard_matmul(a, b, dt)).cpu(), nan), dt
