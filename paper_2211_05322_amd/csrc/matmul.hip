@@ -782,11 +782,14 @@ Sum sum_for(reshard_dtype_t scale_dtype, reshard_dtype_t out_dtype) {
     return scale_dtype == RESHARD_E8M0 ? kScaled : kFloat;
 }
 
+constexpr const char *kLaunch = "matmul launch";
+
 template <Sum SUM>
-void launch_few(const MatmulArgs &g, hipStream_t s) {
+reshard_status_t launch_few(const MatmulArgs &g, hipStream_t s) {
     const dim3 grid(unsigned(ceil_div(g.b.rows, 16)));
-    if (grid.x >= 256) matmul_few_kernel<SUM, 4, 8><<<grid, 4 * kWave, 0, s>>>(g);
-    else matmul_few_kernel<SUM, 16, 2><<<grid, 16 * kWave, 0, s>>>(g);  // more waves a row where rows are few
+    if (grid.x >= 256) return launch(kLaunch, matmul_few_kernel<SUM, 4, 8>, grid, 4 * kWave, 0, s, g);
+    // more waves a row where rows are few
+    return launch(kLaunch, matmul_few_kernel<SUM, 16, 2>, grid, 16 * kWave, 0, s, g);
 }
 
 reshard_status_t check_operand(const char *name, const char *scales_name, const void *q, int64_t rows, int64_t k,
@@ -851,11 +854,7 @@ extern "C" reshard_status_t reshard_matmul(int64_t m, int64_t n, int64_t k, cons
         const hipStream_t s = static_cast<hipStream_t>(stream);
         const Sum sum = sum_for(scale_dtype, out_dtype);
         const Launch p = launch_of(m, n, k, sum);
-        if (p.few) {
-            if (sum == kScaled) launch_few<kScaled>(g, s);
-            else launch_few<kFloat>(g, s);
-            return launched("matmul launch");
-        }
+        if (p.few) return sum == kScaled ? launch_few<kScaled>(g, s) : launch_few<kFloat>(g, s);
         // the tile kernel's loads into LDS: whole 16-byte words, 32-bit offsets within a tile's rows
         const bool aligned = (reinterpret_cast<uintptr_t>(a) | reinterpret_cast<uintptr_t>(b) | uintptr_t(a_pitch) |
                               uintptr_t(b_pitch)) % 16 == 0 &&
@@ -863,10 +862,9 @@ extern "C" reshard_status_t reshard_matmul(int64_t m, int64_t n, int64_t k, cons
         if (!aligned) {
             const dim3 grid(unsigned(ceil_div(m, 128) * ceil_div(n, 128)));
             const uint32_t tiles_n = uint32_t(ceil_div(n, 128));
-            if (sum == kExact || sum == kWide) matmul_kernel<kExact><<<grid, 256, 0, s>>>(g, tiles_n);
-            else if (sum == kScaled) matmul_kernel<kScaled><<<grid, 256, 0, s>>>(g, tiles_n);
-            else matmul_kernel<kFloat><<<grid, 256, 0, s>>>(g, tiles_n);
-            return launched("matmul launch");
+            auto run = [&](auto kernel) { return launch(kLaunch, kernel, grid, 256, 0, s, g, tiles_n); };
+            if (sum == kExact || sum == kWide) return run(matmul_kernel<kExact>);
+            return run(sum == kScaled ? matmul_kernel<kScaled> : matmul_kernel<kFloat>);
         }
         if (p.parts > 1) {
             const int64_t need = int64_t(p.parts) * m * n * int64_t(sizeof(float));
@@ -878,21 +876,18 @@ extern "C" reshard_status_t reshard_matmul(int64_t m, int64_t n, int64_t k, cons
             g.parts = static_cast<float *>(workspace);
         }
         const dim3 grid(unsigned(p.tiles_m * p.tiles_n), unsigned(p.parts));
-        const uint32_t tn = uint32_t(p.tiles_n);
-        auto launch = [&](auto kernel, int threads) { kernel<<<grid, threads, 0, s>>>(g, tn, p.blocks); };
-        if (sum == kWide && p.large) launch(matmul_tile_kernel<kWide, 4, 2, 2, 4>, 512);
-        else if (sum == kWide) launch(matmul_tile_kernel<kWide, 2, 2, 2, 2>, 256);
-        else if (sum == kExact) launch(matmul_tile_kernel<kExact, 2, 2, 2, 2>, 256);
-        else if (sum == kFloat && b_block_rows == kBlock) launch(matmul_tile_kernel<kUniform, 2, 2, 2, 2>, 256);
-        else if (sum == kFloat) launch(matmul_tile_kernel<kFloat, 2, 2, 2, 2>, 256);
-        else if (p.large) launch(matmul_tile_kernel<kScaled, 4, 2, 2, 4>, 512);
-        else launch(matmul_tile_kernel<kScaled, 2, 2, 2, 2>, 256);
-        if (p.parts > 1) {
-            const reshard_status_t started = launched("matmul launch");
-            if (started != RESHARD_OK) return started;
-            const int64_t wgs = std::min<int64_t>(ceil_div(m * ceil_div(n, 8), 256), 4096);
-            matmul_join_kernel<<<dim3(unsigned(wgs)), 256, 0, s>>>(g, p.parts);
-        }
-        return launched("matmul launch");
+        auto run = [&](auto kernel, unsigned threads) {
+            return launch(kLaunch, kernel, grid, threads, 0, s, g, p.tiles_n, p.blocks);
+        };
+        if (sum == kWide && p.large) st = run(matmul_tile_kernel<kWide, 4, 2, 2, 4>, 512);
+        else if (sum == kWide) st = run(matmul_tile_kernel<kWide, 2, 2, 2, 2>, 256);
+        else if (sum == kExact) st = run(matmul_tile_kernel<kExact, 2, 2, 2, 2>, 256);
+        else if (sum == kFloat && b_block_rows == kBlock) st = run(matmul_tile_kernel<kUniform, 2, 2, 2, 2>, 256);
+        else if (sum == kFloat) st = run(matmul_tile_kernel<kFloat, 2, 2, 2, 2>, 256);
+        else if (p.large) st = run(matmul_tile_kernel<kScaled, 4, 2, 2, 4>, 512);
+        else st = run(matmul_tile_kernel<kScaled, 2, 2, 2, 2>, 256);
+        if (st != RESHARD_OK || p.parts == 1) return st;
+        const int64_t wgs = std::min<int64_t>(ceil_div(m * ceil_div(n, 8), 256), 4096);
+        return launch("matmul join launch", matmul_join_kernel, dim3(unsigned(wgs)), 256, 0, s, g, p.parts);
     });
 }

@@ -482,14 +482,17 @@ bool with_columns(int64_t cols, F &&f) {
 }
 
 template <typename T>
-void launch_norm(const NormArgs &a, hipStream_t s) {
+reshard_status_t launch_norm(const NormArgs &a, hipStream_t s) {
+    reshard_status_t st = RESHARD_OK;
     const bool done = with_columns<kVec<T>, 3, 4096>(a.cols, [&](auto threads, auto n) {
         constexpr int THREADS = decltype(threads)::value, ROWS = THREADS < 256 ? 256 / THREADS : 1;
         const int64_t most = 256 * 2048 / (THREADS < 256 ? 256 : THREADS);  // what the CUs hold at once
         const dim3 grid(unsigned(std::min(ceil_div(a.rows, ROWS), most)));
-        norm_kernel<T, THREADS, decltype(n)::value><<<grid, THREADS < 256 ? 256 : THREADS, 0, s>>>(a);
+        st = launch("layer norm launch", norm_kernel<T, THREADS, decltype(n)::value>, grid,
+                    THREADS < 256 ? 256 : THREADS, 0, s, a);
     });
-    if (!done) norm_long_kernel<T><<<dim3(unsigned(std::min(a.rows, kMaxGrid))), 1024, 0, s>>>(a);
+    if (done) return st;
+    return launch("layer norm launch", norm_long_kernel<T>, dim3(unsigned(std::min(a.rows, kMaxGrid))), 1024, 0, s, a);
 }
 
 // Workgroups of the backward pass, whose column sums are kept apart until the
@@ -501,21 +504,24 @@ int64_t norm_groups(int64_t rows, int64_t cols) {
 }
 
 template <typename T>
-void launch_norm_grad(const NormGradArgs &a, int64_t groups, hipStream_t s) {
+reshard_status_t launch_norm_grad(const NormGradArgs &a, int64_t groups, hipStream_t s) {
+    const char *what = "layer norm gradient launch";
+    reshard_status_t st = RESHARD_OK;
     // 16384 columns: the sums of more do not fit
     const bool done = with_columns<kVec<T>, 4, 16384 / kVec<T>>(a.cols, [&](auto threads, auto n) {
         constexpr int THREADS = decltype(threads)::value, ROWS = THREADS < 256 ? 256 / THREADS : 1;
         const dim3 grid{unsigned(groups)};
         const size_t padded = size_t(ceil_div(a.cols, kVec<T>)) * kVec<T>;
         const size_t lds = (padded + (ROWS > 1 ? 2 * a.cols : 0)) * sizeof(float);
-        norm_grad_kernel<T, THREADS, decltype(n)::value><<<grid, THREADS < 256 ? 256 : THREADS, lds, s>>>(a);
+        st = launch(what, norm_grad_kernel<T, THREADS, decltype(n)::value>, grid, THREADS < 256 ? 256 : THREADS, lds, s, a);
     });
-    if (done) return;
+    if (done) return st;
     // the sums first: dx may take dy's place
     if (a.partial)
-        norm_columns_kernel<T>
-            <<<dim3(unsigned(ceil_div(ceil_div(a.cols, kVec<T>), 256)), unsigned(groups)), 256, 0, s>>>(a);
-    if (a.dx) norm_grad_long_kernel<T><<<dim3(unsigned(std::min(a.rows, kMaxGrid))), 1024, 0, s>>>(a);
+        st = launch(what, norm_columns_kernel<T>,
+                    dim3(unsigned(ceil_div(ceil_div(a.cols, kVec<T>), 256)), unsigned(groups)), 256, 0, s, a);
+    if (st != RESHARD_OK || !a.dx) return st;
+    return launch(what, norm_grad_long_kernel<T>, dim3(unsigned(std::min(a.rows, kMaxGrid))), 1024, 0, s, a);
 }
 
 }  // namespace
@@ -542,10 +548,8 @@ extern "C" reshard_status_t reshard_layer_norm(int64_t rows, int64_t cols, const
         const NormArgs a{x, weight, bias, y, mean, rstd, rows, cols, x_pitch, y_pitch, float(eps), int(weight_dtype),
                          rows * cols * es >= int64_t(256) << 20};
         const hipStream_t s = static_cast<hipStream_t>(stream);
-        if (dtype == RESHARD_F32) launch_norm<float>(a, s);
-        else if (dtype == RESHARD_BF16) launch_norm<bf16>(a, s);
-        else launch_norm<f16>(a, s);
-        return launched("layer norm launch");
+        if (dtype == RESHARD_F32) return launch_norm<float>(a, s);
+        return dtype == RESHARD_BF16 ? launch_norm<bf16>(a, s) : launch_norm<f16>(a, s);
     });
 }
 
@@ -589,16 +593,13 @@ extern "C" reshard_status_t reshard_layer_norm_backward(int64_t rows, int64_t co
         if (rows > 0 && (dx || sums)) {
             const NormGradArgs a{dy,   x,    weight,   mean,    rstd,     dx, sums ? static_cast<float *>(workspace) : nullptr,
                                  rows, cols, dy_pitch, x_pitch, dx_pitch, int(weight_dtype)};
-            if (dtype == RESHARD_F32) launch_norm_grad<float>(a, groups, s);
-            else if (dtype == RESHARD_BF16) launch_norm_grad<bf16>(a, groups, s);
-            else launch_norm_grad<f16>(a, groups, s);
-            st = launched("layer norm gradient launch");
+            if (dtype == RESHARD_F32) st = launch_norm_grad<float>(a, groups, s);
+            else st = dtype == RESHARD_BF16 ? launch_norm_grad<bf16>(a, groups, s) : launch_norm_grad<f16>(a, groups, s);
             if (st != RESHARD_OK) return st;
         }
         if (!sums || (rows == 0 && accumulate)) return RESHARD_OK;
         // no rows: the sums are zeros (0 groups to join)
-        norm_join_kernel<<<dim3(unsigned(ceil_div(2 * cols, kWave))), 1024, 0, s>>>(
-            static_cast<const float *>(workspace), groups, cols, dweight, dbias, accumulate);
-        return launched("layer norm gradient join launch");
+        return launch("layer norm gradient join launch", norm_join_kernel, dim3(unsigned(ceil_div(2 * cols, kWave))), 1024,
+                      0, s, static_cast<const float *>(workspace), groups, cols, dweight, dbias, accumulate);
     });
 }

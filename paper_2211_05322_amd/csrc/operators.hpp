@@ -7,6 +7,7 @@
 
 #include <cstdint>
 #include <string>
+#include <tuple>
 #include <type_traits>
 
 #include "../../include/reshard.h"
@@ -154,8 +155,18 @@ inline reshard_status_t check_extent(const char *name, int64_t n) {
     return RESHARD_OK;
 }
 
-inline reshard_status_t launched(const char *what) {
-    const hipError_t e = hipGetLastError();
+// Launches a kernel and reports that launch's error alone: the thread's last
+// error, which <<<>>> leaves to be asked for, may be another call's.
+template <typename... P, typename... A>
+reshard_status_t launch(const char *what, void (*kernel)(P...), dim3 grid, unsigned threads, size_t lds, hipStream_t s,
+                        const A &...a) {
+    std::tuple<P...> args(static_cast<P>(a)...);
+    const hipError_t e = std::apply(
+        [&](P &...p) {
+            void *argv[] = {&p...};
+            return hipLaunchKernel(reinterpret_cast<const void *>(kernel), grid, dim3(threads), argv, lds, s);
+        },
+        args);
     if (e == hipSuccess) return RESHARD_OK;
     return fail(RESHARD_EHIP, std::string(what) + ": " + hipGetErrorString(e));
 }

@@ -339,16 +339,15 @@ __global__ __launch_bounds__(256) void dequantize_kernel(DequantArgs a, uint32_t
 }
 
 template <typename T>
-void launch_quantize(const QuantArgs &a, bool tile, hipStream_t s) {
+reshard_status_t launch_quantize(const QuantArgs &a, bool tile, hipStream_t s) {
+    const char *what = "quantize launch";
     const int64_t across = ceil_div(a.cols, kBlock);
     if (!tile && !a.qt) {
         const int64_t wgs = ceil_div(a.rows * across, 16 * kUnits);
-        quantize_rows_kernel<T><<<dim3(unsigned(wgs)), 256, 0, s>>>(a, uint32_t(across));
-    } else {
-        const dim3 grid(unsigned(across * ceil_div(a.rows, kBlock)));
-        if (tile) quantize_tile_kernel<T, true><<<grid, 256, 0, s>>>(a, uint32_t(across));
-        else quantize_tile_kernel<T, false><<<grid, 256, 0, s>>>(a, uint32_t(across));
+        return launch(what, quantize_rows_kernel<T>, dim3(unsigned(wgs)), 256, 0, s, a, across);
     }
+    const dim3 grid(unsigned(across * ceil_div(a.rows, kBlock)));
+    return launch(what, tile ? quantize_tile_kernel<T, true> : quantize_tile_kernel<T, false>, grid, 256, 0, s, a, across);
 }
 
 // Extents of a blocked matrix that one launch of 2^32 threads holds.
@@ -395,10 +394,8 @@ extern "C" reshard_status_t reshard_quantize(int64_t rows, int64_t cols, const v
                           scale_dtype == RESHARD_E8M0};
         const hipStream_t s = static_cast<hipStream_t>(stream);
         const bool tile = block_rows == kBlock;
-        if (dtype == RESHARD_F32) launch_quantize<float>(a, tile, s);
-        else if (dtype == RESHARD_BF16) launch_quantize<bf16>(a, tile, s);
-        else launch_quantize<f16>(a, tile, s);
-        return launched("quantize launch");
+        if (dtype == RESHARD_F32) return launch_quantize<float>(a, tile, s);
+        return dtype == RESHARD_BF16 ? launch_quantize<bf16>(a, tile, s) : launch_quantize<f16>(a, tile, s);
     });
 }
 
@@ -423,10 +420,9 @@ extern "C" reshard_status_t reshard_dequantize(int64_t rows, int64_t cols, const
                             rows * cols * (dtype == RESHARD_F32 ? 4 : 2) >= int64_t(256) << 20};
         const hipStream_t s = static_cast<hipStream_t>(stream);
         const dim3 grid(unsigned(ceil_div(rows * across, 16 * kUnits)));
-        auto launch = [&](auto kernel) { kernel<<<grid, 256, 0, s>>>(a, uint32_t(across)); };
-        if (dtype == RESHARD_F32) launch(dequantize_kernel<float, false>);
-        else if (dtype == RESHARD_BF16) launch(a.e8m0 ? dequantize_kernel<bf16, false> : dequantize_kernel<bf16, true>);
-        else launch(a.e8m0 ? dequantize_kernel<f16, false> : dequantize_kernel<f16, true>);
-        return launched("dequantize launch");
+        auto run = [&](auto kernel) { return launch("dequantize launch", kernel, grid, 256, 0, s, a, across); };
+        if (dtype == RESHARD_F32) return run(dequantize_kernel<float, false>);
+        if (dtype == RESHARD_BF16) return run(a.e8m0 ? dequantize_kernel<bf16, false> : dequantize_kernel<bf16, true>);
+        return run(a.e8m0 ? dequantize_kernel<f16, false> : dequantize_kernel<f16, true>);
     });
 }

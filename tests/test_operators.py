@@ -1051,3 +1051,42 @@ def test_matmul_nan_into_every_type(extra, scale_dtype, m, n, gpu_lib):
     nan[1:5], nan[:, 7], nan[:, n - 1] = True, True, True
     for dt in HALVES:
         assert torch.equal(torch.isnan(B.reshard_matmul(a, b, dt)).cpu(), nan), dt
+
+
+@gpu
+def test_errors_of_other_calls_are_not_an_operators(gpu_lib):
+    """An error that a caller's own HIP call left behind is not reported as a launch's, and stays for the caller to read."""
+    lib, s = gpu_lib, B._stream_handle(None)
+    x, y = torch.randn(200, 256, device="cuda"), torch.empty(200, 256, device="cuda")
+    mean, rstd, sums = torch.empty(200, device="cuda"), torch.empty(200, device="cuda"), torch.empty(2, 256, device="cuda")
+    need = lib.reshard_layer_norm_backward_workspace(200, 256)
+    work = torch.empty(max(need, lib.reshard_matmul_workspace(200, 200, 2048, 13, 3)), dtype=torch.uint8, device="cuda")
+    q, big = B.reshard_quantize(x), B.reshard_quantize(torch.randn(200, 2048, device="cuda"))
+    odd = B.reshard_quantize(torch.randn(200, 2047, device="cuda"), dense=True)
+    z = torch.empty(200, 200, dtype=torch.bfloat16, device="cuda")
+    few = torch.empty(200, 8, dtype=torch.bfloat16, device="cuda")
+
+    def product(m, n, b, out):
+        k, pitch, (sr, sc) = b.data.shape[1], b.data.stride(0), b.scales.shape
+        return lib.reshard_matmul(m, n, k, b.data.data_ptr(), pitch, 1, b.scales.data_ptr(), sc, b.data.data_ptr(), pitch, 1,
+                                  b.scales.data_ptr(), sc, 13, out.data_ptr(), n, 3, 0, work.data_ptr(), work.numel(), s)
+    calls = {
+        "norm": lambda: lib.reshard_layer_norm(200, 256, x.data_ptr(), 256, 4, None, None, 4, 1e-5, y.data_ptr(), 256,
+                                               mean.data_ptr(), rstd.data_ptr(), s),
+        "norm gradients": lambda: lib.reshard_layer_norm_backward(
+            200, 256, x.data_ptr(), 256, x.data_ptr(), 256, 4, None, 4, mean.data_ptr(), rstd.data_ptr(), y.data_ptr(), 256,
+            sums[0].data_ptr(), sums[1].data_ptr(), 0, work.data_ptr(), work.numel(), s),
+        "quantise": lambda: lib.reshard_quantize(200, 256, x.data_ptr(), 256, 4, 1, 13, q.data.data_ptr(), 256,
+                                                 q.scales.data_ptr(), 2, None, 0, None, 0, s),
+        "dequantise": lambda: lib.reshard_dequantize(200, 256, q.data.data_ptr(), 256, 1, q.scales.data_ptr(), 2, 13,
+                                                     y.data_ptr(), 256, 4, s),
+        "product in tiles": lambda: product(200, 200, q, z), "product in parts": lambda: product(200, 200, big, z),
+        "product of few rows": lambda: product(8, 200, q, few), "unaligned product": lambda: product(200, 200, odd, z)}
+    torch.cuda.synchronize()
+    for name, call in calls.items():
+        assert lib.hipSetDevice(1000) != 0  # no such device
+        status, message = call(), B.reshard_last_error()
+        left = lib.hipGetLastError()
+        torch.cuda.synchronize()
+        assert status == B.RESHARD_OK, (name, message)
+        assert left != 0, name
