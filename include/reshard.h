@@ -420,7 +420,7 @@ reshard_status_t reshard_pipeline_simulate(int32_t stages, int32_t microbatches,
  * ---------------------------
  * What a pipeline stage does with an activation or gradient right before it
  * leaves and right after it arrives: layer norm and its gradients, the 8-bit
- * form in which it crosses in half the bytes (the codes and the scales are
+ * form in which half the bytes cross (the codes and the scales are
  * tensors that a plan moves like any other, types E4M3 and E8M0; a plan's
  * buffers are dense, so rows of codes that it moves have a pitch of cols), and
  * the product that takes that form.
@@ -528,10 +528,12 @@ reshard_status_t reshard_dequantize(int64_t rows, int64_t cols, const void *q, i
  * Into an F32 out, products of codes are exact.  Into a 16-bit out, eight
  * neighbouring ones are cut 13 bits below the largest of the eight before they
  * are summed, as the 8-bit matrix instruction does: at most 2^-10 of it in
- * all, typically 1e-5 to 2e-4 of the sum.  With k = 0 the product is zeros.  Rows of codes and scales may have any pitch and start at
+ * all, typically 1e-5 to 2e-4 of the sum.  (So out_dtype chooses between the
+ * two: where that matters, take an F32 out and round it.)  With k = 0 the
+ * product is zeros.  Rows of codes and scales may have any pitch and start at
  * any byte; rows of codes at 16-byte boundaries, at most 4 MiB apart and long,
- * load fastest.  k is at most 2^36, out at most 2^20 tiles of 128 x 128.  Bytes of a row past k
- * are not read into the result, whatever they hold.
+ * load fastest.  k is at most 2^36, out at most 2^20 tiles of 128 x 128.  Bytes
+ * of a row past k are not read into the result, whatever they hold.
  */
 int64_t reshard_matmul_workspace(int64_t m, int64_t n, int64_t k, reshard_dtype_t scale_dtype,
                                  reshard_dtype_t out_dtype); /* bytes, 0: none needed; -1: bad extents, or too many tiles */

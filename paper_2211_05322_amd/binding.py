@@ -478,7 +478,8 @@ _HERE = contextlib.nullcontext()
 
 
 def _on(stream):
-    """Memory that a call takes comes from the pool of the stream it runs on."""
+    """Memory that a call takes comes from the pool of the stream it runs on.  Its inputs are the caller's to keep until
+    that stream has passed the call (record_stream, where they come from another stream's pool)."""
     if stream is None:
         return _HERE
     return _torch.cuda.stream(_torch.cuda.ExternalStream(stream) if isinstance(stream, int) else stream)

@@ -162,7 +162,8 @@ __device__ inline void store_any_type(const MatmulArgs &g, int64_t i, int64_t j,
 // kernel's 32-bit offsets: codes go through registers, a step ahead, 128 x 128
 // of `out` a workgroup, 64 x 64 a wave.  Bound by those loads, which straddle
 // cache lines, and two barriers a step: 8192 x 8192 x 4096 with rows 4097 apart
-// takes 690 us (246 in tiles on 16-byte boundaries), 800 into float32 (466).
+// takes 692 us (249 in tiles on 16-byte boundaries), 811 into float32 (463; this
+// instantiation spills 3 registers).
 // A row of the LDS tiles is one block, eight 16-byte words; word w of row r
 // lies in slot w ^ (r % 8).
 template <Sum SUM>
@@ -355,15 +356,17 @@ __device__ inline void unrolled(F &&f) {
 // w ^ (r / 2 % 8): lanes that read at once fall on different banks.  The loads
 // write LDS in order, so the order of words is set by the addresses they read.
 //
-// Bound by the matrix instructions and the power they take: 16384 x 12288 x
-// 12288 in 256 x 256 tiles with E8M0 scales runs at 2380 to 2560 TFLOP/s, the
-// instruction busy 74 % of the cycles at a clock of 1.65 GHz (on zeros, which
-// take less power, the same code reaches 3430).  Waves of 128 x 128, which read
-// a third less from LDS, measured the same.  Float scales cost an operation
-// an element and block beside the matrix instruction (1450 to 1590 TFLOP/s with
-// a scale per tile of B, 1320 per row), float32 results the conversion and the
-// bf16 instruction's half rate (1280 TFLOP/s with E8M0 scales, 990 with float
-// ones).
+// With E8M0 scales bound by the matrix instructions, and by the power they take:
+// 16384 x 12288 x 12288 in 256 x 256 tiles runs at 2620 to 2650 TFLOP/s (on
+// zeros, which take less power, at 2920); in 8192 x 4096 x 16384 the instruction
+// is busy 73 % of the cycles.  Waves of 128 x 128, which read a third less from
+// LDS, measured the same.  Float scales cost an operation an element and block
+// beside it: 1540 to 1810 TFLOP/s with a scale per tile of B, 1460 to 1490 with
+// one per row.  There neither unit is the bound (matrix instructions busy 43 %
+// and vector ones 36 % of the cycles, per row 34 and 45) but that they overlap
+// little.  Float32 results cost the conversion and the bf16 instruction's half
+// rate: 1280 TFLOP/s with E8M0 scales, 1020 to 1040 with float ones.  kWide in
+// 256 x 256 tiles spills 21 registers and is faster than 128 x 128 all the same.
 template <int ROWS>
 struct Stage {
     uint4 words[ROWS * 8];
@@ -667,7 +670,7 @@ __global__ __launch_bounds__(256) void matmul_join_kernel(MatmulArgs g, int part
 // of B and all of A's (at most 16); its waves deal the blocks of the reduction
 // among them, load DEPTH blocks' fragments at once straight into registers,
 // and add their sums through LDS.  Bound by memory: 1 x 12288 x 12288 in 30 us,
-// 5.0 TB/s of weights.
+// 5.0 TB/s of weights, and in 31 with float scales; eight rows in 38 and 41.
 template <Sum SUM, int WAVES, int DEPTH>
 __global__ __launch_bounds__(WAVES *kWave) void matmul_few_kernel(MatmulArgs g) {
     __shared__ f32x4 part[WAVES][kWave];
@@ -744,7 +747,8 @@ __global__ __launch_bounds__(WAVES *kWave) void matmul_few_kernel(MatmulArgs g) 
 // of 256 x 256 (E8M0 operands, where there are enough of them: 16384 x 4096 x
 // 8192 into float32 861 us against 934, 4098 x 5130 x 2047 136 against 124) or
 // 128 x 128, and where those are too few for the 256 CUs, the reduction split
-// into parts that are joined.
+// into parts that are joined.  (The times are those that the rules were set by;
+// the kernels' present ones stand with them.)
 struct Launch {
     bool few, large;
     int64_t tile, tiles_m, tiles_n;

@@ -154,7 +154,7 @@ __global__ __launch_bounds__(THREADS < 256 ? 256 : THREADS) void norm_kernel(Nor
 
 // Rows too long for registers, or shorter than one vector: read once for each
 // moment and once for the result, the second and third time mostly from L2.
-// 4096 x 33000 bf16 in 170 us, 3.2 TB/s of its input and output.
+// 4096 x 33000 bf16 in 176 us, 3.1 TB/s of its input and output.
 template <typename T>
 __global__ __launch_bounds__(1024) void norm_long_kernel(NormArgs a) {
     constexpr int V = kVec<T>;
@@ -212,9 +212,10 @@ struct NormGradArgs {
 // before is reduced; no atomics, so the gradients of the weights are the same
 // in every run.  The weights, as float32, lie in LDS: with them the registers
 // would not hold two rows and the sums.  Bound by memory where rows are long
-// (16384 x 12288 bf16 in 249 us, 4.9 TB/s; 16376 x 12300, off 16-byte boundaries,
-// in 263), by the 20 operations an element at two waves a SIMD where they are
-// shorter (8192 x 4096 fp16 in 51 us, 4.0 TB/s).
+// (16384 x 12288 bf16 in 245 us, 4.9 TB/s; 16376 x 12300, off 16-byte boundaries,
+// in 262), by the 20 operations an element at two waves a SIMD where they are
+// shorter (8192 x 4096 fp16 in 50 us, 4.1 TB/s), by 22 spilled registers in float32
+// rows over 12288 (8192 x 16384 in 378 us, 4.3 TB/s; 8192 x 12288 in 229, 5.3).
 template <typename T, int THREADS, int NV>
 __global__ __launch_bounds__(THREADS < 256 ? 256 : THREADS) void norm_grad_kernel(NormGradArgs a) {
     constexpr int ROWS = THREADS < 256 ? 256 / THREADS : 1;

@@ -7,7 +7,8 @@ hidden sharded over a (2, 4) mesh; the receiving stage wants it with batch and
 sequence sharded, hidden whole, on its own (2, 4) mesh.  Each sender takes its
 shard to 8 bits (128 divides the hidden shards, so blocks do not cross
 devices), two plans move codes and scales -- half the bytes of the 16-bit
-reshard -- and every receiver reads them back, normalises its rows and
+reshard, meant for links between GPUs (within one, the 16-bit move is several
+times faster) -- and every receiver reads them back, normalises its rows and
 multiplies them by the stage's first weights in 8 bits.  On the way back the
 receivers take the gradients of the product and of the norm, weight gradients
 adding up over the devices as over micro-batches, and the activation's gradient
