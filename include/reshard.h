@@ -544,6 +544,153 @@ reshard_status_t reshard_matmul(int64_t m, int64_t n, int64_t k, const void *a, 
                                 reshard_dtype_t out_dtype, int accumulate, void *workspace,
                                 int64_t workspace_bytes, void *stream);
 
+/*
+ * Operators of attention
+ * ----------------------
+ * What a stage does between its first product, which makes queries, keys and
+ * values, and its second one.  The conventions above hold.  Besides:
+ *  - Heads of tokens: element (token, head, d) lies at data + token *
+ *    token_pitch + head * head_pitch + d, pitches in elements, both >= 0 (so a
+ *    slice of the product's rows serves as it is).  What is written does not
+ *    overlap itself.
+ *  - heads is a multiple of kv_heads where queries meet keys: query head h
+ *    reads key head h / (heads / kv_heads).
+ *  - Integers that say where to read and write (offsets, slots, pages,
+ *    lengths) are int32 in device memory, so calls need no synchronisation.
+ *    They are clamped or left out where they lead outside their tensors.
+ */
+typedef struct {
+    void *data;
+    int64_t token_pitch, head_pitch;
+} reshard_heads_t;
+
+/* A paged cache: slot s of `pages * page_length` (at most 2^31 - 1) lies in page
+ * s / page_length; element (s, head, d) of keys, and of values, at
+ * s / page_length * page_pitch + s % page_length * slot_pitch + head *
+ * head_pitch + d elements. */
+typedef struct {
+    void *keys, *values;
+    int64_t pages, page_length, page_pitch, slot_pitch, head_pitch;
+} reshard_cache_t;
+
+/*
+ * Each head of q and k divided by its root mean square and rotated:
+ *   xhat = x / sqrt(mean(x^2) + eps),  y = Rot(position) (xhat * weight).
+ * Rot turns the pairs of a head's first `rotary` elements, pair j by
+ * position * frequencies[j]: elements (j, j + rotary / 2), or with interleaved =
+ * 1 (2j, 2j + 1).  The rest of the head is not rotated.  Angles are taken in 64 bits.
+ *
+ * q and q_out [tokens, heads, dim], k and k_out [tokens, kv_heads, dim] are of
+ * `dtype` (F16, BF16 or F32), the weights (dim elements, NULL for 1) of
+ * weight_dtype; frequencies rotary / 2 doubles, positions tokens int32 (both
+ * may be NULL with rotary = 0).  q_out may be q and k_out k, with the same pitches.
+ *
+ * With v and cache (k_out is not looked at): keys and values of token t go to
+ * slot slots[t] of the cache, values as they are; a token with a slot outside
+ * the cache (-1) is not kept.  Two tokens of one call have different slots.
+ *
+ * dim and rotary are even, dim at most 128, heads at most 2^16.
+ */
+reshard_status_t reshard_rotate_heads(int64_t tokens, int64_t heads, int64_t kv_heads, int64_t dim, int64_t rotary,
+                                      int interleaved, reshard_dtype_t dtype, const reshard_heads_t *q,
+                                      const reshard_heads_t *k, const void *q_weight, const void *k_weight,
+                                      reshard_dtype_t weight_dtype, double eps, const double *frequencies,
+                                      const int32_t *positions, const reshard_heads_t *q_out,
+                                      const reshard_heads_t *k_out, const reshard_heads_t *v,
+                                      const reshard_cache_t *cache, const int32_t *slots, void *stream);
+
+/*
+ * Gradients of reshard_rotate_heads: with g = Rot(position)^T dy,
+ *   dx = (g * weight - xhat * mean(g * weight * xhat)) / sqrt(mean(x^2) + eps),
+ *   dweight = sum over tokens and heads of g * xhat.
+ *
+ * dq_out and dk_out are the gradients of q_out and k_out; q and k the forward
+ * pass's inputs.  dq, dk (which may be dq_out, dk_out with the same pitches),
+ * dq_weight and dk_weight (dim floats each) may each be NULL: not wanted.
+ * The weights' gradients are overwritten (accumulate = 0) or added to (1); with
+ * tokens = 0 they are zeros.  The workspace is needed for them only.
+ */
+int64_t reshard_rotate_heads_backward_workspace(int64_t tokens, int64_t heads, int64_t kv_heads,
+                                                int64_t dim); /* bytes; -1: bad extents */
+reshard_status_t reshard_rotate_heads_backward(
+    int64_t tokens, int64_t heads, int64_t kv_heads, int64_t dim, int64_t rotary, int interleaved,
+    reshard_dtype_t dtype, const reshard_heads_t *dq_out, const reshard_heads_t *dk_out, const reshard_heads_t *q,
+    const reshard_heads_t *k, const void *q_weight, const void *k_weight, reshard_dtype_t weight_dtype, double eps,
+    const double *frequencies, const int32_t *positions, const reshard_heads_t *dq, const reshard_heads_t *dk,
+    float *dq_weight, float *dk_weight, int accumulate, void *workspace, int64_t workspace_bytes, void *stream);
+
+/*
+ * Attention of packed sequences: out = softmax(scale q k^T) v for each head.
+ *
+ * Sequence s has the queries q_offsets[s] to q_offsets[s + 1] and the keys
+ * k_offsets[s] to k_offsets[s + 1] (sequences + 1 offsets each, ascending).
+ * With causal = 1 its last query sees all its keys, the one before all but
+ * the last, and so on: query i of lq sees key j of lk where j <= i + lk - lq.  A
+ * query that sees none has zeros in out and -infinity in lse.  Rows that are
+ * no sequence's stay as they were.
+ *
+ * q and out [q_tokens, heads, dim], k and v [k_tokens, kv_heads, dim] are of
+ * `dtype` (F16 or BF16); out overlaps none of the others.  lse [heads, q_tokens]
+ * floats: the logarithm of the sum of exp(scale q k^T) over the keys that a
+ * query sees, which the backward pass reads.  scale > 0.  Sums and statistics
+ * are held in 32 bits, weights (each at most 2^8 times the largest) rounded to
+ * `dtype` for the second product.
+ *
+ * A key that a query does not see does not count, whatever it holds; an
+ * infinite or NaN value may make NaN of any row of its sequence (0 * infinity).
+ * A row whose every score is -infinity counts as seeing none.
+ *
+ * dim is a multiple of 8 up to 128; at most 2^31 - 256 tokens.
+ */
+reshard_status_t reshard_attention(int64_t q_tokens, int64_t k_tokens, int64_t sequences, int64_t heads,
+                                   int64_t kv_heads, int64_t dim, reshard_dtype_t dtype, const reshard_heads_t *q,
+                                   const reshard_heads_t *k, const reshard_heads_t *v, const int32_t *q_offsets,
+                                   const int32_t *k_offsets, double scale, int causal, const reshard_heads_t *out,
+                                   float *lse, void *stream);
+
+/*
+ * Gradients of reshard_attention: with P = exp(scale q k^T - lse) over the keys
+ * that a query sees and delta = sum_d dout * out,
+ *   dS = scale * P * (dout v^T - delta),  dq = dS k,  dk = dS^T q,  dv = P^T dout,
+ * dk and dv summed over the heads that share a key head.
+ *
+ * out and lse are the forward pass's, of the same arguments.  dq, dk and dv are
+ * of `dtype`, rounded once; they overlap none of the others.  Queries that see
+ * no key, and keys that no query sees, have zeros; rows that are no
+ * sequence's stay as they were.  P and dS are rounded to `dtype` for the
+ * products that follow, in F16 times powers of two that keep their digits.
+ */
+int64_t reshard_attention_backward_workspace(int64_t q_tokens, int64_t heads); /* bytes; -1: bad extents */
+reshard_status_t reshard_attention_backward(
+    int64_t q_tokens, int64_t k_tokens, int64_t sequences, int64_t heads, int64_t kv_heads, int64_t dim,
+    reshard_dtype_t dtype, const reshard_heads_t *dout, const reshard_heads_t *q, const reshard_heads_t *k,
+    const reshard_heads_t *v, const reshard_heads_t *out, const float *lse, const int32_t *q_offsets,
+    const int32_t *k_offsets, double scale, int causal, const reshard_heads_t *dq, const reshard_heads_t *dk,
+    const reshard_heads_t *dv, void *workspace, int64_t workspace_bytes, void *stream);
+
+/*
+ * Attention of one token of each sequence over a paged cache:
+ * out[s] = softmax(scale q[s] k^T) v, with the keys and values of the first
+ * lengths[s] tokens of sequence s.  Token t lies in page pages[s * pages_pitch +
+ * t / page_length], at t % page_length there.
+ *
+ * q and out [sequences, heads, dim] (the sequence is the token of
+ * reshard_heads_t) and the cache are of `dtype` (F16 or BF16).  A length above
+ * pages_a_sequence * page_length counts as that, one below 1 as 0: the
+ * sequence's rows of out are zeros.  Tokens whose page is not in the cache do
+ * not count.  What the cache holds behind a sequence's length does not count,
+ * whatever it is; a page may be of several sequences.  scale > 0; dim is a
+ * multiple of 8 up to 128.
+ */
+int64_t reshard_attention_paged_workspace(int64_t sequences, int64_t heads, int64_t kv_heads, int64_t dim,
+                                          int64_t pages_a_sequence, int64_t page_length); /* bytes; -1: bad extents */
+reshard_status_t reshard_attention_paged(int64_t sequences, int64_t heads, int64_t kv_heads, int64_t dim,
+                                         reshard_dtype_t dtype, const reshard_heads_t *q,
+                                         const reshard_cache_t *cache, const int32_t *pages,
+                                         int64_t pages_a_sequence, int64_t pages_pitch, const int32_t *lengths,
+                                         double scale, const reshard_heads_t *out, void *workspace,
+                                         int64_t workspace_bytes, void *stream);
+
 /* Text of the last error on the calling thread ("" if none).  Not an
  * operation of the paper: the error report of this interface, which never
  * throws across it.  Never NULL; owned by the library; valid until the

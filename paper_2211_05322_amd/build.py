@@ -8,6 +8,7 @@ library atomically so a process that already mapped the old file keeps it.
 
 from __future__ import annotations
 
+import concurrent.futures
 import os
 import shutil
 import subprocess
@@ -25,7 +26,8 @@ COMMON = ["-O3", "-fPIC", "-std=c++17", "-Wall", "-Wextra", "-Wno-unused-paramet
 # packed-fp32 instructions are disabled for all device code
 HIP_FLAGS = [f"--offload-arch={ARCH}", "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops"]
 HOST_SOURCES = ["planner.cpp", "capi.cpp", "schedule.cpp", "pipeline.cpp"]
-HIP_SOURCES = ["execute.hip", "norm.hip", "quantize.hip", "matmul.hip"]
+HIP_SOURCES = ["execute.hip", "norm.hip", "quantize.hip", "matmul.hip", "heads.hip", "attention.hip",
+               "attention_grad.hip", "decode.hip"]
 
 
 def _run(cmd, verbose):
@@ -42,16 +44,13 @@ def build(verbose=False, extra_hip_flags=(), out=LIB):
         raise RuntimeError(f"hipcc not found at {HIPCC}")
     tmp = tempfile.mkdtemp(prefix="reshard_build_")
     try:
-        objs = []
-        for src in HOST_SOURCES:
+        def compiled(src):
             obj = os.path.join(tmp, src + ".o")
-            _run(["g++", *COMMON, "-c", os.path.join(CSRC, src), "-o", obj], verbose)
-            objs.append(obj)
-        for src in HIP_SOURCES:
-            obj = os.path.join(tmp, src + ".o")
-            _run([HIPCC, *COMMON, *HIP_FLAGS, *extra_hip_flags, "-c", os.path.join(CSRC, src), "-o", obj],
-                 verbose)
-            objs.append(obj)
+            cc = [HIPCC, *COMMON, *HIP_FLAGS, *extra_hip_flags] if src in HIP_SOURCES else ["g++", *COMMON]
+            _run([*cc, "-c", os.path.join(CSRC, src), "-o", obj], verbose)
+            return obj
+        with concurrent.futures.ThreadPoolExecutor(8) as pool:
+            objs = list(pool.map(compiled, HOST_SOURCES + HIP_SOURCES))
         tmp_lib = os.path.join(tmp, "libreshard.so")
         _run([HIPCC, "-shared", "-fPIC", f"--offload-arch={ARCH}", *objs, "-o", tmp_lib,
               f"-Wl,-rpath,{ROCM}/lib"], verbose)

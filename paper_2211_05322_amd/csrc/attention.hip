@@ -1,0 +1,204 @@
+// attention.hip -- causal attention of packed sequences with grouped heads, and
+// its gradients.
+//
+//   S = scale q k^T, where a query sees the key        lse = log sum_k exp S
+//   out = exp(S - lse) v
+//
+// A sequence's last query sees all its keys, the one before all but the last,
+// and so on: query i of lq sees key j of lk where j <= i + lk - lq.
+#include <algorithm>
+
+#include "attention.hpp"
+
+namespace rs {
+namespace {
+
+constexpr int kThreads = 256, kWaves = kThreads / kWave, kKeys = 64;
+
+struct PromptArgs {
+    Heads q, k, v, out;
+    float *lse;  // [heads][q_tokens]
+    Sequences seq;
+    int heads, group, dim, causal;
+    uint32_t blocks;
+    float scale2;  // scale * log2(e): exponentials are taken to base 2
+};
+
+// S^T = k q^T and out^T = v^T P^T: a lane holds one query's column throughout,
+// its running maximum and sum among it, and P never leaves its registers.  A
+// wave has QB blocks of 32 queries, the workgroup's 4 waves share each tile of 64
+// keys and values, which is loaded while the one before is used.
+// The maximum only rises when a score passes it by 2^8, so that most tiles
+// leave the sums as they are.
+template <typename T, int DP, int QB, bool ASYNC>
+__global__ __launch_bounds__(kThreads, QB == 1 ? 2 : 1) void attention_kernel(PromptArgs a) {
+    constexpr int STEPS = DP / 16, BLOCKS = DP / 32, ROWS = 32 * QB * kWaves;
+    constexpr int SHIFT = QB == 1 ? 7 : 8;
+    // four arrays by name: only so does the compiler see that loads into one pair leave the other alone
+    __shared__ uint4 k0[kKeys * TileShape<DP>::words], v0[kKeys * TileShape<DP>::words];
+    __shared__ uint4 k1[kKeys * TileShape<DP>::words], v1[kKeys * TileShape<DP>::words];
+    const Task task = task_of(blockIdx.x, a.blocks, a.heads, a.group);
+    Sequence s;
+    if (!find_sequence(a.seq, false, a.blocks - 1 - task.block, SHIFT, &s)) return;
+    const int lane = threadIdx.x % kWave, wave = threadIdx.x / kWave, half = lane / 32;
+    const int kv_head = task.head / a.group;
+    const int row0 = s.block * ROWS + wave * 32 * QB;
+    const T *k = a.k.template at<const T>(s.k0, kv_head), *v = a.v.template at<const T>(s.k0, kv_head);
+
+    Operand8<T> q[QB][STEPS];
+    int last[QB];  // the last key that the lane's query sees
+#pragma unroll
+    for (int b = 0; b < QB; ++b) {
+        const int row = row0 + b * 32 + lane % 32;
+        const T *at = a.q.template at<const T>(s.q0 + min(row, s.lq - 1), task.head);
+#pragma unroll
+        for (int i = 0; i < STEPS; ++i) q[b][i] = global_operand(at, true, i, lane, a.dim);
+        last[b] = a.causal ? min(row, s.lq - 1) + s.lk - s.lq : s.lk - 1;
+    }
+    const int to = a.causal ? min(s.lk, min(s.lq, (s.block + 1) * ROWS) + s.lk - s.lq) : s.lk;  // the workgroup's keys
+    const int wave_to = a.causal ? min(s.lk, min(s.lq, row0 + 32 * QB) + s.lk - s.lq) : s.lk;
+    const int all_see = a.causal ? row0 + 1 + s.lk - s.lq : s.lk;  // keys that each of the wave's queries sees
+
+    f32x16 o[QB][BLOCKS];
+    float m[QB], l[QB];
+#pragma unroll
+    for (int b = 0; b < QB; ++b) {
+        m[b] = -3.402823466e38f;
+        l[b] = 0;
+#pragma unroll
+        for (int d = 0; d < BLOCKS; ++d) o[b][d] = zero16();
+    }
+    TileLoader<T, DP, kKeys, kThreads, ASYNC> kl(threadIdx.x, a.dim, a.k.token_pitch), vl(threadIdx.x, a.dim, a.v.token_pitch);
+    if (to > 0) {
+        kl.start(k, s.lk, k0);
+        vl.start(v, s.lk, v0);
+        kl.finish(k0);
+        vl.finish(v0);
+    }
+    __syncthreads();
+    auto step = [&](int key0, const auto &kt, const auto &vt, auto &k_next, auto &v_next) {
+        const bool more = key0 + kKeys < to;
+        if (more) {
+            kl.start(k + (key0 + kKeys) * a.k.token_pitch, s.lk - key0 - kKeys, k_next);
+            vl.start(v + (key0 + kKeys) * a.v.token_pitch, s.lk - key0 - kKeys, v_next);
+        }
+        if (key0 < wave_to) {
+            f32x16 x[QB][2];
+#pragma unroll
+            for (int b = 0; b < QB; ++b) x[b][0] = x[b][1] = zero16();
+#pragma unroll
+            for (int i = 0; i < STEPS; ++i)
+#pragma unroll
+                for (int n = 0; n < 2; ++n) {
+                    const Operand8<T> kk = row_operand<T, DP>(kt, n * 32, i, lane);
+#pragma unroll
+                    for (int b = 0; b < QB; ++b) x[b][n] = mfma(kk, q[b][i], x[b][n]);
+                }
+            if (key0 + kKeys > all_see || key0 + kKeys > s.lk) {
+#pragma unroll
+                for (int b = 0; b < QB; ++b)
+#pragma unroll
+                    for (int n = 0; n < 2; ++n)
+#pragma unroll
+                        for (int r = 0; r < 16; ++r)
+                            if (key0 + n * 32 + result_row(r, half) > last[b]) x[b][n][r] = -INFINITY;
+            }
+            Operand8<T> p[QB][4];
+#pragma unroll
+            for (int b = 0; b < QB; ++b) {
+                float top = x[b][0][0];
+#pragma unroll
+                for (int n = 0; n < 2; ++n)
+#pragma unroll
+                    for (int r = 0; r < 16; ++r) top = fmaxf(top, x[b][n][r]);
+                top = halves_max(top) * a.scale2;
+                if (__builtin_amdgcn_ballot_w64(top > m[b] + 8)) {
+                    const float next = fmaxf(m[b], top), shrink = exp2_fast(m[b] - next);
+                    m[b] = next;
+                    l[b] *= shrink;
+#pragma unroll
+                    for (int d = 0; d < BLOCKS; ++d)
+#pragma unroll
+                        for (int r = 0; r < 16; ++r) o[b][d][r] *= shrink;
+                }
+                float sum = 0;
+#pragma unroll
+                for (int n = 0; n < 2; ++n)
+#pragma unroll
+                    for (int r = 0; r < 16; ++r) {
+                        const float e = exp2_fast(fmaf(x[b][n][r], a.scale2, -m[b]));
+                        sum += e;
+                        p[b][n * 2 + r / 8].e[r % 8] = T(e);
+                    }
+                l[b] += sum;
+            }
+#pragma unroll
+            for (int t = 0; t < 4; ++t)
+#pragma unroll
+                for (int d = 0; d < BLOCKS; ++d) {
+                    const Operand8<T> vv = column_operand<T, DP>(vt, t * 16, d, lane);
+#pragma unroll
+                    for (int b = 0; b < QB; ++b) o[b][d] = mfma(vv, p[b][t], o[b][d]);
+                }
+        }
+        if (more) {
+            kl.finish(k_next);
+            vl.finish(v_next);
+        }
+        __syncthreads();
+    };
+    for (int key0 = 0; key0 < to; key0 += 2 * kKeys) {
+        step(key0, k0, v0, k1, v1);
+        if (key0 + kKeys < to) step(key0 + kKeys, k1, v1, k0, v0);
+    }
+#pragma unroll
+    for (int b = 0; b < QB; ++b) {
+        const int row = row0 + b * 32 + lane % 32;
+        const float sum = halves_sum(l[b]), over = sum == 0 ? 0.0f : 1.0f / sum;
+        T *to_row = a.out.template at<T>(s.q0 + min(row, s.lq - 1), task.head);
+#pragma unroll
+        for (int d = 0; d < BLOCKS; ++d) store_columns(to_row, row < s.lq, o[b][d], over, d, lane, a.dim);
+        if (half == 0 && row < s.lq)
+            a.lse[int64_t(task.head) * a.seq.q_tokens + s.q0 + row] =
+                sum == 0 ? -INFINITY : (m[b] + log2f(sum)) * kLn2;
+    }
+}
+
+}  // namespace
+}  // namespace rs
+
+extern "C" reshard_status_t reshard_attention(int64_t q_tokens, int64_t k_tokens, int64_t sequences, int64_t heads,
+                                              int64_t kv_heads, int64_t dim, reshard_dtype_t dtype,
+                                              const reshard_heads_t *q, const reshard_heads_t *k,
+                                              const reshard_heads_t *v, const int32_t *q_offsets,
+                                              const int32_t *k_offsets, double scale, int causal,
+                                              const reshard_heads_t *out, float *lse, void *stream) {
+    return rs::guarded([&]() -> reshard_status_t {
+        using namespace rs;
+        reshard_status_t st = check_attention(q_tokens, k_tokens, sequences, heads, kv_heads, dim, dtype, q_offsets,
+                                              k_offsets, scale, causal);
+        PromptArgs a{};
+        if (st == RESHARD_OK) st = check_heads("q", q, q_tokens, heads, dim, 2, false, &a.q);
+        if (st == RESHARD_OK) st = check_heads("k", k, k_tokens, kv_heads, dim, 2, false, &a.k);
+        if (st == RESHARD_OK) st = check_heads("v", v, k_tokens, kv_heads, dim, 2, false, &a.v);
+        if (st == RESHARD_OK) st = check_heads("out", out, q_tokens, heads, dim, 2, true, &a.out);
+        if (st == RESHARD_OK) st = check_matrix("lse", lse, heads, q_tokens, q_tokens, 4);
+        if (st != RESHARD_OK || q_tokens == 0 || sequences == 0) return st;
+        a.lse = lse;
+        a.seq = Sequences{q_offsets, k_offsets, int(sequences), q_tokens, k_tokens};
+        a.heads = int(heads);
+        a.group = int(heads / kv_heads);
+        a.dim = int(dim);
+        a.causal = causal;
+        a.scale2 = float(scale) * kLog2e;
+        const bool async = aligned16(a.k, 2) && aligned16(a.v, 2);
+        return with_dim(dtype, dim, [&](auto zero, auto padded) {
+            using T = decltype(zero);
+            constexpr int DP = decltype(padded)::value;
+            reshard_status_t status = check_grid(blocks_of(q_tokens, sequences, 7), heads, &a.blocks);
+            if (status != RESHARD_OK) return status;
+            return launch("attention launch", async ? attention_kernel<T, DP, 1, true> : attention_kernel<T, DP, 1, false>,
+                          dim3(unsigned(a.blocks * heads)), kThreads, 0, static_cast<hipStream_t>(stream), a);
+        });
+    });
+}

@@ -1,0 +1,312 @@
+// attention.hpp -- what the kernels of attention share: matrix instructions of
+// both 16-bit types, tiles of heads in LDS, and the sequences of a packed batch.
+//
+// Every product is made with the 32 x 32 x 16 instruction, whose operands hold
+// 8 neighbouring elements of the contracted dimension a lane: lane l has row
+// (or column) l % 32 and the elements of half l / 32.  Its result has column
+// l % 32 in lane l, and rows 8 (r / 4) + 4 (l / 32) + r % 4 in register r.  A
+// result that is contracted over its rows next goes in as an operand without
+// leaving its lane, if the other operand takes the same order of the
+// contracted elements: 4 rows from 4 h on, then 4 from 8 + 4 h on.  That other
+// operand lies across its rows in LDS and is read by the transposing load,
+// which gives 16 lanes 4 rows of a column each.
+#pragma once
+
+#include <algorithm>
+
+#include "heads.hpp"
+
+namespace rs {
+
+typedef float f32x16 __attribute__((ext_vector_type(16)));
+typedef float f32x4 __attribute__((ext_vector_type(4)));
+typedef short s16x4 __attribute__((ext_vector_type(4)));
+typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
+
+template <typename T>
+struct Vec8 {
+    typedef T type __attribute__((ext_vector_type(8)));
+};
+
+template <typename T>
+union Operand8 {
+    uint4 w;
+    s16x4 half[2];
+    typename Vec8<T>::type v;
+    T e[8];
+};
+
+__device__ inline f32x16 mfma(const Operand8<bf16> &a, const Operand8<bf16> &b, f32x16 c) {
+    return __builtin_amdgcn_mfma_f32_32x32x16_bf16(a.v, b.v, c, 0, 0, 0);
+}
+__device__ inline f32x16 mfma(const Operand8<f16> &a, const Operand8<f16> &b, f32x16 c) {
+    return __builtin_amdgcn_mfma_f32_32x32x16_f16(a.v, b.v, c, 0, 0, 0);
+}
+__device__ inline f32x4 mfma(const Operand8<bf16> &a, const Operand8<bf16> &b, f32x4 c) {
+    return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a.v, b.v, c, 0, 0, 0);
+}
+__device__ inline f32x4 mfma(const Operand8<f16> &a, const Operand8<f16> &b, f32x4 c) {
+    return __builtin_amdgcn_mfma_f32_16x16x32_f16(a.v, b.v, c, 0, 0, 0);
+}
+
+__device__ inline f32x16 zero16() {
+    f32x16 z;
+#pragma unroll
+    for (int e = 0; e < 16; ++e) z[e] = 0;
+    return z;
+}
+
+// The row of a 32 x 32 result in register r of a lane of half h.
+__device__ constexpr int result_row(int r, int h) { return 8 * (r / 4) + 4 * h + r % 4; }
+
+// The other half's value beside a lane's own: {lower's, upper's} in both.
+__device__ inline u32x2 both_halves(float x) {
+    const uint32_t w = __float_as_uint(x);
+    return __builtin_amdgcn_permlane32_swap(w, w, false, false);
+}
+__device__ inline float halves_max(float x) {
+    const u32x2 p = both_halves(x);
+    return fmaxf(__uint_as_float(p[0]), __uint_as_float(p[1]));
+}
+__device__ inline float halves_sum(float x) {
+    const u32x2 p = both_halves(x);
+    return __uint_as_float(p[0]) + __uint_as_float(p[1]);
+}
+
+// A tile's rows of DP elements in LDS: 8 or 16 words of 16 bytes, the words of
+// a row in the order word ^ swizzle(row).  Reads of one word from 16 rows, and
+// transposing reads of 4 neighbouring words from 4 rows, so meet every bank once.
+template <int DP>
+struct TileShape {
+    static constexpr int words = DP <= 64 ? 8 : 16;
+    __device__ static int swizzle(int row) {
+        return words == 16 ? (row & 3) << 2 | ((row >> 2) & 3) : ((row >> 1) & 1) << 2 | ((row >> 2) & 3);
+    }
+    __device__ static int at(int row, int word) { return row * words + (word ^ swizzle(row)); }
+};
+
+// Lane l's 8 elements 16 s + 8 (l / 32) of row `row` + l % 32.
+template <typename T, int DP>
+__device__ inline Operand8<T> row_operand(const uint4 *tile, int row, int s, int lane) {
+    Operand8<T> o;
+    o.w = tile[TileShape<DP>::at(row + lane % 32, 2 * s + lane / 32)];
+    return o;
+}
+
+// Column `32 * block + l % 32` of the 16 rows from `row` on, in a result's order.
+template <typename T, int DP>
+__device__ inline Operand8<T> column_operand(const uint4 *tile, int row, int block, int lane) {
+    typedef __attribute__((address_space(3))) s16x4 lds_s16x4;
+    const int i = lane % 16, r = row + lane / 32 * 4 + i / 4, word = block * 4 + (lane / 16 % 2) * 2 + i % 4 / 2;
+    Operand8<T> o;
+#pragma unroll
+    for (int p = 0; p < 2; ++p) {
+        const char *at = reinterpret_cast<const char *>(tile + TileShape<DP>::at(r + 8 * p, word)) + i % 2 * 8;
+        o.half[p] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4 *)at);
+    }
+    return o;
+}
+
+// Brings ROWS rows of a head into LDS, a word a thread and turn.  Rows past the
+// sequence's end and elements from dim on become zeros.  Where rows start on
+// 16-byte boundaries (ASYNC) words go to LDS by themselves, to be waited for;
+// otherwise through registers, which `finish` writes.
+constexpr int64_t kMaxAsyncPitch = int64_t(1) << 24;  // bytes: offsets in a tile stay below 2^31
+
+template <typename T, int DP, int ROWS, int THREADS, bool ASYNC>
+struct TileLoader {
+    using Shape = TileShape<DP>;
+    static constexpr int words = ROWS * Shape::words, turns = words / THREADS, rows_a_turn = THREADS / Shape::words;
+    static_assert(words % THREADS == 0 && rows_a_turn % 16 == 0, "a thread's word has one place in every turn");
+    uint4 held[ASYNC ? 1 : turns];
+    int row, word;
+    uint32_t offset, next;
+    int64_t pitch;  // elements
+    int dim;
+
+    __device__ TileLoader(int thread, int dim_, int64_t pitch_) : pitch(pitch_), dim(dim_) {
+        row = thread / Shape::words;
+        word = (thread % Shape::words) ^ Shape::swizzle(row);
+        // past every range: gives zeros
+        offset = word * 8 < dim ? uint32_t(row * pitch * int64_t(sizeof(T))) + word * 16 : 0x80000000u;
+        next = uint32_t(rows_a_turn * pitch * int64_t(sizeof(T)));
+    }
+    __device__ void start(const T *base, int rows, uint4 *lds) {
+        if constexpr (ASYNC) {
+            const __amdgpu_buffer_rsrc_t from =
+                bytes_from(base, rows > 0 ? ((min(rows, ROWS) - 1) * pitch + dim) * int64_t(sizeof(T)) : 0);
+            const int wave = __builtin_amdgcn_readfirstlane(int(threadIdx.x) / kWave);
+#pragma unroll
+            for (int u = 0; u < turns; ++u) load_to_lds(from, offset + u * next, lds + u * THREADS + wave * kWave);
+        } else {
+#pragma unroll
+            for (int u = 0; u < turns; ++u) {
+                const int r = row + u * rows_a_turn;
+                held[u] = make_uint4(0, 0, 0, 0);
+                if (r < rows && word * 8 < dim) held[u] = load_any<uint4>(base + r * pitch + word * 8);
+            }
+        }
+    }
+    __device__ void finish(uint4 *lds) {
+        if constexpr (ASYNC) {
+            loads_done();
+        } else {
+#pragma unroll
+            for (int u = 0; u < turns; ++u) lds[u * THREADS + threadIdx.x] = held[u];
+        }
+    }
+};
+
+// A wave's operand straight from memory: lane l's 8 elements of row l % 32.
+template <typename T>
+__device__ inline Operand8<T> global_operand(const T *row, bool there, int s, int lane, int dim) {
+    Operand8<T> o;
+    o.w = make_uint4(0, 0, 0, 0);
+    const int d = 16 * s + lane / 32 * 8;
+    if (there && d < dim) o.w = load_any<uint4>(row + d);
+    return o;
+}
+
+// Stores 32 x 32 results, columns of which are rows of `to`: a lane has 4
+// neighbouring elements of its row 4 times; halves trade, so that each has 8.
+template <typename T>
+__device__ inline void store_columns(T *row, bool there, f32x16 x, float scale, int block, int lane, int dim) {
+    typedef T T4 __attribute__((ext_vector_type(4)));
+#pragma unroll
+    for (int j = 0; j < 2; ++j) {
+        union {
+            T4 v;
+            uint32_t w[2];
+        } a, b;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            a.v[e] = T(x[8 * j + e] * scale);
+            b.v[e] = T(x[8 * j + 4 + e] * scale);
+        }
+        const u32x2 p = __builtin_amdgcn_permlane32_swap(a.w[0], b.w[0], false, false);
+        const u32x2 q = __builtin_amdgcn_permlane32_swap(a.w[1], b.w[1], false, false);
+        const int d = block * 32 + j * 16 + lane / 32 * 8;
+        if (there && d < dim) store_any(row + d, make_uint4(p[0], q[0], p[1], q[1]));
+    }
+}
+
+// A packed batch: sequence s has the rows offsets[s] to offsets[s + 1].  Blocks
+// of 1 << shift rows are numbered so that sequence s starts at block
+// (offsets[s] >> shift) + s, which leaves each one enough; some numbers are
+// nobody's.  Offsets are clamped to the tensor, so bad ones read and write inside it.
+struct Sequences {
+    const int32_t *q_offsets, *k_offsets;
+    int count;
+    int64_t q_tokens, k_tokens;
+};
+
+struct Sequence {
+    int64_t q0, k0;
+    int lq, lk, block;  // block: the number within the sequence
+};
+
+__device__ inline int64_t clamped(int64_t x, int64_t lo, int64_t hi) { return max(lo, min(x, hi)); }
+
+// False where `block` is nobody's.  The same for the whole wave; every probe of
+// the search is 64 numbers at once.
+__device__ inline bool find_sequence(const Sequences &s, bool by_keys, int64_t block, int shift, Sequence *out) {
+    const int32_t *offsets = by_keys ? s.k_offsets : s.q_offsets;
+    const int64_t total = by_keys ? s.k_tokens : s.q_tokens;
+    const int lane = threadIdx.x % kWave;
+    auto start = [&](int i) { return (clamped(offsets[i], 0, total) >> shift) + i; };
+    int lo = 0, count = s.count;
+    bool first = true;
+    while (first || count > 1) {
+        const int step = (count + kWave - 1) / kWave, i = lane * step;
+        const uint64_t below = __builtin_amdgcn_ballot_w64(i < count && start(lo + min(i, count - 1)) <= block);
+        if (below == 0) {
+            if (first) return false;
+            break;
+        }
+        const int top = (63 - __builtin_clzll(below)) * step;
+        lo += top;
+        count = min(step, count - top);
+        first = false;
+    }
+    lo = __builtin_amdgcn_readfirstlane(lo);
+    out->q0 = clamped(s.q_offsets[lo], 0, s.q_tokens);
+    out->k0 = clamped(s.k_offsets[lo], 0, s.k_tokens);
+    out->lq = int(clamped(s.q_offsets[lo + 1], out->q0, s.q_tokens) - out->q0);
+    out->lk = int(clamped(s.k_offsets[lo + 1], out->k0, s.k_tokens) - out->k0);
+    out->block = int(block - start(lo));
+    return (int64_t(out->block) << shift) < (by_keys ? out->lk : out->lq);
+}
+
+inline int64_t blocks_of(int64_t tokens, int64_t sequences, int shift) { return (tokens >> shift) + sequences; }
+
+constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
+
+// Workgroups start on the 8 XCDs in turn.  Where their number divides the key
+// heads', each XCD takes whole ones, so that the keys and values in flight there
+// share its L2; long blocks, which are a sequence's last, start first.
+struct Task {
+    uint32_t block, head;
+};
+__device__ inline Task task_of(uint32_t wg, uint32_t blocks, uint32_t heads, uint32_t group) {
+    const uint32_t kv = heads / group;
+    uint32_t block, head;
+    if (kv % 8 == 0) {
+        const uint32_t r = wg / 8, each = blocks * group, of = r / each, p = r - of * each;
+        block = p / group;
+        head = (of * 8 + wg % 8) * group + (p - block * group);
+    } else {
+        block = wg / heads;
+        head = wg - block * heads;
+    }
+    return Task{uint32_t(__builtin_amdgcn_readfirstlane(block)), uint32_t(__builtin_amdgcn_readfirstlane(head))};
+}
+
+// exp2 of arguments at or below about 8; far below, zero.
+__device__ inline float exp2_fast(float x) { return __builtin_amdgcn_exp2f(x); }
+
+inline bool aligned16(const Heads &h, int64_t bytes) {
+    return reinterpret_cast<uintptr_t>(h.data) % 16 == 0 && h.token_pitch * bytes % 16 == 0 &&
+           h.head_pitch * bytes % 16 == 0 && h.token_pitch * bytes <= kMaxAsyncPitch;
+}
+
+// Calls f(zero of the type, elements a head is padded to).
+template <typename F>
+inline reshard_status_t with_dim(reshard_dtype_t dtype, int64_t dim, F &&f) {
+    using std::integral_constant;
+    auto go = [&](auto zero) {
+        if (dim <= 32) return f(zero, integral_constant<int, 32>{});
+        if (dim <= 64) return f(zero, integral_constant<int, 64>{});
+        if (dim <= 96) return f(zero, integral_constant<int, 96>{});
+        return f(zero, integral_constant<int, 128>{});
+    };
+    return dtype == RESHARD_BF16 ? go(bf16{}) : go(f16{});
+}
+
+inline reshard_status_t check_attention(int64_t q_tokens, int64_t k_tokens, int64_t sequences, int64_t heads, int64_t kv_heads,
+                                 int64_t dim, reshard_dtype_t dtype, const int32_t *q_offsets,
+                                 const int32_t *k_offsets, double scale, int causal) {
+    reshard_status_t st = check_head_counts(heads, kv_heads);
+    if (st != RESHARD_OK) return st;
+    for (int64_t n : {q_tokens, k_tokens, sequences}) {
+        if (n < 0) return fail(RESHARD_EINVAL, "q_tokens, k_tokens or sequences is negative");
+        if (n > 0x7fffff00) return fail(RESHARD_EUNSUPPORTED, "q_tokens, k_tokens or sequences is above 2^31 - 256");
+    }
+    if (heads % kv_heads) return fail(RESHARD_EINVAL, "heads must be a multiple of kv_heads");
+    if (dim < 1) return fail(RESHARD_EINVAL, "dim must be >= 1");
+    if (dim % 8 || dim > kMaxDim)
+        return fail(RESHARD_EUNSUPPORTED, "dim must be a multiple of 8 up to " + std::to_string(kMaxDim));
+    if (dtype != RESHARD_F16 && dtype != RESHARD_BF16) return fail(RESHARD_EINVAL, "dtype must be F16 or BF16");
+    if (!(scale > 0 && scale < 1e30)) return fail(RESHARD_EINVAL, "scale must be positive and finite");
+    if (causal & ~1) return fail(RESHARD_EINVAL, "causal must be 0 or 1");
+    st = check_matrix("q_offsets", q_offsets, 1, sequences + 1, sequences + 1, 4);
+    if (st == RESHARD_OK) st = check_matrix("k_offsets", k_offsets, 1, sequences + 1, sequences + 1, 4);
+    return st;
+}
+
+inline reshard_status_t check_grid(int64_t blocks, int64_t heads, uint32_t *out) {
+    if (blocks * heads > int64_t(1) << 30) return fail(RESHARD_EUNSUPPORTED, "more than 2^30 blocks of rows and heads");
+    *out = uint32_t(blocks);
+    return RESHARD_OK;
+}
+
+}  // namespace rs

@@ -1,0 +1,342 @@
+// attention_grad.hip -- gradients of attention over packed sequences.
+//
+//   P = exp(scale q k^T - lse)         dP = dout v^T       delta = sum_d dout out
+//   dS = scale P (dP - delta)          dq = dS k           dk = dS^T q      dv = P^T dout
+//
+// Two kernels: the first holds queries and passes over their keys, the second
+// holds keys and passes over their queries, heads of a group among them.  The
+// scores are made in both, 7 products where 5 would do, and no sum is taken in
+// memory: results do not depend on the order in which workgroups run.
+//
+// In float16, P and dS leave the range in which the type keeps its digits (a
+// weight of 16384 equal ones is 2^-14).  P, at most 1, is multiplied by 2^14.  dS
+// is multiplied by a power of two for each column of the result, which falls
+// when a larger dS comes, as the maximum of a softmax rises.
+#include <algorithm>
+
+#include "attention.hpp"
+
+namespace rs {
+namespace {
+
+constexpr int kThreads = 256, kRows = 128, kShift = 7;
+
+struct GradArgs {
+    Heads dout, q, k, v, out, dq, dk, dv;
+    const float *lse;  // [heads][q_tokens]
+    float2 *row;       // [heads][q_tokens]: lse * log2(e), infinite where a query sees no key; delta
+    Sequences seq;
+    int heads, group, dim, causal;
+    uint32_t blocks;
+    float scale, scale2;
+};
+
+template <typename T>
+constexpr bool kNarrow = std::is_same<T, f16>::value;
+template <typename T>
+constexpr float kRaised = kNarrow<T> ? 14.0f : 0.0f;  // log2 of P's factor
+
+// dS = P (dP - delta) of a lane's column, rounded to T; in float16 times `factor`.
+template <typename T, int BLOCKS>
+__device__ inline void round_scores(const f32x16 &ds, float &factor, f32x16 (&sums)[BLOCKS], Operand8<T> (&to)[2]) {
+    if constexpr (kNarrow<T>) {
+        float top = 0;
+#pragma unroll
+        for (int r = 0; r < 16; ++r) top = fmaxf(top, fabsf(ds[r]));
+        top = halves_max(top);
+        if (__builtin_amdgcn_ballot_w64(top * factor > 32768.0f)) {
+            // 2^14 over the largest's power of two
+            const float lower = __uint_as_float((254 + 14 - (__float_as_uint(top) >> 23)) << 23);
+            const float next = top * factor > 32768.0f ? lower : factor, ratio = next / factor;
+            factor = next;
+#pragma unroll
+            for (int d = 0; d < BLOCKS; ++d)
+#pragma unroll
+                for (int r = 0; r < 16; ++r) sums[d][r] *= ratio;
+        }
+#pragma unroll
+        for (int r = 0; r < 16; ++r) to[r / 8].e[r % 8] = T(ds[r] * factor);
+    } else {
+#pragma unroll
+        for (int r = 0; r < 16; ++r) to[r / 8].e[r % 8] = T(ds[r]);
+    }
+}
+
+constexpr float kFirstFactor = 1.152921504606846976e18f;  // 2^60: dS below 2^-74 may vanish
+
+// Queries: as in the forward pass a lane holds one's column throughout, so that
+// its statistics are the lane's and dS goes into the next product as it is.
+template <typename T, int DP, bool ASYNC>
+__global__ __launch_bounds__(kThreads, 2) void attention_dq_kernel(GradArgs a) {
+    constexpr int STEPS = DP / 16, BLOCKS = DP / 32, KEYS = 64, WORDS = TileShape<DP>::words;
+    __shared__ uint4 k0[KEYS * WORDS], v0[KEYS * WORDS], k1[KEYS * WORDS], v1[KEYS * WORDS];
+    const Task task = task_of(blockIdx.x, a.blocks, a.heads, a.group);
+    Sequence s;
+    if (!find_sequence(a.seq, false, a.blocks - 1 - task.block, kShift, &s)) return;
+    const int lane = threadIdx.x % kWave, wave = threadIdx.x / kWave, half = lane / 32;
+    const int kv_head = task.head / a.group, row0 = s.block * kRows + wave * 32;
+    const int row = row0 + lane % 32, held = min(row, s.lq - 1);
+    const T *k = a.k.template at<const T>(s.k0, kv_head), *v = a.v.template at<const T>(s.k0, kv_head);
+
+    Operand8<T> q[STEPS], dout[STEPS];
+    float delta = 0;
+#pragma unroll
+    for (int i = 0; i < STEPS; ++i) {
+        q[i] = global_operand(a.q.template at<const T>(s.q0 + held, task.head), true, i, lane, a.dim);
+        dout[i] = global_operand(a.dout.template at<const T>(s.q0 + held, task.head), true, i, lane, a.dim);
+        const Operand8<T> out = global_operand(a.out.template at<const T>(s.q0 + held, task.head), true, i, lane, a.dim);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) delta = fmaf(float(dout[i].e[e]), float(out.e[e]), delta);
+    }
+    delta = halves_sum(delta);
+    const int64_t stat = int64_t(task.head) * a.seq.q_tokens + s.q0 + held;
+    float lse2 = a.lse[stat] * kLog2e;
+    if (lse2 == -INFINITY) lse2 = INFINITY;
+    if (half == 0 && row < s.lq) a.row[stat] = make_float2(lse2, delta);
+    const int last = a.causal ? held + s.lk - s.lq : s.lk - 1;
+    const int to = a.causal ? min(s.lk, min(s.lq, (s.block + 1) * kRows) + s.lk - s.lq) : s.lk;
+    const int wave_to = a.causal ? min(s.lk, min(s.lq, row0 + 32) + s.lk - s.lq) : s.lk;
+    const int all_see = a.causal ? row0 + 1 + s.lk - s.lq : s.lk;
+
+    f32x16 dq[BLOCKS];
+#pragma unroll
+    for (int d = 0; d < BLOCKS; ++d) dq[d] = zero16();
+    float factor = kFirstFactor;
+    TileLoader<T, DP, KEYS, kThreads, ASYNC> kl(threadIdx.x, a.dim, a.k.token_pitch), vl(threadIdx.x, a.dim, a.v.token_pitch);
+    if (to > 0) {
+        kl.start(k, s.lk, k0);
+        vl.start(v, s.lk, v0);
+        kl.finish(k0);
+        vl.finish(v0);
+    }
+    __syncthreads();
+    auto step = [&](int key0, const auto &kt, const auto &vt, auto &k_next, auto &v_next) {
+        const bool more = key0 + KEYS < to;
+        if (more) {
+            kl.start(k + (key0 + KEYS) * a.k.token_pitch, s.lk - key0 - KEYS, k_next);
+            vl.start(v + (key0 + KEYS) * a.v.token_pitch, s.lk - key0 - KEYS, v_next);
+        }
+#pragma unroll
+        for (int n = 0; n < 2; ++n) {
+            if (key0 + n * 32 >= wave_to) continue;
+            f32x16 x = zero16(), dp = zero16();
+#pragma unroll
+            for (int i = 0; i < STEPS; ++i) {
+                x = mfma(row_operand<T, DP>(kt, n * 32, i, lane), q[i], x);
+                dp = mfma(row_operand<T, DP>(vt, n * 32, i, lane), dout[i], dp);
+            }
+            if (key0 + n * 32 + 32 > all_see || key0 + n * 32 + 32 > s.lk) {
+#pragma unroll
+                for (int r = 0; r < 16; ++r)
+                    if (key0 + n * 32 + result_row(r, half) > last) x[r] = -INFINITY;
+            }
+#pragma unroll
+            for (int r = 0; r < 16; ++r)
+                x[r] = __builtin_amdgcn_exp2f(fmaf(x[r], a.scale2, -lse2)) * (dp[r] - delta);
+            Operand8<T> ds[2];
+            round_scores<T>(x, factor, dq, ds);
+#pragma unroll
+            for (int t = 0; t < 2; ++t)
+#pragma unroll
+                for (int d = 0; d < BLOCKS; ++d)
+                    dq[d] = mfma(column_operand<T, DP>(kt, n * 32 + t * 16, d, lane), ds[t], dq[d]);
+        }
+        if (more) {
+            kl.finish(k_next);
+            vl.finish(v_next);
+        }
+        __syncthreads();
+    };
+    for (int key0 = 0; key0 < to; key0 += 2 * KEYS) {
+        step(key0, k0, v0, k1, v1);
+        if (key0 + KEYS < to) step(key0 + KEYS, k1, v1, k0, v0);
+    }
+    T *to_row = a.dq.template at<T>(s.q0 + held, task.head);
+    const float scale = kNarrow<T> ? a.scale / factor : a.scale;
+#pragma unroll
+    for (int d = 0; d < BLOCKS; ++d) store_columns(to_row, row < s.lq, dq[d], scale, d, lane, a.dim);
+}
+
+// Keys: a lane holds one key's column, and passes over the queries that see
+// it, 32 at a time, of every head of its group.
+template <typename T, int DP, bool ASYNC>
+__global__ __launch_bounds__(kThreads, DP <= 64 ? 2 : 1) void attention_dkv_kernel(GradArgs a) {
+    constexpr int STEPS = DP / 16, BLOCKS = DP / 32, QUERIES = 64, WORDS = TileShape<DP>::words;
+    __shared__ uint4 q0[QUERIES * WORDS], d0[QUERIES * WORDS], q1[QUERIES * WORDS], d1[QUERIES * WORDS];
+    __shared__ float lse_lds[2][QUERIES], delta_lds[2][QUERIES];
+    const Task task = task_of(blockIdx.x, a.blocks, a.heads / a.group, 1);
+    Sequence s;
+    if (!find_sequence(a.seq, true, task.block, kShift, &s)) return;
+    const int lane = threadIdx.x % kWave, wave = threadIdx.x / kWave, half = lane / 32;
+    const int key0 = s.block * kRows + wave * 32, key = key0 + lane % 32, held = min(key, s.lk - 1);
+
+    Operand8<T> k[STEPS], v[STEPS];
+#pragma unroll
+    for (int i = 0; i < STEPS; ++i) {
+        k[i] = global_operand(a.k.template at<const T>(s.k0 + held, task.head), true, i, lane, a.dim);
+        v[i] = global_operand(a.v.template at<const T>(s.k0 + held, task.head), true, i, lane, a.dim);
+    }
+    // the first query that sees the lane's key; of the workgroup's and of the wave's keys; the first that sees all the wave's
+    const int first = a.causal ? key - (s.lk - s.lq) : 0;
+    const int from = a.causal ? max(0, s.block * kRows - (s.lk - s.lq)) / QUERIES * QUERIES : 0;
+    const int wave_from = a.causal ? key0 - (s.lk - s.lq) : 0, all_see = a.causal ? wave_from + 31 : 0;
+    const int tiles = s.lq > from ? (s.lq - from + QUERIES - 1) / QUERIES : 0, turns = tiles * a.group;
+
+    f32x16 dk[BLOCKS], dv[BLOCKS];
+#pragma unroll
+    for (int d = 0; d < BLOCKS; ++d) dk[d] = dv[d] = zero16();
+    float factor = kFirstFactor;
+    TileLoader<T, DP, QUERIES, kThreads, ASYNC> ql(threadIdx.x, a.dim, a.q.token_pitch), dl(threadIdx.x, a.dim, a.dout.token_pitch);
+    int next_head = task.head * a.group, next_row = from;  // of the tile to be loaded
+    float2 stat;
+    auto start = [&](auto &q_to, auto &d_to) {
+        ql.start(a.q.template at<const T>(s.q0 + next_row, next_head), s.lq - next_row, q_to);
+        dl.start(a.dout.template at<const T>(s.q0 + next_row, next_head), s.lq - next_row, d_to);
+        stat = make_float2(INFINITY, 0);
+        if (threadIdx.x < QUERIES && next_row + int(threadIdx.x) < s.lq)
+            stat = a.row[int64_t(next_head) * a.seq.q_tokens + s.q0 + next_row + threadIdx.x];
+        next_row += QUERIES;
+        if (next_row >= s.lq) {
+            next_row = from;
+            ++next_head;
+        }
+    };
+    auto finish = [&](int which, auto &q_to, auto &d_to) {
+        if (threadIdx.x < QUERIES) {
+            lse_lds[which][threadIdx.x] = stat.x;
+            delta_lds[which][threadIdx.x] = stat.y;
+        }
+        ql.finish(q_to);
+        dl.finish(d_to);
+    };
+    if (turns > 0) {
+        start(q0, d0);
+        finish(0, q0, d0);
+    }
+    __syncthreads();
+    int row0 = from;
+    auto step = [&](int turn, int which, const auto &qt, const auto &dt, auto &q_next, auto &d_next) {
+        const bool more = turn + 1 < turns;
+        if (more) start(q_next, d_next);
+#pragma unroll
+        for (int n = 0; n < 2; ++n) {
+            const int r0 = row0 + n * 32;
+            if (r0 + 31 < wave_from || r0 >= s.lq) continue;
+            f32x16 x = zero16(), dp = zero16();
+#pragma unroll
+            for (int i = 0; i < STEPS; ++i) {
+                x = mfma(row_operand<T, DP>(qt, n * 32, i, lane), k[i], x);
+                dp = mfma(row_operand<T, DP>(dt, n * 32, i, lane), v[i], dp);
+            }
+            if (r0 < all_see) {
+#pragma unroll
+                for (int r = 0; r < 16; ++r)
+                    if (r0 + result_row(r, half) < first) x[r] = -INFINITY;
+            }
+            Operand8<T> p[2], ds[2];
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                const f32x4 lse = *reinterpret_cast<const f32x4 *>(&lse_lds[which][n * 32 + result_row(4 * j, half)]);
+                const f32x4 delta = *reinterpret_cast<const f32x4 *>(&delta_lds[which][n * 32 + result_row(4 * j, half)]);
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    const int r = 4 * j + e;
+                    const float w = __builtin_amdgcn_exp2f(fmaf(x[r], a.scale2, kRaised<T> - lse[e]));
+                    p[r / 8].e[r % 8] = T(w);
+                    x[r] = w * (dp[r] - delta[e]);
+                }
+            }
+            round_scores<T>(x, factor, dk, ds);
+#pragma unroll
+            for (int t = 0; t < 2; ++t)
+#pragma unroll
+                for (int d = 0; d < BLOCKS; ++d) {
+                    dv[d] = mfma(column_operand<T, DP>(dt, n * 32 + t * 16, d, lane), p[t], dv[d]);
+                    dk[d] = mfma(column_operand<T, DP>(qt, n * 32 + t * 16, d, lane), ds[t], dk[d]);
+                }
+        }
+        row0 += QUERIES;
+        if (row0 >= s.lq) row0 = from;
+        if (more) finish(which ^ 1, q_next, d_next);
+        __syncthreads();
+    };
+    for (int turn = 0; turn < turns; turn += 2) {
+        step(turn, 0, q0, d0, q1, d1);
+        if (turn + 1 < turns) step(turn + 1, 1, q1, d1, q0, d0);
+    }
+    T *to_dk = a.dk.template at<T>(s.k0 + held, task.head), *to_dv = a.dv.template at<T>(s.k0 + held, task.head);
+    const float down = kNarrow<T> ? 1.0f / 16384 : 1.0f, scale = kNarrow<T> ? a.scale / factor * down : a.scale;
+#pragma unroll
+    for (int d = 0; d < BLOCKS; ++d) {
+        store_columns(to_dk, key < s.lk, dk[d], scale, d, lane, a.dim);
+        store_columns(to_dv, key < s.lk, dv[d], down, d, lane, a.dim);
+    }
+}
+
+}  // namespace
+}  // namespace rs
+
+extern "C" int64_t reshard_attention_backward_workspace(int64_t q_tokens, int64_t heads) {
+    if (q_tokens < 0 || q_tokens > 0x7fffff00 || heads < 1 || heads > rs::kMaxHeads) return -1;
+    return q_tokens * heads * 8;
+}
+
+extern "C" reshard_status_t reshard_attention_backward(
+    int64_t q_tokens, int64_t k_tokens, int64_t sequences, int64_t heads, int64_t kv_heads, int64_t dim,
+    reshard_dtype_t dtype, const reshard_heads_t *dout, const reshard_heads_t *q, const reshard_heads_t *k,
+    const reshard_heads_t *v, const reshard_heads_t *out, const float *lse, const int32_t *q_offsets,
+    const int32_t *k_offsets, double scale, int causal, const reshard_heads_t *dq, const reshard_heads_t *dk,
+    const reshard_heads_t *dv, void *workspace, int64_t workspace_bytes, void *stream) {
+    return rs::guarded([&]() -> reshard_status_t {
+        using namespace rs;
+        reshard_status_t st = check_attention(q_tokens, k_tokens, sequences, heads, kv_heads, dim, dtype, q_offsets,
+                                              k_offsets, scale, causal);
+        GradArgs a{};
+        if (st == RESHARD_OK) st = check_heads("dout", dout, q_tokens, heads, dim, 2, false, &a.dout);
+        if (st == RESHARD_OK) st = check_heads("q", q, q_tokens, heads, dim, 2, false, &a.q);
+        if (st == RESHARD_OK) st = check_heads("k", k, k_tokens, kv_heads, dim, 2, false, &a.k);
+        if (st == RESHARD_OK) st = check_heads("v", v, k_tokens, kv_heads, dim, 2, false, &a.v);
+        if (st == RESHARD_OK) st = check_heads("out", out, q_tokens, heads, dim, 2, false, &a.out);
+        if (st == RESHARD_OK) st = check_matrix("lse", lse, heads, q_tokens, q_tokens, 4);
+        if (st == RESHARD_OK) st = check_heads("dq", dq, q_tokens, heads, dim, 2, true, &a.dq);
+        if (st == RESHARD_OK) st = check_heads("dk", dk, k_tokens, kv_heads, dim, 2, true, &a.dk);
+        if (st == RESHARD_OK) st = check_heads("dv", dv, k_tokens, kv_heads, dim, 2, true, &a.dv);
+        if (st != RESHARD_OK || sequences == 0) return st;
+        if (q_tokens > 0) {
+            st = check_workspace("the queries' statistics need", workspace, workspace_bytes,
+                                 reshard_attention_backward_workspace(q_tokens, heads));
+            if (st != RESHARD_OK) return st;
+        }
+        a.lse = lse;
+        a.row = static_cast<float2 *>(workspace);
+        a.seq = Sequences{q_offsets, k_offsets, int(sequences), q_tokens, k_tokens};
+        a.heads = int(heads);
+        a.group = int(heads / kv_heads);
+        a.dim = int(dim);
+        a.causal = causal;
+        a.scale = float(scale);
+        a.scale2 = float(scale) * kLog2e;
+        const hipStream_t stm = static_cast<hipStream_t>(stream);
+        return with_dim(dtype, dim, [&](auto zero, auto padded) {
+            using T = decltype(zero);
+            constexpr int DP = decltype(padded)::value;
+            reshard_status_t status = RESHARD_OK;
+            if (q_tokens > 0) {
+                status = check_grid(blocks_of(q_tokens, sequences, kShift), heads, &a.blocks);
+                if (status != RESHARD_OK) return status;
+                const bool async = aligned16(a.k, 2) && aligned16(a.v, 2);
+                status = launch("attention gradient launch",
+                                async ? attention_dq_kernel<T, DP, true> : attention_dq_kernel<T, DP, false>,
+                                dim3(unsigned(a.blocks * heads)), kThreads, 0, stm, a);
+                if (status != RESHARD_OK) return status;
+            }
+            if (k_tokens == 0) return status;
+            status = check_grid(blocks_of(k_tokens, sequences, kShift), kv_heads, &a.blocks);
+            if (status != RESHARD_OK) return status;
+            const bool async = aligned16(a.q, 2) && aligned16(a.dout, 2);
+            return launch("attention gradient launch",
+                          async ? attention_dkv_kernel<T, DP, true> : attention_dkv_kernel<T, DP, false>,
+                          dim3(unsigned(a.blocks * kv_heads)), kThreads, 0, stm, a);
+        });
+    });
+}

@@ -1,0 +1,569 @@
+// heads.hip -- queries' and keys' heads between the product that makes them
+// and the attention that reads them: root-mean-square norm and rotation by the
+// token's position, with keys and values into a paged cache, and its gradients.
+//
+//   r = 1 / sqrt(sum_d x^2 / D + eps)    xhat = x r    y = Rot(position) (xhat w)
+//   g = Rot(position)^T dy               dw = sum over tokens and heads of g xhat
+//   dx = r (g w - xhat mean_d(g w xhat))
+//
+// Rot turns the pairs of a head's first `rotary` elements: (j, j + rotary / 2),
+// or neighbours (2j, 2j + 1), by position * frequency[j].  That product and its
+// reduction to a quarter turn are taken in 64 bits: a position of 2^20 leaves
+// 4 bits of an angle in 32.
+//
+// Both are bound by memory: heads are read once and written once, angles are
+// computed once for a token's heads of a workgroup.
+#include <algorithm>
+
+#include "heads.hpp"
+
+namespace rs {
+namespace {
+
+// cos and sin of position * frequency.  The quarter turns come off in 64 bits;
+// Taylor's series on the rest, |x| <= pi / 4, are off by 2e-9 and 7e-9 at most.
+__device__ inline float2 turn(int32_t position, double frequency) {
+    const double t = double(position) * frequency * 0.63661977236758134308;  // 2 / pi
+    const double quarters = rint(t);
+    const float x = float((t - quarters) * 1.57079632679489661923), x2 = x * x;
+    const float s = x * fmaf(x2, fmaf(x2, fmaf(x2, fmaf(x2, 1.0f / 362880, -1.0f / 5040), 1.0f / 120), -1.0f / 6), 1.0f);
+    const float c =
+        fmaf(x2, fmaf(x2, fmaf(x2, fmaf(x2, fmaf(x2, -1.0f / 3628800, 1.0f / 40320), -1.0f / 720), 1.0f / 24), -0.5f), 1.0f);
+    const int n = int(quarters - 4 * floor(quarters * 0.25));
+    const float a = n & 1 ? s : c, b = n & 1 ? c : s;
+    return make_float2(n == 1 || n == 2 ? -a : a, n >= 2 ? -b : b);
+}
+
+// Sum over 1 << shift neighbouring lanes, in each of them.  Inside 16 lanes by
+// data-parallel moves: neighbours, pairs, then mirrors of what is already alike.
+__device__ inline float lanes_sum(float x, int shift) {
+    auto moved = [&](auto ctrl) {
+        return __int_as_float(
+            __builtin_amdgcn_update_dpp(0, __float_as_int(x), decltype(ctrl)::value, 0xf, 0xf, true));
+    };
+    using std::integral_constant;
+    if (shift > 0) x += moved(integral_constant<int, 0xB1>{});   // 1 0 3 2
+    if (shift > 1) x += moved(integral_constant<int, 0x4E>{});   // 2 3 0 1
+    if (shift > 2) x += moved(integral_constant<int, 0x141>{});  // half a row mirrored
+    if (shift > 3) x += moved(integral_constant<int, 0x140>{});  // a row mirrored
+    if (shift > 4) x += __shfl_xor(x, 16);
+    if (shift > 5) x += __shfl_xor(x, 32);
+    return x;
+}
+
+template <typename T, int VP>
+struct alignas(VP * sizeof(T)) Part {
+    T e[VP];
+};
+
+// A thread's 2 VP elements of a head: VP pairs.  Where halves are paired, two
+// runs of VP elements (the elements behind the rotated ones count as pairs of
+// their halves, turned by nothing); where neighbours are, one run of 2 VP.
+template <typename T, int VP, bool NEIGHBOURS>
+struct Pairs {
+    float a[VP], b[VP];  // first and second elements
+
+    __device__ void load(const T *x, int e0, int e1) {
+        Part<T, VP> p, q;
+        __builtin_memcpy(&p, x + e0, sizeof p);
+        __builtin_memcpy(&q, x + e1, sizeof q);
+        set(p, q);
+    }
+    __device__ void set(const Part<T, VP> &p, const Part<T, VP> &q) {
+#pragma unroll
+        for (int i = 0; i < VP; ++i) {
+            if constexpr (NEIGHBOURS) {
+                a[i] = float(2 * i < VP ? p.e[(2 * i) % VP] : q.e[(2 * i) % VP]);
+                b[i] = float(2 * i + 1 < VP ? p.e[(2 * i + 1) % VP] : q.e[(2 * i + 1) % VP]);
+            } else {
+                a[i] = float(p.e[i]);
+                b[i] = float(q.e[i]);
+            }
+        }
+    }
+    __device__ void store(T *y, int e0, int e1) const {
+        Part<T, VP> p, q;
+#pragma unroll
+        for (int i = 0; i < VP; ++i) {
+            if constexpr (NEIGHBOURS) {
+                (2 * i < VP ? p : q).e[(2 * i) % VP] = T(a[i]);
+                (2 * i + 1 < VP ? p : q).e[(2 * i + 1) % VP] = T(b[i]);
+            } else {
+                p.e[i] = T(a[i]);
+                q.e[i] = T(b[i]);
+            }
+        }
+        __builtin_memcpy(y + e0, &p, sizeof p);
+        __builtin_memcpy(y + e1, &q, sizeof q);
+    }
+};
+
+// Where a lane's pairs lie.
+template <int VP, bool NEIGHBOURS>
+struct Place {
+    int pair, e0, e1;
+    bool any;
+    __device__ Place(int lane, int dim, int rotary) {
+        pair = lane * VP;
+        any = pair < dim / 2;
+        if (!any) pair = 0;
+        if constexpr (NEIGHBOURS) {
+            e0 = 2 * pair;
+            e1 = e0 + VP;
+        } else if (pair < rotary / 2) {
+            e0 = pair;
+            e1 = pair + rotary / 2;
+        } else {
+            e0 = rotary + pair - rotary / 2;
+            e1 = e0 + (dim - rotary) / 2;
+        }
+    }
+};
+
+// The workgroup's tables: each of its tokens' turns (1, 0 behind the rotated
+// pairs), and weights as float32 in the order of pairs (first elements, then second).
+template <bool NEIGHBOURS>
+__device__ inline void fill_turns(float2 *turns, const int32_t *positions, const double *frequencies, int64_t token,
+                                  int64_t tokens, int count, int dim, int rotary) {
+    const int pairs = dim / 2;
+    for (int i = threadIdx.x; i < count * pairs; i += blockDim.x) {
+        const int t = i / pairs, p = i - t * pairs;
+        turns[i] = p < rotary / 2 ? turn(positions[min(token + t, tokens - 1)], frequencies[p]) : make_float2(1, 0);
+    }
+}
+
+__device__ inline float weight_at(const void *w, int dtype, int e) {
+    if (!w) return 1.0f;
+    if (dtype == RESHARD_F32) return static_cast<const float *>(w)[e];
+    if (dtype == RESHARD_BF16) return float(static_cast<const bf16 *>(w)[e]);
+    return float(static_cast<const f16 *>(w)[e]);
+}
+
+template <bool NEIGHBOURS>
+__device__ inline void fill_weights(float *out, const void *w, int dtype, int dim, int rotary) {
+    const int pairs = dim / 2;
+    for (int i = threadIdx.x; i < dim; i += blockDim.x) {
+        const int p = i < pairs ? i : i - pairs, second = i >= pairs;
+        const Place<1, NEIGHBOURS> at(p, dim, rotary);
+        out[i] = weight_at(w, dtype, second ? at.e1 : at.e0);
+    }
+}
+
+struct HeadsArgs {
+    Heads q, k, v, q_out, k_out;
+    Cache cache;
+    const void *q_weight, *k_weight;
+    const double *frequencies;
+    const int32_t *positions, *slots;
+    int64_t tokens;
+    int heads, kv_heads, dim, rotary, weight_dtype;
+    int lanes_shift;  // lanes of a head: 1 << lanes_shift
+    int each;         // heads of a token: queries', keys', and values' where there is a cache
+    int span;         // tokens that a workgroup's heads belong to, at most
+    float eps;
+};
+
+constexpr int kHeadsThreads = 256, kHeadsTurns = 2;
+
+// A workgroup takes a run of (token, head)s, 1 << lanes_shift lanes a head and
+// kHeadsTurns heads for each group of lanes, loaded before the angles are
+// computed.
+template <typename T, int VP, bool NEIGHBOURS>
+__global__ __launch_bounds__(kHeadsThreads) void heads_kernel(HeadsArgs a) {
+    extern __shared__ float2 turns[];  // [span][dim / 2], then the weights
+    float *weights = reinterpret_cast<float *>(turns + a.span * (a.dim / 2));
+    const int groups = kHeadsThreads >> a.lanes_shift, group = threadIdx.x >> a.lanes_shift;
+    const Place<VP, NEIGHBOURS> at(threadIdx.x & ((1 << a.lanes_shift) - 1), a.dim, a.rotary);
+    const int64_t first = int64_t(blockIdx.x) * (groups * kHeadsTurns), token0 = first / a.each;
+    const int rest = int(first - token0 * a.each);
+    Part<T, VP> p[kHeadsTurns], q[kHeadsTurns];
+    int token[kHeadsTurns], head[kHeadsTurns];
+    int64_t to[kHeadsTurns];
+#pragma unroll
+    for (int u = 0; u < kHeadsTurns; ++u) {
+        const int i = rest + u * groups + group;
+        token[u] = i / a.each;
+        head[u] = i - token[u] * a.each;
+        const int64_t t = token0 + token[u];
+        if (t >= a.tokens || !at.any) head[u] = -1;
+        if (head[u] < 0) continue;
+        const T *x;
+        if (head[u] < a.heads) x = a.q.template at<const T>(t, head[u]);
+        else if (head[u] < a.heads + a.kv_heads) x = a.k.template at<const T>(t, head[u] - a.heads);
+        else x = a.v.template at<const T>(t, head[u] - a.heads - a.kv_heads);
+        __builtin_memcpy(&p[u], x + at.e0, sizeof p[u]);
+        __builtin_memcpy(&q[u], x + at.e1, sizeof q[u]);
+        if (a.slots && head[u] >= a.heads) to[u] = a.slots[t];
+    }
+    fill_turns<NEIGHBOURS>(turns, a.positions, a.frequencies, token0, a.tokens, a.span, a.dim, a.rotary);
+    fill_weights<NEIGHBOURS>(weights, a.q_weight, a.weight_dtype, a.dim, a.rotary);
+    fill_weights<NEIGHBOURS>(weights + a.dim, a.k_weight, a.weight_dtype, a.dim, a.rotary);
+    __syncthreads();
+#pragma unroll
+    for (int u = 0; u < kHeadsTurns; ++u) {
+        Pairs<T, VP, NEIGHBOURS> x;
+        float sum = 0;
+        if (head[u] >= 0) {
+            x.set(p[u], q[u]);
+#pragma unroll
+            for (int i = 0; i < VP; ++i) sum = fmaf(x.a[i], x.a[i], fmaf(x.b[i], x.b[i], sum));
+        }
+        sum = lanes_sum(sum, a.lanes_shift);
+        if (head[u] < 0) continue;
+        const int64_t t = token0 + token[u];
+        const bool is_q = head[u] < a.heads, is_v = head[u] >= a.heads + a.kv_heads;
+        const int h = is_q ? head[u] : is_v ? head[u] - a.heads - a.kv_heads : head[u] - a.heads;
+        T *y;
+        if (is_q) {
+            y = a.q_out.template at<T>(t, h);
+        } else if (a.slots) {
+            // a slot outside the cache: the token is not kept
+            if (to[u] < 0 || to[u] >= a.cache.pages * a.cache.page_length) continue;
+            y = (is_v ? static_cast<T *>(a.cache.values) : static_cast<T *>(a.cache.keys)) + a.cache.offset(int(to[u]), h);
+        } else {
+            y = a.k_out.template at<T>(t, h);
+        }
+        if (is_v) {
+            __builtin_memcpy(y + at.e0, &p[u], sizeof p[u]);
+            __builtin_memcpy(y + at.e1, &q[u], sizeof q[u]);
+            continue;
+        }
+        const float r = 1.0f / sqrtf(sum / float(a.dim) + a.eps);
+        const float2 *c = turns + token[u] * (a.dim / 2) + at.pair;
+        const float *w = weights + (is_q ? 0 : a.dim) + at.pair;
+#pragma unroll
+        for (int i = 0; i < VP; ++i) {
+            const float f = x.a[i] * r * w[i], g = x.b[i] * r * w[a.dim / 2 + i];
+            x.a[i] = f * c[i].x - g * c[i].y;
+            x.b[i] = g * c[i].x + f * c[i].y;
+        }
+        x.store(y, at.e0, at.e1);
+    }
+}
+
+struct HeadsGradArgs {
+    Heads d[2], x[2], dx[2];  // of queries and of keys
+    const void *weight[2];
+    const double *frequencies;
+    const int32_t *positions;
+    float *partial;  // [workgroups][dim]: sums of g xhat, queries' workgroups first
+    int64_t tokens;
+    int heads[2], workgroups[2];
+    int dim, rotary, weight_dtype, lanes_shift, span;
+    float eps;
+};
+
+// The first workgroups take queries, the others keys, each a contiguous run of
+// (token, head)s, of which every group of lanes holds its columns' sums in
+// registers; no atomics.
+template <typename T, int VP, bool NEIGHBOURS>
+__global__ __launch_bounds__(kHeadsThreads) void heads_grad_kernel(HeadsGradArgs a) {
+    extern __shared__ float2 turns[];  // [2][span][dim / 2]; at the end a sum for each group and column
+    const int k = int(blockIdx.x) >= a.workgroups[0], wg = int(blockIdx.x) - (k ? a.workgroups[0] : 0);
+    const int groups = kHeadsThreads >> a.lanes_shift, group = threadIdx.x >> a.lanes_shift;
+    const Place<VP, NEIGHBOURS> at(threadIdx.x & ((1 << a.lanes_shift) - 1), a.dim, a.rotary);
+    const int each = a.heads[k];
+    const int64_t total = a.tokens * each, step = groups * kHeadsTurns;
+    const int64_t steps = ceil_div(total, step), n = a.workgroups[k];
+    const int64_t from = steps * wg / n, until = steps * (wg + 1) / n;
+    float w0[VP], w1[VP], s0[VP], s1[VP];
+#pragma unroll
+    for (int i = 0; i < VP; ++i) {
+        const Place<1, NEIGHBOURS> e(at.pair + i, a.dim, a.rotary);
+        w0[i] = weight_at(a.weight[k], a.weight_dtype, e.e0);
+        w1[i] = weight_at(a.weight[k], a.weight_dtype, e.e1);
+        s0[i] = s1[i] = 0;
+    }
+    int turn_of = 0;
+    for (int64_t s = from; s < until; ++s, turn_of ^= 1) {
+        const int64_t first = s * step, token0 = first / each;
+        const int rest = int(first - token0 * each);
+        Part<T, VP> px[kHeadsTurns][2], pd[kHeadsTurns][2];
+        int token[kHeadsTurns], head[kHeadsTurns];
+#pragma unroll
+        for (int u = 0; u < kHeadsTurns; ++u) {
+            const int i = rest + u * groups + group;
+            token[u] = i / each;
+            head[u] = i - token[u] * each;
+            const int64_t t = token0 + token[u];
+            if (t >= a.tokens || !at.any) head[u] = -1;
+            if (head[u] < 0) continue;
+            const T *x = a.x[k].template at<const T>(t, head[u]), *d = a.d[k].template at<const T>(t, head[u]);
+            __builtin_memcpy(&px[u][0], x + at.e0, sizeof px[u][0]);
+            __builtin_memcpy(&px[u][1], x + at.e1, sizeof px[u][0]);
+            __builtin_memcpy(&pd[u][0], d + at.e0, sizeof px[u][0]);
+            __builtin_memcpy(&pd[u][1], d + at.e1, sizeof px[u][0]);
+        }
+        float2 *table = turns + turn_of * a.span * (a.dim / 2);
+        fill_turns<NEIGHBOURS>(table, a.positions, a.frequencies, token0, a.tokens, a.span, a.dim, a.rotary);
+        __syncthreads();  // the other half was read before the barrier ahead of this one
+#pragma unroll
+        for (int u = 0; u < kHeadsTurns; ++u) {
+            Pairs<T, VP, NEIGHBOURS> x, d;
+            float sum = 0, along = 0;
+            if (head[u] >= 0) {
+                x.set(px[u][0], px[u][1]);
+                d.set(pd[u][0], pd[u][1]);
+                const float2 *c = table + token[u] * (a.dim / 2) + at.pair;
+#pragma unroll
+                for (int i = 0; i < VP; ++i) {
+                    sum = fmaf(x.a[i], x.a[i], fmaf(x.b[i], x.b[i], sum));
+                    const float f = d.a[i] * c[i].x + d.b[i] * c[i].y, g = d.b[i] * c[i].x - d.a[i] * c[i].y;
+                    d.a[i] = f;
+                    d.b[i] = g;
+                    along = fmaf(f * w0[i], x.a[i], fmaf(g * w1[i], x.b[i], along));
+                }
+            }
+            sum = lanes_sum(sum, a.lanes_shift);
+            along = lanes_sum(along, a.lanes_shift);
+            if (head[u] < 0) continue;
+            const float r = 1.0f / sqrtf(sum / float(a.dim) + a.eps);
+            const float mean = along * r / float(a.dim);
+#pragma unroll
+            for (int i = 0; i < VP; ++i) {
+                const float h0 = x.a[i] * r, h1 = x.b[i] * r;
+                s0[i] = fmaf(d.a[i], h0, s0[i]);
+                s1[i] = fmaf(d.b[i], h1, s1[i]);
+                x.a[i] = r * (d.a[i] * w0[i] - h0 * mean);
+                x.b[i] = r * (d.b[i] * w1[i] - h1 * mean);
+            }
+            if (a.dx[k].data) x.store(a.dx[k].template at<T>(token0 + token[u], head[u]), at.e0, at.e1);
+        }
+    }
+    if (!a.partial) return;
+    __syncthreads();
+    float *sums = reinterpret_cast<float *>(turns);  // [groups][dim]
+    if (at.any) {
+#pragma unroll
+        for (int i = 0; i < VP; ++i) {
+            const Place<1, NEIGHBOURS> e(at.pair + i, a.dim, a.rotary);
+            sums[group * a.dim + e.e0] = s0[i];
+            sums[group * a.dim + e.e1] = s1[i];
+        }
+    }
+    __syncthreads();
+    for (int c = threadIdx.x; c < a.dim; c += kHeadsThreads) {
+        float s = 0;
+        for (int g = 0; g < groups; ++g) s += sums[g * a.dim + c];
+        a.partial[int64_t(blockIdx.x) * a.dim + c] = s;
+    }
+}
+
+// Adds up the workgroups' sums, 16 columns a workgroup and 64 threads a column.
+__global__ __launch_bounds__(1024) void heads_join_kernel(const float *partial, int dim, int q_parts, int k_parts,
+                                                          float *dwq, float *dwk, int accumulate) {
+    __shared__ float part[64][17];
+    const int c = blockIdx.x * 16 + threadIdx.x % 16, row = threadIdx.x / 16;
+    float *out = blockIdx.y ? dwk : dwq;
+    const int from = blockIdx.y ? q_parts : 0, parts = blockIdx.y ? k_parts : q_parts;
+    float s = 0;
+    if (c < dim)
+        for (int i = row; i < parts; i += 64) s += partial[int64_t(from + i) * dim + c];
+    part[row][threadIdx.x % 16] = s;
+    __syncthreads();
+    if (row || c >= dim || !out) return;
+    s = 0;
+    for (int i = 0; i < 64; ++i) s += part[i][threadIdx.x];
+    out[c] = accumulate ? out[c] + s : s;
+}
+
+// Pairs of a thread: the most, up to 16 bytes of first elements, that divide
+// the rotated pairs and the others, where halves are paired.
+int pairs_of(int dim, int rotary, bool neighbours, int most) {
+    int n = most;
+    while (n > 1 && (dim / 2 % n || (!neighbours && rotary / 2 % n))) n /= 2;
+    return n;
+}
+
+int shift_of(int lanes) {
+    int s = 0;
+    while ((1 << s) < lanes) ++s;
+    return s;
+}
+
+// Calls f(type's zero, pairs, neighbours) with the last two as constants.
+template <typename T, typename F>
+reshard_status_t with_pairs(int n, bool neighbours, F &&f) {
+    using std::integral_constant;
+    auto go = [&](auto vp) {
+        return neighbours ? f(T{}, vp, integral_constant<bool, true>{}) : f(T{}, vp, integral_constant<bool, false>{});
+    };
+    if constexpr (sizeof(T) == 2)
+        if (n == 8) return go(integral_constant<int, 8>{});
+    if (n == 4) return go(integral_constant<int, 4>{});
+    if (n == 2) return go(integral_constant<int, 2>{});
+    return go(integral_constant<int, 1>{});
+}
+
+template <typename F>
+reshard_status_t with_heads(reshard_dtype_t dtype, int dim, int rotary, bool neighbours, F &&f) {
+    const int n = pairs_of(dim, rotary, neighbours, dtype == RESHARD_F32 ? 4 : 8);
+    if (dtype == RESHARD_F32) return with_pairs<float>(n, neighbours, f);
+    if (dtype == RESHARD_BF16) return with_pairs<bf16>(n, neighbours, f);
+    return with_pairs<f16>(n, neighbours, f);
+}
+
+reshard_status_t check_rotation(int64_t tokens, int64_t heads, int64_t kv_heads, int64_t dim, int64_t rotary,
+                                int neighbours, reshard_dtype_t dtype, bool weights, reshard_dtype_t weight_dtype,
+                                double eps, const double *frequencies, const int32_t *positions) {
+    reshard_status_t st = check_extent("tokens", tokens);
+    if (st == RESHARD_OK) st = check_head_counts(heads, kv_heads);
+    if (st != RESHARD_OK) return st;
+    if (dim < 2 || dim % 2) return fail(RESHARD_EINVAL, "dim must be even and >= 2");
+    if (dim > kMaxDim) return fail(RESHARD_EUNSUPPORTED, "dim is above " + std::to_string(kMaxDim));
+    if (rotary < 0 || rotary > dim || rotary % 2) return fail(RESHARD_EINVAL, "rotary must be even, from 0 to dim");
+    if (neighbours & ~1) return fail(RESHARD_EINVAL, "interleaved must be 0 or 1");
+    if (!is_float_type(dtype)) return fail(RESHARD_EINVAL, "dtype must be F16, BF16 or F32");
+    if (weights && !is_float_type(weight_dtype)) return fail(RESHARD_EINVAL, "weight_dtype must be F16, BF16 or F32");
+    if (!(eps >= 0)) return fail(RESHARD_EINVAL, "eps must be >= 0");
+    if (rotary > 0) {
+        st = check_matrix("frequencies", frequencies, 1, rotary / 2, rotary / 2, 8);
+        if (st == RESHARD_OK) st = check_matrix("positions", positions, 1, tokens, tokens, 4);
+    }
+    return st;
+}
+
+// Tokens that a run of `items` heads can touch where a token has `each`.
+int span_of(int items, int each) { return (items + each - 2) / each + 1; }
+
+constexpr int kGradWorkgroups = 1024;
+
+// Workgroups of the gradients: queries' and keys' share by their heads.
+void split_workgroups(int64_t tokens, int64_t heads, int64_t kv_heads, int *q, int *k) {
+    const int64_t most = std::min<int64_t>(kGradWorkgroups, ceil_div(tokens * (heads + kv_heads), 8));
+    *k = int(std::max<int64_t>(1, most * kv_heads / (heads + kv_heads)));
+    *q = int(std::max<int64_t>(1, most - *k));
+}
+
+}  // namespace
+}  // namespace rs
+
+extern "C" reshard_status_t reshard_rotate_heads(int64_t tokens, int64_t heads, int64_t kv_heads, int64_t dim,
+                                                 int64_t rotary, int interleaved, reshard_dtype_t dtype,
+                                                 const reshard_heads_t *q, const reshard_heads_t *k,
+                                                 const void *q_weight, const void *k_weight,
+                                                 reshard_dtype_t weight_dtype, double eps, const double *frequencies,
+                                                 const int32_t *positions, const reshard_heads_t *q_out,
+                                                 const reshard_heads_t *k_out, const reshard_heads_t *v,
+                                                 const reshard_cache_t *cache, const int32_t *slots, void *stream) {
+    return rs::guarded([&]() -> reshard_status_t {
+        using namespace rs;
+        reshard_status_t st = check_rotation(tokens, heads, kv_heads, dim, rotary, interleaved, dtype,
+                                             q_weight || k_weight, weight_dtype, eps, frequencies, positions);
+        const int64_t es = dtype == RESHARD_F32 ? 4 : 2, ws = weight_dtype == RESHARD_F32 ? 4 : 2;
+        HeadsArgs a{};
+        if (st == RESHARD_OK) st = check_heads("q", q, tokens, heads, dim, es, false, &a.q);
+        if (st == RESHARD_OK) st = check_heads("k", k, tokens, kv_heads, dim, es, false, &a.k);
+        if (st == RESHARD_OK) st = check_heads("q_out", q_out, tokens, heads, dim, es, true, &a.q_out);
+        if (st == RESHARD_OK && q_weight) st = check_matrix("q_weight", q_weight, 1, dim, dim, ws);
+        if (st == RESHARD_OK && k_weight) st = check_matrix("k_weight", k_weight, 1, dim, dim, ws);
+        if (st == RESHARD_OK && !cache != !v)
+            st = fail(RESHARD_EINVAL, "v and cache go together: values are only read to be cached");
+        if (st == RESHARD_OK && cache) {
+            st = check_cache(cache, kv_heads, dim, es, &a.cache);
+            if (st == RESHARD_OK) st = check_heads("v", v, tokens, kv_heads, dim, es, false, &a.v);
+            if (st == RESHARD_OK) st = check_matrix("slots", slots, 1, tokens, tokens, 4);
+        } else if (st == RESHARD_OK) {
+            st = check_heads("k_out", k_out, tokens, kv_heads, dim, es, true, &a.k_out);
+        }
+        if (st != RESHARD_OK || tokens == 0) return st;
+        a.q_weight = q_weight;
+        a.k_weight = k_weight;
+        a.frequencies = frequencies;
+        a.positions = positions;
+        a.slots = cache ? slots : nullptr;
+        a.tokens = tokens;
+        a.heads = int(heads);
+        a.kv_heads = int(kv_heads);
+        a.dim = int(dim);
+        a.rotary = int(rotary);
+        a.weight_dtype = int(weight_dtype);
+        a.eps = float(eps);
+        a.each = int(heads + kv_heads * (cache ? 2 : 1));
+        return with_heads(dtype, a.dim, a.rotary, interleaved, [&](auto zero, auto vp, auto neighbours) {
+            constexpr int VP = decltype(vp)::value;
+            a.lanes_shift = shift_of(a.dim / 2 / VP);
+            const int items = (kHeadsThreads >> a.lanes_shift) * kHeadsTurns;
+            a.span = span_of(items, a.each);
+            const int64_t grid = ceil_div(tokens * a.each, items);
+            if (grid > int64_t(1) << 30) return fail(RESHARD_EUNSUPPORTED, "tokens * heads is above 2^30 workgroups");
+            const size_t lds = size_t(a.span) * (a.dim / 2) * 8 + size_t(a.dim) * 8;
+            return launch("heads launch", heads_kernel<decltype(zero), VP, decltype(neighbours)::value>,
+                          dim3(unsigned(grid)), kHeadsThreads, lds, static_cast<hipStream_t>(stream), a);
+        });
+    });
+}
+
+extern "C" int64_t reshard_rotate_heads_backward_workspace(int64_t tokens, int64_t heads, int64_t kv_heads,
+                                                           int64_t dim) {
+    if (tokens < 0 || tokens > int64_t(1) << 40 || heads < 1 || kv_heads < 1 || heads > rs::kMaxHeads ||
+        kv_heads > rs::kMaxHeads || dim < 2 || dim > rs::kMaxDim)
+        return -1;
+    int q, k;
+    rs::split_workgroups(tokens, heads, kv_heads, &q, &k);
+    return int64_t(q + k) * dim * int64_t(sizeof(float));
+}
+
+extern "C" reshard_status_t reshard_rotate_heads_backward(
+    int64_t tokens, int64_t heads, int64_t kv_heads, int64_t dim, int64_t rotary, int interleaved,
+    reshard_dtype_t dtype, const reshard_heads_t *dq_out, const reshard_heads_t *dk_out, const reshard_heads_t *q,
+    const reshard_heads_t *k, const void *q_weight, const void *k_weight, reshard_dtype_t weight_dtype, double eps,
+    const double *frequencies, const int32_t *positions, const reshard_heads_t *dq, const reshard_heads_t *dk,
+    float *dq_weight, float *dk_weight, int accumulate, void *workspace, int64_t workspace_bytes, void *stream) {
+    return rs::guarded([&]() -> reshard_status_t {
+        using namespace rs;
+        reshard_status_t st = check_rotation(tokens, heads, kv_heads, dim, rotary, interleaved, dtype,
+                                             q_weight || k_weight, weight_dtype, eps, frequencies, positions);
+        const int64_t es = dtype == RESHARD_F32 ? 4 : 2, ws = weight_dtype == RESHARD_F32 ? 4 : 2;
+        HeadsGradArgs a{};
+        if (st == RESHARD_OK) st = check_heads("dq_out", dq_out, tokens, heads, dim, es, false, &a.d[0]);
+        if (st == RESHARD_OK) st = check_heads("dk_out", dk_out, tokens, kv_heads, dim, es, false, &a.d[1]);
+        if (st == RESHARD_OK) st = check_heads("q", q, tokens, heads, dim, es, false, &a.x[0]);
+        if (st == RESHARD_OK) st = check_heads("k", k, tokens, kv_heads, dim, es, false, &a.x[1]);
+        if (st == RESHARD_OK && dq) st = check_heads("dq", dq, tokens, heads, dim, es, true, &a.dx[0]);
+        if (st == RESHARD_OK && dk) st = check_heads("dk", dk, tokens, kv_heads, dim, es, true, &a.dx[1]);
+        if (st == RESHARD_OK && q_weight) st = check_matrix("q_weight", q_weight, 1, dim, dim, ws);
+        if (st == RESHARD_OK && k_weight) st = check_matrix("k_weight", k_weight, 1, dim, dim, ws);
+        if (st == RESHARD_OK && dq_weight) st = check_matrix("dq_weight", dq_weight, 1, dim, dim, 4);
+        if (st == RESHARD_OK && dk_weight) st = check_matrix("dk_weight", dk_weight, 1, dim, dim, 4);
+        if (st == RESHARD_OK && (accumulate & ~1)) st = fail(RESHARD_EINVAL, "accumulate must be 0 or 1");
+        if (st != RESHARD_OK) return st;
+        const bool sums = dq_weight || dk_weight;
+        const int64_t need = reshard_rotate_heads_backward_workspace(tokens, heads, kv_heads, dim);
+        if (sums && tokens > 0) {
+            st = check_workspace("the gradients of the weights need", workspace, workspace_bytes, need);
+            if (st != RESHARD_OK) return st;
+        }
+        const hipStream_t s = static_cast<hipStream_t>(stream);
+        split_workgroups(tokens, heads, kv_heads, &a.workgroups[0], &a.workgroups[1]);
+        if (tokens > 0 && (dq || dk || sums)) {
+            a.weight[0] = q_weight;
+            a.weight[1] = k_weight;
+            a.frequencies = frequencies;
+            a.positions = positions;
+            a.partial = sums ? static_cast<float *>(workspace) : nullptr;
+            a.tokens = tokens;
+            a.heads[0] = int(heads);
+            a.heads[1] = int(kv_heads);
+            a.dim = int(dim);
+            a.rotary = int(rotary);
+            a.weight_dtype = int(weight_dtype);
+            a.eps = float(eps);
+            st = with_heads(dtype, a.dim, a.rotary, interleaved, [&](auto zero, auto vp, auto neighbours) {
+                constexpr int VP = decltype(vp)::value;
+                a.lanes_shift = shift_of(a.dim / 2 / VP);
+                const int groups = kHeadsThreads >> a.lanes_shift, items = groups * kHeadsTurns;
+                a.span = span_of(items, int(std::min(heads, kv_heads)));
+                const size_t lds = std::max(size_t(2) * a.span * (a.dim / 2) * 8, size_t(groups) * a.dim * 4);
+                return launch("heads gradient launch", heads_grad_kernel<decltype(zero), VP, decltype(neighbours)::value>,
+                              dim3(unsigned(a.workgroups[0] + a.workgroups[1])), kHeadsThreads, lds, s, a);
+            });
+            if (st != RESHARD_OK) return st;
+        }
+        if (!sums || (tokens == 0 && accumulate)) return RESHARD_OK;
+        // no tokens: the sums are zeros
+        const int q_parts = tokens ? a.workgroups[0] : 0, k_parts = tokens ? a.workgroups[1] : 0;
+        return launch("heads gradient join launch", heads_join_kernel, dim3(unsigned(ceil_div(dim, 16)), 2), 1024, 0, s,
+                      static_cast<const float *>(workspace), int(dim), q_parts, k_parts, dq_weight, dk_weight, accumulate);
+    });
+}

@@ -1,0 +1,87 @@
+// heads.hpp -- what the operators on attention's heads (heads.hip,
+// attention.hip, decode.hip) share: how heads and paged caches lie, and their checks.
+#pragma once
+
+#include "operators.hpp"
+
+namespace rs {
+
+constexpr int64_t kMaxDim = 128, kMaxHeads = int64_t(1) << 16;
+
+// Element (token, head, d) of heads.
+struct Heads {
+    void *data;
+    int64_t token_pitch, head_pitch;
+    template <typename T>
+    __device__ T *at(int64_t token, int64_t head) const {
+        return static_cast<T *>(data) + token * token_pitch + head * head_pitch;
+    }
+};
+
+struct Cache {
+    void *keys, *values;
+    int64_t pages, page_pitch, slot_pitch, head_pitch;
+    int page_length;
+    __device__ int64_t offset(int slot, int64_t head) const {
+        const int page = slot / page_length;
+        return page * page_pitch + (slot - page * page_length) * slot_pitch + head * head_pitch;
+    }
+};
+
+inline reshard_status_t check_head_counts(int64_t heads, int64_t kv_heads) {
+    if (heads < 1 || kv_heads < 1) return fail(RESHARD_EINVAL, "heads and kv_heads must be >= 1");
+    if (heads > kMaxHeads || kv_heads > kMaxHeads) return fail(RESHARD_EUNSUPPORTED, "heads or kv_heads is above 2^16");
+    return RESHARD_OK;
+}
+
+inline bool spans_too_much(int64_t n, int64_t pitch, int64_t bytes) {
+    return pitch < 0 || (n > 1 && pitch > (int64_t(1) << 55) / (n * bytes));
+}
+
+// What is written must not overlap itself: heads of a token beside each other, or tokens of a head.
+inline reshard_status_t check_heads(const char *name, const reshard_heads_t *h, int64_t tokens, int64_t heads,
+                                    int64_t dim, int64_t elem_bytes, bool written, Heads *out) {
+    if (!h || (tokens > 0 && !h->data)) return fail(RESHARD_EINVAL, std::string(name) + " is NULL");
+    const int64_t t = h->token_pitch, s = h->head_pitch;
+    if (spans_too_much(tokens, t, elem_bytes) || spans_too_much(heads, s, elem_bytes))
+        return fail(RESHARD_EUNSUPPORTED, std::string(name) + ": a pitch is negative or spans more than 2^55 bytes");
+    const bool apart = (tokens <= 1 || t >= (heads - 1) * s + dim) && (heads <= 1 || s >= dim);
+    const bool across = (heads <= 1 || s >= (tokens - 1) * t + dim) && (tokens <= 1 || t >= dim);
+    if (written && tokens > 0 && !apart && !across)
+        return fail(RESHARD_EINVAL, std::string(name) + ": heads overlap, their pitches are " + std::to_string(t) +
+                                        " and " + std::to_string(s));
+    if (reinterpret_cast<uintptr_t>(h->data) % uintptr_t(elem_bytes))
+        return fail(RESHARD_EINVAL, std::string(name) + " is not aligned to its " + std::to_string(elem_bytes) +
+                                        "-byte elements");
+    *out = Heads{h->data, t, s};
+    return RESHARD_OK;
+}
+
+inline reshard_status_t check_cache(const reshard_cache_t *c, int64_t kv_heads, int64_t dim, int64_t elem_bytes,
+                                    Cache *out) {
+    if (c->pages < 0 || c->page_length < 1) return fail(RESHARD_EINVAL, "cache: pages must be >= 0, page_length >= 1");
+    if (c->pages > int64_t(0x7fffffff) / c->page_length)
+        return fail(RESHARD_EUNSUPPORTED, "cache: above 2^31 - 1 slots");
+    if (c->pages > 0 && (!c->keys || !c->values)) return fail(RESHARD_EINVAL, "cache: keys or values is NULL");
+    if (spans_too_much(c->pages, c->page_pitch, elem_bytes) || spans_too_much(c->page_length, c->slot_pitch, elem_bytes) ||
+        spans_too_much(kv_heads, c->head_pitch, elem_bytes))
+        return fail(RESHARD_EUNSUPPORTED, "cache: a pitch is negative or spans more than 2^55 bytes");
+    if ((c->pages > 1 && c->page_pitch < dim) || (c->page_length > 1 && c->slot_pitch < dim) ||
+        (kv_heads > 1 && c->head_pitch < dim))
+        return fail(RESHARD_EINVAL, "cache: a pitch is less than dim");
+    if (reinterpret_cast<uintptr_t>(c->keys) % uintptr_t(elem_bytes) ||
+        reinterpret_cast<uintptr_t>(c->values) % uintptr_t(elem_bytes))
+        return fail(RESHARD_EINVAL, "cache: not aligned to its elements");
+    *out = Cache{c->keys, c->values, c->pages, c->page_pitch, c->slot_pitch, c->head_pitch, int(c->page_length)};
+    return RESHARD_OK;
+}
+
+inline reshard_status_t check_workspace(const char *what, const void *p, int64_t bytes, int64_t need) {
+    if (!p || bytes < need)
+        return fail(RESHARD_EINVAL, std::string(what) + " a workspace of " + std::to_string(need) + " bytes, got " +
+                                        std::to_string(p ? bytes : 0));
+    if (reinterpret_cast<uintptr_t>(p) % 16) return fail(RESHARD_EINVAL, "workspace is not aligned to 16 bytes");
+    return RESHARD_OK;
+}
+
+}  // namespace rs

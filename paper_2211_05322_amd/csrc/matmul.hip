@@ -289,28 +289,6 @@ __device__ inline void store_run(const MatmulArgs &g, int64_t i, int64_t j, f32x
     else store_eight<f16>(g, i, j, lo, hi);
 }
 
-// A descriptor for `bytes` bytes from p, the same in every lane.  Loads from an
-// offset past the end give zeros.
-__device__ inline __amdgpu_buffer_rsrc_t bytes_from(const uint8_t *p, int64_t bytes) {
-    const uint64_t a = reinterpret_cast<uint64_t>(p);
-    const uint64_t lo = uint32_t(__builtin_amdgcn_readfirstlane(int(a)));
-    const uint64_t hi = uint32_t(__builtin_amdgcn_readfirstlane(int(a >> 32)));
-    const int n = __builtin_amdgcn_readfirstlane(int(bytes < 0xffffffff ? uint32_t(bytes) : 0xffffffffu));
-    return __builtin_amdgcn_make_buffer_rsrc(reinterpret_cast<void *>(hi << 32 | lo), 0, n, 0x00020000);
-}
-
-// 16 bytes of a lane's straight into LDS, from `base` + its offset; lane l's
-// go to `to` + 16 l, `to` being the wave's.  The whole offset is the lane's:
-// the instruction's scalar offset is subtracted from the descriptor's size in
-// the range check, which past a matrix's last rows would be below zero.
-__device__ inline void load_to_lds(__amdgpu_buffer_rsrc_t base, uint32_t offset, uint4 *to) {
-    __builtin_amdgcn_raw_ptr_buffer_load_lds(base, (__attribute__((address_space(3))) void *)to, 16, offset, 0, 0, 0);
-}
-
-// Before a barrier behind which other waves read what this one loaded into
-// LDS: the barrier itself waits for LDS accesses, not for such loads.
-__device__ inline void loads_done() { __builtin_amdgcn_s_waitcnt(0x0f70); }  // vmcnt(0)
-
 struct Tile {
     uint32_t i, j;
 };

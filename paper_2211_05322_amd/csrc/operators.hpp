@@ -124,6 +124,28 @@ __device__ inline float wave_sum(float x) {
     return __int_as_float(__builtin_amdgcn_readlane(__float_as_int(x), kWave - 1));
 }
 
+// A descriptor for `bytes` bytes from p, the same in every lane.  Loads from an
+// offset past the end give zeros.
+__device__ inline __amdgpu_buffer_rsrc_t bytes_from(const void *p, int64_t bytes) {
+    const uint64_t a = reinterpret_cast<uint64_t>(p);
+    const uint64_t lo = uint32_t(__builtin_amdgcn_readfirstlane(int(a)));
+    const uint64_t hi = uint32_t(__builtin_amdgcn_readfirstlane(int(a >> 32)));
+    const int n = __builtin_amdgcn_readfirstlane(int(bytes < 0xffffffff ? uint32_t(bytes) : 0xffffffffu));
+    return __builtin_amdgcn_make_buffer_rsrc(reinterpret_cast<void *>(hi << 32 | lo), 0, n, 0x00020000);
+}
+
+// 16 bytes of a lane's straight into LDS, from `base` + its offset; lane l's
+// go to `to` + 16 l, `to` being the wave's.  The whole offset is the lane's:
+// the instruction's scalar offset is subtracted from the descriptor's size in
+// the range check, which past a matrix's last rows would be below zero.
+__device__ inline void load_to_lds(__amdgpu_buffer_rsrc_t base, uint32_t offset, uint4 *to) {
+    __builtin_amdgcn_raw_ptr_buffer_load_lds(base, (__attribute__((address_space(3))) void *)to, 16, offset, 0, 0, 0);
+}
+
+// Before a barrier behind which other waves read what this one loaded into
+// LDS: the barrier itself waits for LDS accesses, not for such loads.
+__device__ inline void loads_done() { __builtin_amdgcn_s_waitcnt(0x0f70); }  // vmcnt(0)
+
 __device__ inline float e8m0_value(uint8_t code) {
     // 2^(code - 127); code 0 is 2^-127, a subnormal, and 255 NaN
     return code == 255 ? __builtin_nanf("") : code ? __uint_as_float(uint32_t(code) << 23) : __uint_as_float(0x400000u);

@@ -1,0 +1,810 @@
+"""The operators of attention against plain implementations in 64 bits.
+
+Norm and rotation of heads with their cache, attention of packed sequences and
+of single tokens over a paged cache, and the gradients.  Tolerances follow from
+what the kernels round.  U is half a unit in the last place of the type.  A
+float32 sum of terms t in a chain of at most d additions is off by at most
+d * 2^-24 * sum|t|; inside a matrix instruction the order and the rounding of
+additions are not documented, and 2^-23 is counted there.
+
+GPU tests unless marked otherwise; refusals run on the CPU.
+"""
+
+import itertools
+import math
+import zlib
+
+import pytest
+import torch
+
+from paper_2211_05322_amd import binding as B
+
+gpu = pytest.mark.gpu
+U = {torch.float32: 2.0 ** -24, torch.float16: 2.0 ** -11, torch.bfloat16: 2.0 ** -8}
+TINY = {torch.float32: 2.0 ** -150, torch.float16: 2.0 ** -25, torch.bfloat16: 2.0 ** -134}
+F32 = 2.0 ** -24
+HALVES = [torch.float16, torch.bfloat16]
+
+
+def _seed(*what):
+    return torch.Generator().manual_seed(zlib.crc32(repr(what).encode()))
+
+
+def _randn(g, *shape):
+    return torch.randn(*shape, generator=g, dtype=torch.float64)
+
+
+def _int32(values):
+    return torch.tensor(values, dtype=torch.int32, device="cuda")
+
+
+def _near(got, want, bound, what):
+    got, want, bound = (v.double().cpu() for v in (got, want, bound))
+    assert got.shape == want.shape, (what, got.shape, want.shape)
+    assert torch.equal(torch.isnan(got), torch.isnan(want)), what
+    same = (got == want) | torch.isnan(want)
+    off = torch.where(same, torch.zeros_like(got), (got - want).abs() - bound)
+    worst = off.max().item() if off.numel() else 0.0
+    assert worst <= 0, f"{what}: {worst:.3e} over the bound, at {off.argmax().item()} of {tuple(off.shape)}"
+
+
+def _within(t, head_room, fill=0x5A, token_room=0):
+    """t [tokens, heads, dim] as a slice of a larger tensor, whose other bytes are `fill`; and a check that they still are.
+    head_room more heads a token, token_room more elements between tokens."""
+    tokens, heads, dim = t.shape
+    pitch = (heads + head_room) * dim + token_room
+    flat = torch.full(((tokens + 1) * pitch * t.element_size(),), fill, dtype=torch.uint8, device="cuda")
+    view = flat.view(t.dtype).as_strided((tokens, heads, dim), (pitch, dim, 1))
+    view.copy_(t)
+
+    def untouched():
+        left = flat.clone()
+        left.view(t.dtype).as_strided((tokens, heads, dim), (pitch, dim, 1)).view(torch.uint8).fill_(fill)
+        return bool((left == fill).all())
+    return view, untouched
+
+
+# ------------------------------------------------------------------ heads
+
+def _turn64(x, positions, frequencies, interleaved, way):
+    """x [tokens, heads, dim] rotated, one pair at a time."""
+    x, y = x.double(), x.double().clone()
+    half = len(frequencies)
+    for j, f in enumerate(frequencies.tolist()):
+        a, b = (2 * j, 2 * j + 1) if interleaved else (j, j + half)
+        angle = positions.double() * f
+        c, s = angle.cos()[:, None], way * angle.sin()[:, None]
+        y[..., a] = x[..., a] * c - x[..., b] * s
+        y[..., b] = x[..., b] * c + x[..., a] * s
+    return y
+
+
+def _pairs_abs(x, half, interleaved):
+    """|a| + |b| of each element's pair (the element's own magnitude where it is not rotated)."""
+    y = x.abs().clone()
+    if interleaved:
+        s = y[..., 0:2 * half:2] + y[..., 1:2 * half:2]
+        y[..., 0:2 * half:2], y[..., 1:2 * half:2] = s, s
+    else:
+        s = y[..., :half] + y[..., half:2 * half]
+        y[..., :half], y[..., half:2 * half] = s, s
+    return y
+
+
+# roundings of a head's value on its way: the mean of squares (at most 16 elements a lane, 6 additions across lanes; half
+# of it counts), root and quotient, three products, and the turn's, whose cosine and sine are off by 3 * 2^-24 at most
+ROUNDED = 16 + 10
+
+
+def _heads64(x, w, eps, positions, frequencies, interleaved):
+    x64 = x.double()
+    r = (x64.square().mean(-1, keepdim=True) + eps) ** -0.5
+    y = x64 * r * (1.0 if w is None else w.double())
+    return _turn64(y, positions, frequencies, interleaved, 1), ROUNDED * F32 * _pairs_abs(y, len(frequencies), interleaved)
+
+
+def _heads_grad64(dy, x, w, eps, positions, frequencies, interleaved):
+    """(dx, its bound before rounding, dw, its bound)"""
+    x64 = x.double()
+    g = _turn64(dy, positions, frequencies, interleaved, -1)
+    size = _pairs_abs(dy.double(), len(frequencies), interleaved)
+    r = (x64.square().mean(-1, keepdim=True) + eps) ** -0.5
+    xhat, w64 = x64 * r, (torch.ones_like(x64) if w is None else w.double().expand_as(x64))
+    gw, gw_size = g * w64, size * w64.abs()
+    mean, mean_size = (gw * xhat).mean(-1, keepdim=True), (gw_size * xhat.abs()).mean(-1, keepdim=True)
+    dx = r * (gw - xhat * mean)
+    c = 2 * ROUNDED * F32
+    n = x.shape[0] * x.shape[1]
+    dw_size = (size * xhat.abs()).sum((0, 1))
+    return dx, c * r * (gw_size + xhat.abs() * mean_size), (g * xhat).sum((0, 1)), (c + (n + 400) * F32) * dw_size
+
+
+def _rounded(want, bound, dtype):
+    return bound + U[dtype] * (want.abs() + bound) + TINY[dtype]
+
+
+# dim, rotary: every number of pairs that a thread takes, rotated whole, in part and not at all
+HEADS = [(2, 2), (6, 2), (8, 8), (24, 12), (64, 64), (80, 40), (126, 126), (128, 128), (128, 64), (96, 0), (112, 80)]
+
+
+@gpu
+@pytest.mark.parametrize("dim,rotary", HEADS)
+@pytest.mark.parametrize("dtype", list(U), ids=str)
+@pytest.mark.parametrize("interleaved", [False, True])
+def test_rotate_heads(interleaved, dtype, dim, rotary, gpu_lib):
+    g = _seed("heads", interleaved, dtype, dim, rotary)
+    for (tokens, heads, kv), wt in zip([(1, 1, 1), (67, 5, 1), (13, 40, 8), (300, 3, 2)], [dtype, torch.float32] * 2):
+        x = [(_randn(g, tokens, n, dim) * torch.exp(_randn(g, tokens, n, 1))).to(dtype) for n in (heads, kv)]
+        dy = [_randn(g, tokens, n, dim).to(dtype) for n in (heads, kv)]
+        w = [(1 + 0.3 * _randn(g, dim)).to(wt) for _ in range(2)]
+        positions = torch.randint(0, 1 << 20, (tokens,), generator=g, dtype=torch.int32)
+        frequencies = 10000.0 ** (-torch.arange(rotary // 2, dtype=torch.float64) / max(1, rotary // 2))
+        args = [t.cuda() for t in w] + [1e-6, frequencies.cuda(), positions.cuda(), interleaved]
+        room = tokens % 2  # rows on and off 16-byte boundaries
+        (q, _), (k, _) = (_within(t, 2, 0xFF, room) for t in x)  # NaN around them
+        outs = [_within(torch.empty(t.shape, dtype=dtype), 1, token_room=room) for t in x]
+        got = B.reshard_rotate_heads(q, k, *args, q_out=outs[0][0], k_out=outs[1][0])
+        for i, name in enumerate(("q", "k")):
+            want, bound = _heads64(x[i], w[i], 1e-6, positions, frequencies, interleaved)
+            _near(got[i], want, _rounded(want, bound, dtype), f"{name} {tokens} {heads} {kv}")
+            assert outs[i][1](), name
+        (dq, _), (dk, _) = (_within(t, 1, 0xFF, room) for t in dy)
+        outs = [_within(torch.empty(t.shape, dtype=dtype), 1, token_room=room) for t in x]
+        got = B.reshard_rotate_heads_backward(dq, dk, q, k, *args, dq=outs[0][0], dk=outs[1][0])
+        for i, name in enumerate(("dq", "dk")):
+            want, bound, dw, dw_bound = _heads_grad64(dy[i], x[i], w[i], 1e-6, positions, frequencies, interleaved)
+            _near(got[i], want, _rounded(want, bound, dtype), f"{name} {tokens} {heads} {kv}")
+            _near(got[2 + i], dw, dw_bound, f"{name}'s weight {tokens} {heads} {kv}")
+            assert outs[i][1](), name
+
+
+@gpu
+@pytest.mark.parametrize("page,head_major", [(1, False), (16, True), (24, False)])
+@pytest.mark.parametrize("dtype", list(U), ids=str)
+def test_heads_into_the_cache(dtype, page, head_major, gpu_lib):
+    """Keys and values in their slots, as without a cache; other slots as they were; slots outside the cache left out."""
+    g = _seed("cache", dtype, page)
+    tokens, heads, kv, dim = 37, 6, 2, 80
+    pages = tokens // page + 3
+    shape = (pages, kv, page, dim) if head_major else (pages, page, kv, dim)
+    caches = [_randn(g, *shape).to(dtype).cuda() for _ in range(2)]
+    if head_major:
+        caches = [c.transpose(1, 2) for c in caches]
+    qkv = _randn(g, tokens, heads + 2 * kv, dim).to(dtype).cuda()
+    q, k, v = qkv[:, :heads], qkv[:, heads:heads + kv], qkv[:, heads + kv:]
+    slots = torch.randperm(pages * page, generator=g)[:tokens].int()
+    slots[3], slots[4], slots[36], slots[0] = -1, pages * page, -(1 << 31), (1 << 31) - 1
+    positions = torch.randint(0, 1000, (tokens,), generator=g, dtype=torch.int32).cuda()
+    f = 10000.0 ** (-torch.arange(20, dtype=torch.float64) / 20).cuda()
+    w = (1 + 0.3 * _randn(g, dim)).float().cuda()
+    want_q, want_k = B.reshard_rotate_heads(q, k, None, w, 1e-5, f, positions)
+    want = [c.clone() for c in caches]
+    for t, s in enumerate(slots.tolist()):
+        if 0 <= s < pages * page:
+            want[0][s // page, s % page], want[1][s // page, s % page] = want_k[t], v[t]
+    got_q, none = B.reshard_rotate_heads(q, k, None, w, 1e-5, f, positions, v=v, cache=caches, slots=slots.cuda())
+    assert none is None and torch.equal(got_q, want_q)
+    assert all(torch.equal(c, d) for c, d in zip(caches, want))
+
+
+@gpu
+def test_heads_in_place_without_tokens_and_added_up(gpu_lib):
+    g = _seed("in place")
+    q, k = _randn(g, 9, 4, 64).half().cuda(), _randn(g, 9, 2, 64).half().cuda()
+    dy = [torch.randn_like(t) for t in (q, k)]
+    f, at = torch.ones(16, dtype=torch.float64, device="cuda"), torch.arange(9, dtype=torch.int32, device="cuda")
+    want = B.reshard_rotate_heads(q, k, None, None, 0.0, f, at)
+    grads = B.reshard_rotate_heads_backward(*dy, q, k, None, None, 0.0, f, at)
+    w = torch.ones(64, device="cuda")
+    assert all(torch.equal(a, b) for a, b in zip(grads, B.reshard_rotate_heads_backward(*dy, q, k, w, w, 0.0, f, at)))
+    sums = [t.clone() for t in grads[2:]]
+    d = [t.clone() for t in dy]
+    again = B.reshard_rotate_heads_backward(*d, q, k, None, None, 0.0, f, at, dq_weight=sums[0], dk_weight=sums[1],
+                                            accumulate=True, dq=d[0], dk=d[1])
+    assert all(torch.equal(a, b) for a, b in zip(again[:2], grads[:2]))
+    assert all(torch.equal(a, 2 * b) for a, b in zip(sums, grads[2:]))
+    B.reshard_rotate_heads(q, k, None, None, 0.0, f, at, q_out=q, k_out=k)
+    assert torch.equal(q, want[0]) and torch.equal(k, want[1])
+    none = B.reshard_rotate_heads(q[:0], k[:0], None, None, 0.0, f, at[:0])
+    assert none[0].shape == (0, 4, 64)
+    none = B.reshard_rotate_heads_backward(dy[0][:0], dy[1][:0], q[:0], k[:0], w, w, 0.0, f, at[:0])
+    assert none[1].shape == (0, 2, 64) and not none[2].any() and not none[3].any()
+    plain = B.reshard_rotate_heads(q, k)  # no rotation, no weights
+    r = (q.double().square().mean(-1, keepdim=True) + 1e-6) ** -0.5 * q.double()
+    _near(plain[0], r, _rounded(r, ROUNDED * F32 * r.abs(), torch.float16), "norm alone")
+
+
+@gpu
+def test_heads_backward_against_differences(gpu_lib):
+    """The gradients in float32 against central differences of the plain forward pass in 64 bits."""
+    g = _seed("differences")
+    q, k = _randn(g, 3, 2, 8), _randn(g, 3, 1, 8)
+    dq, dk, w = _randn(g, 3, 2, 8), _randn(g, 3, 1, 8), 1 + 0.3 * _randn(g, 8)
+    q, k, dq, dk, w = (t.float().double() for t in (q, k, dq, dk, w))
+    f, at = torch.tensor([1.0, 0.3, 0.01], dtype=torch.float64), torch.tensor([0, 7, 1 << 20], dtype=torch.int32)
+
+    def loss(q, w):
+        return (_heads64(q, w, 1e-6, at, f, True)[0] * dq).sum()
+    got = B.reshard_rotate_heads_backward(*(t.float().cuda() for t in (dq, dk, q, k, w, w)), 1e-6, f.cuda(), at.cuda(), True)
+    step = 1e-5
+    for which, have in ((0, got[0]), (1, got[2])):
+        point = (q, w)[which]
+        want = torch.empty_like(point)
+        for i in range(point.numel()):
+            ends = []
+            for s in (step, -step):
+                moved = point.clone()
+                moved.view(-1)[i] += s
+                ends.append(loss(*((moved, w) if which == 0 else (q, moved))))
+            want.view(-1)[i] = (ends[0] - ends[1]) / (2 * step)
+        # third derivatives times step^2, and 2^-53 of the loss over the step, are far below float32's roundings
+        _near(have, want, 1e-5 * (1 + want.abs()), which)
+
+
+# ------------------------------------------------------------------ attention of packed sequences
+
+def _attention64(q, k, v, scale, causal):
+    """One sequence: (out, lse, P, scores' bound, scores), heads first."""
+    lq, lk, group = q.shape[0], k.shape[0], q.shape[1] // k.shape[1]
+    q64 = q.double().transpose(0, 1)
+    k64, v64 = (t.double().transpose(0, 1).repeat_interleave(group, 0) for t in (k, v))
+    x = scale * (q64 @ k64.transpose(1, 2))
+    bound = scale * q.shape[2] * 2 * F32 * (q64.abs() @ k64.abs().transpose(1, 2))
+    if causal:
+        seen = torch.ones(lq, lk, dtype=torch.bool, device=q.device).tril(lk - lq)
+        x = x.masked_fill(~seen, -math.inf)
+    lse = torch.logsumexp(x, -1) if lk else torch.full((q.shape[1], lq), -math.inf, dtype=torch.float64, device=q.device)
+    p = torch.exp(x - lse.masked_fill(lse == -math.inf, 0.0)[..., None])
+    return p @ v64, lse, p, bound, x
+
+
+def _weights_off(x, bound, lse):
+    """How far a weight may be off, relative: its score's bound and the roundings of the exponent (at most 2^-23 of the
+    largest exponent met, in which the maximum and scores take part) and of the exponential (2^-22)."""
+    finite = x.masked_fill(torch.isinf(x), 0.0)
+    size = finite.abs().amax(-1) if x.shape[-1] else torch.zeros_like(lse)
+    return (bound.amax(-1) if x.shape[-1] else 0) + 4 * F32 * (2 * size + lse.masked_fill(torch.isinf(lse), 0).abs() + 2)
+
+
+def _case(g, dtype, lengths, heads, kv, dim, before=0, behind=0, room=0):
+    """Packed q, k, v on the GPU as slices of wider rows, and their offsets; rows before the first sequence and behind the last."""
+    at = [[before], [before]]
+    for pair in lengths:
+        for a, n in zip(at, pair):
+            a.append(a[-1] + n)
+    wide = torch.where(torch.rand(heads, dim, generator=g) < 1 / 16, 4.0, 1.0).double()
+    q = (_randn(g, at[0][-1] + behind, heads, dim) * wide).to(dtype)
+    k, v = (_randn(g, at[1][-1] + behind, kv, dim).to(dtype) for _ in range(2))
+    return [_within(t, 1, 0xFF, room)[0] for t in (q, k, v)], at
+
+
+def _check_attention(q, k, v, at, scale, causal, out, lse, what):
+    dtype = q.dtype
+    for q0, q1, k0, k1 in zip(at[0], at[0][1:], at[1], at[1][1:]):
+        want, want_lse, p, bound, x = _attention64(q[q0:q1], k[k0:k1], v[k0:k1], scale, causal)
+        if q1 == q0:
+            continue
+        group, n = q.shape[1] // k.shape[1], k1 - k0
+        size = v[k0:k1].double().abs().transpose(0, 1).repeat_interleave(group, 0)
+        off = _weights_off(x, bound, want_lse)
+        # a weight is rounded to the type, or below its range to a multiple of TINY; the sums of weights and of weighted values
+        within = (p @ size) * (U[dtype] + 3 * off[..., None] + 3 * n * F32) + TINY[dtype] * size.sum(1, keepdim=True)
+        _near(out[q0:q1].transpose(0, 1), want, _rounded(want, within, dtype), f"{what}: out of {q1 - q0} over {n}")
+        _near(lse[:, q0:q1], want_lse, off + 2 * n * F32 + 8 * F32 * want_lse.abs().nan_to_num(posinf=0),
+              f"{what}: lse of {q1 - q0} over {n}")
+
+
+def _check_grads(dout, q, k, v, out, lse, at, scale, causal, grads, what):
+    dtype, group = q.dtype, q.shape[1] // k.shape[1]
+    for q0, q1, k0, k1 in zip(at[0], at[0][1:], at[1], at[1][1:]):
+        lq, lk = q1 - q0, k1 - k0
+        _, own, _, bound, x = _attention64(q[q0:q1], k[k0:k1], v[k0:k1], scale, causal)
+        q64, do64, o64 = (t[q0:q1].double().transpose(0, 1) for t in (q, dout, out))
+        k64, v64 = (t[k0:k1].double().transpose(0, 1).repeat_interleave(group, 0) for t in (k, v))
+        stat = lse[:, q0:q1].double()
+        p = torch.exp(x - stat.masked_fill(stat == -math.inf, math.inf)[..., None])
+        dp, dp_size = do64 @ v64.transpose(1, 2), do64.abs() @ v64.abs().transpose(1, 2)
+        delta, delta_size = (do64 * o64).sum(-1, keepdim=True), (do64 * o64).abs().sum(-1, keepdim=True)
+        ds = p * (dp - delta)
+        off = _weights_off(x, bound, own)[..., None]
+        u, dim = U[dtype], q.shape[2]
+        # the weights' rounding in float16 is to 2^-25 / 2^14 at least; dS's to 2^-25 of 2^-13 of its column's largest, in
+        # either pass; in bfloat16 both are far below
+        p_off = p * (u + off) + 2.0 ** -39
+        largest = torch.maximum(ds.abs().amax(-1, keepdim=True) if lk else ds.sum(-1, keepdim=True),
+                                ds.abs().amax(-2, keepdim=True) if lq else ds.sum(-2, keepdim=True))
+        ds_off = p * (2 * dim * F32 * (dp_size + delta_size)) + ds.abs() * (u + off + 4 * F32) + 2.0 ** -38 * largest + 2.0 ** -84
+
+        def keys(t):  # over the heads of a group
+            return t.unflatten(0, (-1, group)).sum(1).transpose(0, 1)
+
+        def queries(t):
+            return t.transpose(0, 1)
+        tr = lambda t: t.transpose(1, 2)  # noqa: E731
+        n = lq * group
+        for name, got, want, within in (
+                ("dq", grads[0][q0:q1], queries(scale * ds @ k64),
+                 queries(scale * ((ds_off + 2 * lk * F32 * ds.abs()) @ k64.abs()))),
+                ("dk", grads[1][k0:k1], keys(scale * tr(ds) @ q64), keys(scale * (tr(ds_off + 2 * n * F32 * ds.abs()) @ q64.abs()))),
+                ("dv", grads[2][k0:k1], keys(tr(p) @ do64), keys(tr(p_off + 2 * n * F32 * p) @ do64.abs()))):
+            _near(got, want, _rounded(want, within, dtype), f"{what}: {name} of {lq} over {lk}")
+
+
+# (queries, keys) of each sequence: none, one, tiles' ends, prefixes, and queries that see no key
+LENGTHS = [[(1, 1)], [(0, 0), (3, 3), (0, 5), (1, 130)], [(61, 61), (1, 1), (130, 130), (64, 64)], [(33, 97), (128, 128), (5, 700)],
+           [(200, 70), (4, 0), (129, 65)], [(257, 257), (31, 32), (300, 450)]]
+SHAPES = [(1, 1, 64), (5, 1, 128), (4, 2, 40), (8, 8, 128), (10, 2, 80), (3, 3, 8), (16, 8, 96), (6, 2, 32)]
+
+
+@gpu
+@pytest.mark.parametrize("lengths", LENGTHS, ids=lambda x: "_".join(f"{a}.{b}" for a, b in x))
+@pytest.mark.parametrize("heads,kv,dim", SHAPES)
+@pytest.mark.parametrize("dtype", HALVES, ids=str)
+def test_attention_and_its_gradients(dtype, heads, kv, dim, lengths, gpu_lib):
+    g = _seed("attention", dtype, heads, kv, dim, lengths)
+    for causal, room in ((True, 0), (False, 3)):
+        before, behind = (0, 0) if causal else (2, 3)
+        (q, k, v), at = _case(g, dtype, lengths, heads, kv, dim, before, behind, room)
+        scale = dim ** -0.5 if causal else 0.2
+        offsets = [_int32(a) for a in at]
+        what = f"causal {causal}"
+        out, untouched = _within(torch.empty(q.shape, dtype=dtype), 1, token_room=room)
+        out.view(torch.int16).fill_(0x5A5A)
+        lse = torch.full((heads, q.shape[0]), 77.0, device="cuda")
+        B.reshard_attention(q, k, v, *offsets, scale, causal, out=out, lse=lse)
+        assert untouched()
+        _check_attention(q, k, v, at, scale, causal, out, lse, what)
+        nobody = [r for r in range(q.shape[0]) if not at[0][0] <= r < at[0][-1]]
+        assert (out[nobody].view(torch.int16) == 0x5A5A).all() and (lse[:, nobody] == 77).all()
+        dout = (0.02 * _randn(g, *q.shape) * torch.exp(_randn(g, q.shape[0], 1, 1))).to(dtype)
+        dout = _within(dout, 1, 0xFF, room)[0]
+        grads = [_within(torch.empty(t.shape, dtype=dtype), 1, token_room=room) for t in (q, k, v)]
+        for t, _ in grads:
+            t.view(torch.int16).fill_(0x5A5A)
+        B.reshard_attention_backward(dout, q, k, v, out, lse, *offsets, scale, causal, *(t for t, _ in grads))
+        assert all(f() for _, f in grads)
+        _check_grads(dout, q, k, v, out, lse, at, scale, causal, [t for t, _ in grads], what)
+        for t, a in zip(grads, (at[0], at[1], at[1])):
+            nobody = [r for r in range(len(t[0])) if not a[0] <= r < a[-1]]
+            assert (t[0][nobody].view(torch.int16) == 0x5A5A).all()
+
+
+@gpu
+@pytest.mark.parametrize("dtype", HALVES, ids=str)
+def test_attention_of_many_sequences(dtype, gpu_lib):
+    """More sequences than a wave has lanes, and more than its square."""
+    for n, longest in ((150, 40), (4200, 3)):
+        g = _seed("many", dtype, n)
+        lengths = [(a, a + b) for a, b in torch.randint(0, longest, (n, 2), generator=g).tolist()]
+        (q, k, v), at = _case(g, dtype, lengths, 2, 1, 32)
+        offsets = [_int32(a) for a in at]
+        out, lse = B.reshard_attention(q, k, v, *offsets)
+        dout = torch.randn_like(out)
+        grads = B.reshard_attention_backward(dout, q, k, v, out, lse, *offsets)
+        if n < 1000:
+            _check_attention(q, k, v, at, 32 ** -0.5, True, out, lse, n)
+            _check_grads(dout, q, k, v, out, lse, at, 32 ** -0.5, True, grads, n)
+            continue
+        for i in range(0, n, 97):  # each of a few by itself, bit for bit
+            rows, cols = slice(at[0][i], at[0][i + 1]), slice(at[1][i], at[1][i + 1])
+            alone = [_int32([0, at[j][i + 1] - at[j][i]]) for j in range(2)]
+            o, s = B.reshard_attention(q[rows], k[cols], v[cols], *alone)
+            assert torch.equal(o, out[rows]) and torch.equal(s, lse[:, rows])
+            for a, b, r in zip(B.reshard_attention_backward(dout[rows], q[rows], k[cols], v[cols], o, s.contiguous(), *alone),
+                               grads, (rows, cols, cols)):
+                assert torch.equal(a, b[r])
+
+
+@gpu
+@pytest.mark.parametrize("dtype", HALVES, ids=str)
+def test_attention_of_extreme_scores(dtype, gpu_lib):
+    """Scores that rise by thousands along the keys, fall, or are all far below zero; and one key far above the rest."""
+    g = _seed("extreme", dtype)
+    n, dim = 300, 64
+    for kind in range(4):
+        q, k, v = (_randn(g, n, 1, dim) for _ in range(3))
+        q[..., 0], k[..., 0] = 40.0, torch.linspace(-60, 60, n)[:, None] * (-1) ** kind
+        if kind == 2:
+            k[..., 0] = -60.0
+        if kind == 3:
+            k[..., 0] = 0.0
+            k[137, 0, 0] = 100.0
+        q, k, v = (t.to(dtype).cuda() for t in (q, k, v))
+        at = [[0, n]] * 2
+        out, lse = B.reshard_attention(q, k, v, _int32([0, n]), _int32([0, n]), 1.0)
+        _check_attention(q, k, v, at, 1.0, True, out, lse, kind)
+        dout = _randn(g, n, 1, dim).to(dtype).cuda()
+        grads = B.reshard_attention_backward(dout, q, k, v, out, lse, _int32([0, n]), _int32([0, n]), 1.0)
+        _check_grads(dout, q, k, v, out, lse, at, 1.0, True, grads, kind)
+
+
+@gpu
+@pytest.mark.parametrize("size", [2.0 ** -20, 1.0, 2.0 ** 10, 2.0 ** 12])
+def test_gradients_in_float16_of_any_size(size, gpu_lib):
+    """Gradients at the ends of the type, over more keys than a weight has digits for, and of another size from row to row."""
+    g = _seed("size", size)
+    (q, k, v), at = _case(g, torch.float16, [(700, 700)], 2, 1, 64)
+    q.mul_(0.1)
+    offsets = [_int32(a) for a in at]
+    out, lse = B.reshard_attention(q, k, v, *offsets)
+    dout = (size * _randn(g, 700, 2, 64) * torch.exp2(torch.linspace(-3, 3, 700))[:, None, None]).half().cuda()
+    # of 2^12 some rows' gradients are infinite: theirs alone are their queries' gradients
+    finite = dout.isfinite().all(-1, keepdim=True)
+    assert bool(finite.all()) == (size < 2.0 ** 12)
+    held = torch.where(finite, dout, torch.zeros_like(dout))
+    grads = B.reshard_attention_backward(held, q, k, v, out, lse, *offsets)
+    _check_grads(held, q, k, v, out, lse, at, 0.125, True, grads, size)
+    dq = B.reshard_attention_backward(dout, q, k, v, out, lse, *offsets)[0]
+    rows = finite.squeeze(-1)
+    assert torch.equal(dq[rows], grads[0][rows])
+
+
+@gpu
+@pytest.mark.parametrize("dtype", HALVES, ids=str)
+def test_attention_of_infinities_and_nan(dtype, gpu_lib):
+    """NaN in another sequence, behind the keys, and in keys that are not seen, do not count; a row's own do."""
+    g = _seed("nan", dtype)
+    (q, k, v), at = _case(g, dtype, [(40, 40), (70, 70), (20, 20)], 2, 1, 64, behind=9)
+    offsets = [_int32(a) for a in at]
+    want, want_lse = B.reshard_attention(q, k, v, *offsets)
+    k[:40], v[:40], q[:40] = math.nan, math.inf, math.nan
+    k[130:], v[130:] = math.inf, math.nan
+    k[109] = math.nan  # the second sequence's last: only its last query sees it
+    got, lse = B.reshard_attention(q, k, v, *offsets)
+    assert got[:40].isnan().all()
+    assert torch.equal(got[40:109], want[40:109]) and torch.equal(lse[:, 40:109], want_lse[:, 40:109])
+    assert got[109].isnan().all() and torch.equal(got[110:130], want[110:130])
+    k[130:], v[130:] = 0, 0
+    q[60] = math.nan
+    got, _ = B.reshard_attention(q, k, v, *offsets)
+    assert got[60].isnan().all() and torch.equal(got[40:60], want[40:60]) and torch.equal(got[61:109], want[61:109])
+
+
+@gpu
+def test_attention_backward_against_differences(gpu_lib):
+    """dout . out's central differences in 64 bits, at inputs that float16 holds."""
+    g = _seed("attention differences")
+    (q, k, v), at = _case(g, torch.float16, [(3, 5), (2, 2)], 2, 1, 8)
+    offsets = [_int32(a) for a in at]
+    dout = _randn(g, 5, 2, 8).half().cuda()
+    out, lse = B.reshard_attention(q, k, v, *offsets, 0.5)
+    grads = B.reshard_attention_backward(dout, q, k, v, out, lse, *offsets, 0.5)
+    base = [t.double().contiguous() for t in (q, k, v)]
+
+    def loss(t):
+        return sum((_attention64(t[0][a:b], t[1][c:d], t[2][c:d], 0.5, True)[0].transpose(0, 1) * dout[a:b].double()).sum()
+                   for a, b, c, d in zip(at[0], at[0][1:], at[1], at[1][1:])).item()
+    for which in range(3):
+        want = torch.empty_like(base[which])
+        for i in range(want.numel()):
+            ends = []
+            for s in (1e-5, -1e-5):
+                moved = [t.clone() for t in base]
+                moved[which].view(-1)[i] += s
+                ends.append(loss(moved))
+            want.view(-1)[i] = (ends[0] - ends[1]) / 2e-5
+        # weights, dS and the result rounded to float16, out to float16 in delta: terms of a few units, 10 of them
+        _near(grads[which], want, 20 * 2.0 ** -11 * (2 + want.abs()), "qkv"[which])
+
+
+# ------------------------------------------------------------------ attention of one token
+
+def _paged_case(g, dtype, lengths, kv, dim, page, width, head_major=False):
+    need = [-(-max(0, n) // page) for n in lengths]
+    pool = sum(need) + 3
+    order = torch.randperm(pool, generator=g).int()
+    table = torch.full((len(lengths), width), -7, dtype=torch.int32)
+    shape = (pool, kv, page, dim) if head_major else (pool, page, kv, dim)
+    caches = [torch.full(shape, math.nan, dtype=dtype) for _ in range(2)]
+    if head_major:
+        caches = [c.transpose(1, 2) for c in caches]
+    at = 0
+    for i, n in enumerate(lengths):
+        table[i, :need[i]] = order[at:at + need[i]]
+        at += need[i]
+        for t in range(0, max(n, 0), page):
+            rows = min(page, n - t)
+            for c in caches:
+                c[table[i, t // page], :rows] = _randn(g, rows, kv, dim).to(dtype)
+    strides = [c.stride() for c in caches]
+    caches = [torch.empty_strided(c.shape, s, dtype=dtype, device="cuda").copy_(c) for c, s in zip(caches, strides)]
+    return caches, table.cuda()
+
+
+def _check_paged(q, caches, table, lengths, scale, out, what):
+    page = caches[0].shape[1]
+    for i, n in enumerate(lengths):
+        if n <= 0:
+            assert not out[i].any(), what
+            continue
+        t = torch.arange(n, device="cuda")
+        rows = table[i].long()[t // page], t % page
+        _check_attention(q[i:i + 1], caches[0][rows], caches[1][rows], [[0, 1], [0, n]], scale, False, out[i:i + 1],
+                         _attention64(q[i:i + 1], caches[0][rows], caches[1][rows], scale, False)[1].float(), f"{what} {i}")
+
+
+@gpu
+@pytest.mark.parametrize("page,head_major", [(1, False), (16, False), (48, True), (256, False)])
+@pytest.mark.parametrize("heads,kv,dim", [(1, 1, 64), (5, 1, 128), (8, 8, 40), (32, 8, 128), (40, 2, 96), (6, 3, 8)])
+@pytest.mark.parametrize("dtype", HALVES, ids=str)
+def test_attention_paged(dtype, heads, kv, dim, page, head_major, gpu_lib):
+    g = _seed("paged", dtype, heads, kv, dim, page)
+    for lengths in ([1], [2047], [0, 1, 31, 32, 33, -5, 127, 128, 129, 700, 0], [300] * 7):
+        width = max(1, -(-max(lengths) // page)) + 2
+        caches, table = _paged_case(g, dtype, lengths, kv, dim, page, width, head_major)  # NaN behind every length
+        q = _within(_randn(g, len(lengths), heads, dim).to(dtype), 2, 0xFF)[0]
+        out, untouched = _within(torch.empty(q.shape, dtype=dtype), 1)
+        B.reshard_attention_paged(q, *caches, table, _int32(lengths), out=out)
+        assert untouched()
+        _check_paged(q, caches, table, lengths, dim ** -0.5, out, f"{len(lengths)} of {max(lengths)}")
+
+
+@gpu
+def test_attention_paged_over_many_and_long(gpu_lib):
+    """More sequences than threads, and sequences that many workgroups share, at page lengths that no tile divides."""
+    g = _seed("long")
+    for lengths, kv, heads, page in (([int(x) for x in torch.randint(0, 90, (700,), generator=g)], 2, 2, 24), ([20011, 3, 9000], 1, 3, 40)):
+        caches, table = _paged_case(g, torch.bfloat16, lengths, kv, 64, page, -(-max(lengths) // page))
+        q = _randn(g, len(lengths), heads, 64).bfloat16().cuda()
+        out = B.reshard_attention_paged(q, *caches, table, _int32(lengths))
+        _check_paged(q, caches, table, lengths, 0.125, out, len(lengths))
+        assert torch.equal(out, B.reshard_attention_paged(q, *caches, table, _int32(lengths)))
+
+
+@gpu
+def test_attention_paged_of_pages_outside_the_cache(gpu_lib):
+    """Their tokens do not count; a length past the table is the table's."""
+    g = _seed("outside")
+    caches, table = _paged_case(g, torch.float16, [64, 64, 64], 2, 64, 16, 4)
+    q = _randn(g, 3, 4, 64).half().cuda()
+    whole = B.reshard_attention_paged(q, *caches, table, _int32([64] * 3))
+    assert torch.equal(B.reshard_attention_paged(q, *caches, table, _int32([64, 65, (1 << 31) - 1])), whole)
+    bad = table.clone()
+    bad[0, 3], bad[1, 2:], bad[2] = -1, len(caches[0]), (1 << 31) - 1
+    got = B.reshard_attention_paged(q, *caches, bad, _int32([64] * 3))
+    few = B.reshard_attention_paged(q, *caches, table, _int32([48, 32, 0]))
+    assert torch.equal(got, few) and not got[2].any()
+
+
+@gpu
+def test_offsets_past_32_bits(gpu_lib):
+    """Pages and tokens so far apart that the last lie past 2^32 bytes and 2^31 elements from the first."""
+    g = _seed("far")
+    far = (1 << 30) + 64
+    store = torch.zeros(3 * far + 4096, dtype=torch.float16, device="cuda")
+    keys = store.as_strided((3, 4, 2, 64), (far, 128, 64, 1))
+    vals = store[2048:].as_strided((3, 4, 2, 64), (far, 128, 64, 1))
+    near = [_randn(g, 3, 4, 2, 64).half().cuda() for _ in range(2)]
+    keys.copy_(near[0])
+    vals.copy_(near[1])
+    q = _randn(g, 2, 4, 64).half().cuda()
+    table, lengths = _int32([[2, 0, 1], [1, 2, 0]]), _int32([12, 7])
+    assert torch.equal(B.reshard_attention_paged(q, keys, vals, table, lengths), B.reshard_attention_paged(q, *near, table, lengths))
+    rows = store[8192 - 4096:].as_strided((3, 2, 64), (far, 64, 1))
+    x = _randn(g, 3, 2, 64).half().cuda()
+    rows.copy_(x)
+    at = _int32([0, 3])
+    want = B.reshard_attention(x, x, x, at, at)
+    got = B.reshard_attention(rows, rows, rows, at, at)
+    assert torch.equal(got[0], want[0]) and torch.equal(got[1], want[1])
+    for a, b in zip(B.reshard_attention_backward(x, rows, rows, rows, *want, at, at), B.reshard_attention_backward(x, x, x, x, *want, at, at)):
+        assert torch.equal(a, b)
+    for a, b in zip(B.reshard_rotate_heads(rows, rows), B.reshard_rotate_heads(x, x)):
+        assert torch.equal(a, b)
+
+
+# ------------------------------------------------------------------ together
+
+def _layer(g, dtype, tokens, heads, kv, dim):
+    qkv = _randn(g, tokens, heads + 2 * kv, dim).to(dtype).cuda()
+    w = [(1 + 0.2 * _randn(g, dim)).float().cuda() for _ in range(2)]
+    f = 10000.0 ** (-torch.arange(dim // 2, dtype=torch.float64) / (dim // 2)).cuda()
+    return qkv, qkv[:, :heads], qkv[:, heads:heads + kv], qkv[:, heads + kv:], w, f
+
+
+@gpu
+@pytest.mark.parametrize("dtype", HALVES, ids=str)
+def test_a_prompt_token_by_token(dtype, gpu_lib):
+    """Two prompts at once, and the same made token by token over a paged cache: the outputs agree to their roundings."""
+    g = _seed("together", dtype)
+    heads, kv, dim, page, lengths = 8, 2, 64, 16, [37, 20]
+    total = sum(lengths)
+    qkv, q, k, v, w, f = _layer(g, dtype, total, heads, kv, dim)
+    positions = torch.cat([torch.arange(n, dtype=torch.int32) for n in lengths]).cuda()
+    at = [0, 37, 57]
+    rq, rk = B.reshard_rotate_heads(q, k, *w, 1e-6, f, positions)
+    out, lse = B.reshard_attention(rq, rk, v, _int32(at), _int32(at))
+    caches = [torch.full((9, page, kv, dim), math.nan, dtype=dtype, device="cuda") for _ in range(2)]
+    table = torch.randperm(9, generator=g).int()[:6].view(2, 3)
+    for t in range(max(lengths)):
+        live = [i for i, n in enumerate(lengths) if t < n]
+        rows = [at[i] + t for i in live]
+        slots = [int(table[i, t // page]) * page + t % page for i in live]
+        step_q, _ = B.reshard_rotate_heads(q[rows], k[rows], *w, 1e-6, f, positions[rows], v=v[rows], cache=caches,
+                                           slots=_int32(slots))
+        assert torch.equal(step_q, rq[rows])
+        one = B.reshard_attention_paged(step_q, *caches, table[live].contiguous().cuda(), _int32([t + 1] * len(live)))
+        for i, r in enumerate(rows):
+            keys, vals = rk[at[live[i]]:r + 1], v[at[live[i]]:r + 1]
+            for o in (one[i:i + 1], out[r:r + 1]):
+                _check_attention(rq[r:r + 1], keys, vals, [[0, 1], [0, t + 1]], 0.125, False, o, lse[:, r:r + 1], t)
+
+
+@gpu
+def test_training_pass_in_a_graph_and_on_another_stream(gpu_lib):
+    """A layer's attention forward and backward and a decode step: eager, on a side stream, captured and replayed with new
+    inputs, two graphs of one pool among them, every replay equal to the eager result."""
+    g = _seed("graph")
+    heads, kv, dim = 6, 2, 128
+    qkv, q, k, v, w, f = _layer(g, torch.bfloat16, 333, heads, kv, dim)
+    positions = torch.arange(333, dtype=torch.int32, device="cuda")
+    at = _int32([0, 100, 333])
+    cache = [torch.zeros(30, 16, kv, dim, dtype=torch.bfloat16, device="cuda") for _ in range(2)]
+    table, lengths = torch.randperm(30, generator=g).int().view(2, 15).cuda(), _int32([200, 77])
+    slots = torch.randperm(480, generator=g).int()[:333].cuda()
+
+    def step(stream=None):
+        kw = {"stream": stream}
+        rq, rk = B.reshard_rotate_heads(q, k, *w, 1e-6, f, positions, **kw)
+        out, lse = B.reshard_attention(rq, rk, v, at, at, **kw)
+        dq, dk, dv = B.reshard_attention_backward(out, rq, rk, v, out, lse, at, at, **kw)
+        back = B.reshard_rotate_heads_backward(dq, dk, q, k, *w, 1e-6, f, positions, **kw)
+        B.reshard_rotate_heads(q, k, *w, 1e-6, f, positions, v=v, cache=cache, slots=slots, **kw)
+        return [out, lse, dv, *back, B.reshard_attention_paged(rq[:2], *cache, table, lengths, **kw)]
+    want = [t.clone() for t in step()]
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    got = step(side)
+    side.synchronize()
+    assert all(torch.equal(a, b) for a, b in zip(got, want))
+    graphs = [torch.cuda.CUDAGraph() for _ in range(2)]
+    outs = []
+    for graph in graphs:
+        with torch.cuda.graph(graph, pool=graphs[0].pool() if outs else None):
+            outs.append(step())
+    for turn in range(4):
+        qkv.copy_(_randn(g, *qkv.shape).bfloat16())
+        want = [t.clone() for t in step()]
+        torch.cuda.synchronize()
+        for graph, got in zip(graphs, outs):
+            graph.replay()
+            torch.cuda.synchronize()
+            assert all(torch.equal(a, b) for a, b in zip(got, want)), f"replay {turn}"
+
+
+# ------------------------------------------------------------------ refusals (CPU)
+
+P = 1 << 20  # an aligned address that is never used
+
+
+def _refused(status, want, text):
+    message = B.reshard_last_error()
+    assert status == want and text in message, (status, message)
+
+
+def _at(data=P, token=1 << 10, head=64):
+    return B.reshard_heads_t(data, token, head)
+
+
+EI, EU = B.RESHARD_EINVAL, B.RESHARD_EUNSUPPORTED
+
+
+def test_rotate_heads_refusals():
+    lib = B.load()
+
+    def fwd(tokens=4, heads=8, kv=2, dim=64, rot=64, il=0, dt=3, q=_at(), k=_at(), w=P, wt=4, eps=1e-6, f=P, pos=P, qo=_at(),
+            ko=_at(), v=None, cache=None, slots=None):
+        return lib.reshard_rotate_heads(tokens, heads, kv, dim, rot, il, dt, q, k, w, w, wt, eps, f, pos, qo, ko, v, cache, slots, None)
+
+    def bwd(tokens=4, d=_at(), dq=_at(), dw=P, acc=0, work=P, nbytes=1 << 30, dt=3):
+        return lib.reshard_rotate_heads_backward(tokens, 8, 2, 64, 64, 0, dt, d, d, _at(), _at(), P, P, 4, 1e-6, P, P, dq, dq, dw,
+                                                 dw, acc, work, nbytes, None)
+    cache = B.reshard_cache_t(P, P, 10, 16, 16 * 128, 128, 64)
+    for call, status, text in (
+            (dict(tokens=-1), EI, "tokens"), (dict(heads=0), EI, "heads"), (dict(kv=0), EI, "heads"), (dict(heads=1 << 17), EU, "2^16"),
+            (dict(dim=63, rot=0), EI, "dim"), (dict(dim=130, rot=0), EU, "dim"), (dict(rot=66), EI, "rotary"), (dict(rot=3), EI, "rotary"),
+            (dict(il=2), EI, "interleaved"), (dict(dt=6), EI, "dtype"), (dict(wt=0), EI, "weight_dtype"), (dict(eps=-1.0), EI, "eps"),
+            (dict(eps=math.nan), EI, "eps"), (dict(f=None), EI, "frequencies"), (dict(pos=None), EI, "positions"), (dict(q=None), EI, "q is"),
+            (dict(k=_at(None)), EI, "k is"), (dict(qo=_at(head=63)), EI, "overlap"), (dict(qo=_at(token=511)), EI, "overlap"),
+            (dict(ko=_at(P + 1)), EI, "aligned"), (dict(q=_at(token=-1)), EU, "pitch"), (dict(q=_at(token=1 << 60)), EU, "pitch"),
+            (dict(v=_at()), EI, "go together"), (dict(cache=cache), EI, "go together"), (dict(v=_at(), cache=cache), EI, "slots"),
+            (dict(v=_at(), cache=B.reshard_cache_t(P, P, 10, 0, 1, 1, 1), slots=P), EI, "page_length"),
+            (dict(v=_at(), cache=B.reshard_cache_t(P, None, 10, 16, 2048, 128, 64), slots=P), EI, "values"),
+            (dict(v=_at(), cache=B.reshard_cache_t(P, P, 10, 16, 2048, 63, 64), slots=P), EI, "less than dim"),
+            (dict(v=_at(), cache=B.reshard_cache_t(P, P, 1 << 30, 16, 2048, 128, 64), slots=P), EU, "slots")):
+        _refused(fwd(**call), status, text)
+    for call, text in ((dict(d=None), "dq_out"), (dict(dq=_at(token=8)), "overlap"), (dict(acc=2), "accumulate"), (dict(work=None), "workspace"),
+                       (dict(nbytes=16), "workspace"), (dict(work=P + 4), "workspace"), (dict(dw=P + 2), "dq_weight"), (dict(dt=1), "dtype")):
+        _refused(bwd(**call), EI, text)
+    assert lib.reshard_rotate_heads_backward_workspace(-1, 1, 1, 64) == -1
+    assert lib.reshard_rotate_heads_backward_workspace(4, 0, 1, 64) == -1
+
+
+def test_attention_refusals():
+    lib = B.load()
+
+    def fwd(nq=4, nk=4, n=1, heads=8, kv=2, dim=64, dt=3, q=_at(), k=_at(), qo=P, scale=1.0, causal=1, out=_at(), lse=P):
+        return lib.reshard_attention(nq, nk, n, heads, kv, dim, dt, q, k, k, qo, P, scale, causal, out, lse, None)
+
+    def bwd(d=_at(), out=_at(), lse=P, dq=_at(), dk=_at(), work=P, nbytes=1 << 30, dt=3):
+        return lib.reshard_attention_backward(4, 4, 1, 8, 2, 64, dt, d, _at(), _at(), _at(), out, lse, P, P, 1.0, 1, dq, dk, dk, work,
+                                              nbytes, None)
+    for call, status, text in (
+            (dict(nq=-1), EI, "negative"), (dict(n=-1), EI, "negative"), (dict(nk=1 << 31), EU, "2^31"), (dict(heads=7), EI, "multiple"),
+            (dict(kv=0), EI, "heads"), (dict(dim=0), EI, "dim"), (dict(dim=36), EU, "multiple of 8"), (dict(dim=136), EU, "multiple of 8"),
+            (dict(dt=4), EI, "dtype"), (dict(scale=0.0), EI, "scale"), (dict(scale=math.nan), EI, "scale"), (dict(scale=math.inf), EI, "scale"),
+            (dict(causal=2), EI, "causal"), (dict(q=None), EI, "q is"), (dict(k=_at(None)), EI, "k is"), (dict(qo=None), EI, "q_offsets"),
+            (dict(out=_at(token=8)), EI, "overlap"), (dict(lse=None), EI, "lse"), (dict(q=_at(P + 1)), EI, "aligned"),
+            (dict(nq=1 << 30, heads=1 << 16, kv=1, q=_at(token=0, head=0), out=_at(token=1 << 22)), EU, "2^30")):
+        _refused(fwd(**call), status, text)
+    for call, text in ((dict(d=None), "dout"), (dict(out=_at(None)), "out"), (dict(lse=None), "lse"), (dict(dq=_at(head=0)), "overlap"),
+                       (dict(dk=None), "dk"), (dict(work=None), "workspace"), (dict(nbytes=255), "workspace"), (dict(work=P + 8), "workspace"),
+                       (dict(dt=4), "dtype")):
+        _refused(bwd(**call), EI, text)
+    assert lib.reshard_attention_backward_workspace(-1, 1) == -1 and lib.reshard_attention_backward_workspace(1, 0) == -1
+
+
+def test_attention_paged_refusals():
+    lib = B.load()
+    good = B.reshard_cache_t(P, P, 10, 16, 16 * 128, 128, 64)
+
+    def call(n=4, heads=8, kv=2, dim=64, dt=3, q=_at(), cache=good, pages=P, width=8, pitch=8, lengths=P, scale=1.0, out=_at(), work=P,
+             nbytes=1 << 30):
+        return lib.reshard_attention_paged(n, heads, kv, dim, dt, q, cache, pages, width, pitch, lengths, scale, out, work, nbytes, None)
+    for args, status, text in (
+            (dict(n=-1), EI, "negative"), (dict(width=-1), EI, "negative"), (dict(heads=9), EI, "multiple"), (dict(dim=36), EU, "multiple of 8"),
+            (dict(dt=4), EI, "dtype"), (dict(scale=-1.0), EI, "scale"), (dict(cache=None), EI, "cache"), (dict(q=None), EI, "q is"),
+            (dict(out=_at(head=8)), EI, "overlap"), (dict(pages=None), EI, "pages"), (dict(pitch=7), EI, "pitch"), (dict(lengths=None), EI, "lengths"),
+            (dict(work=None), EI, "workspace"), (dict(nbytes=64), EI, "workspace"), (dict(work=P + 8), EI, "workspace"),
+            (dict(width=1 << 28, pitch=1 << 28), EU, "2^31"), (dict(cache=B.reshard_cache_t(P + 1, P, 10, 16, 2048, 128, 64)), EI, "aligned")):
+        _refused(call(**args), status, text)
+    for bad in ((-1, 8, 2, 64, 8, 16), (4, 8, 3, 64, 8, 16), (4, 8, 2, 200, 8, 16), (4, 8, 2, 64, 8, 0), (4, 8, 2, 64, 1 << 30, 16)):
+        assert lib.reshard_attention_paged_workspace(*bad) == -1
+
+
+def test_binding_refusals():
+    q, k = torch.zeros(4, 8, 64), torch.zeros(4, 2, 64)
+    f, at, n = torch.ones(16, dtype=torch.float64), torch.zeros(4, dtype=torch.int32), torch.zeros(2, dtype=torch.int32)
+    h, hk = q.half(), k.half()
+    cache, table = torch.zeros(5, 16, 2, 64).half(), torch.zeros(4, 3, dtype=torch.int32)
+    lse = torch.zeros(8, 4)
+    for call, text in (
+            (lambda: B.reshard_rotate_heads(q[0], k), "tokens, heads, dim"), (lambda: B.reshard_rotate_heads(q, k.half()), "k must be"),
+            (lambda: B.reshard_rotate_heads(q, k[:3]), "k must be"), (lambda: B.reshard_rotate_heads(q.transpose(1, 2), k), "dense"),
+            (lambda: B.reshard_rotate_heads(q, k, torch.ones(63)), "q_weight"),
+            (lambda: B.reshard_rotate_heads(q, k, torch.ones(64), torch.ones(64).half()), "k_weight"),
+            (lambda: B.reshard_rotate_heads(q, k, frequencies=f), "positions"),
+            (lambda: B.reshard_rotate_heads(q, k, frequencies=f.float(), positions=at), "frequencies"),
+            (lambda: B.reshard_rotate_heads(q, k, frequencies=f, positions=at.long()), "positions"),
+            (lambda: B.reshard_rotate_heads(q, k, v=k), "go together"),
+            (lambda: B.reshard_rotate_heads(h, hk, v=hk, cache=(cache, cache[:, :8]), slots=at), "cache's values"),
+            (lambda: B.reshard_rotate_heads(h, hk, v=hk, cache=(cache, cache), slots=at, k_out=hk), "not to both"),
+            (lambda: B.reshard_rotate_heads(h, hk, v=hk, cache=(cache[0], cache[0]), slots=at), "cache must be"),
+            (lambda: B.reshard_rotate_heads(h, hk, v=hk, cache=(cache, cache), slots=at[:3]), "slots"),
+            (lambda: B.reshard_rotate_heads_backward(q, k.half(), q, k), "dk_out"),
+            (lambda: B.reshard_rotate_heads_backward(q, k, q, k, accumulate=True), "accumulate"),
+            (lambda: B.reshard_attention(h, hk[..., :32], hk, n, n), "k must be"), (lambda: B.reshard_attention(h, hk, hk[:3], n, n), "v must be"),
+            (lambda: B.reshard_attention(h, hk, hk, n, n[:1]), "k_offsets"), (lambda: B.reshard_attention(h, hk, hk, n[:0], n[:0]), "q_offsets"),
+            (lambda: B.reshard_attention(h, hk, hk, n.long(), n), "q_offsets"),
+            (lambda: B.reshard_attention_paged(h, cache, cache, table[:3], at), "pages must be"),
+            (lambda: B.reshard_attention_paged(h, cache, cache, table.t().contiguous().t(), at), "pages must be"),
+            (lambda: B.reshard_attention_paged(h, cache[0], cache, table, at), "cache must be"),
+            (lambda: B.reshard_attention_paged(h, cache, cache, table, at.long()), "lengths"),
+            (lambda: B.reshard_rotate_heads(q, k), "on the GPU"), (lambda: B.reshard_rotate_heads_backward(q, k, q, k), "on the GPU"),
+            (lambda: B.reshard_attention(h, hk, hk, n, n), "on the GPU"), (lambda: B.reshard_attention_paged(h, cache, cache, table, at), "on the GPU"),
+            (lambda: B.reshard_attention_backward(h, h, hk, hk, h, lse, n, n), "on the GPU")):
+        with pytest.raises(ValueError, match=text):
+            call()
+
+
+@gpu
+def test_outputs_of_a_caller(gpu_lib):
+    q, k = (torch.randn(4, n, 64, device="cuda").half() for n in (8, 2))
+    at = _int32([0, 4])
+    for bad in (q[:3], q.float(), q.cpu()):
+        with pytest.raises(ValueError, match="out must be"):
+            B.reshard_attention(q, k, k, at, at, out=bad)
+    with pytest.raises(ValueError, match="lse"):
+        B.reshard_attention(q, k, k, at, at, lse=torch.empty(4, 8, device="cuda"))
+    with pytest.raises(B.ReshardError, match="dtype"):
+        B.reshard_attention(q.float(), k.float(), k.float(), at, at)
