@@ -39,7 +39,7 @@ __global__ __launch_bounds__(kThreads, QB == 1 ? 2 : 1) void attention_kernel(Pr
     __shared__ uint4 k1[kKeys * TileShape<DP>::words], v1[kKeys * TileShape<DP>::words];
     const Task task = task_of(blockIdx.x, a.blocks, a.heads, a.group);
     Sequence s;
-    if (!find_sequence(a.seq, false, a.blocks - 1 - task.block, SHIFT, &s)) return;
+    if (!ranked_sequence(a.seq, false, a.causal, a.blocks, task.block, SHIFT, &s)) return;
     const int lane = threadIdx.x % kWave, wave = threadIdx.x / kWave, half = lane / 32;
     const int kv_head = task.head / a.group;
     const int row0 = s.block * ROWS + wave * 32 * QB;
@@ -59,6 +59,7 @@ __global__ __launch_bounds__(kThreads, QB == 1 ? 2 : 1) void attention_kernel(Pr
     const int wave_to = a.causal ? min(s.lk, min(s.lq, row0 + 32 * QB) + s.lk - s.lq) : s.lk;
     const int all_see = a.causal ? row0 + 1 + s.lk - s.lq : s.lk;  // keys that each of the wave's queries sees
 
+    const LanePlaces places = LanePlaces::of<DP>(lane);
     f32x16 o[QB][BLOCKS];
     float m[QB], l[QB];
 #pragma unroll
@@ -90,7 +91,7 @@ __global__ __launch_bounds__(kThreads, QB == 1 ? 2 : 1) void attention_kernel(Pr
             for (int i = 0; i < STEPS; ++i)
 #pragma unroll
                 for (int n = 0; n < 2; ++n) {
-                    const Operand8<T> kk = row_operand<T, DP>(kt, n * 32, i, lane);
+                    const Operand8<T> kk = row_operand<T, DP>(kt, n * 32, i, places);
 #pragma unroll
                     for (int b = 0; b < QB; ++b) x[b][n] = mfma(kk, q[b][i], x[b][n]);
                 }
@@ -136,7 +137,7 @@ __global__ __launch_bounds__(kThreads, QB == 1 ? 2 : 1) void attention_kernel(Pr
             for (int t = 0; t < 4; ++t)
 #pragma unroll
                 for (int d = 0; d < BLOCKS; ++d) {
-                    const Operand8<T> vv = column_operand<T, DP>(vt, t * 16, d, lane);
+                    const Operand8<T> vv = column_operand<T, DP>(vt, t * 16, d, places);
 #pragma unroll
                     for (int b = 0; b < QB; ++b) o[b][d] = mfma(vv, p[b][t], o[b][d]);
                 }

@@ -85,23 +85,39 @@ struct TileShape {
     __device__ static int at(int row, int word) { return row * words + (word ^ swizzle(row)); }
 };
 
+// A lane's places in tiles.  Whatever the tile, its first row (a multiple of 16)
+// and the word, only a constant is added to them and another, below, comes by
+// exclusive or: so a few registers hold the addresses of all reads.
+struct LanePlaces {
+    uint32_t row, column;  // bytes
+    template <int DP>
+    __device__ static LanePlaces of(int lane, int row0 = 0) {  // from row0 on, a multiple of 16
+        using Shape = TileShape<DP>;
+        const int i = lane % 16;
+        return LanePlaces{
+            uint32_t(Shape::at(row0 + lane % 32, lane / 32) * 16),
+            uint32_t(Shape::at(row0 + lane / 32 * 4 + i / 4, (lane / 16 % 2) * 2 + i % 4 / 2) * 16 + i % 2 * 8)};
+    }
+};
+
 // Lane l's 8 elements 16 s + 8 (l / 32) of row `row` + l % 32.
 template <typename T, int DP>
-__device__ inline Operand8<T> row_operand(const uint4 *tile, int row, int s, int lane) {
+__device__ inline Operand8<T> row_operand(const uint4 *tile, int row, int s, const LanePlaces &places) {
     Operand8<T> o;
-    o.w = tile[TileShape<DP>::at(row + lane % 32, 2 * s + lane / 32)];
+    o.w = *reinterpret_cast<const uint4 *>(reinterpret_cast<const char *>(tile + row * TileShape<DP>::words) +
+                                           (places.row ^ (s * 32)));
     return o;
 }
 
 // Column `32 * block + l % 32` of the 16 rows from `row` on, in a result's order.
 template <typename T, int DP>
-__device__ inline Operand8<T> column_operand(const uint4 *tile, int row, int block, int lane) {
+__device__ inline Operand8<T> column_operand(const uint4 *tile, int row, int block, const LanePlaces &places) {
     typedef __attribute__((address_space(3))) s16x4 lds_s16x4;
-    const int i = lane % 16, r = row + lane / 32 * 4 + i / 4, word = block * 4 + (lane / 16 % 2) * 2 + i % 4 / 2;
     Operand8<T> o;
 #pragma unroll
     for (int p = 0; p < 2; ++p) {
-        const char *at = reinterpret_cast<const char *>(tile + TileShape<DP>::at(r + 8 * p, word)) + i % 2 * 8;
+        const char *at = reinterpret_cast<const char *>(tile + (row + 8 * p) * TileShape<DP>::words) +
+                         (places.column ^ (block * 64) ^ (p * 32));
         o.half[p] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4 *)at);
     }
     return o;
@@ -235,6 +251,98 @@ __device__ inline bool find_sequence(const Sequences &s, bool by_keys, int64_t b
     out->lk = int(clamped(s.k_offsets[lo + 1], out->k0, s.k_tokens) - out->k0);
     out->block = int(block - start(lo));
     return (int64_t(out->block) << shift) < (by_keys ? out->lk : out->lq);
+}
+
+// Sum over the wave, as of floats (operators.hpp).
+__device__ inline int wave_sum(int x) {
+    auto moved = [&](auto ctrl, auto rows) {
+        return __builtin_amdgcn_update_dpp(0, x, decltype(ctrl)::value, decltype(rows)::value, 0xf, true);
+    };
+    using std::integral_constant;
+    constexpr integral_constant<int, 0xf> all{};
+    x += moved(integral_constant<int, 0x111>{}, all);
+    x += moved(integral_constant<int, 0x112>{}, all);
+    x += moved(integral_constant<int, 0x114>{}, all);
+    x += moved(integral_constant<int, 0x118>{}, all);
+    x += moved(integral_constant<int, 0x142>{}, integral_constant<int, 0xa>{});
+    x += moved(integral_constant<int, 0x143>{}, integral_constant<int, 0xc>{});
+    return __builtin_amdgcn_readlane(x, kWave - 1);
+}
+
+// The batch's block that comes in place `rank` by falling work, so that the
+// longest start first, whatever the order of the sequences.  A block's work is
+// counted in blocks of the other side that it meets; count(w) is how many
+// blocks of a sequence have at least w, and the largest w that more than `rank`
+// blocks of all sequences have is searched for by halves.  Up to 256 sequences,
+// which the wave's lanes hold; of more, blocks are taken in the order of
+// find_sequence.
+constexpr int kRanked = 256;
+
+__device__ inline bool ranked_sequence(const Sequences &s, bool by_keys, bool causal, int64_t blocks, int64_t rank,
+                                       int shift, Sequence *out) {
+    if (s.count > kRanked) return find_sequence(s, by_keys, by_keys ? rank : blocks - 1 - rank, shift, out);
+    const int lane = threadIdx.x % kWave;
+    int own[kRanked / kWave], other[kRanked / kWave];
+    int highest = 0;
+#pragma unroll
+    for (int c = 0; c < kRanked / kWave; ++c) {
+        own[c] = other[c] = 0;
+        const int i = c * kWave + lane;
+        if (i >= s.count) continue;
+        const int64_t q0 = clamped(s.q_offsets[i], 0, s.q_tokens), k0 = clamped(s.k_offsets[i], 0, s.k_tokens);
+        const int lq = int(clamped(s.q_offsets[i + 1], q0, s.q_tokens) - q0);
+        const int lk = int(clamped(s.k_offsets[i + 1], k0, s.k_tokens) - k0);
+        const int bq = int((int64_t(lq) + (1 << shift) - 1) >> shift), bk = int((int64_t(lk) + (1 << shift) - 1) >> shift);
+        own[c] = by_keys ? bk : bq;
+        other[c] = by_keys ? bq : bk;
+        if (own[c] > 0) highest = max(highest, other[c]);
+    }
+    auto count = [&](int c, int w) {
+        if (w <= 0) return own[c];
+        if (w > other[c]) return 0;
+        return causal ? min(max((by_keys ? own[c] : other[c]) - w + 1, 0), own[c]) : own[c];
+    };
+    auto counts = [&](int w) {
+        int n = count(0, w);
+        for (int c = 1; c * kWave < s.count; ++c) n += c == 1 ? count(1, w) : c == 2 ? count(2, w) : count(3, w);
+        return wave_sum(n);
+    };
+    if (rank >= counts(0)) return false;
+#pragma unroll
+    for (int d = 1; d < kWave; d *= 2) highest = max(highest, __shfl_xor(highest, d));
+    int low = 0, high = __builtin_amdgcn_readfirstlane(highest) + 1;  // counts(low) > rank >= counts(high)
+    while (high - low > 1) {
+        const int mid = low + (high - low) / 2;
+        if (counts(mid) > rank) low = mid;
+        else high = mid;
+    }
+    int before = counts(high), found = 0, place = 0;
+    for (int c = 0; c * kWave < s.count; ++c) {
+        const int more = c == 0 ? count(0, high) : c == 1 ? count(1, high) : c == 2 ? count(2, high) : count(3, high);
+        const int mine = (c == 0 ? count(0, low) : c == 1 ? count(1, low) : c == 2 ? count(2, low) : count(3, low)) - more;
+        int upto = mine;
+#pragma unroll
+        for (int d = 1; d < kWave; d *= 2) {
+            const int x = __shfl_up(upto, d);
+            if (lane >= d) upto += x;
+        }
+        const int at = int(rank) - before;
+        const uint64_t holds = __builtin_amdgcn_ballot_w64(upto > at && upto - mine <= at);
+        if (holds) {
+            const int l = __builtin_ctzll(holds);
+            found = c * kWave + l;
+            place = __builtin_amdgcn_readlane(more + at - (upto - mine), l);
+            break;
+        }
+        before += __builtin_amdgcn_readlane(upto, kWave - 1);
+    }
+    out->q0 = clamped(s.q_offsets[found], 0, s.q_tokens);
+    out->k0 = clamped(s.k_offsets[found], 0, s.k_tokens);
+    out->lq = int(clamped(s.q_offsets[found + 1], out->q0, s.q_tokens) - out->q0);
+    out->lk = int(clamped(s.k_offsets[found + 1], out->k0, s.k_tokens) - out->k0);
+    const int rows = by_keys ? out->lk : out->lq;
+    out->block = by_keys ? place : ((rows - 1) >> shift) - place;
+    return true;
 }
 
 inline int64_t blocks_of(int64_t tokens, int64_t sequences, int shift) { return (tokens >> shift) + sequences; }

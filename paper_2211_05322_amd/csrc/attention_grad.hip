@@ -72,7 +72,7 @@ __global__ __launch_bounds__(kThreads, 2) void attention_dq_kernel(GradArgs a) {
     __shared__ uint4 k0[KEYS * WORDS], v0[KEYS * WORDS], k1[KEYS * WORDS], v1[KEYS * WORDS];
     const Task task = task_of(blockIdx.x, a.blocks, a.heads, a.group);
     Sequence s;
-    if (!find_sequence(a.seq, false, a.blocks - 1 - task.block, kShift, &s)) return;
+    if (!ranked_sequence(a.seq, false, a.causal, a.blocks, task.block, kShift, &s)) return;
     const int lane = threadIdx.x % kWave, wave = threadIdx.x / kWave, half = lane / 32;
     const int kv_head = task.head / a.group, row0 = s.block * kRows + wave * 32;
     const int row = row0 + lane % 32, held = min(row, s.lq - 1);
@@ -98,6 +98,7 @@ __global__ __launch_bounds__(kThreads, 2) void attention_dq_kernel(GradArgs a) {
     const int wave_to = a.causal ? min(s.lk, min(s.lq, row0 + 32) + s.lk - s.lq) : s.lk;
     const int all_see = a.causal ? row0 + 1 + s.lk - s.lq : s.lk;
 
+    const LanePlaces places = LanePlaces::of<DP>(lane);
     f32x16 dq[BLOCKS];
 #pragma unroll
     for (int d = 0; d < BLOCKS; ++d) dq[d] = zero16();
@@ -122,8 +123,8 @@ __global__ __launch_bounds__(kThreads, 2) void attention_dq_kernel(GradArgs a) {
             f32x16 x = zero16(), dp = zero16();
 #pragma unroll
             for (int i = 0; i < STEPS; ++i) {
-                x = mfma(row_operand<T, DP>(kt, n * 32, i, lane), q[i], x);
-                dp = mfma(row_operand<T, DP>(vt, n * 32, i, lane), dout[i], dp);
+                x = mfma(row_operand<T, DP>(kt, n * 32, i, places), q[i], x);
+                dp = mfma(row_operand<T, DP>(vt, n * 32, i, places), dout[i], dp);
             }
             if (key0 + n * 32 + 32 > all_see || key0 + n * 32 + 32 > s.lk) {
 #pragma unroll
@@ -139,7 +140,7 @@ __global__ __launch_bounds__(kThreads, 2) void attention_dq_kernel(GradArgs a) {
             for (int t = 0; t < 2; ++t)
 #pragma unroll
                 for (int d = 0; d < BLOCKS; ++d)
-                    dq[d] = mfma(column_operand<T, DP>(kt, n * 32 + t * 16, d, lane), ds[t], dq[d]);
+                    dq[d] = mfma(column_operand<T, DP>(kt, n * 32 + t * 16, d, places), ds[t], dq[d]);
         }
         if (more) {
             kl.finish(k_next);
@@ -158,23 +159,32 @@ __global__ __launch_bounds__(kThreads, 2) void attention_dq_kernel(GradArgs a) {
 }
 
 // Keys: a lane holds one key's column, and passes over the queries that see
-// it, 32 at a time, of every head of its group.
+// it, of every head of its group.  Of a tile of 64 queries the first 4 waves take
+// the first half, the other 4 the second, for the same 128 keys, and add up at the
+// end: two waves a SIMD, one's exponentials beside the other's products.  Where
+// registers do not hold two operands and two sums, values stay in LDS.
+constexpr int kKeyThreads = 512;
+
 template <typename T, int DP, bool ASYNC>
-__global__ __launch_bounds__(kThreads, DP <= 64 ? 2 : 1) void attention_dkv_kernel(GradArgs a) {
+__global__ __launch_bounds__(kKeyThreads, 2) void attention_dkv_kernel(GradArgs a) {
     constexpr int STEPS = DP / 16, BLOCKS = DP / 32, QUERIES = 64, WORDS = TileShape<DP>::words;
+    constexpr bool VALUES_IN_LDS = DP > 64;
     __shared__ uint4 q0[QUERIES * WORDS], d0[QUERIES * WORDS], q1[QUERIES * WORDS], d1[QUERIES * WORDS];
+    __shared__ uint4 values[VALUES_IN_LDS ? kRows * WORDS : 1];
     __shared__ float lse_lds[2][QUERIES], delta_lds[2][QUERIES];
     const Task task = task_of(blockIdx.x, a.blocks, a.heads / a.group, 1);
     Sequence s;
-    if (!find_sequence(a.seq, true, task.block, kShift, &s)) return;
-    const int lane = threadIdx.x % kWave, wave = threadIdx.x / kWave, half = lane / 32;
-    const int key0 = s.block * kRows + wave * 32, key = key0 + lane % 32, held = min(key, s.lk - 1);
+    if (!ranked_sequence(a.seq, true, a.causal, a.blocks, task.block, kShift, &s)) return;
+    const int lane = threadIdx.x % kWave, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave), half = lane / 32;
+    const int part = wave / 4, keys_of = wave % 4;
+    const int key0 = s.block * kRows + keys_of * 32, key = key0 + lane % 32, held = min(key, s.lk - 1);
 
-    Operand8<T> k[STEPS], v[STEPS];
+    Operand8<T> k[STEPS], v[VALUES_IN_LDS ? 1 : STEPS];
 #pragma unroll
     for (int i = 0; i < STEPS; ++i) {
         k[i] = global_operand(a.k.template at<const T>(s.k0 + held, task.head), true, i, lane, a.dim);
-        v[i] = global_operand(a.v.template at<const T>(s.k0 + held, task.head), true, i, lane, a.dim);
+        if constexpr (!VALUES_IN_LDS)
+            v[i] = global_operand(a.v.template at<const T>(s.k0 + held, task.head), true, i, lane, a.dim);
     }
     // the first query that sees the lane's key; of the workgroup's and of the wave's keys; the first that sees all the wave's
     const int first = a.causal ? key - (s.lk - s.lq) : 0;
@@ -182,11 +192,12 @@ __global__ __launch_bounds__(kThreads, DP <= 64 ? 2 : 1) void attention_dkv_kern
     const int wave_from = a.causal ? key0 - (s.lk - s.lq) : 0, all_see = a.causal ? wave_from + 31 : 0;
     const int tiles = s.lq > from ? (s.lq - from + QUERIES - 1) / QUERIES : 0, turns = tiles * a.group;
 
+    const LanePlaces places = LanePlaces::of<DP>(lane, part * 32), v_places = LanePlaces::of<DP>(lane, keys_of * 32);
     f32x16 dk[BLOCKS], dv[BLOCKS];
 #pragma unroll
     for (int d = 0; d < BLOCKS; ++d) dk[d] = dv[d] = zero16();
     float factor = kFirstFactor;
-    TileLoader<T, DP, QUERIES, kThreads, ASYNC> ql(threadIdx.x, a.dim, a.q.token_pitch), dl(threadIdx.x, a.dim, a.dout.token_pitch);
+    TileLoader<T, DP, QUERIES, kKeyThreads, ASYNC> ql(threadIdx.x, a.dim, a.q.token_pitch), dl(threadIdx.x, a.dim, a.dout.token_pitch);
     int next_head = task.head * a.group, next_row = from;  // of the tile to be loaded
     float2 stat;
     auto start = [&](auto &q_to, auto &d_to) {
@@ -210,6 +221,11 @@ __global__ __launch_bounds__(kThreads, DP <= 64 ? 2 : 1) void attention_dkv_kern
         dl.finish(d_to);
     };
     if (turns > 0) {
+        if constexpr (VALUES_IN_LDS) {
+            TileLoader<T, DP, kRows, kKeyThreads, ASYNC> vl(threadIdx.x, a.dim, a.v.token_pitch);
+            vl.start(a.v.template at<const T>(s.k0 + s.block * kRows, task.head), s.lk - s.block * kRows, values);
+            vl.finish(values);
+        }
         start(q0, d0);
         finish(0, q0, d0);
     }
@@ -218,15 +234,19 @@ __global__ __launch_bounds__(kThreads, DP <= 64 ? 2 : 1) void attention_dkv_kern
     auto step = [&](int turn, int which, const auto &qt, const auto &dt, auto &q_next, auto &d_next) {
         const bool more = turn + 1 < turns;
         if (more) start(q_next, d_next);
-#pragma unroll
-        for (int n = 0; n < 2; ++n) {
-            const int r0 = row0 + n * 32;
-            if (r0 + 31 < wave_from || r0 >= s.lq) continue;
+        const int r0 = row0 + part * 32;
+        if (r0 + 31 >= wave_from && r0 < s.lq) {
             f32x16 x = zero16(), dp = zero16();
 #pragma unroll
             for (int i = 0; i < STEPS; ++i) {
-                x = mfma(row_operand<T, DP>(qt, n * 32, i, lane), k[i], x);
-                dp = mfma(row_operand<T, DP>(dt, n * 32, i, lane), v[i], dp);
+                x = mfma(row_operand<T, DP>(qt, 0, i, places), k[i], x);
+                if constexpr (!VALUES_IN_LDS) dp = mfma(row_operand<T, DP>(dt, 0, i, places), v[i], dp);
+            }
+            if constexpr (VALUES_IN_LDS) {
+#pragma unroll
+                for (int i = 0; i < STEPS; ++i) {
+                    dp = mfma(row_operand<T, DP>(dt, 0, i, places), row_operand<T, DP>(values, 0, i, v_places), dp);
+                }
             }
             if (r0 < all_see) {
 #pragma unroll
@@ -236,8 +256,8 @@ __global__ __launch_bounds__(kThreads, DP <= 64 ? 2 : 1) void attention_dkv_kern
             Operand8<T> p[2], ds[2];
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
-                const f32x4 lse = *reinterpret_cast<const f32x4 *>(&lse_lds[which][n * 32 + result_row(4 * j, half)]);
-                const f32x4 delta = *reinterpret_cast<const f32x4 *>(&delta_lds[which][n * 32 + result_row(4 * j, half)]);
+                const f32x4 lse = *reinterpret_cast<const f32x4 *>(&lse_lds[which][part * 32 + result_row(4 * j, half)]);
+                const f32x4 delta = *reinterpret_cast<const f32x4 *>(&delta_lds[which][part * 32 + result_row(4 * j, half)]);
 #pragma unroll
                 for (int e = 0; e < 4; ++e) {
                     const int r = 4 * j + e;
@@ -251,8 +271,8 @@ __global__ __launch_bounds__(kThreads, DP <= 64 ? 2 : 1) void attention_dkv_kern
             for (int t = 0; t < 2; ++t)
 #pragma unroll
                 for (int d = 0; d < BLOCKS; ++d) {
-                    dv[d] = mfma(column_operand<T, DP>(dt, n * 32 + t * 16, d, lane), p[t], dv[d]);
-                    dk[d] = mfma(column_operand<T, DP>(qt, n * 32 + t * 16, d, lane), ds[t], dk[d]);
+                    dv[d] = mfma(column_operand<T, DP>(dt, t * 16, d, places), p[t], dv[d]);
+                    dk[d] = mfma(column_operand<T, DP>(qt, t * 16, d, places), ds[t], dk[d]);
                 }
         }
         row0 += QUERIES;
@@ -264,12 +284,40 @@ __global__ __launch_bounds__(kThreads, DP <= 64 ? 2 : 1) void attention_dkv_kern
         step(turn, 0, q0, d0, q1, d1);
         if (turn + 1 < turns) step(turn + 1, 1, q1, d1, q0, d0);
     }
-    T *to_dk = a.dk.template at<T>(s.k0 + held, task.head), *to_dv = a.dv.template at<T>(s.k0 + held, task.head);
     const float down = kNarrow<T> ? 1.0f / 16384 : 1.0f, scale = kNarrow<T> ? a.scale / factor * down : a.scale;
+    // the second half's sums to the first, through the tiles' memory
+    uint4 *tile = keys_of == 0 ? q0 : keys_of == 1 ? d0 : keys_of == 2 ? q1 : d1;
+    auto *trade = reinterpret_cast<f32x4 *>(tile) + lane;
+    auto join = [&](f32x16(&sums)[BLOCKS], float by) {
+        if (part == 1) {
+#pragma unroll
+            for (int d = 0; d < BLOCKS; ++d)
+#pragma unroll
+                for (int j = 0; j < 4; ++j)
+                    trade[(d * 4 + j) * kWave] = f32x4{sums[d][4 * j] * by, sums[d][4 * j + 1] * by, sums[d][4 * j + 2] * by,
+                                                       sums[d][4 * j + 3] * by};
+        }
+        __syncthreads();
+        if (part == 0) {
+#pragma unroll
+            for (int d = 0; d < BLOCKS; ++d)
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    const f32x4 x = trade[(d * 4 + j) * kWave];
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) sums[d][4 * j + e] = fmaf(sums[d][4 * j + e], by, x[e]);
+                }
+        }
+        __syncthreads();
+    };
+    join(dk, scale);
+    join(dv, down);
+    if (part == 1) return;
+    T *to_dk = a.dk.template at<T>(s.k0 + held, task.head), *to_dv = a.dv.template at<T>(s.k0 + held, task.head);
 #pragma unroll
     for (int d = 0; d < BLOCKS; ++d) {
-        store_columns(to_dk, key < s.lk, dk[d], scale, d, lane, a.dim);
-        store_columns(to_dv, key < s.lk, dv[d], down, d, lane, a.dim);
+        store_columns(to_dk, key < s.lk, dk[d], 1.0f, d, lane, a.dim);
+        store_columns(to_dv, key < s.lk, dv[d], 1.0f, d, lane, a.dim);
     }
 }
 
@@ -333,10 +381,10 @@ extern "C" reshard_status_t reshard_attention_backward(
             if (k_tokens == 0) return status;
             status = check_grid(blocks_of(k_tokens, sequences, kShift), kv_heads, &a.blocks);
             if (status != RESHARD_OK) return status;
-            const bool async = aligned16(a.q, 2) && aligned16(a.dout, 2);
+            const bool async = aligned16(a.q, 2) && aligned16(a.dout, 2) && aligned16(a.v, 2);
             return launch("attention gradient launch",
                           async ? attention_dkv_kernel<T, DP, true> : attention_dkv_kernel<T, DP, false>,
-                          dim3(unsigned(a.blocks * kv_heads)), kThreads, 0, stm, a);
+                          dim3(unsigned(a.blocks * kv_heads)), kKeyThreads, 0, stm, a);
         });
     });
 }

@@ -4,10 +4,10 @@
 //
 // Bound by memory: the cache is read once, and each of its elements is used by
 // the few query heads that share it.  So the work is dealt by what is read: the
-// tiles of 128 tokens of all sequences and key heads lie in one line, which the
-// workgroups cut into equal runs, whatever the lengths.  A run may end inside
-// a sequence; its part (weighted values, their sum, the maximum) then goes to
-// the workspace, and a second kernel joins parts in their order.
+// tiles of 32 tokens of all sequences and key heads lie in one line, which the
+// waves cut into equal runs, whatever the lengths.  A run may end inside a
+// sequence; its part (weighted values, their sum, the maximum) then goes to the
+// workspace, and a second kernel joins parts in their order.
 #include <algorithm>
 
 #include "attention.hpp"
@@ -16,8 +16,8 @@ namespace rs {
 namespace {
 
 constexpr int kThreads = 256, kWaves = kThreads / kWave;
-constexpr int kWaveKeys = 32, kTileKeys = kWaves * kWaveKeys;  // a wave's and a workgroup's tokens of a tile
-constexpr int kQueries = 16;                                   // heads of a group that one pass takes
+constexpr int kTile = 32;     // tokens of a tile
+constexpr int kQueries = 16;  // heads of a group that one pass takes
 constexpr float kLowest = -3.402823466e38f;
 
 struct PagedArgs {
@@ -26,298 +26,335 @@ struct PagedArgs {
     const int32_t *pages, *lengths;
     int64_t pages_pitch;
     int64_t *line;  // [sequences + 1]: tiles before each sequence, of one key head
-    float *parts;   // [workgroups][2][group's rows up to 16][dim + 2]
+    float *parts;   // [waves][2]: values [group's rows up to 16][dim], then maximum and sum [rows][2]
     int sequences, width, kv_heads, group, passes, dim, rows;
     uint32_t magic, magic_shift;  // slot / page_length
     float scale2;
 };
 
-__device__ inline int64_t tiles_of(const PagedArgs &a, int s) {
-    const int64_t most = int64_t(a.width) * a.cache.page_length;
-    const int64_t n = min(int64_t(max(a.lengths[s], 0)), most);
-    return (n + kTileKeys - 1) / kTileKeys;
+__device__ inline int length_of(const PagedArgs &a, int s) {
+    return int(min(int64_t(max(a.lengths[s], 0)), int64_t(a.width) * a.cache.page_length));
 }
+__device__ inline int tiles_of(int length) { return int((uint32_t(length) + kTile - 1) / kTile); }
 
-// The number of tiles before each thread's share of the sequences, and of all.
-__device__ inline int64_t scan(int64_t mine, int64_t *total, int64_t *part) {
-    const int lane = threadIdx.x % kWave, wave = threadIdx.x / kWave;
-    int64_t sum = mine;
-#pragma unroll
-    for (int d = 1; d < kWave; d *= 2) {
-        const int64_t other = __shfl_up(sum, d);
-        if (lane >= d) sum += other;
+// A tile of the line: its sequence, key head and pass, and number among the unit's tiles.
+struct Place {
+    int s, unit, t, tiles, length;
+    __device__ void sequence(const PagedArgs &a, int s_) {
+        s = s_;
+        length = length_of(a, s);
+        tiles = tiles_of(length);
     }
-    if (lane == kWave - 1) part[wave] = sum;
-    __syncthreads();
-    int64_t before = 0, all = 0;
-#pragma unroll
-    for (int w = 0; w < kWaves; ++w) {
-        before += w < wave ? part[w] : 0;
-        all += part[w];
+    __device__ void next(const PagedArgs &a, int units) {
+        if (++t < tiles) return;
+        t = 0;
+        if (++unit < units) return;
+        unit = 0;
+        do {
+            if (s + 1 >= a.sequences) return;  // the line's end: of no use
+            sequence(a, s + 1);
+        } while (tiles == 0);
     }
-    *total = all;
-    return before + sum - mine;
-}
+};
 
-// A wave's keys are the instruction's rows and the group's queries its columns:
-// a lane has 8 scores of one query, whose weights then go into the second
-// product as they are.  Keys come straight into the operands' registers; values
-// pass through LDS, where the transposing load finds their columns, in a part
-// that is the wave's own.  The next tile's are on their way meanwhile.
+// Keys are the instruction's rows and the group's queries its columns: a lane has
+// 8 scores of one query, whose weights then go into the second product as they
+// are.  Keys come straight into the operands' registers; values pass through LDS,
+// where the transposing load finds their columns, in a part that is the wave's
+// own, so that waves never wait for each other.  The next tile is on its way
+// meanwhile, and the page numbers of the one after it.
 template <typename T, int DP>
 __global__ __launch_bounds__(kThreads, 2) void paged_kernel(PagedArgs a) {
     constexpr int STEPS = DP / 32, BLOCKS = DP / 16, WORDS = TileShape<DP>::words;
-    constexpr int ROWS_AT_ONCE = kWave / WORDS, VALUES = kWaveKeys / ROWS_AT_ONCE;
-    __shared__ uint4 values[kWaves][kWaveKeys * WORDS];
-    __shared__ float maxima[kWaves][kQueries], sums[kWaves][kQueries];
-    __shared__ int64_t part[kWaves], found[2];
-    const int lane = threadIdx.x % kWave, wave = threadIdx.x / kWave, column = lane % 16, quarter = lane / 16;
-    const int units = a.kv_heads * a.passes;
+    constexpr int ROWS_AT_ONCE = kWave / WORDS, VALUES = kTile / ROWS_AT_ONCE;
+    __shared__ uint4 values[kWaves][kTile * WORDS];
+    const int lane = threadIdx.x % kWave, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
+    const int column = lane % 16, quarter = lane / 16, units = a.kv_heads * a.passes;
+    const int64_t number = int64_t(blockIdx.x) * kWaves + wave;
 
-    // this workgroup's run of the line
-    const int share = (a.sequences + kThreads - 1) / kThreads;
-    const int from_s = min(int(threadIdx.x) * share, a.sequences), to_s = min(from_s + share, a.sequences);
-    int64_t mine = 0, total;
-    for (int s = from_s; s < to_s; ++s) mine += tiles_of(a, s);
-    int64_t before = scan(mine, &total, part);
-    const int64_t all = total * units, runs = min(all, int64_t(gridDim.x));
-    if (blockIdx.x == 0) {  // for the joining kernel
+    // this wave's run of the line
+    const int share = (a.sequences + kWave - 1) / kWave;
+    const int from_s = min(lane * share, a.sequences), to_s = min(from_s + share, a.sequences);
+    int64_t mine = 0;
+    for (int s = from_s; s < to_s; ++s) mine += tiles_of(length_of(a, s));
+    int64_t before = mine;
+#pragma unroll
+    for (int d = 1; d < kWave; d *= 2) {
+        const int64_t other = __shfl_up(before, d);
+        if (lane >= d) before += other;
+    }
+    const int64_t total = __shfl(before, kWave - 1), all = total * units;
+    before -= mine;
+    if (number == 0) {  // for the joining kernel
         int64_t n = before;
         for (int s = from_s; s < to_s; ++s) {
             a.line[s] = n;
-            n += tiles_of(a, s);
+            n += tiles_of(length_of(a, s));
         }
-        if (threadIdx.x == 0) a.line[a.sequences] = total;
+        if (lane == 0) a.line[a.sequences] = total;
     }
-    if (blockIdx.x >= runs) return;
-    const int64_t at = all * blockIdx.x / runs, end = all * (blockIdx.x + 1) / runs;
-    if (mine > 0 && before * units <= at && at < (before + mine) * units) {
-        int s = from_s;
-        for (int64_t n; (before + (n = tiles_of(a, s))) * units <= at; ++s) before += n;
-        found[0] = s;
-        found[1] = before;
+    const int64_t runs = min(all, int64_t(gridDim.x) * kWaves);
+    if (number >= runs) return;
+    const int64_t at = all * number / runs;
+    int64_t left = all * (number + 1) / runs - at;  // at least one tile
+    int s0 = from_s;
+    const bool here = mine > 0 && before * units <= at && at < (before + mine) * units;
+    if (here) {
+        for (int64_t n; (before + (n = tiles_of(length_of(a, s0)))) * units <= at; ++s0) before += n;
     }
-    __syncthreads();
-    int s = int(found[0]);
-    int64_t line = found[1] * units, tiles = tiles_of(a, s);
+    const int holder = __builtin_ctzll(__builtin_amdgcn_ballot_w64(here));
+    Place place;
+    place.sequence(a, __builtin_amdgcn_readfirstlane(__shfl(s0, holder)));
+    {
+        const int64_t in = at - __shfl(before, holder) * units;
+        place.unit = __builtin_amdgcn_readfirstlane(int(in / place.tiles));
+        place.t = __builtin_amdgcn_readfirstlane(int(in - int64_t(place.unit) * place.tiles));
+    }
 
-    for (int64_t tile = at; tile < end;) {
-        while (tile >= line + tiles * units) {
-            line += tiles * units;
-            tiles = tiles_of(a, ++s);
-        }
-        const int unit = int((tile - line) / tiles);
-        const int64_t unit_at = line + unit * tiles;
-        const int first = int(tile - unit_at), last = int(min(tiles, end - unit_at));  // of the unit's tiles
-        const int head = unit / a.passes, pass = unit - head * a.passes;
-        const int group0 = pass * kQueries, rows = min(kQueries, a.group - group0);
-        const int length = int(min(int64_t(a.lengths[s]), int64_t(a.width) * a.cache.page_length));
-        const int32_t *table = a.pages + s * a.pages_pitch;
-
-        Operand8<T> q[STEPS];
+    auto page_of = [&](const Place &p, bool there) {
+        const uint32_t key = uint32_t(p.t) * kTile + lane % kTile;
+        if (!there || key >= uint32_t(p.length)) return -1;
+        return int(a.pages[p.s * a.pages_pitch + ((__umulhi(a.magic, key) + key) >> a.magic_shift)]);
+    };
+    // where a lane's token of a tile lies (-1: nowhere)
+    auto offset_of = [&](const Place &p, int page) -> int64_t {
+        const uint32_t key = uint32_t(p.t) * kTile + lane % kTile;
+        if (page < 0 || page >= a.cache.pages) return -1;
+        const uint32_t n = (__umulhi(a.magic, key) + key) >> a.magic_shift;
+        return page * a.cache.page_pitch + (key - n * a.cache.page_length) * a.cache.slot_pitch +
+               p.unit / a.passes * a.cache.head_pitch;
+    };
+    auto of_lane = [](int64_t x, int l) -> int64_t {
+        const uint32_t lo = uint32_t(__shfl(int(x), l)), hi = uint32_t(__shfl(int(x >> 32), l));
+        return int64_t(uint64_t(hi) << 32 | lo);
+    };
+    Operand8<T> q[STEPS], k[2][STEPS];
+    uint4 v[VALUES];
+    auto load_queries = [&](const Place &p) {
+        const int head = p.unit / a.passes, row = (p.unit - head * a.passes) * kQueries + column;
 #pragma unroll
         for (int i = 0; i < STEPS; ++i) {
             const int d = i * 32 + quarter * 8;
             q[i].w = make_uint4(0, 0, 0, 0);
-            if (column < rows && d < a.dim)
-                q[i].w = load_any<uint4>(a.q.template at<const T>(s, int64_t(head) * a.group + group0 + column) + d);
+            if (row < a.group && d < a.dim)
+                q[i].w = load_any<uint4>(a.q.template at<const T>(p.s, int64_t(head) * a.group + row) + d);
         }
-        // where a lane's token of a tile lies (-1: nowhere)
-        auto page_of = [&](int t) {
-            const int key = t * kTileKeys + wave * kWaveKeys + lane % kWaveKeys;
-            if (t >= last || key >= length) return -1;
-            return int(table[(__umulhi(a.magic, uint32_t(key)) + uint32_t(key)) >> a.magic_shift]);
-        };
-        auto offset_of = [&](int t, int page) -> int64_t {
-            const int key = t * kTileKeys + wave * kWaveKeys + lane % kWaveKeys;
-            if (t >= last || key >= length || page < 0 || page >= a.cache.pages) return -1;
-            const uint32_t number = (__umulhi(a.magic, uint32_t(key)) + uint32_t(key)) >> a.magic_shift;
-            return page * a.cache.page_pitch + (key - int(number) * a.cache.page_length) * a.cache.slot_pitch +
-                   head * a.cache.head_pitch;
-        };
-        auto of_lane = [](int64_t x, int l) -> int64_t {
-            const uint32_t lo = uint32_t(__shfl(int(x), l)), hi = uint32_t(__shfl(int(x >> 32), l));
-            return int64_t(uint64_t(hi) << 32 | lo);
-        };
-        Operand8<T> k[2][STEPS];
-        uint4 v[VALUES];
-        const T *keys = static_cast<const T *>(a.cache.keys), *vals = static_cast<const T *>(a.cache.values);
-        auto load_keys = [&](int64_t offset) {
+    };
+    auto load_keys = [&](int64_t offset) {
 #pragma unroll
-            for (int b = 0; b < 2; ++b) {
-                const int64_t o = of_lane(offset, b * 16 + column);
+        for (int b = 0; b < 2; ++b) {
+            const int64_t o = of_lane(offset, b * 16 + column);
 #pragma unroll
-                for (int i = 0; i < STEPS; ++i) {
-                    const int d = i * 32 + quarter * 8;
-                    k[b][i].w = make_uint4(0, 0, 0, 0);
-                    if (o >= 0 && d < a.dim) k[b][i].w = load_any<uint4>(keys + o + d);
-                }
+            for (int i = 0; i < STEPS; ++i) {
+                const int d = i * 32 + quarter * 8;
+                k[b][i].w = make_uint4(0, 0, 0, 0);
+                if (o >= 0 && d < a.dim) k[b][i].w = load_any<uint4>(static_cast<const T *>(a.cache.keys) + o + d);
             }
-        };
-        auto load_values = [&](int64_t offset) {
+        }
+    };
+    auto load_values = [&](int64_t offset) {
 #pragma unroll
-            for (int u = 0; u < VALUES; ++u) {
-                const int64_t o = of_lane(offset, u * ROWS_AT_ONCE + lane / WORDS);
-                const int d = lane % WORDS * 8;
-                v[u] = make_uint4(0, 0, 0, 0);
-                if (o >= 0 && d < a.dim) v[u] = load_any<uint4>(vals + o + d);
-            }
-        };
+        for (int u = 0; u < VALUES; ++u) {
+            const int64_t o = of_lane(offset, u * ROWS_AT_ONCE + lane / WORDS);
+            const int d = lane % WORDS * 8;
+            v[u] = make_uint4(0, 0, 0, 0);
+            if (o >= 0 && d < a.dim) v[u] = load_any<uint4>(static_cast<const T *>(a.cache.values) + o + d);
+        }
+    };
 
-        f32x4 o[BLOCKS];
+    f32x4 o[BLOCKS];
 #pragma unroll
-        for (int d = 0; d < BLOCKS; ++d) o[d] = f32x4{0, 0, 0, 0};
-        float m = kLowest, l = 0;
-        int64_t now = offset_of(first, page_of(first)), next = offset_of(first + 1, page_of(first + 1));
-        load_keys(now);
-        load_values(now);
-        for (int t = first; t < last; ++t) {
-            const int page = page_of(t + 2);
-            f32x4 x[2];
+    for (int d = 0; d < BLOCKS; ++d) o[d] = f32x4{0, 0, 0, 0};
+    float m = kLowest, l = 0;
+    bool begun = place.t == 0;  // whether the unit's first tile is this wave's
+    Place ahead = place;
+    int64_t now = offset_of(place, page_of(place, true)), next;
+    load_queries(place);
+    load_keys(now);
+    load_values(now);
+    ahead.next(a, units);
+    next = offset_of(ahead, page_of(ahead, left > 1));
+    for (;;) {
+        Place second = ahead;
+        second.next(a, units);
+        const int page = page_of(second, left > 2);
+        f32x4 x[2];
+#pragma unroll
+        for (int b = 0; b < 2; ++b) {
+            x[b] = f32x4{0, 0, 0, 0};
+#pragma unroll
+            for (int i = 0; i < STEPS; ++i) x[b] = mfma(k[b][i], q[i], x[b]);
+        }
+        load_keys(next);
+        const uint64_t there = __builtin_amdgcn_ballot_w64(now >= 0);  // bit j: token j of the tile
+        float top = kLowest;
+#pragma unroll
+        for (int b = 0; b < 2; ++b)
+#pragma unroll
+            for (int r = 0; r < 4; ++r) {
+                if (!(there >> (b * 16 + quarter * 4 + r) & 1)) x[b][r] = -INFINITY;
+                top = fmaxf(top, x[b][r] * a.scale2);
+            }
+        if (__builtin_amdgcn_ballot_w64(top > m + 8)) {
+            top = fmaxf(top, __shfl_xor(top, 16));
+            top = fmaxf(top, __shfl_xor(top, 32));
+            top = fmaxf(top, m);
+            const float shrink = __builtin_amdgcn_exp2f(m - top);
+            m = top;
+            l *= shrink;
+#pragma unroll
+            for (int d = 0; d < BLOCKS; ++d) o[d] *= shrink;
+        }
+        Operand8<T> p;
+#pragma unroll
+        for (int b = 0; b < 2; ++b)
+#pragma unroll
+            for (int r = 0; r < 4; ++r) {
+                const float e = __builtin_amdgcn_exp2f(fmaf(x[b][r], a.scale2, -m));
+                l += e;
+                p.e[b * 4 + r] = T(e);
+            }
+#pragma unroll
+        for (int u = 0; u < VALUES; ++u)
+            values[wave][TileShape<DP>::at(u * ROWS_AT_ONCE + lane / WORDS, lane % WORDS)] = v[u];
+        load_values(next);
+        now = next;
+        next = offset_of(second, page);
+        __builtin_amdgcn_wave_barrier();  // a wave's LDS accesses are done in their order
+#pragma unroll
+        for (int d = 0; d < BLOCKS; ++d) {
+            typedef __attribute__((address_space(3))) s16x4 lds_s16x4;
+            Operand8<T> vv;
 #pragma unroll
             for (int b = 0; b < 2; ++b) {
-                x[b] = f32x4{0, 0, 0, 0};
-#pragma unroll
-                for (int i = 0; i < STEPS; ++i) x[b] = mfma(k[b][i], q[i], x[b]);
+                const int row = b * 16 + quarter * 4 + column / 4;
+                const char *from =
+                    reinterpret_cast<const char *>(&values[wave][TileShape<DP>::at(row, d * 2 + column % 4 / 2)]);
+                vv.half[b] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4 *)(from + column % 2 * 8));
             }
-            load_keys(next);
-            const uint64_t there = __builtin_amdgcn_ballot_w64(now >= 0);  // bit j: token j of the wave's 32
-            float top = kLowest;
-#pragma unroll
-            for (int b = 0; b < 2; ++b)
-#pragma unroll
-                for (int r = 0; r < 4; ++r) {
-                    if (!(there >> (b * 16 + quarter * 4 + r) & 1)) x[b][r] = -INFINITY;
-                    top = fmaxf(top, x[b][r] * a.scale2);
-                }
-            if (__builtin_amdgcn_ballot_w64(top > m + 8)) {
-                top = fmaxf(top, __shfl_xor(top, 16));
-                top = fmaxf(top, __shfl_xor(top, 32));
-                top = fmaxf(top, m);
-                const float shrink = __builtin_amdgcn_exp2f(m - top);
-                m = top;
-                l *= shrink;
-#pragma unroll
-                for (int d = 0; d < BLOCKS; ++d) o[d] *= shrink;
-            }
-            Operand8<T> p;
-#pragma unroll
-            for (int b = 0; b < 2; ++b)
-#pragma unroll
-                for (int r = 0; r < 4; ++r) {
-                    const float e = __builtin_amdgcn_exp2f(fmaf(x[b][r], a.scale2, -m));
-                    l += e;
-                    p.e[b * 4 + r] = T(e);
-                }
-#pragma unroll
-            for (int u = 0; u < VALUES; ++u)
-                values[wave][TileShape<DP>::at(u * ROWS_AT_ONCE + lane / WORDS, lane % WORDS)] = v[u];
-            load_values(next);
-            now = next;
-            next = offset_of(t + 2, page);
-            __builtin_amdgcn_wave_barrier();  // a wave's LDS accesses are done in their order
-#pragma unroll
-            for (int d = 0; d < BLOCKS; ++d) {
-                typedef __attribute__((address_space(3))) s16x4 lds_s16x4;
-                Operand8<T> vv;
-#pragma unroll
-                for (int b = 0; b < 2; ++b) {
-                    const int row = b * 16 + quarter * 4 + column / 4;
-                    const char *from =
-                        reinterpret_cast<const char *>(&values[wave][TileShape<DP>::at(row, d * 2 + column % 4 / 2)]);
-                    vv.half[b] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4 *)(from + column % 2 * 8));
-                }
-                o[d] = mfma(vv, p, o[d]);
-            }
-            __builtin_amdgcn_wave_barrier();
+            o[d] = mfma(vv, p, o[d]);
         }
-        // the waves' parts, one query a lane of 16 and 4 elements a block
-        l += __shfl_xor(l, 16);
-        l += __shfl_xor(l, 32);
-        __syncthreads();
-        float *mine_o = reinterpret_cast<float *>(values[wave]);  // [queries][DP / 2 of it]: half the elements at a time
-        if (quarter == 0) {
-            maxima[wave][column] = m;
-            sums[wave][column] = l;
-        }
-        const bool whole = first == 0 && last == tiles;
-        float *to = a.parts + ((int64_t(blockIdx.x) * 2 + (first == 0)) * a.rows) * (a.dim + 2);
-        constexpr int HALF = DP / 2;
+        __builtin_amdgcn_wave_barrier();
+        --left;
+        const bool ends = place.t + 1 == place.tiles;
+        if (ends || left == 0) {  // the unit's results, or this wave's part of them
+            l += __shfl_xor(l, 16);
+            l += __shfl_xor(l, 32);
+            const int head = place.unit / a.passes, group0 = (place.unit - head * a.passes) * kQueries;
+            if (column < a.group - group0) {
+                if (begun && ends) {
+                    const float over = l == 0 ? 0.0f : 1.0f / l;
+                    T *to = a.out.template at<T>(place.s, int64_t(head) * a.group + group0 + column);
+                    typedef T T4 __attribute__((ext_vector_type(4)));
 #pragma unroll
-        for (int h = 0; h < 2; ++h) {
-            __syncthreads();
+                    for (int d = 0; d < BLOCKS; ++d) {
+                        T4 y;
 #pragma unroll
-            for (int d = 0; d < BLOCKS / 2; ++d)
-                *reinterpret_cast<f32x4 *>(mine_o + column * HALF + d * 16 + quarter * 4) = o[h * (BLOCKS / 2) + d];
-            __syncthreads();
-            for (int i = threadIdx.x; i < rows * HALF; i += kThreads) {
-                const int r = i / HALF, d = i - r * HALF;
-                float top = maxima[0][r];
-#pragma unroll
-                for (int w = 1; w < kWaves; ++w) top = fmaxf(top, maxima[w][r]);
-                float sum = 0, value = 0;
-#pragma unroll
-                for (int w = 0; w < kWaves; ++w) {
-                    const float f = __builtin_amdgcn_exp2f(maxima[w][r] - top);
-                    sum = fmaf(f, sums[w][r], sum);
-                    value = fmaf(f, reinterpret_cast<const float *>(values[w])[i], value);
-                }
-                if (h * HALF + d >= a.dim) continue;
-                if (whole) {
-                    a.out.template at<T>(s, int64_t(head) * a.group + group0 + r)[h * HALF + d] =
-                        T(sum == 0 ? 0.0f : value / sum);
-                } else {
-                    float *row = to + r * (a.dim + 2);
-                    row[h * HALF + d] = value;
-                    if (h == 0 && d == 0) {
-                        row[a.dim] = top;
-                        row[a.dim + 1] = sum;
+                        for (int e = 0; e < 4; ++e) y[e] = T(o[d][e] * over);
+                        if (d * 16 + quarter * 4 < a.dim) store_any(to + d * 16 + quarter * 4, y);
                     }
+                } else {
+                    float *to = a.parts + (number * 2 + begun) * a.rows * (a.dim + 2);
+#pragma unroll
+                    for (int d = 0; d < BLOCKS; ++d)
+                        if (d * 16 + quarter * 4 < a.dim) store_any(to + column * a.dim + d * 16 + quarter * 4, o[d]);
+                    if (quarter == 0) store_any(to + a.rows * a.dim + column * 2, make_float2(m, l));
                 }
             }
+            if (left == 0) return;
+            begun = true;
+            load_queries(ahead);
+#pragma unroll
+            for (int d = 0; d < BLOCKS; ++d) o[d] = f32x4{0, 0, 0, 0};
+            m = kLowest;
+            l = 0;
         }
-        __syncthreads();
-        tile = unit_at + last;
+        place = ahead;
+        ahead = second;
     }
 }
 
-// Joins the parts of each unit that more than one workgroup had, and writes the
-// zeros of sequences without tokens.  A workgroup a sequence and key head and pass.
+// Joins the parts of each unit that more than one wave had, and writes the zeros
+// of sequences without tokens.  A workgroup a unit; where its vectors of 4
+// elements are fewer than threads, groups of threads share the parts.
 template <typename T>
-__global__ __launch_bounds__(kThreads) void paged_join_kernel(PagedArgs a, uint32_t workgroups) {
+__global__ __launch_bounds__(kThreads) void paged_join_kernel(PagedArgs a, uint32_t waves) {
+    __shared__ float tops[kQueries][kThreads / kQueries];
+    __shared__ f32x4 shared_value[kThreads];
+    __shared__ float shared_sum[kThreads];
     const int units = a.kv_heads * a.passes, s = blockIdx.x / units, unit = blockIdx.x - s * units;
     const int head = unit / a.passes, group0 = (unit - head * a.passes) * kQueries, rows = min(kQueries, a.group - group0);
     const int64_t tiles = a.line[s + 1] - a.line[s], all = a.line[a.sequences] * units;
     const int64_t at = a.line[s] * units + unit * tiles;
-    int64_t w0 = 0, w1 = -1;
+    int64_t w0 = 0;
+    int parts = 0;
     if (tiles > 0) {
-        // the workgroup whose run holds tile x: the last w with all * w / runs <= x; no run is empty
-        const int64_t runs = min(all, int64_t(workgroups));
+        // the wave whose run holds tile x: the last w with all * w / runs <= x; no run is empty
+        const int64_t runs = min(all, int64_t(waves));
         w0 = ((at + 1) * runs - 1) / all;
-        w1 = ((at + tiles) * runs - 1) / all;
-        if (w0 == w1) return;
+        parts = int(((at + tiles) * runs - 1) / all - w0) + 1;
+        if (parts == 1) return;
     }
-    const int stride = a.dim + 2;
-    for (int i = threadIdx.x; i < rows * a.dim; i += kThreads) {
-        const int r = i / a.dim, d = i - r * a.dim;
-        float top = kLowest, sum = 0, value = 0;
-        for (int64_t w = w0; w <= w1; ++w)
-            top = fmaxf(top, a.parts[((w * 2 + (w == w0)) * a.rows + r) * stride + a.dim]);
-        for (int64_t w = w0; w <= w1; ++w) {
-            const float *row = a.parts + ((w * 2 + (w == w0)) * a.rows + r) * stride;
-            const float f = __builtin_amdgcn_exp2f(row[a.dim] - top);
-            sum = fmaf(f, row[a.dim + 1], sum);
-            value = fmaf(f, row[d], value);
+    const int64_t size = int64_t(a.rows) * (a.dim + 2);
+    // the first wave began the unit, the others came into it
+    auto part = [&](int i) { return a.parts + ((w0 + i) * 2 + (i == 0)) * size; };
+    {
+        const int r = threadIdx.x % kQueries, j = threadIdx.x / kQueries;
+        float top = kLowest;
+        if (r < rows) {
+#pragma unroll 4
+            for (int i = j; i < parts; i += kThreads / kQueries) top = fmaxf(top, part(i)[a.rows * a.dim + r * 2]);
         }
-        a.out.template at<T>(s, int64_t(head) * a.group + group0 + r)[d] = T(sum == 0 ? 0.0f : value / sum);
+        tops[r][j] = top;
+    }
+    __syncthreads();
+    const int vectors = rows * (a.dim / 4), groups = max(1, kThreads / vectors);
+    for (int e0 = 0; e0 < vectors; e0 += kThreads) {
+        const int group = threadIdx.x / min(vectors, kThreads), e = e0 + threadIdx.x - group * min(vectors, kThreads);
+        const int r = e / (a.dim / 4), d = (e - r * (a.dim / 4)) * 4;
+        f32x4 value{0, 0, 0, 0};
+        float sum = 0;
+        if (group < groups && e < vectors) {
+            float top = tops[r][0];
+#pragma unroll
+            for (int j = 1; j < kThreads / kQueries; ++j) top = fmaxf(top, tops[r][j]);
+#pragma unroll 4
+            for (int i = group; i < parts; i += groups) {
+                const float *from = part(i);
+                const float2 stat = load_any<float2>(from + a.rows * a.dim + r * 2);
+                const f32x4 x = load_any<f32x4>(from + r * a.dim + d);
+                const float f = __builtin_amdgcn_exp2f(stat.x - top);
+                sum = fmaf(f, stat.y, sum);
+#pragma unroll
+                for (int c = 0; c < 4; ++c) value[c] = fmaf(f, x[c], value[c]);
+            }
+        }
+        if (groups > 1) {  // then all vectors are in one round
+            shared_value[threadIdx.x] = value;
+            shared_sum[threadIdx.x] = sum;
+            __syncthreads();
+            if (group == 0) {
+                for (int g = 1; g < groups; ++g) {
+                    value += shared_value[g * vectors + threadIdx.x];
+                    sum += shared_sum[g * vectors + threadIdx.x];
+                }
+            }
+        }
+        if (group == 0 && e < vectors) {
+            T *to = a.out.template at<T>(s, int64_t(head) * a.group + group0 + r) + d;
+#pragma unroll
+            for (int c = 0; c < 4; ++c) to[c] = T(sum == 0 ? 0.0f : value[c] / sum);
+        }
     }
 }
 
-// Two workgroups a CU, or one a tile where there are fewer.
+// Two workgroups a CU, or a wave a tile where there are fewer.
 int64_t workgroups_of(int64_t sequences, int64_t kv_heads, int64_t passes, int64_t slots) {
-    const int64_t tiles = ceil_div(slots, kTileKeys), most = 512;
+    const int64_t tiles = ceil_div(slots, kTile), most = 512;
     if (tiles == 0) return 1;
-    return std::max<int64_t>(1, tiles >= most ? most : std::min(most, sequences * kv_heads * passes * tiles));
+    return std::max<int64_t>(1, tiles >= most * kWaves
+                                    ? most
+                                    : std::min(most, ceil_div(sequences * kv_heads * passes * tiles, kWaves)));
 }
 
 }  // namespace
@@ -332,7 +369,7 @@ extern "C" int64_t reshard_attention_paged_workspace(int64_t sequences, int64_t 
         return -1;
     const int64_t group = heads / kv_heads, passes = ceil_div(group, kQueries);
     const int64_t n = workgroups_of(sequences, kv_heads, passes, pages_a_sequence * page_length);
-    return (sequences + 2) / 2 * 16 + n * 2 * std::min<int64_t>(group, kQueries) * (dim + 2) * 4;
+    return (sequences + 2) / 2 * 16 + n * kWaves * 2 * std::min<int64_t>(group, kQueries) * (dim + 2) * 4;
 }
 
 extern "C" reshard_status_t reshard_attention_paged(int64_t sequences, int64_t heads, int64_t kv_heads, int64_t dim,
@@ -398,7 +435,7 @@ extern "C" reshard_status_t reshard_attention_paged(int64_t sequences, int64_t h
             reshard_status_t status = launch("paged attention launch", kernel, dim3(n), kThreads, 0, s, a);
             if (status != RESHARD_OK) return status;
             return launch("paged attention join launch", paged_join_kernel<T>,
-                          dim3(unsigned(sequences * kv_heads * passes)), kThreads, 0, s, a, n);
+                          dim3(unsigned(sequences * kv_heads * passes)), kThreads, 0, s, a, n * kWaves);
         };
         return dtype == RESHARD_BF16 ? go(bf16{}) : go(f16{});
     });
