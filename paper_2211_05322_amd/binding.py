@@ -13,6 +13,7 @@ from __future__ import annotations
 import contextlib
 import ctypes
 import os
+import struct
 from typing import NamedTuple
 
 PKG = os.path.dirname(os.path.abspath(__file__))
@@ -155,7 +156,7 @@ def _declare_operators(lib):
     lib.reshard_matmul_workspace.restype = i64
     lib.reshard_matmul.argtypes = [i64, i64, i64, vp, i64, ci, vp, i64, vp, i64, ci, vp, i64, ci, vp, i64, ci, ci,
                                    vp, i64, vp]
-    hp, cp, f64 = ctypes.POINTER(reshard_heads_t), ctypes.POINTER(reshard_cache_t), ctypes.c_double
+    hp, cp, f64 = vp, vp, ctypes.c_double  # reshard_heads_t and reshard_cache_t: the address, or their bytes
     turned = [i64] * 5 + [ci, ci]
     lib.reshard_rotate_heads.argtypes = [*turned, hp, hp, vp, vp, ci, f64, vp, vp, hp, hp, hp, cp, vp, vp]
     lib.reshard_rotate_heads_backward_workspace.argtypes = [i64] * 4
@@ -715,26 +716,40 @@ def reshard_matmul(a, b, out_dtype=None, out=None, accumulate=False, stream=None
 
 # ------------------------------------------------- operators of attention
 
-def _heads(name, t):
-    """(tokens, heads, dim, reshard_heads_t) of a tensor [tokens, heads, dim] whose last dimension is dense."""
+_pack_heads = struct.Struct("Pqq").pack  # reshard_heads_t
+_pack_cache = struct.Struct("PPqqqqq").pack  # reshard_cache_t
+
+
+def _heads(name, t, shape, beside):
+    """reshard_heads_t (as bytes: a ctypes object takes four times as long to make) of a tensor that must have this
+    shape, with its last dimension dense, and the type and device of `beside`."""
+    if t.shape != shape or t.dtype != beside.dtype or t.get_device() != beside.get_device():
+        raise ValueError(f"{name} must be {beside.dtype} {tuple(shape)} on {beside.device}, "
+                         f"got {t.dtype} {tuple(t.shape)} on {t.device}")
+    token, head, last = t.stride()
+    if last != 1 and shape[2] > 1:
+        raise ValueError(f"{name}: the last dimension must be dense, its stride is {last}")
+    return _pack_heads(t.data_ptr(), token, head)
+
+
+def _three(name, t):
     if t.dim() != 3:
         raise ValueError(f"{name} must be [tokens, heads, dim], got {tuple(t.shape)}")
-    (tokens, heads, dim), strides = t.shape, t.stride()
-    if dim > 1 and strides[2] != 1:
-        raise ValueError(f"{name}: the last dimension must be dense, its stride is {strides[2]}")
-    return tokens, heads, dim, reshard_heads_t(t.data_ptr(), strides[0], strides[1])
+    return t.shape
 
 
-def _heads_like(name, t, shape, beside):
-    """reshard_heads_t of a tensor that must have this shape, and the type and device of `beside`."""
-    return _heads(name, _like(name, t, shape, beside.dtype, beside.device))[3]
-
-
-def _here(name, t):
-    """Kernels run on the current device, so that is where tensors must be."""
-    _on_gpu(name, t)
-    if t.get_device() != _torch.cuda.current_device():
-        raise ValueError(f"{name} is on {t.device}, the current device is cuda:{_torch.cuda.current_device()}")
+def _here(name, t, stream):
+    """The stream's handle.  Kernels run on the current device, so that is where tensors must be."""
+    device = t.get_device()
+    if device < 0:
+        raise ValueError(f"{name} must be on the GPU, got {t.device}")
+    try:
+        current = _torch._C._cuda_getDevice()
+    except AttributeError:  # a torch without these private functions
+        current = _torch.cuda.current_device()
+    if device != current:
+        raise ValueError(f"{name} is on {t.device}, the current device is cuda:{current}")
+    return _stream_handle(stream)
 
 
 def _numbers(name, t, shape, beside):
@@ -746,19 +761,22 @@ def _cache(cache, kv_heads, dim, beside):
     keys, values = cache
     if keys.dim() != 4 or keys.shape[2:] != (kv_heads, dim):
         raise ValueError(f"cache must be [pages, page_length, {kv_heads}, {dim}], got {tuple(keys.shape)}")
-    for name, t in (("the cache's keys", keys), ("the cache's values", values)):
-        _like(name, t, keys.shape, beside.dtype, beside.device)
+    for name, t in (("keys", keys), ("values", values)):
+        if t.shape != keys.shape or t.dtype != beside.dtype or t.get_device() != beside.get_device():
+            raise ValueError(f"the cache's {name} must be {beside.dtype} {tuple(keys.shape)} on {beside.device}, "
+                             f"got {t.dtype} {tuple(t.shape)} on {t.device}")
     if keys.stride() != values.stride() or dim > 1 and keys.stride(3) != 1:
         raise ValueError(f"the cache's keys and values must be laid out alike, with dense heads, "
                          f"their strides are {keys.stride()} and {values.stride()}")
-    return reshard_cache_t(keys.data_ptr(), values.data_ptr(), keys.shape[0], keys.shape[1], *keys.stride()[:3])
+    page, slot, head, _ = keys.stride()
+    return _pack_cache(keys.data_ptr(), values.data_ptr(), keys.shape[0], keys.shape[1], page, slot, head)
 
 
 def _rotation(q, k, q_weight, k_weight, frequencies, positions):
     """What both passes check: (tokens, heads, kv_heads, dim, rotary), q, k and the weights' type."""
-    tokens, heads, dim, q_at = _heads("q", q)
-    kv_heads = k.shape[1] if k.dim() == 3 else -1
-    k_at = _heads_like("k", k, (tokens, kv_heads, dim), q)
+    tokens, heads, dim = _three("q", q)
+    kv_heads = _three("k", k)[1]
+    q_at, k_at = _heads("q", q, q.shape, q), _heads("k", k, (tokens, kv_heads, dim), q)
     weight = q_weight if q_weight is not None else k_weight if k_weight is not None else q
     for name, w in (("q_weight", q_weight), ("k_weight", k_weight)):
         if w is not None:
@@ -790,19 +808,19 @@ def reshard_rotate_heads(q, k, q_weight=None, k_weight=None, eps=1e-6, frequenci
         raise ValueError("keys go to the cache or to k_out, not to both")
     v_at = cache_at = None
     if cache is not None:
-        v_at = _heads_like("v", v, k.shape, q)
+        v_at = _heads("v", v, k.shape, q)
         cache_at = _cache(cache, kv_heads, dim, q)
         _numbers("slots", slots, (tokens,), q)
-    _here("q", q)
+    handle = _here("q", q, stream)
     with _on(stream):
         q_out = q.new_empty(q.shape) if q_out is None else q_out
         if cache is None and k_out is None:
             k_out = k.new_empty(k.shape)
-    qo_at = _heads_like("q_out", q_out, q.shape, q)
-    ko_at = None if cache is not None else _heads_like("k_out", k_out, k.shape, q)
+    qo_at = _heads("q_out", q_out, q.shape, q)
+    ko_at = None if cache is not None else _heads("k_out", k_out, k.shape, q)
     status = lib.reshard_rotate_heads(*sizes, int(bool(interleaved)), _dtype_code(q.dtype), q_at, k_at, _ptr(q_weight),
                                       _ptr(k_weight), wdt, eps, _ptr(frequencies), _ptr(positions), qo_at, ko_at, v_at,
-                                      cache_at, _ptr(slots), _stream_handle(stream))
+                                      cache_at, _ptr(slots), handle)
     if status != RESHARD_OK:
         _check(status)
     return q_out, k_out
@@ -816,11 +834,11 @@ def reshard_rotate_heads_backward(dq_out, dk_out, q, k, q_weight=None, k_weight=
     lib = _lib or load()
     sizes, q_at, k_at, wdt = _rotation(q, k, q_weight, k_weight, frequencies, positions)
     tokens, heads, kv_heads, dim, _ = sizes
-    dqo_at = _heads_like("dq_out", dq_out, q.shape, q)
-    dko_at = _heads_like("dk_out", dk_out, k.shape, q)
+    dqo_at = _heads("dq_out", dq_out, q.shape, q)
+    dko_at = _heads("dk_out", dk_out, k.shape, q)
     if accumulate and (dq_weight is None or dk_weight is None):
         raise ValueError("accumulate needs the dq_weight and dk_weight to add to")
-    _here("q", q)
+    handle = _here("q", q, stream)
     need = lib.reshard_rotate_heads_backward_workspace(tokens, heads, kv_heads, dim)
     with _on(stream):
         dq = q.new_empty(q.shape) if dq is None else dq
@@ -828,32 +846,32 @@ def reshard_rotate_heads_backward(dq_out, dk_out, q, k, q_weight=None, k_weight=
         dq_weight = q.new_empty(dim, dtype=_torch.float32) if dq_weight is None else dq_weight
         dk_weight = q.new_empty(dim, dtype=_torch.float32) if dk_weight is None else dk_weight
         work = q.new_empty(max(0, need), dtype=_torch.uint8)
-    dq_at, dk_at = _heads_like("dq", dq, q.shape, q), _heads_like("dk", dk, k.shape, q)
+    dq_at, dk_at = _heads("dq", dq, q.shape, q), _heads("dk", dk, k.shape, q)
     _dense("dq_weight", dq_weight, (dim,), q, _torch.float32)
     _dense("dk_weight", dk_weight, (dim,), q, _torch.float32)
     status = lib.reshard_rotate_heads_backward(
         *sizes, int(bool(interleaved)), _dtype_code(q.dtype), dqo_at, dko_at, q_at, k_at, _ptr(q_weight), _ptr(k_weight),
         wdt, eps, _ptr(frequencies), _ptr(positions), dq_at, dk_at, dq_weight.data_ptr(), dk_weight.data_ptr(),
-        int(bool(accumulate)), work.data_ptr(), max(0, need), _stream_handle(stream))
+        int(bool(accumulate)), work.data_ptr(), max(0, need), handle)
     if status != RESHARD_OK:
         _check(status)
     return dq, dk, dq_weight, dk_weight
 
 
-def _packed(q, k, v, q_offsets, k_offsets, scale):
-    """(sizes, q, k, v, scale) of attention over packed sequences, checked."""
-    q_tokens, heads, dim, q_at = _heads("q", q)
-    if k.dim() != 3 or k.shape[2] != dim:
+def _packed(q, k, v, q_offsets, k_offsets, scale, stream):
+    """(sizes, q, k, v, scale, the stream's handle) of attention over packed sequences, checked."""
+    q_tokens, heads, dim = _three("q", q)
+    k_tokens, kv_heads, k_dim = _three("k", k)
+    if k_dim != dim:
         raise ValueError(f"k must be [tokens, kv_heads, {dim}], got {tuple(k.shape)}")
-    k_at = _heads_like("k", k, k.shape, q)
-    v_at = _heads_like("v", v, k.shape, q)
+    q_at, k_at, v_at = _heads("q", q, q.shape, q), _heads("k", k, k.shape, q), _heads("v", v, k.shape, q)
     n = q_offsets.numel()
     if n < 1:
         raise ValueError("q_offsets must hold one number more than there are sequences")
     _numbers("q_offsets", q_offsets, (n,), q)
     _numbers("k_offsets", k_offsets, (n,), q)
-    _here("q", q)
-    return (q_tokens, k.shape[0], n - 1, heads, k.shape[1], dim), q_at, k_at, v_at, dim ** -0.5 if scale is None else scale
+    return ((q_tokens, k_tokens, n - 1, heads, kv_heads, dim), q_at, k_at, v_at, dim ** -0.5 if scale is None else scale,
+            _here("q", q, stream))
 
 
 def reshard_attention(q, k, v, q_offsets, k_offsets, scale=None, causal=True, out=None, lse=None, stream=None):
@@ -864,15 +882,15 @@ def reshard_attention(q, k, v, q_offsets, k_offsets, scale=None, causal=True, ou
     dim ** -0.5 by default.  lse [heads, q_tokens] float32 is for the backward pass.  Rows that are no sequence's keep
     what a given out holds there."""
     lib = _lib or load()
-    sizes, q_at, k_at, v_at, scale = _packed(q, k, v, q_offsets, k_offsets, scale)
+    sizes, q_at, k_at, v_at, scale, handle = _packed(q, k, v, q_offsets, k_offsets, scale, stream)
     with _on(stream):
         out = q.new_empty(q.shape) if out is None else out
         lse = q.new_empty((sizes[3], sizes[0]), dtype=_torch.float32) if lse is None else lse
-    out_at = _heads_like("out", out, q.shape, q)
+    out_at = _heads("out", out, q.shape, q)
     _dense("lse", lse, (sizes[3], sizes[0]), q, _torch.float32)
     status = lib.reshard_attention(*sizes, _dtype_code(q.dtype), q_at, k_at, v_at, q_offsets.data_ptr(),
                                    k_offsets.data_ptr(), scale, int(bool(causal)), out_at, lse.data_ptr(),
-                                   _stream_handle(stream))
+                                   handle)
     if status != RESHARD_OK:
         _check(status)
     return out, lse
@@ -883,8 +901,8 @@ def reshard_attention_backward(dout, q, k, v, out, lse, q_offsets, k_offsets, sc
     """(dq, dk, dv) of reshard_attention, whose out and lse these are, with its other arguments.  Rows that are no
     sequence's keep what a given result holds there."""
     lib = _lib or load()
-    sizes, q_at, k_at, v_at, scale = _packed(q, k, v, q_offsets, k_offsets, scale)
-    dout_at, out_at = _heads_like("dout", dout, q.shape, q), _heads_like("out", out, q.shape, q)
+    sizes, q_at, k_at, v_at, scale, handle = _packed(q, k, v, q_offsets, k_offsets, scale, stream)
+    dout_at, out_at = _heads("dout", dout, q.shape, q), _heads("out", out, q.shape, q)
     _dense("lse", lse, (sizes[3], sizes[0]), q, _torch.float32)
     need = lib.reshard_attention_backward_workspace(sizes[0], sizes[3])
     with _on(stream):
@@ -892,11 +910,11 @@ def reshard_attention_backward(dout, q, k, v, out, lse, q_offsets, k_offsets, sc
         dk = k.new_empty(k.shape) if dk is None else dk
         dv = k.new_empty(k.shape) if dv is None else dv
         work = q.new_empty(max(0, need), dtype=_torch.uint8)
-    dq_at, dk_at, dv_at = (_heads_like(*x, q) for x in (("dq", dq, q.shape), ("dk", dk, k.shape), ("dv", dv, k.shape)))
+    dq_at, dk_at, dv_at = (_heads(*x, q) for x in (("dq", dq, q.shape), ("dk", dk, k.shape), ("dv", dv, k.shape)))
     status = lib.reshard_attention_backward(
         *sizes, _dtype_code(q.dtype), dout_at, q_at, k_at, v_at, out_at, lse.data_ptr(), q_offsets.data_ptr(),
         k_offsets.data_ptr(), scale, int(bool(causal)), dq_at, dk_at, dv_at, work.data_ptr(), max(0, need),
-        _stream_handle(stream))
+        handle)
     if status != RESHARD_OK:
         _check(status)
     return dq, dk, dv
@@ -906,7 +924,8 @@ def reshard_attention_paged(q, k_cache, v_cache, pages, lengths, scale=None, out
     """Attention of one token of each sequence, q [sequences, heads, dim], over a cache in pages [pages, page_length,
     kv_heads, dim].  Token t of sequence s, t < lengths[s], lies in page pages[s, t // page_length] (int32)."""
     lib = _lib or load()
-    n, heads, dim, q_at = _heads("q", q)
+    n, heads, dim = _three("q", q)
+    q_at = _heads("q", q, q.shape, q)
     kv_heads = k_cache.shape[2] if k_cache.dim() == 4 else -1
     cache_at = _cache((k_cache, v_cache), kv_heads, dim, q)
     if pages.dim() != 2 or pages.shape[0] != n or pages.dtype != _torch.int32 or pages.device != q.device or (
@@ -914,16 +933,16 @@ def reshard_attention_paged(q, k_cache, v_cache, pages, lengths, scale=None, out
         raise ValueError(f"pages must be int32 [{n}, pages of a sequence] on {q.device} with dense rows, "
                          f"got {pages.dtype} {tuple(pages.shape)}, strides {pages.stride()}, on {pages.device}")
     _numbers("lengths", lengths, (n,), q)
-    _here("q", q)
+    handle = _here("q", q, stream)
     need = lib.reshard_attention_paged_workspace(n, heads, kv_heads, dim, pages.shape[1], k_cache.shape[1])
     with _on(stream):
         out = q.new_empty(q.shape) if out is None else out
         work = q.new_empty(max(0, need), dtype=_torch.uint8)
-    out_at = _heads_like("out", out, q.shape, q)
+    out_at = _heads("out", out, q.shape, q)
     status = lib.reshard_attention_paged(n, heads, kv_heads, dim, _dtype_code(q.dtype), q_at, cache_at, pages.data_ptr(),
                                          pages.shape[1], pages.stride(0), lengths.data_ptr(),
                                          dim ** -0.5 if scale is None else scale, out_at, work.data_ptr(), max(0, need),
-                                         _stream_handle(stream))
+                                         handle)
     if status != RESHARD_OK:
         _check(status)
     return out

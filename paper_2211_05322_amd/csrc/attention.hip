@@ -13,7 +13,7 @@
 namespace rs {
 namespace {
 
-constexpr int kThreads = 256, kWaves = kThreads / kWave, kKeys = 64;
+constexpr int kThreads = 256, kWaves = kThreads / kWave;
 
 struct PromptArgs {
     Heads q, k, v, out;
@@ -32,11 +32,10 @@ struct PromptArgs {
 // leave the sums as they are.
 template <typename T, int DP, int QB, bool ASYNC>
 __global__ __launch_bounds__(kThreads, QB == 1 ? 2 : 1) void attention_kernel(PromptArgs a) {
-    constexpr int STEPS = DP / 16, BLOCKS = DP / 32, ROWS = 32 * QB * kWaves;
-    constexpr int SHIFT = QB == 1 ? 7 : 8;
-    // four arrays by name: only so does the compiler see that loads into one pair leave the other alone
-    __shared__ uint4 k0[kKeys * TileShape<DP>::words], v0[kKeys * TileShape<DP>::words];
-    __shared__ uint4 k1[kKeys * TileShape<DP>::words], v1[kKeys * TileShape<DP>::words];
+    constexpr int STEPS = DP / 16, BLOCKS = DP / 32, ROWS = 32 * QB * kWaves, KEYS = 64, PARTS = KEYS / 32;
+    constexpr int SHIFT = QB == 1 ? 7 : 8, WORDS = KEYS * TileShape<DP>::words;
+    // arrays by name: only so does the compiler see that loads into one leave the others alone
+    __shared__ uint4 k0[WORDS], v0[WORDS], k1[WORDS], v1[WORDS];
     const Task task = task_of(blockIdx.x, a.blocks, a.heads, a.group);
     Sequence s;
     if (!ranked_sequence(a.seq, false, a.causal, a.blocks, task.block, SHIFT, &s)) return;
@@ -69,47 +68,48 @@ __global__ __launch_bounds__(kThreads, QB == 1 ? 2 : 1) void attention_kernel(Pr
 #pragma unroll
         for (int d = 0; d < BLOCKS; ++d) o[b][d] = zero16();
     }
-    TileLoader<T, DP, kKeys, kThreads, ASYNC> kl(threadIdx.x, a.dim, a.k.token_pitch), vl(threadIdx.x, a.dim, a.v.token_pitch);
-    if (to > 0) {
-        kl.start(k, s.lk, k0);
-        vl.start(v, s.lk, v0);
-        kl.finish(k0);
-        vl.finish(v0);
-    }
-    __syncthreads();
+    TileLoader<T, DP, KEYS, kThreads, ASYNC> kl(threadIdx.x, a.dim, a.k.token_pitch), vl(threadIdx.x, a.dim, a.v.token_pitch);
+    // a tile behind the last is asked for too, and is zeros without a read
+    const int64_t k_step = KEYS * a.k.token_pitch, v_step = KEYS * a.v.token_pitch;
+    auto load = [&](int key0, auto &k_to, auto &v_to) {
+        kl.start(k, s.lk - key0, k_to);
+        vl.start(v, s.lk - key0, v_to);
+        k += k_step;
+        v += v_step;
+    };
     auto step = [&](int key0, const auto &kt, const auto &vt, auto &k_next, auto &v_next) {
-        const bool more = key0 + kKeys < to;
-        if (more) {
-            kl.start(k + (key0 + kKeys) * a.k.token_pitch, s.lk - key0 - kKeys, k_next);
-            vl.start(v + (key0 + kKeys) * a.v.token_pitch, s.lk - key0 - kKeys, v_next);
-        }
+        if constexpr (ASYNC) loads_done();
+        __syncthreads();
+        load(key0 + KEYS, k_next, v_next);
         if (key0 < wave_to) {
-            f32x16 x[QB][2];
+            f32x16 x[QB][PARTS];
 #pragma unroll
-            for (int b = 0; b < QB; ++b) x[b][0] = x[b][1] = zero16();
+            for (int b = 0; b < QB; ++b)
+#pragma unroll
+                for (int n = 0; n < PARTS; ++n) x[b][n] = zero16();
 #pragma unroll
             for (int i = 0; i < STEPS; ++i)
 #pragma unroll
-                for (int n = 0; n < 2; ++n) {
+                for (int n = 0; n < PARTS; ++n) {
                     const Operand8<T> kk = row_operand<T, DP>(kt, n * 32, i, places);
 #pragma unroll
                     for (int b = 0; b < QB; ++b) x[b][n] = mfma(kk, q[b][i], x[b][n]);
                 }
-            if (key0 + kKeys > all_see || key0 + kKeys > s.lk) {
+            if (key0 + KEYS > all_see || key0 + KEYS > s.lk) {
 #pragma unroll
                 for (int b = 0; b < QB; ++b)
 #pragma unroll
-                    for (int n = 0; n < 2; ++n)
+                    for (int n = 0; n < PARTS; ++n)
 #pragma unroll
                         for (int r = 0; r < 16; ++r)
                             if (key0 + n * 32 + result_row(r, half) > last[b]) x[b][n][r] = -INFINITY;
             }
-            Operand8<T> p[QB][4];
+            Operand8<T> p[QB][2 * PARTS];
 #pragma unroll
             for (int b = 0; b < QB; ++b) {
                 float top = x[b][0][0];
 #pragma unroll
-                for (int n = 0; n < 2; ++n)
+                for (int n = 0; n < PARTS; ++n)
 #pragma unroll
                     for (int r = 0; r < 16; ++r) top = fmaxf(top, x[b][n][r]);
                 top = halves_max(top) * a.scale2;
@@ -124,7 +124,7 @@ __global__ __launch_bounds__(kThreads, QB == 1 ? 2 : 1) void attention_kernel(Pr
                 }
                 float sum = 0;
 #pragma unroll
-                for (int n = 0; n < 2; ++n)
+                for (int n = 0; n < PARTS; ++n)
 #pragma unroll
                     for (int r = 0; r < 16; ++r) {
                         const float e = exp2_fast(fmaf(x[b][n][r], a.scale2, -m[b]));
@@ -134,7 +134,7 @@ __global__ __launch_bounds__(kThreads, QB == 1 ? 2 : 1) void attention_kernel(Pr
                 l[b] += sum;
             }
 #pragma unroll
-            for (int t = 0; t < 4; ++t)
+            for (int t = 0; t < 2 * PARTS; ++t)
 #pragma unroll
                 for (int d = 0; d < BLOCKS; ++d) {
                     const Operand8<T> vv = column_operand<T, DP>(vt, t * 16, d, places);
@@ -142,16 +142,21 @@ __global__ __launch_bounds__(kThreads, QB == 1 ? 2 : 1) void attention_kernel(Pr
                     for (int b = 0; b < QB; ++b) o[b][d] = mfma(vv, p[b][t], o[b][d]);
                 }
         }
-        if (more) {
-            kl.finish(k_next);
-            vl.finish(v_next);
+        if constexpr (!ASYNC) {
+            kl.write(k_next);
+            vl.write(v_next);
         }
-        __syncthreads();
     };
-    for (int key0 = 0; key0 < to; key0 += 2 * kKeys) {
-        step(key0, k0, v0, k1, v1);
-        if (key0 + kKeys < to) step(key0 + kKeys, k1, v1, k0, v0);
+    if (to > 0) {
+        load(0, k0, v0);
+        kl.write(k0);
+        vl.write(v0);
     }
+    for (int key0 = 0; key0 < to; key0 += 2 * KEYS) {
+        step(key0, k0, v0, k1, v1);
+        if (key0 + KEYS < to) step(key0 + KEYS, k1, v1, k0, v0);
+    }
+    loads_done();  // none may write into LDS that is another workgroup's by then
 #pragma unroll
     for (int b = 0; b < QB; ++b) {
         const int row = row0 + b * 32 + lane % 32;

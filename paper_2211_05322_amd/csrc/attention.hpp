@@ -13,6 +13,7 @@
 #pragma once
 
 #include <algorithm>
+#include <utility>
 
 #include "heads.hpp"
 
@@ -123,6 +124,12 @@ __device__ inline Operand8<T> column_operand(const uint4 *tile, int row, int blo
     return o;
 }
 
+// 4 bytes of a lane's straight into LDS, as load_to_lds does 16.
+__device__ inline void load_word_to_lds(__amdgpu_buffer_rsrc_t base, uint32_t offset, float *to) {
+    __builtin_amdgcn_raw_ptr_buffer_load_lds(base, (__attribute__((address_space(3))) void *)to, 4, offset, 0, 0, 0);
+}
+
+
 // Brings ROWS rows of a head into LDS, a word a thread and turn.  Rows past the
 // sequence's end and elements from dim on become zeros.  Where rows start on
 // 16-byte boundaries (ASYNC) words go to LDS by themselves, to be waited for;
@@ -136,7 +143,7 @@ struct TileLoader {
     static_assert(words % THREADS == 0 && rows_a_turn % 16 == 0, "a thread's word has one place in every turn");
     uint4 held[ASYNC ? 1 : turns];
     int row, word;
-    uint32_t offset, next;
+    uint32_t offset, next, row_bytes, last_bytes;
     int64_t pitch;  // elements
     int dim;
 
@@ -146,11 +153,13 @@ struct TileLoader {
         // past every range: gives zeros
         offset = word * 8 < dim ? uint32_t(row * pitch * int64_t(sizeof(T))) + word * 16 : 0x80000000u;
         next = uint32_t(rows_a_turn * pitch * int64_t(sizeof(T)));
+        row_bytes = uint32_t(pitch * int64_t(sizeof(T)));
+        last_bytes = uint32_t(dim * sizeof(T));
     }
     __device__ void start(const T *base, int rows, uint4 *lds) {
         if constexpr (ASYNC) {
             const __amdgpu_buffer_rsrc_t from =
-                bytes_from(base, rows > 0 ? ((min(rows, ROWS) - 1) * pitch + dim) * int64_t(sizeof(T)) : 0);
+                bytes_from(base, rows > 0 ? uint32_t(min(rows, ROWS) - 1) * row_bytes + last_bytes : 0u);
             const int wave = __builtin_amdgcn_readfirstlane(int(threadIdx.x) / kWave);
 #pragma unroll
             for (int u = 0; u < turns; ++u) load_to_lds(from, offset + u * next, lds + u * THREADS + wave * kWave);
@@ -167,11 +176,41 @@ struct TileLoader {
         if constexpr (ASYNC) {
             loads_done();
         } else {
+            write(lds);
+        }
+    }
+    __device__ void write(uint4 *lds) {  // what start left in registers
+        if constexpr (!ASYNC) {
 #pragma unroll
             for (int u = 0; u < turns; ++u) lds[u * THREADS + threadIdx.x] = held[u];
         }
     }
 };
+
+template <typename F, int... I>
+__device__ inline void unrolled_(F &&f, std::integer_sequence<int, I...>) {
+    (f(std::integral_constant<int, I>{}), ...);
+}
+template <int N, typename F>
+__device__ inline void unrolled(F &&f) {
+    unrolled_(f, std::make_integer_sequence<int, N>{});
+}
+
+// N steps of matrix instructions, use(i), whose operands read(i) brings from LDS
+// a step ahead: by itself the compiler reads an operand right before its
+// instruction and waits for it, or reads all at once and spills.  With BEGUN the
+// first step's were read before.
+template <int N, bool BEGUN = false, typename R, typename U>
+__device__ inline void pipelined(R &&read, U &&use) {
+    if constexpr (!BEGUN) read(std::integral_constant<int, 0>{});
+    unrolled<N>([&](auto i_) {
+        constexpr int i = decltype(i_)::value;
+        if constexpr (i + 1 < N) read(std::integral_constant<int, i + 1>{});
+        __builtin_amdgcn_sched_barrier(0);
+        use(i_);
+        __builtin_amdgcn_sched_barrier(0);
+    });
+}
 
 // A wave's operand straight from memory: lane l's 8 elements of row l % 32.
 template <typename T>

@@ -24,7 +24,7 @@ constexpr int kThreads = 256, kRows = 128, kShift = 7;
 struct GradArgs {
     Heads dout, q, k, v, out, dq, dk, dv;
     const float *lse;  // [heads][q_tokens]
-    float2 *row;       // [heads][q_tokens]: lse * log2(e), infinite where a query sees no key; delta
+    float *minus_lse, *minus_delta;  // [heads][q_tokens]: what the second kernel adds to exponents and to dP
     Sequences seq;
     int heads, group, dim, causal;
     uint32_t blocks;
@@ -92,40 +92,59 @@ __global__ __launch_bounds__(kThreads, 2) void attention_dq_kernel(GradArgs a) {
     const int64_t stat = int64_t(task.head) * a.seq.q_tokens + s.q0 + held;
     float lse2 = a.lse[stat] * kLog2e;
     if (lse2 == -INFINITY) lse2 = INFINITY;
-    if (half == 0 && row < s.lq) a.row[stat] = make_float2(lse2, delta);
+    if (half == 0 && row < s.lq) {
+        a.minus_lse[stat] = kRaised<T> - lse2;
+        a.minus_delta[stat] = -delta;
+    }
     const int last = a.causal ? held + s.lk - s.lq : s.lk - 1;
     const int to = a.causal ? min(s.lk, min(s.lq, (s.block + 1) * kRows) + s.lk - s.lq) : s.lk;
     const int wave_to = a.causal ? min(s.lk, min(s.lq, row0 + 32) + s.lk - s.lq) : s.lk;
     const int all_see = a.causal ? row0 + 1 + s.lk - s.lq : s.lk;
 
     const LanePlaces places = LanePlaces::of<DP>(lane);
-    f32x16 dq[BLOCKS];
+    f32x16 dq[BLOCKS], below;  // -delta: what dP - delta is summed from
+#pragma unroll
+    for (int r = 0; r < 16; ++r) below[r] = -delta;
 #pragma unroll
     for (int d = 0; d < BLOCKS; ++d) dq[d] = zero16();
     float factor = kFirstFactor;
     TileLoader<T, DP, KEYS, kThreads, ASYNC> kl(threadIdx.x, a.dim, a.k.token_pitch), vl(threadIdx.x, a.dim, a.v.token_pitch);
+    const int64_t k_step = KEYS * a.k.token_pitch, v_step = KEYS * a.v.token_pitch;
+    auto load = [&](int key0, auto &k_to, auto &v_to) {
+        kl.start(k, s.lk - key0, k_to);
+        vl.start(v, s.lk - key0, v_to);
+        k += k_step;
+        v += v_step;
+    };
     if (to > 0) {
-        kl.start(k, s.lk, k0);
-        vl.start(v, s.lk, v0);
+        load(0, k0, v0);
         kl.finish(k0);
         vl.finish(v0);
     }
     __syncthreads();
     auto step = [&](int key0, const auto &kt, const auto &vt, auto &k_next, auto &v_next) {
         const bool more = key0 + KEYS < to;
-        if (more) {
-            kl.start(k + (key0 + KEYS) * a.k.token_pitch, s.lk - key0 - KEYS, k_next);
-            vl.start(v + (key0 + KEYS) * a.v.token_pitch, s.lk - key0 - KEYS, v_next);
-        }
+        if (more) load(key0 + KEYS, k_next, v_next);
 #pragma unroll
         for (int n = 0; n < 2; ++n) {
             if (key0 + n * 32 >= wave_to) continue;
-            f32x16 x = zero16(), dp = zero16();
-#pragma unroll
-            for (int i = 0; i < STEPS; ++i) {
-                x = mfma(row_operand<T, DP>(kt, n * 32, i, places), q[i], x);
-                dp = mfma(row_operand<T, DP>(vt, n * 32, i, places), dout[i], dp);
-            }
+            f32x16 x = zero16(), dp = below;
+            Operand8<T> left[2][2];
+            pipelined<STEPS>(
+                [&](auto i) {
+                    left[i % 2][0] = row_operand<T, DP>(kt, n * 32, i, places);
+                    left[i % 2][1] = row_operand<T, DP>(vt, n * 32, i, places);
+                },
+                [&](auto i) {
+                    x = mfma(left[i % 2][0], q[i], x);
+                    dp = mfma(left[i % 2][1], dout[i], dp);
+                });
+            // pairs of steps over the keys: a column block at once
+            auto read_columns = [&](auto i) {
+                left[i % 2][0] = column_operand<T, DP>(kt, n * 32, i, places);
+                left[i % 2][1] = column_operand<T, DP>(kt, n * 32 + 16, i, places);
+            };
+            read_columns(std::integral_constant<int, 0>{});
             if (key0 + n * 32 + 32 > all_see || key0 + n * 32 + 32 > s.lk) {
 #pragma unroll
                 for (int r = 0; r < 16; ++r)
@@ -133,14 +152,13 @@ __global__ __launch_bounds__(kThreads, 2) void attention_dq_kernel(GradArgs a) {
             }
 #pragma unroll
             for (int r = 0; r < 16; ++r)
-                x[r] = __builtin_amdgcn_exp2f(fmaf(x[r], a.scale2, -lse2)) * (dp[r] - delta);
+                x[r] = __builtin_amdgcn_exp2f(fmaf(x[r], a.scale2, -lse2)) * dp[r];
             Operand8<T> ds[2];
             round_scores<T>(x, factor, dq, ds);
-#pragma unroll
-            for (int t = 0; t < 2; ++t)
-#pragma unroll
-                for (int d = 0; d < BLOCKS; ++d)
-                    dq[d] = mfma(column_operand<T, DP>(kt, n * 32 + t * 16, d, places), ds[t], dq[d]);
+            pipelined<BLOCKS, true>(read_columns, [&](auto i) {
+                dq[i] = mfma(left[i % 2][0], ds[0], dq[i]);
+                dq[i] = mfma(left[i % 2][1], ds[1], dq[i]);
+            });
         }
         if (more) {
             kl.finish(k_next);
@@ -158,26 +176,31 @@ __global__ __launch_bounds__(kThreads, 2) void attention_dq_kernel(GradArgs a) {
     for (int d = 0; d < BLOCKS; ++d) store_columns(to_row, row < s.lq, dq[d], scale, d, lane, a.dim);
 }
 
-// Keys: a lane holds one key's column, and passes over the queries that see
-// it, of every head of its group.  Of a tile of 64 queries the first 4 waves take
-// the first half, the other 4 the second, for the same 128 keys, and add up at the
-// end: two waves a SIMD, one's exponentials beside the other's products.  Where
+// Keys: a lane holds one key's column, and passes over the queries that see it,
+// of every head of its group.  GROUPS waves hold 32 keys each, and PARTS such sets
+// share a tile's queries, 32 each, and add up at the end.  (4, 1): two
+// workgroups a CU, which do not wait for each other, so that one's exponentials run
+// beside the other's products (8 x 2048 tokens, 96 heads of 128: 1.83 ms, 903 TFLOP/s; (4, 2)
+// in one workgroup 2.34).  Where that gives fewer than 2048 workgroups, the longest
+// of which would be waited for, more waves share its keys' queries: (2, 2) for heads
+// up to 64, (2, 4) for larger ones (13 sequences of up to 2047 tokens, 8 key heads of
+// 64: 162 us, (4, 1) 268; but on the case above (2, 4) takes 2.85 ms).  Where
 // registers do not hold two operands and two sums, values stay in LDS.
-constexpr int kKeyThreads = 512;
-
-template <typename T, int DP, bool ASYNC>
-__global__ __launch_bounds__(kKeyThreads, 2) void attention_dkv_kernel(GradArgs a) {
-    constexpr int STEPS = DP / 16, BLOCKS = DP / 32, QUERIES = 64, WORDS = TileShape<DP>::words;
+template <typename T, int DP, int GROUPS, int PARTS, bool ASYNC>
+__global__ __launch_bounds__(kWave *GROUPS *PARTS, 2) void attention_dkv_kernel(GradArgs a) {
+    constexpr int STEPS = DP / 16, BLOCKS = DP / 32, QUERIES = 32 * PARTS, WORDS = TileShape<DP>::words;
+    constexpr int THREADS = kWave * GROUPS * PARTS, KEYS = 32 * GROUPS, SHIFT = GROUPS == 4 ? 7 : 6;
     constexpr bool VALUES_IN_LDS = DP > 64;
+    constexpr int STATS = QUERIES < kWave ? kWave : QUERIES;
     __shared__ uint4 q0[QUERIES * WORDS], d0[QUERIES * WORDS], q1[QUERIES * WORDS], d1[QUERIES * WORDS];
-    __shared__ uint4 values[VALUES_IN_LDS ? kRows * WORDS : 1];
-    __shared__ float lse_lds[2][QUERIES], delta_lds[2][QUERIES];
+    __shared__ __align__(16) float s0[2][STATS], s1[2][STATS];  // -lse, -delta
+    __shared__ uint4 values[VALUES_IN_LDS ? KEYS * WORDS : 1];
     const Task task = task_of(blockIdx.x, a.blocks, a.heads / a.group, 1);
     Sequence s;
-    if (!ranked_sequence(a.seq, true, a.causal, a.blocks, task.block, kShift, &s)) return;
+    if (!ranked_sequence(a.seq, true, a.causal, a.blocks, task.block, SHIFT, &s)) return;
     const int lane = threadIdx.x % kWave, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave), half = lane / 32;
-    const int part = wave / 4, keys_of = wave % 4;
-    const int key0 = s.block * kRows + keys_of * 32, key = key0 + lane % 32, held = min(key, s.lk - 1);
+    const int part = wave / GROUPS, keys_of = wave % GROUPS;
+    const int key0 = s.block * KEYS + keys_of * 32, key = key0 + lane % 32, held = min(key, s.lk - 1);
 
     Operand8<T> k[STEPS], v[VALUES_IN_LDS ? 1 : STEPS];
 #pragma unroll
@@ -188,7 +211,7 @@ __global__ __launch_bounds__(kKeyThreads, 2) void attention_dkv_kernel(GradArgs 
     }
     // the first query that sees the lane's key; of the workgroup's and of the wave's keys; the first that sees all the wave's
     const int first = a.causal ? key - (s.lk - s.lq) : 0;
-    const int from = a.causal ? max(0, s.block * kRows - (s.lk - s.lq)) / QUERIES * QUERIES : 0;
+    const int from = a.causal ? max(0, s.block * KEYS - (s.lk - s.lq)) / QUERIES * QUERIES : 0;
     const int wave_from = a.causal ? key0 - (s.lk - s.lq) : 0, all_see = a.causal ? wave_from + 31 : 0;
     const int tiles = s.lq > from ? (s.lq - from + QUERIES - 1) / QUERIES : 0, turns = tiles * a.group;
 
@@ -197,57 +220,103 @@ __global__ __launch_bounds__(kKeyThreads, 2) void attention_dkv_kernel(GradArgs 
 #pragma unroll
     for (int d = 0; d < BLOCKS; ++d) dk[d] = dv[d] = zero16();
     float factor = kFirstFactor;
-    TileLoader<T, DP, QUERIES, kKeyThreads, ASYNC> ql(threadIdx.x, a.dim, a.q.token_pitch), dl(threadIdx.x, a.dim, a.dout.token_pitch);
-    int next_head = task.head * a.group, next_row = from;  // of the tile to be loaded
-    float2 stat;
-    auto start = [&](auto &q_to, auto &d_to) {
-        ql.start(a.q.template at<const T>(s.q0 + next_row, next_head), s.lq - next_row, q_to);
-        dl.start(a.dout.template at<const T>(s.q0 + next_row, next_head), s.lq - next_row, d_to);
-        stat = make_float2(INFINITY, 0);
-        if (threadIdx.x < QUERIES && next_row + int(threadIdx.x) < s.lq)
-            stat = a.row[int64_t(next_head) * a.seq.q_tokens + s.q0 + next_row + threadIdx.x];
-        next_row += QUERIES;
-        if (next_row >= s.lq) {
-            next_row = from;
+    TileLoader<T, DP, QUERIES, THREADS, ASYNC> ql(threadIdx.x, a.dim, a.q.token_pitch), dl(threadIdx.x, a.dim, a.dout.token_pitch);
+    // the tile to be loaded: its head, the rows from it to the sequence's end, and where they are
+    int next_head = task.head * a.group, rows_left = s.lq - from;
+    const T *q_at = a.q.template at<const T>(s.q0 + from, next_head), *d_at = a.dout.template at<const T>(s.q0 + from, next_head);
+    const float *lse_at = a.minus_lse + int64_t(next_head) * a.seq.q_tokens + s.q0 + from;
+    const float *delta_at = a.minus_delta + int64_t(next_head) * a.seq.q_tokens + s.q0 + from;
+    const int64_t q_step = QUERIES * a.q.token_pitch, d_step = QUERIES * a.dout.token_pitch;
+    float stat[2];
+    // a tile behind the last is asked for too, and is zeros without a read.  A query behind its sequence's end so has zeros for statistics, and weights 1 that meet zeros.
+    auto load = [&](int turn, auto &q_to, auto &d_to, auto &s_to) {
+        const int rows = turn < turns ? rows_left : 0;
+        ql.start(q_at, rows, q_to);
+        dl.start(d_at, rows, d_to);
+        if constexpr (ASYNC) {
+            const __amdgpu_buffer_rsrc_t lse = bytes_from(lse_at, uint32_t(min(rows, QUERIES)) * 4),
+                                         delta = bytes_from(delta_at, uint32_t(min(rows, QUERIES)) * 4);
+#pragma unroll
+            for (int u = 0; u < STATS / kWave; ++u) {  // by every wave the same
+                load_word_to_lds(lse, (u * kWave + lane) * 4, &s_to[0][u * kWave]);
+                load_word_to_lds(delta, (u * kWave + lane) * 4, &s_to[1][u * kWave]);
+            }
+        } else if (threadIdx.x < QUERIES) {
+            const bool there = int(threadIdx.x) < rows;
+            stat[0] = there ? lse_at[threadIdx.x] : 0.0f;
+            stat[1] = there ? delta_at[threadIdx.x] : 0.0f;
+        }
+        rows_left -= QUERIES;
+        q_at += q_step;
+        d_at += d_step;
+        lse_at += QUERIES;
+        delta_at += QUERIES;
+        if (rows_left <= 0 && turn + 1 < turns) {
             ++next_head;
+            rows_left = s.lq - from;
+            q_at = a.q.template at<const T>(s.q0 + from, next_head);
+            d_at = a.dout.template at<const T>(s.q0 + from, next_head);
+            lse_at = a.minus_lse + int64_t(next_head) * a.seq.q_tokens + s.q0 + from;
+            delta_at = a.minus_delta + int64_t(next_head) * a.seq.q_tokens + s.q0 + from;
         }
     };
-    auto finish = [&](int which, auto &q_to, auto &d_to) {
-        if (threadIdx.x < QUERIES) {
-            lse_lds[which][threadIdx.x] = stat.x;
-            delta_lds[which][threadIdx.x] = stat.y;
+    auto write = [&](auto &q_to, auto &d_to, auto &s_to) {
+        if constexpr (!ASYNC) {
+            ql.write(q_to);
+            dl.write(d_to);
+            if (threadIdx.x < QUERIES) {
+                s_to[0][threadIdx.x] = stat[0];
+                s_to[1][threadIdx.x] = stat[1];
+            }
         }
-        ql.finish(q_to);
-        dl.finish(d_to);
     };
     if (turns > 0) {
         if constexpr (VALUES_IN_LDS) {
-            TileLoader<T, DP, kRows, kKeyThreads, ASYNC> vl(threadIdx.x, a.dim, a.v.token_pitch);
-            vl.start(a.v.template at<const T>(s.k0 + s.block * kRows, task.head), s.lk - s.block * kRows, values);
+            TileLoader<T, DP, KEYS, THREADS, ASYNC> vl(threadIdx.x, a.dim, a.v.token_pitch);
+            vl.start(a.v.template at<const T>(s.k0 + s.block * KEYS, task.head), s.lk - s.block * KEYS, values);
             vl.finish(values);
         }
-        start(q0, d0);
-        finish(0, q0, d0);
+        load(0, q0, d0, s0);
+        write(q0, d0, s0);
     }
-    __syncthreads();
+    if (THREADS == 512 && wave < 4) __builtin_amdgcn_s_setprio(1);
     int row0 = from;
-    auto step = [&](int turn, int which, const auto &qt, const auto &dt, auto &q_next, auto &d_next) {
-        const bool more = turn + 1 < turns;
-        if (more) start(q_next, d_next);
+    auto step = [&](int turn, const auto &qt, const auto &dt, const auto &stats, auto &q_next, auto &d_next, auto &s_next) {
+        if constexpr (ASYNC) loads_done();
+        __syncthreads();
+        load(turn + 1, q_next, d_next, s_next);
         const int r0 = row0 + part * 32;
         if (r0 + 31 >= wave_from && r0 < s.lq) {
-            f32x16 x = zero16(), dp = zero16();
+            f32x16 x = zero16(), dp;  // dP - delta, summed from -delta on
 #pragma unroll
-            for (int i = 0; i < STEPS; ++i) {
-                x = mfma(row_operand<T, DP>(qt, 0, i, places), k[i], x);
-                if constexpr (!VALUES_IN_LDS) dp = mfma(row_operand<T, DP>(dt, 0, i, places), v[i], dp);
+            for (int j = 0; j < 4; ++j) {
+                const f32x4 delta = *reinterpret_cast<const f32x4 *>(&stats[1][part * 32 + result_row(4 * j, half)]);
+#pragma unroll
+                for (int e = 0; e < 4; ++e) dp[4 * j + e] = delta[e];
             }
-            if constexpr (VALUES_IN_LDS) {
+            Operand8<T> left[2][2];
+            if constexpr (VALUES_IN_LDS) {  // pipelined, it spills
 #pragma unroll
-                for (int i = 0; i < STEPS; ++i) {
+                for (int i = 0; i < STEPS; ++i) x = mfma(row_operand<T, DP>(qt, 0, i, places), k[i], x);
+#pragma unroll
+                for (int i = 0; i < STEPS; ++i)
                     dp = mfma(row_operand<T, DP>(dt, 0, i, places), row_operand<T, DP>(values, 0, i, v_places), dp);
-                }
+            } else {
+                pipelined<STEPS>(
+                    [&](auto i) {
+                        left[i % 2][0] = row_operand<T, DP>(qt, 0, i, places);
+                        left[i % 2][1] = row_operand<T, DP>(dt, 0, i, places);
+                    },
+                    [&](auto i) {
+                        x = mfma(left[i % 2][0], k[i], x);
+                        dp = mfma(left[i % 2][1], v[i], dp);
+                    });
             }
+            auto read_columns = [&](auto i) {
+                left[i % 2][0] = column_operand<T, DP>(dt, i / BLOCKS * 16, i % BLOCKS, places);
+                left[i % 2][1] = column_operand<T, DP>(qt, i / BLOCKS * 16, i % BLOCKS, places);
+            };
+            if constexpr (!VALUES_IN_LDS) read_columns(std::integral_constant<int, 0>{});
             if (r0 < all_see) {
 #pragma unroll
                 for (int r = 0; r < 16; ++r)
@@ -256,68 +325,84 @@ __global__ __launch_bounds__(kKeyThreads, 2) void attention_dkv_kernel(GradArgs 
             Operand8<T> p[2], ds[2];
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
-                const f32x4 lse = *reinterpret_cast<const f32x4 *>(&lse_lds[which][part * 32 + result_row(4 * j, half)]);
-                const f32x4 delta = *reinterpret_cast<const f32x4 *>(&delta_lds[which][part * 32 + result_row(4 * j, half)]);
+                const f32x4 lse = *reinterpret_cast<const f32x4 *>(&stats[0][part * 32 + result_row(4 * j, half)]);
 #pragma unroll
                 for (int e = 0; e < 4; ++e) {
                     const int r = 4 * j + e;
-                    const float w = __builtin_amdgcn_exp2f(fmaf(x[r], a.scale2, kRaised<T> - lse[e]));
+                    const float w = __builtin_amdgcn_exp2f(fmaf(x[r], a.scale2, lse[e]));
                     p[r / 8].e[r % 8] = T(w);
-                    x[r] = w * (dp[r] - delta[e]);
+                    x[r] = w * dp[r];
                 }
             }
             round_scores<T>(x, factor, dk, ds);
-#pragma unroll
-            for (int t = 0; t < 2; ++t)
-#pragma unroll
-                for (int d = 0; d < BLOCKS; ++d) {
-                    dv[d] = mfma(column_operand<T, DP>(dt, t * 16, d, places), p[t], dv[d]);
-                    dk[d] = mfma(column_operand<T, DP>(qt, t * 16, d, places), ds[t], dk[d]);
-                }
+            auto add_columns = [&](auto i) {
+                dv[i % BLOCKS] = mfma(left[i % 2][0], p[i / BLOCKS], dv[i % BLOCKS]);
+                dk[i % BLOCKS] = mfma(left[i % 2][1], ds[i / BLOCKS], dk[i % BLOCKS]);
+            };
+            if constexpr (VALUES_IN_LDS) {
+                unrolled<2 * BLOCKS>([&](auto i) {
+                    read_columns(i);
+                    add_columns(i);
+                });
+            } else {
+                pipelined<2 * BLOCKS, true>(read_columns, add_columns);
+            }
         }
         row0 += QUERIES;
         if (row0 >= s.lq) row0 = from;
-        if (more) finish(which ^ 1, q_next, d_next);
-        __syncthreads();
+        write(q_next, d_next, s_next);
     };
     for (int turn = 0; turn < turns; turn += 2) {
-        step(turn, 0, q0, d0, q1, d1);
-        if (turn + 1 < turns) step(turn + 1, 1, q1, d1, q0, d0);
+        step(turn, q0, d0, s0, q1, d1, s1);
+        if (turn + 1 < turns) step(turn + 1, q1, d1, s1, q0, d0, s0);
     }
+    loads_done();  // none may write into LDS that is used otherwise, or another workgroup's, by then
+    __syncthreads();
     const float down = kNarrow<T> ? 1.0f / 16384 : 1.0f, scale = kNarrow<T> ? a.scale / factor * down : a.scale;
-    // the second half's sums to the first, through the tiles' memory
-    uint4 *tile = keys_of == 0 ? q0 : keys_of == 1 ? d0 : keys_of == 2 ? q1 : d1;
-    auto *trade = reinterpret_cast<f32x4 *>(tile) + lane;
-    auto join = [&](f32x16(&sums)[BLOCKS], float by) {
-        if (part == 1) {
+    if constexpr (PARTS > 1) {  // the parts' sums to the first, in order, through the tiles' memory
+        constexpr int SLOT = 32 * DP / 4, EACH = QUERIES * WORDS / SLOT;  // 16-byte words; slots of an array
+        static_assert(EACH * 4 >= (PARTS - 1) * GROUPS, "");
+        auto slot = [&](int p) {
+            const int n = (p - 1) * GROUPS + keys_of, in = n / EACH;
+            uint4 *tile = in == 0 ? q0 : in == 1 ? d0 : in == 2 ? q1 : d1;
+            return reinterpret_cast<f32x4 *>(tile + (n - in * EACH) * SLOT) + lane;
+        };
+        auto join = [&](f32x16(&sums)[BLOCKS], float by) {
 #pragma unroll
-            for (int d = 0; d < BLOCKS; ++d)
+            for (int d = 0; d < BLOCKS; ++d) sums[d] *= by;
+            if (part > 0) {
+                f32x4 *to = slot(part);
 #pragma unroll
-                for (int j = 0; j < 4; ++j)
-                    trade[(d * 4 + j) * kWave] = f32x4{sums[d][4 * j] * by, sums[d][4 * j + 1] * by, sums[d][4 * j + 2] * by,
-                                                       sums[d][4 * j + 3] * by};
-        }
-        __syncthreads();
-        if (part == 0) {
+                for (int d = 0; d < BLOCKS; ++d)
 #pragma unroll
-            for (int d = 0; d < BLOCKS; ++d)
+                    for (int j = 0; j < 4; ++j)
+                        to[(d * 4 + j) * kWave] = f32x4{sums[d][4 * j], sums[d][4 * j + 1], sums[d][4 * j + 2], sums[d][4 * j + 3]};
+            }
+            __syncthreads();
+            if (part == 0) {
+                for (int p = 1; p < PARTS; ++p) {
+                    const f32x4 *from = slot(p);
 #pragma unroll
-                for (int j = 0; j < 4; ++j) {
-                    const f32x4 x = trade[(d * 4 + j) * kWave];
+                    for (int d = 0; d < BLOCKS; ++d)
 #pragma unroll
-                    for (int e = 0; e < 4; ++e) sums[d][4 * j + e] = fmaf(sums[d][4 * j + e], by, x[e]);
+                        for (int j = 0; j < 4; ++j) {
+                            const f32x4 x = from[(d * 4 + j) * kWave];
+#pragma unroll
+                            for (int e = 0; e < 4; ++e) sums[d][4 * j + e] += x[e];
+                        }
                 }
-        }
-        __syncthreads();
-    };
-    join(dk, scale);
-    join(dv, down);
-    if (part == 1) return;
+            }
+            __syncthreads();
+        };
+        join(dk, scale);
+        join(dv, down);
+        if (part > 0) return;
+    }
     T *to_dk = a.dk.template at<T>(s.k0 + held, task.head), *to_dv = a.dv.template at<T>(s.k0 + held, task.head);
 #pragma unroll
     for (int d = 0; d < BLOCKS; ++d) {
-        store_columns(to_dk, key < s.lk, dk[d], 1.0f, d, lane, a.dim);
-        store_columns(to_dv, key < s.lk, dv[d], 1.0f, d, lane, a.dim);
+        store_columns(to_dk, key < s.lk, dk[d], PARTS > 1 ? 1.0f : scale, d, lane, a.dim);
+        store_columns(to_dv, key < s.lk, dv[d], PARTS > 1 ? 1.0f : down, d, lane, a.dim);
     }
 }
 
@@ -356,7 +441,8 @@ extern "C" reshard_status_t reshard_attention_backward(
             if (st != RESHARD_OK) return st;
         }
         a.lse = lse;
-        a.row = static_cast<float2 *>(workspace);
+        a.minus_lse = static_cast<float *>(workspace);
+        a.minus_delta = a.minus_lse + q_tokens * heads;
         a.seq = Sequences{q_offsets, k_offsets, int(sequences), q_tokens, k_tokens};
         a.heads = int(heads);
         a.group = int(heads / kv_heads);
@@ -379,12 +465,20 @@ extern "C" reshard_status_t reshard_attention_backward(
                 if (status != RESHARD_OK) return status;
             }
             if (k_tokens == 0) return status;
-            status = check_grid(blocks_of(k_tokens, sequences, kShift), kv_heads, &a.blocks);
-            if (status != RESHARD_OK) return status;
             const bool async = aligned16(a.q, 2) && aligned16(a.dout, 2) && aligned16(a.v, 2);
-            return launch("attention gradient launch",
-                          async ? attention_dkv_kernel<T, DP, true> : attention_dkv_kernel<T, DP, false>,
-                          dim3(unsigned(a.blocks * kv_heads)), kKeyThreads, 0, stm, a);
+            auto go = [&](auto groups, auto parts) {
+                constexpr int GROUPS = decltype(groups)::value, PARTS = decltype(parts)::value;
+                reshard_status_t st = check_grid(blocks_of(k_tokens, sequences, GROUPS == 4 ? 7 : 6), kv_heads, &a.blocks);
+                if (st != RESHARD_OK) return st;
+                return launch("attention gradient launch",
+                              async ? attention_dkv_kernel<T, DP, GROUPS, PARTS, true>
+                                    : attention_dkv_kernel<T, DP, GROUPS, PARTS, false>,
+                              dim3(unsigned(a.blocks * kv_heads)), kWave * GROUPS * PARTS, 0, stm, a);
+            };
+            using std::integral_constant;
+            if (blocks_of(k_tokens, sequences, 7) * kv_heads < 2048)
+                return go(integral_constant<int, 2>{}, integral_constant<int, DP <= 64 ? 2 : 4>{});
+            return go(integral_constant<int, 4>{}, integral_constant<int, 1>{});
         });
     });
 }

@@ -10,7 +10,7 @@ additions are not documented, and 2^-23 is counted there.
 GPU tests unless marked otherwise; refusals run on the CPU.
 """
 
-import itertools
+import ctypes
 import math
 import zlib
 
@@ -682,8 +682,12 @@ def _refused(status, want, text):
     assert status == want and text in message, (status, message)
 
 
+def _cache(*fields):
+    return ctypes.byref(B.reshard_cache_t(*fields))
+
+
 def _at(data=P, token=1 << 10, head=64):
-    return B.reshard_heads_t(data, token, head)
+    return ctypes.byref(B.reshard_heads_t(data, token, head))
 
 
 EI, EU = B.RESHARD_EINVAL, B.RESHARD_EUNSUPPORTED
@@ -699,7 +703,7 @@ def test_rotate_heads_refusals():
     def bwd(tokens=4, d=_at(), dq=_at(), dw=P, acc=0, work=P, nbytes=1 << 30, dt=3):
         return lib.reshard_rotate_heads_backward(tokens, 8, 2, 64, 64, 0, dt, d, d, _at(), _at(), P, P, 4, 1e-6, P, P, dq, dq, dw,
                                                  dw, acc, work, nbytes, None)
-    cache = B.reshard_cache_t(P, P, 10, 16, 16 * 128, 128, 64)
+    cache = _cache(P, P, 10, 16, 16 * 128, 128, 64)
     for call, status, text in (
             (dict(tokens=-1), EI, "tokens"), (dict(heads=0), EI, "heads"), (dict(kv=0), EI, "heads"), (dict(heads=1 << 17), EU, "2^16"),
             (dict(dim=63, rot=0), EI, "dim"), (dict(dim=130, rot=0), EU, "dim"), (dict(rot=66), EI, "rotary"), (dict(rot=3), EI, "rotary"),
@@ -708,10 +712,10 @@ def test_rotate_heads_refusals():
             (dict(k=_at(None)), EI, "k is"), (dict(qo=_at(head=63)), EI, "overlap"), (dict(qo=_at(token=511)), EI, "overlap"),
             (dict(ko=_at(P + 1)), EI, "aligned"), (dict(q=_at(token=-1)), EU, "pitch"), (dict(q=_at(token=1 << 60)), EU, "pitch"),
             (dict(v=_at()), EI, "go together"), (dict(cache=cache), EI, "go together"), (dict(v=_at(), cache=cache), EI, "slots"),
-            (dict(v=_at(), cache=B.reshard_cache_t(P, P, 10, 0, 1, 1, 1), slots=P), EI, "page_length"),
-            (dict(v=_at(), cache=B.reshard_cache_t(P, None, 10, 16, 2048, 128, 64), slots=P), EI, "values"),
-            (dict(v=_at(), cache=B.reshard_cache_t(P, P, 10, 16, 2048, 63, 64), slots=P), EI, "less than dim"),
-            (dict(v=_at(), cache=B.reshard_cache_t(P, P, 1 << 30, 16, 2048, 128, 64), slots=P), EU, "slots")):
+            (dict(v=_at(), cache=_cache(P, P, 10, 0, 1, 1, 1), slots=P), EI, "page_length"),
+            (dict(v=_at(), cache=_cache(P, None, 10, 16, 2048, 128, 64), slots=P), EI, "values"),
+            (dict(v=_at(), cache=_cache(P, P, 10, 16, 2048, 63, 64), slots=P), EI, "less than dim"),
+            (dict(v=_at(), cache=_cache(P, P, 1 << 30, 16, 2048, 128, 64), slots=P), EU, "slots")):
         _refused(fwd(**call), status, text)
     for call, text in ((dict(d=None), "dq_out"), (dict(dq=_at(token=8)), "overlap"), (dict(acc=2), "accumulate"), (dict(work=None), "workspace"),
                        (dict(nbytes=16), "workspace"), (dict(work=P + 4), "workspace"), (dict(dw=P + 2), "dq_weight"), (dict(dt=1), "dtype")):
@@ -746,7 +750,7 @@ def test_attention_refusals():
 
 def test_attention_paged_refusals():
     lib = B.load()
-    good = B.reshard_cache_t(P, P, 10, 16, 16 * 128, 128, 64)
+    good = _cache(P, P, 10, 16, 16 * 128, 128, 64)
 
     def call(n=4, heads=8, kv=2, dim=64, dt=3, q=_at(), cache=good, pages=P, width=8, pitch=8, lengths=P, scale=1.0, out=_at(), work=P,
              nbytes=1 << 30):
@@ -756,7 +760,7 @@ def test_attention_paged_refusals():
             (dict(dt=4), EI, "dtype"), (dict(scale=-1.0), EI, "scale"), (dict(cache=None), EI, "cache"), (dict(q=None), EI, "q is"),
             (dict(out=_at(head=8)), EI, "overlap"), (dict(pages=None), EI, "pages"), (dict(pitch=7), EI, "pitch"), (dict(lengths=None), EI, "lengths"),
             (dict(work=None), EI, "workspace"), (dict(nbytes=64), EI, "workspace"), (dict(work=P + 8), EI, "workspace"),
-            (dict(width=1 << 28, pitch=1 << 28), EU, "2^31"), (dict(cache=B.reshard_cache_t(P + 1, P, 10, 16, 2048, 128, 64)), EI, "aligned")):
+            (dict(width=1 << 28, pitch=1 << 28), EU, "2^31"), (dict(cache=_cache(P + 1, P, 10, 16, 2048, 128, 64)), EI, "aligned")):
         _refused(call(**args), status, text)
     for bad in ((-1, 8, 2, 64, 8, 16), (4, 8, 3, 64, 8, 16), (4, 8, 2, 200, 8, 16), (4, 8, 2, 64, 8, 0), (4, 8, 2, 64, 1 << 30, 16)):
         assert lib.reshard_attention_paged_workspace(*bad) == -1
