@@ -720,11 +720,11 @@ _pack_heads = struct.Struct("Pqq").pack  # reshard_heads_t
 _pack_cache = struct.Struct("PPqqqqq").pack  # reshard_cache_t
 
 
-def _heads(name, t, shape, beside):
+def _heads(name, t, shape, dtype, device):
     """reshard_heads_t (as bytes: a ctypes object takes four times as long to make) of a tensor that must have this
-    shape, with its last dimension dense, and the type and device of `beside`."""
-    if t.shape != shape or t.dtype != beside.dtype or t.get_device() != beside.get_device():
-        raise ValueError(f"{name} must be {beside.dtype} {tuple(shape)} on {beside.device}, "
+    shape, with its last dimension dense, this type, and this device's number."""
+    if t.shape != shape or t.dtype is not dtype or t.get_device() != device:
+        raise ValueError(f"{name} must be {dtype} {tuple(shape)} on device {device}, "
                          f"got {t.dtype} {tuple(t.shape)} on {t.device}")
     token, head, last = t.stride()
     if last != 1 and shape[2] > 1:
@@ -738,6 +738,13 @@ def _three(name, t):
     return t.shape
 
 
+def _int32(name, t, n, device):
+    if t.shape != (n,) or t.dtype is not _torch.int32 or t.get_device() != device or not t.is_contiguous():
+        raise ValueError(f"{name} must be {n} dense int32 on device {device}, "
+                         f"got {t.dtype} {tuple(t.shape)}, strides {t.stride()}, on {t.device}")
+    return t.data_ptr()
+
+
 def _here(name, t, stream):
     """The stream's handle.  Kernels run on the current device, so that is where tensors must be."""
     device = t.get_device()
@@ -745,50 +752,57 @@ def _here(name, t, stream):
         raise ValueError(f"{name} must be on the GPU, got {t.device}")
     try:
         current = _torch._C._cuda_getDevice()
+        handle = _torch._C._cuda_getCurrentRawStream(device) if stream is None else _stream_handle(stream)
     except AttributeError:  # a torch without these private functions
-        current = _torch.cuda.current_device()
+        current, handle = _torch.cuda.current_device(), _stream_handle(stream)
     if device != current:
         raise ValueError(f"{name} is on {t.device}, the current device is cuda:{current}")
-    return _stream_handle(stream)
+    return handle
 
 
-def _numbers(name, t, shape, beside):
-    return _dense(name, t, shape, beside, _torch.int32)
+def _new(t):
+    """A dense tensor of t's shape and type beside it (empty_like is the faster call, and dense where t is)."""
+    return _torch.empty_like(t) if t.is_contiguous() else t.new_empty(t.shape)
 
 
-def _cache(cache, kv_heads, dim, beside):
+def _cache(cache, kv_heads, dim, dtype, device):
     """reshard_cache_t of (keys, values), both [pages, page_length, kv_heads, dim] and laid out alike."""
     keys, values = cache
-    if keys.dim() != 4 or keys.shape[2:] != (kv_heads, dim):
-        raise ValueError(f"cache must be [pages, page_length, {kv_heads}, {dim}], got {tuple(keys.shape)}")
+    shape = keys.shape
+    if len(shape) != 4 or shape[2] != kv_heads or shape[3] != dim:
+        raise ValueError(f"cache must be [pages, page_length, {kv_heads}, {dim}], got {tuple(shape)}")
     for name, t in (("keys", keys), ("values", values)):
-        if t.shape != keys.shape or t.dtype != beside.dtype or t.get_device() != beside.get_device():
-            raise ValueError(f"the cache's {name} must be {beside.dtype} {tuple(keys.shape)} on {beside.device}, "
+        if t.shape != shape or t.dtype is not dtype or t.get_device() != device:
+            raise ValueError(f"the cache's {name} must be {dtype} {tuple(shape)} on device {device}, "
                              f"got {t.dtype} {tuple(t.shape)} on {t.device}")
-    if keys.stride() != values.stride() or dim > 1 and keys.stride(3) != 1:
+    strides = keys.stride()
+    page, slot, head, last = strides
+    if values.stride() != strides or dim > 1 and last != 1:
         raise ValueError(f"the cache's keys and values must be laid out alike, with dense heads, "
-                         f"their strides are {keys.stride()} and {values.stride()}")
-    page, slot, head, _ = keys.stride()
-    return _pack_cache(keys.data_ptr(), values.data_ptr(), keys.shape[0], keys.shape[1], page, slot, head)
+                         f"their strides are {strides} and {values.stride()}")
+    return _pack_cache(keys.data_ptr(), values.data_ptr(), shape[0], shape[1], page, slot, head)
 
 
 def _rotation(q, k, q_weight, k_weight, frequencies, positions):
-    """What both passes check: (tokens, heads, kv_heads, dim, rotary), q, k and the weights' type."""
+    """What both passes check: (tokens, heads, kv_heads, dim, rotary), q, k, the weights' type, positions, q's type and
+    device."""
     tokens, heads, dim = _three("q", q)
     kv_heads = _three("k", k)[1]
-    q_at, k_at = _heads("q", q, q.shape, q), _heads("k", k, (tokens, kv_heads, dim), q)
-    weight = q_weight if q_weight is not None else k_weight if k_weight is not None else q
-    for name, w in (("q_weight", q_weight), ("k_weight", k_weight)):
-        if w is not None:
-            _dense(name, w, (dim,), q, weight.dtype)
-    half = 0
+    dtype, device = q.dtype, q.get_device()
+    q_at, k_at = _heads("q", q, q.shape, dtype, device), _heads("k", k, (tokens, kv_heads, dim), dtype, device)
+    weight = (q_weight if q_weight is not None else k_weight if k_weight is not None else q).dtype
+    if q_weight is not None:
+        _dense("q_weight", q_weight, (dim,), q, weight)
+    if k_weight is not None:
+        _dense("k_weight", k_weight, (dim,), q, weight)
+    half, at = 0, None
     if frequencies is not None:
         half = frequencies.numel()
         _dense("frequencies", frequencies, (half,), q, _torch.float64)
         if positions is None:
             raise ValueError("frequencies need the tokens' positions")
-        _numbers("positions", positions, (tokens,), q)
-    return (tokens, heads, kv_heads, dim, 2 * half), q_at, k_at, _dtype_code(weight.dtype)
+        at = _int32("positions", positions, tokens, device)
+    return (tokens, heads, kv_heads, dim, 2 * half), q_at, k_at, _dtype_code(weight), at, dtype, device
 
 
 def reshard_rotate_heads(q, k, q_weight=None, k_weight=None, eps=1e-6, frequencies=None, positions=None,
@@ -800,27 +814,27 @@ def reshard_rotate_heads(q, k, q_weight=None, k_weight=None, eps=1e-6, frequenci
     With v, cache (keys, values: [pages, page_length, kv_heads, dim]) and slots (int32, -1: not kept), keys and values go
     to their slots there, and the k returned is None."""
     lib = _lib or load()
-    sizes, q_at, k_at, wdt = _rotation(q, k, q_weight, k_weight, frequencies, positions)
-    tokens, _, kv_heads, dim, _ = sizes
+    sizes, q_at, k_at, wdt, at, dtype, device = _rotation(q, k, q_weight, k_weight, frequencies, positions)
     if (v is None) != (cache is None) or (cache is None) != (slots is None):
         raise ValueError("v, cache and slots go together")
-    if cache is not None and k_out is not None:
-        raise ValueError("keys go to the cache or to k_out, not to both")
-    v_at = cache_at = None
+    v_at = cache_at = slots_at = ko_at = None
     if cache is not None:
-        v_at = _heads("v", v, k.shape, q)
-        cache_at = _cache(cache, kv_heads, dim, q)
-        _numbers("slots", slots, (tokens,), q)
+        if k_out is not None:
+            raise ValueError("keys go to the cache or to k_out, not to both")
+        v_at = _heads("v", v, k.shape, dtype, device)
+        cache_at = _cache(cache, sizes[2], sizes[3], dtype, device)
+        slots_at = _int32("slots", slots, sizes[0], device)
     handle = _here("q", q, stream)
     with _on(stream):
-        q_out = q.new_empty(q.shape) if q_out is None else q_out
+        q_out = _new(q) if q_out is None else q_out
         if cache is None and k_out is None:
-            k_out = k.new_empty(k.shape)
-    qo_at = _heads("q_out", q_out, q.shape, q)
-    ko_at = None if cache is not None else _heads("k_out", k_out, k.shape, q)
-    status = lib.reshard_rotate_heads(*sizes, int(bool(interleaved)), _dtype_code(q.dtype), q_at, k_at, _ptr(q_weight),
-                                      _ptr(k_weight), wdt, eps, _ptr(frequencies), _ptr(positions), qo_at, ko_at, v_at,
-                                      cache_at, _ptr(slots), handle)
+            k_out = _new(k)
+    qo_at = _heads("q_out", q_out, q.shape, dtype, device)
+    if cache is None:
+        ko_at = _heads("k_out", k_out, k.shape, dtype, device)
+    status = lib.reshard_rotate_heads(*sizes, 1 if interleaved else 0, _dtype_code(dtype), q_at, k_at, _ptr(q_weight),
+                                      _ptr(k_weight), wdt, eps, _ptr(frequencies), at, qo_at, ko_at, v_at, cache_at,
+                                      slots_at, handle)
     if status != RESHARD_OK:
         _check(status)
     return q_out, k_out
@@ -832,46 +846,46 @@ def reshard_rotate_heads_backward(dq_out, dk_out, q, k, q_weight=None, k_weight=
     """(dq, dk, dq_weight, dk_weight) of reshard_rotate_heads, from the gradients of what it returned and its inputs.
     The weights' gradients are float32; given ones are overwritten, or added to with accumulate."""
     lib = _lib or load()
-    sizes, q_at, k_at, wdt = _rotation(q, k, q_weight, k_weight, frequencies, positions)
+    sizes, q_at, k_at, wdt, at, dtype, device = _rotation(q, k, q_weight, k_weight, frequencies, positions)
     tokens, heads, kv_heads, dim, _ = sizes
-    dqo_at = _heads("dq_out", dq_out, q.shape, q)
-    dko_at = _heads("dk_out", dk_out, k.shape, q)
+    dqo_at = _heads("dq_out", dq_out, q.shape, dtype, device)
+    dko_at = _heads("dk_out", dk_out, k.shape, dtype, device)
     if accumulate and (dq_weight is None or dk_weight is None):
         raise ValueError("accumulate needs the dq_weight and dk_weight to add to")
     handle = _here("q", q, stream)
     need = lib.reshard_rotate_heads_backward_workspace(tokens, heads, kv_heads, dim)
     with _on(stream):
-        dq = q.new_empty(q.shape) if dq is None else dq
-        dk = k.new_empty(k.shape) if dk is None else dk
+        dq = _new(q) if dq is None else dq
+        dk = _new(k) if dk is None else dk
         dq_weight = q.new_empty(dim, dtype=_torch.float32) if dq_weight is None else dq_weight
         dk_weight = q.new_empty(dim, dtype=_torch.float32) if dk_weight is None else dk_weight
         work = q.new_empty(max(0, need), dtype=_torch.uint8)
-    dq_at, dk_at = _heads("dq", dq, q.shape, q), _heads("dk", dk, k.shape, q)
+    dq_at, dk_at = _heads("dq", dq, q.shape, dtype, device), _heads("dk", dk, k.shape, dtype, device)
     _dense("dq_weight", dq_weight, (dim,), q, _torch.float32)
     _dense("dk_weight", dk_weight, (dim,), q, _torch.float32)
     status = lib.reshard_rotate_heads_backward(
-        *sizes, int(bool(interleaved)), _dtype_code(q.dtype), dqo_at, dko_at, q_at, k_at, _ptr(q_weight), _ptr(k_weight),
-        wdt, eps, _ptr(frequencies), _ptr(positions), dq_at, dk_at, dq_weight.data_ptr(), dk_weight.data_ptr(),
-        int(bool(accumulate)), work.data_ptr(), max(0, need), handle)
+        *sizes, 1 if interleaved else 0, _dtype_code(dtype), dqo_at, dko_at, q_at, k_at, _ptr(q_weight), _ptr(k_weight),
+        wdt, eps, _ptr(frequencies), at, dq_at, dk_at, dq_weight.data_ptr(), dk_weight.data_ptr(), 1 if accumulate else 0,
+        work.data_ptr(), need, handle)
     if status != RESHARD_OK:
         _check(status)
     return dq, dk, dq_weight, dk_weight
 
 
 def _packed(q, k, v, q_offsets, k_offsets, scale, stream):
-    """(sizes, q, k, v, scale, the stream's handle) of attention over packed sequences, checked."""
+    """What both passes check: sizes, q, k, v, offsets, scale, the stream's handle, q's type and device."""
     q_tokens, heads, dim = _three("q", q)
     k_tokens, kv_heads, k_dim = _three("k", k)
     if k_dim != dim:
         raise ValueError(f"k must be [tokens, kv_heads, {dim}], got {tuple(k.shape)}")
-    q_at, k_at, v_at = _heads("q", q, q.shape, q), _heads("k", k, k.shape, q), _heads("v", v, k.shape, q)
+    dtype, device, shape = q.dtype, q.get_device(), k.shape
     n = q_offsets.numel()
     if n < 1:
         raise ValueError("q_offsets must hold one number more than there are sequences")
-    _numbers("q_offsets", q_offsets, (n,), q)
-    _numbers("k_offsets", k_offsets, (n,), q)
-    return ((q_tokens, k_tokens, n - 1, heads, kv_heads, dim), q_at, k_at, v_at, dim ** -0.5 if scale is None else scale,
-            _here("q", q, stream))
+    return ((q_tokens, k_tokens, n - 1, heads, kv_heads, dim), _heads("q", q, q.shape, dtype, device),
+            _heads("k", k, shape, dtype, device), _heads("v", v, shape, dtype, device),
+            _int32("q_offsets", q_offsets, n, device), _int32("k_offsets", k_offsets, n, device),
+            dim ** -0.5 if scale is None else scale, _here("q", q, stream), dtype, device)
 
 
 def reshard_attention(q, k, v, q_offsets, k_offsets, scale=None, causal=True, out=None, lse=None, stream=None):
@@ -882,15 +896,16 @@ def reshard_attention(q, k, v, q_offsets, k_offsets, scale=None, causal=True, ou
     dim ** -0.5 by default.  lse [heads, q_tokens] float32 is for the backward pass.  Rows that are no sequence's keep
     what a given out holds there."""
     lib = _lib or load()
-    sizes, q_at, k_at, v_at, scale, handle = _packed(q, k, v, q_offsets, k_offsets, scale, stream)
+    sizes, q_at, k_at, v_at, q_offsets, k_offsets, scale, handle, dtype, device = _packed(q, k, v, q_offsets, k_offsets,
+                                                                                          scale, stream)
     with _on(stream):
-        out = q.new_empty(q.shape) if out is None else out
-        lse = q.new_empty((sizes[3], sizes[0]), dtype=_torch.float32) if lse is None else lse
-    out_at = _heads("out", out, q.shape, q)
-    _dense("lse", lse, (sizes[3], sizes[0]), q, _torch.float32)
-    status = lib.reshard_attention(*sizes, _dtype_code(q.dtype), q_at, k_at, v_at, q_offsets.data_ptr(),
-                                   k_offsets.data_ptr(), scale, int(bool(causal)), out_at, lse.data_ptr(),
-                                   handle)
+        out = _new(q) if out is None else out
+        if lse is None:
+            lse = q.new_empty((sizes[3], sizes[0]), dtype=_torch.float32)
+        else:
+            _dense("lse", lse, (sizes[3], sizes[0]), q, _torch.float32)
+    status = lib.reshard_attention(*sizes, _dtype_code(dtype), q_at, k_at, v_at, q_offsets, k_offsets, scale,
+                                   1 if causal else 0, _heads("out", out, q.shape, dtype, device), lse.data_ptr(), handle)
     if status != RESHARD_OK:
         _check(status)
     return out, lse
@@ -901,20 +916,21 @@ def reshard_attention_backward(dout, q, k, v, out, lse, q_offsets, k_offsets, sc
     """(dq, dk, dv) of reshard_attention, whose out and lse these are, with its other arguments.  Rows that are no
     sequence's keep what a given result holds there."""
     lib = _lib or load()
-    sizes, q_at, k_at, v_at, scale, handle = _packed(q, k, v, q_offsets, k_offsets, scale, stream)
-    dout_at, out_at = _heads("dout", dout, q.shape, q), _heads("out", out, q.shape, q)
+    sizes, q_at, k_at, v_at, q_offsets, k_offsets, scale, handle, dtype, device = _packed(q, k, v, q_offsets, k_offsets,
+                                                                                          scale, stream)
+    dout_at, out_at = _heads("dout", dout, q.shape, dtype, device), _heads("out", out, q.shape, dtype, device)
     _dense("lse", lse, (sizes[3], sizes[0]), q, _torch.float32)
     need = lib.reshard_attention_backward_workspace(sizes[0], sizes[3])
     with _on(stream):
-        dq = q.new_empty(q.shape) if dq is None else dq
-        dk = k.new_empty(k.shape) if dk is None else dk
-        dv = k.new_empty(k.shape) if dv is None else dv
+        dq = _new(q) if dq is None else dq
+        dk = _new(k) if dk is None else dk
+        dv = _new(k) if dv is None else dv
         work = q.new_empty(max(0, need), dtype=_torch.uint8)
-    dq_at, dk_at, dv_at = (_heads(*x, q) for x in (("dq", dq, q.shape), ("dk", dk, k.shape), ("dv", dv, k.shape)))
+    dq_at = _heads("dq", dq, q.shape, dtype, device)
+    dk_at, dv_at = _heads("dk", dk, k.shape, dtype, device), _heads("dv", dv, k.shape, dtype, device)
     status = lib.reshard_attention_backward(
-        *sizes, _dtype_code(q.dtype), dout_at, q_at, k_at, v_at, out_at, lse.data_ptr(), q_offsets.data_ptr(),
-        k_offsets.data_ptr(), scale, int(bool(causal)), dq_at, dk_at, dv_at, work.data_ptr(), max(0, need),
-        handle)
+        *sizes, _dtype_code(dtype), dout_at, q_at, k_at, v_at, out_at, lse.data_ptr(), q_offsets, k_offsets, scale,
+        1 if causal else 0, dq_at, dk_at, dv_at, work.data_ptr(), need, handle)
     if status != RESHARD_OK:
         _check(status)
     return dq, dk, dv
@@ -925,24 +941,24 @@ def reshard_attention_paged(q, k_cache, v_cache, pages, lengths, scale=None, out
     kv_heads, dim].  Token t of sequence s, t < lengths[s], lies in page pages[s, t // page_length] (int32)."""
     lib = _lib or load()
     n, heads, dim = _three("q", q)
-    q_at = _heads("q", q, q.shape, q)
+    dtype, device = q.dtype, q.get_device()
+    q_at = _heads("q", q, q.shape, dtype, device)
     kv_heads = k_cache.shape[2] if k_cache.dim() == 4 else -1
-    cache_at = _cache((k_cache, v_cache), kv_heads, dim, q)
-    if pages.dim() != 2 or pages.shape[0] != n or pages.dtype != _torch.int32 or pages.device != q.device or (
+    cache_at = _cache((k_cache, v_cache), kv_heads, dim, dtype, device)
+    if pages.dim() != 2 or pages.shape[0] != n or pages.dtype is not _torch.int32 or pages.get_device() != device or (
             pages.shape[1] > 1 and pages.stride(1) != 1):
         raise ValueError(f"pages must be int32 [{n}, pages of a sequence] on {q.device} with dense rows, "
                          f"got {pages.dtype} {tuple(pages.shape)}, strides {pages.stride()}, on {pages.device}")
-    _numbers("lengths", lengths, (n,), q)
+    lengths = _int32("lengths", lengths, n, device)
     handle = _here("q", q, stream)
-    need = lib.reshard_attention_paged_workspace(n, heads, kv_heads, dim, pages.shape[1], k_cache.shape[1])
+    width = pages.shape[1]
+    need = lib.reshard_attention_paged_workspace(n, heads, kv_heads, dim, width, k_cache.shape[1])
     with _on(stream):
-        out = q.new_empty(q.shape) if out is None else out
-        work = q.new_empty(max(0, need), dtype=_torch.uint8)
-    out_at = _heads("out", out, q.shape, q)
-    status = lib.reshard_attention_paged(n, heads, kv_heads, dim, _dtype_code(q.dtype), q_at, cache_at, pages.data_ptr(),
-                                         pages.shape[1], pages.stride(0), lengths.data_ptr(),
-                                         dim ** -0.5 if scale is None else scale, out_at, work.data_ptr(), max(0, need),
-                                         handle)
+        out = _new(q) if out is None else out
+        work = q.new_empty(need, dtype=_torch.uint8) if need > 0 else None
+    status = lib.reshard_attention_paged(n, heads, kv_heads, dim, _dtype_code(dtype), q_at, cache_at, pages.data_ptr(),
+                                         width, pages.stride(0), lengths, dim ** -0.5 if scale is None else scale,
+                                         _heads("out", out, q.shape, dtype, device), _ptr(work), max(0, need), handle)
     if status != RESHARD_OK:
         _check(status)
     return out

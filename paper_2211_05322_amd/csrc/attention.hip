@@ -55,7 +55,7 @@ __global__ __launch_bounds__(kThreads, QB == 1 ? 2 : 1) void attention_kernel(Pr
         last[b] = a.causal ? min(row, s.lq - 1) + s.lk - s.lq : s.lk - 1;
     }
     const int to = a.causal ? min(s.lk, min(s.lq, (s.block + 1) * ROWS) + s.lk - s.lq) : s.lk;  // the workgroup's keys
-    const int wave_to = a.causal ? min(s.lk, min(s.lq, row0 + 32 * QB) + s.lk - s.lq) : s.lk;
+    const int wave_to = row0 >= s.lq ? 0 : a.causal ? min(s.lk, min(s.lq, row0 + 32 * QB) + s.lk - s.lq) : s.lk;
     const int all_see = a.causal ? row0 + 1 + s.lk - s.lq : s.lk;  // keys that each of the wave's queries sees
 
     const LanePlaces places = LanePlaces::of<DP>(lane);

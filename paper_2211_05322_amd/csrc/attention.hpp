@@ -50,6 +50,15 @@ __device__ inline f32x4 mfma(const Operand8<f16> &a, const Operand8<f16> &b, f32
     return __builtin_amdgcn_mfma_f32_16x16x32_f16(a.v, b.v, c, 0, 0, 0);
 }
 
+template <typename F, int... I>
+__device__ inline void unrolled_(F &&f, std::integer_sequence<int, I...>) {
+    (f(std::integral_constant<int, I>{}), ...);
+}
+template <int N, typename F>
+__device__ inline void unrolled(F &&f) {
+    unrolled_(f, std::make_integer_sequence<int, N>{});
+}
+
 __device__ inline f32x16 zero16() {
     f32x16 z;
 #pragma unroll
@@ -187,15 +196,6 @@ struct TileLoader {
     }
 };
 
-template <typename F, int... I>
-__device__ inline void unrolled_(F &&f, std::integer_sequence<int, I...>) {
-    (f(std::integral_constant<int, I>{}), ...);
-}
-template <int N, typename F>
-__device__ inline void unrolled(F &&f) {
-    unrolled_(f, std::make_integer_sequence<int, N>{});
-}
-
 // N steps of matrix instructions, use(i), whose operands read(i) brings from LDS
 // a step ahead: by itself the compiler reads an operand right before its
 // instruction and waits for it, or reads all at once and spills.  With BEGUN the
@@ -320,30 +320,35 @@ constexpr int kRanked = 256;
 __device__ inline bool ranked_sequence(const Sequences &s, bool by_keys, bool causal, int64_t blocks, int64_t rank,
                                        int shift, Sequence *out) {
     if (s.count > kRanked) return find_sequence(s, by_keys, by_keys ? rank : blocks - 1 - rank, shift, out);
+    constexpr int CHUNKS = kRanked / kWave;
     const int lane = threadIdx.x % kWave;
-    int own[kRanked / kWave], other[kRanked / kWave];
+    int q0[CHUNKS], k0[CHUNKS], lq[CHUNKS], lk[CHUNKS];
+    auto each = [&](auto &&f) {  // over the chunks that there are
+        unrolled<CHUNKS>([&](auto c) {
+            if (c == 0 || c * kWave < s.count) f(c);
+        });
+    };
+    auto ceil = [&](int n) { return int((int64_t(n) + (1 << shift) - 1) >> shift); };
+    auto own = [&](int c) { return ceil(by_keys ? lk[c] : lq[c]); };
+    auto other = [&](int c) { return ceil(by_keys ? lq[c] : lk[c]); };
     int highest = 0;
-#pragma unroll
-    for (int c = 0; c < kRanked / kWave; ++c) {
-        own[c] = other[c] = 0;
-        const int i = c * kWave + lane;
-        if (i >= s.count) continue;
-        const int64_t q0 = clamped(s.q_offsets[i], 0, s.q_tokens), k0 = clamped(s.k_offsets[i], 0, s.k_tokens);
-        const int lq = int(clamped(s.q_offsets[i + 1], q0, s.q_tokens) - q0);
-        const int lk = int(clamped(s.k_offsets[i + 1], k0, s.k_tokens) - k0);
-        const int bq = int((int64_t(lq) + (1 << shift) - 1) >> shift), bk = int((int64_t(lk) + (1 << shift) - 1) >> shift);
-        own[c] = by_keys ? bk : bq;
-        other[c] = by_keys ? bq : bk;
-        if (own[c] > 0) highest = max(highest, other[c]);
-    }
+    each([&](auto c) {
+        const int i = min(c * kWave + lane, s.count - 1);
+        q0[c] = int(clamped(s.q_offsets[i], 0, s.q_tokens));
+        k0[c] = int(clamped(s.k_offsets[i], 0, s.k_tokens));
+        lq[c] = int(clamped(s.q_offsets[i + 1], q0[c], s.q_tokens)) - q0[c];
+        lk[c] = int(clamped(s.k_offsets[i + 1], k0[c], s.k_tokens)) - k0[c];
+        if (c * kWave + lane >= s.count) lq[c] = lk[c] = 0;
+        if (own(c) > 0) highest = max(highest, other(c));
+    });
     auto count = [&](int c, int w) {
-        if (w <= 0) return own[c];
-        if (w > other[c]) return 0;
-        return causal ? min(max((by_keys ? own[c] : other[c]) - w + 1, 0), own[c]) : own[c];
+        if (w <= 0) return own(c);
+        if (w > other(c)) return 0;
+        return causal ? min(max((by_keys ? own(c) : other(c)) - w + 1, 0), own(c)) : own(c);
     };
     auto counts = [&](int w) {
-        int n = count(0, w);
-        for (int c = 1; c * kWave < s.count; ++c) n += c == 1 ? count(1, w) : c == 2 ? count(2, w) : count(3, w);
+        int n = 0;
+        each([&](auto c) { n += count(c, w); });
         return wave_sum(n);
     };
     if (rank >= counts(0)) return false;
@@ -355,10 +360,11 @@ __device__ inline bool ranked_sequence(const Sequences &s, bool by_keys, bool ca
         if (counts(mid) > rank) low = mid;
         else high = mid;
     }
-    int before = counts(high), found = 0, place = 0;
-    for (int c = 0; c * kWave < s.count; ++c) {
-        const int more = c == 0 ? count(0, high) : c == 1 ? count(1, high) : c == 2 ? count(2, high) : count(3, high);
-        const int mine = (c == 0 ? count(0, low) : c == 1 ? count(1, low) : c == 2 ? count(2, low) : count(3, low)) - more;
+    int before = counts(high);
+    bool found = false;
+    each([&](auto c) {
+        if (found) return;
+        const int more = count(c, high), mine = count(c, low) - more;
         int upto = mine;
 #pragma unroll
         for (int d = 1; d < kWave; d *= 2) {
@@ -369,18 +375,13 @@ __device__ inline bool ranked_sequence(const Sequences &s, bool by_keys, bool ca
         const uint64_t holds = __builtin_amdgcn_ballot_w64(upto > at && upto - mine <= at);
         if (holds) {
             const int l = __builtin_ctzll(holds);
-            found = c * kWave + l;
-            place = __builtin_amdgcn_readlane(more + at - (upto - mine), l);
-            break;
+            auto of = [&](int x) { return __builtin_amdgcn_readlane(x, l); };
+            *out = Sequence{of(q0[c]), of(k0[c]), of(lq[c]), of(lk[c]), of(more + at - (upto - mine))};
+            found = true;
         }
         before += __builtin_amdgcn_readlane(upto, kWave - 1);
-    }
-    out->q0 = clamped(s.q_offsets[found], 0, s.q_tokens);
-    out->k0 = clamped(s.k_offsets[found], 0, s.k_tokens);
-    out->lq = int(clamped(s.q_offsets[found + 1], out->q0, s.q_tokens) - out->q0);
-    out->lk = int(clamped(s.k_offsets[found + 1], out->k0, s.k_tokens) - out->k0);
-    const int rows = by_keys ? out->lk : out->lq;
-    out->block = by_keys ? place : ((rows - 1) >> shift) - place;
+    });
+    if (!by_keys) out->block = ((out->lq - 1) >> shift) - out->block;
     return true;
 }
 

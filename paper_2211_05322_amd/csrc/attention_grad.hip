@@ -98,7 +98,7 @@ __global__ __launch_bounds__(kThreads, 2) void attention_dq_kernel(GradArgs a) {
     }
     const int last = a.causal ? held + s.lk - s.lq : s.lk - 1;
     const int to = a.causal ? min(s.lk, min(s.lq, (s.block + 1) * kRows) + s.lk - s.lq) : s.lk;
-    const int wave_to = a.causal ? min(s.lk, min(s.lq, row0 + 32) + s.lk - s.lq) : s.lk;
+    const int wave_to = row0 >= s.lq ? 0 : a.causal ? min(s.lk, min(s.lq, row0 + 32) + s.lk - s.lq) : s.lk;
     const int all_see = a.causal ? row0 + 1 + s.lk - s.lq : s.lk;
 
     const LanePlaces places = LanePlaces::of<DP>(lane);

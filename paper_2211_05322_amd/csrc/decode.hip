@@ -57,58 +57,92 @@ struct Place {
     }
 };
 
+// A unit's results from one wave's sums: a lane has 4 neighbouring elements of its query in each block.
+template <typename T, int BLOCKS>
+__device__ inline void store_unit(const PagedArgs &a, const Place &p, const f32x4 (&o)[BLOCKS], float sum, int column,
+                                  int quarter) {
+    const int head = p.unit / a.passes, row = (p.unit - head * a.passes) * kQueries + column;
+    if (row >= a.group) return;
+    const float over = sum == 0 ? 0.0f : 1.0f / sum;
+    T *to = a.out.template at<T>(p.s, int64_t(head) * a.group + row);
+    typedef T T4 __attribute__((ext_vector_type(4)));
+#pragma unroll
+    for (int d = 0; d < BLOCKS; ++d) {
+        T4 y;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) y[e] = T(o[d][e] * over);
+        if (d * 16 + quarter * 4 < a.dim) store_any(to + d * 16 + quarter * 4, y);
+    }
+}
+
 // Keys are the instruction's rows and the group's queries its columns: a lane has
 // 8 scores of one query, whose weights then go into the second product as they
 // are.  Keys come straight into the operands' registers; values pass through LDS,
 // where the transposing load finds their columns, in a part that is the wave's
 // own, so that waves never wait for each other.  The next tile is on its way
 // meanwhile, and the page numbers of the one after it.
-template <typename T, int DP>
-__global__ __launch_bounds__(kThreads, 2) void paged_kernel(PagedArgs a) {
+//
+// TEAM = 0 deals runs of the line.  Short work is dealt in whole units, to teams
+// of 1 or 8 waves, which need no second kernel: a team's waves cut the unit's
+// tiles and join their parts in LDS.
+template <typename T, int DP, int TEAM>
+__global__ __launch_bounds__(TEAM == 8 ? 512 : kThreads, 2) void paged_kernel(PagedArgs a) {
     constexpr int STEPS = DP / 32, BLOCKS = DP / 16, WORDS = TileShape<DP>::words;
     constexpr int ROWS_AT_ONCE = kWave / WORDS, VALUES = kTile / ROWS_AT_ONCE;
-    __shared__ uint4 values[kWaves][kTile * WORDS];
+    constexpr int WAVES = TEAM == 8 ? 8 : kWaves;
+    __shared__ uint4 values[WAVES][kTile * WORDS];
+    __shared__ float2 stats[TEAM > 1 ? TEAM : 1][kQueries];  // maximum and sum
     const int lane = threadIdx.x % kWave, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
     const int column = lane % 16, quarter = lane / 16, units = a.kv_heads * a.passes;
-    const int64_t number = int64_t(blockIdx.x) * kWaves + wave;
-
-    // this wave's run of the line
-    const int share = (a.sequences + kWave - 1) / kWave;
-    const int from_s = min(lane * share, a.sequences), to_s = min(from_s + share, a.sequences);
-    int64_t mine = 0;
-    for (int s = from_s; s < to_s; ++s) mine += tiles_of(length_of(a, s));
-    int64_t before = mine;
-#pragma unroll
-    for (int d = 1; d < kWave; d *= 2) {
-        const int64_t other = __shfl_up(before, d);
-        if (lane >= d) before += other;
-    }
-    const int64_t total = __shfl(before, kWave - 1), all = total * units;
-    before -= mine;
-    if (number == 0) {  // for the joining kernel
-        int64_t n = before;
-        for (int s = from_s; s < to_s; ++s) {
-            a.line[s] = n;
-            n += tiles_of(length_of(a, s));
-        }
-        if (lane == 0) a.line[a.sequences] = total;
-    }
-    const int64_t runs = min(all, int64_t(gridDim.x) * kWaves);
-    if (number >= runs) return;
-    const int64_t at = all * number / runs;
-    int64_t left = all * (number + 1) / runs - at;  // at least one tile
-    int s0 = from_s;
-    const bool here = mine > 0 && before * units <= at && at < (before + mine) * units;
-    if (here) {
-        for (int64_t n; (before + (n = tiles_of(length_of(a, s0)))) * units <= at; ++s0) before += n;
-    }
-    const int holder = __builtin_ctzll(__builtin_amdgcn_ballot_w64(here));
+    const int64_t number = int64_t(blockIdx.x) * WAVES + wave;
     Place place;
-    place.sequence(a, __builtin_amdgcn_readfirstlane(__shfl(s0, holder)));
-    {
-        const int64_t in = at - __shfl(before, holder) * units;
-        place.unit = __builtin_amdgcn_readfirstlane(int(in / place.tiles));
-        place.t = __builtin_amdgcn_readfirstlane(int(in - int64_t(place.unit) * place.tiles));
+    int64_t left;  // tiles of this wave
+    if constexpr (TEAM == 0) {
+        // this wave's run of the line
+        const int share = (a.sequences + kWave - 1) / kWave;
+        const int from_s = min(lane * share, a.sequences), to_s = min(from_s + share, a.sequences);
+        int64_t mine = 0;
+        for (int s = from_s; s < to_s; ++s) mine += tiles_of(length_of(a, s));
+        int64_t before = mine;
+    #pragma unroll
+        for (int d = 1; d < kWave; d *= 2) {
+            const int64_t other = __shfl_up(before, d);
+            if (lane >= d) before += other;
+        }
+        const int64_t total = __shfl(before, kWave - 1), all = total * units;
+        before -= mine;
+        if (number == 0) {  // for the joining kernel
+            int64_t n = before;
+            for (int s = from_s; s < to_s; ++s) {
+                a.line[s] = n;
+                n += tiles_of(length_of(a, s));
+            }
+            if (lane == 0) a.line[a.sequences] = total;
+        }
+        const int64_t runs = min(all, int64_t(gridDim.x) * kWaves);
+        if (number >= runs) return;
+        const int64_t at = all * number / runs;
+        left = all * (number + 1) / runs - at;  // at least one tile
+        int s0 = from_s;
+        const bool here = mine > 0 && before * units <= at && at < (before + mine) * units;
+        if (here) {
+            for (int64_t n; (before + (n = tiles_of(length_of(a, s0)))) * units <= at; ++s0) before += n;
+        }
+        const int holder = __builtin_ctzll(__builtin_amdgcn_ballot_w64(here));
+        place.sequence(a, __builtin_amdgcn_readfirstlane(__shfl(s0, holder)));
+        {
+            const int64_t in = at - __shfl(before, holder) * units;
+            place.unit = __builtin_amdgcn_readfirstlane(int(in / place.tiles));
+            place.t = __builtin_amdgcn_readfirstlane(int(in - int64_t(place.unit) * place.tiles));
+        }
+    } else {
+        const int64_t team = number / TEAM;
+        if (team >= int64_t(a.sequences) * units) return;  // of 8 waves: a whole workgroup
+        place.sequence(a, int(team / units));
+        place.unit = int(team - int64_t(place.s) * units);
+        const int part = wave % TEAM;
+        place.t = int(int64_t(place.tiles) * part / TEAM);
+        left = int64_t(place.tiles) * (part + 1) / TEAM - place.t;
     }
 
     auto page_of = [&](const Place &p, bool there) {
@@ -166,17 +200,21 @@ __global__ __launch_bounds__(kThreads, 2) void paged_kernel(PagedArgs a) {
 #pragma unroll
     for (int d = 0; d < BLOCKS; ++d) o[d] = f32x4{0, 0, 0, 0};
     float m = kLowest, l = 0;
-    bool begun = place.t == 0;  // whether the unit's first tile is this wave's
-    Place ahead = place;
-    int64_t now = offset_of(place, page_of(place, true)), next;
+    bool begun = TEAM > 0 || place.t == 0;  // whether the unit's first tile is this wave's
+    auto following = [&](Place p) {
+        if constexpr (TEAM > 0) ++p.t;
+        else p.next(a, units);
+        return p;
+    };
+    Place ahead = following(place);
+    int64_t now = offset_of(place, page_of(place, left > 0)), next;
+    const int page_ahead = page_of(ahead, left > 1);
     load_queries(place);
     load_keys(now);
     load_values(now);
-    ahead.next(a, units);
-    next = offset_of(ahead, page_of(ahead, left > 1));
-    for (;;) {
-        Place second = ahead;
-        second.next(a, units);
+    next = offset_of(ahead, page_ahead);
+    while (left > 0) {
+        const Place second = following(ahead);
         const int page = page_of(second, left > 2);
         f32x4 x[2];
 #pragma unroll
@@ -237,31 +275,18 @@ __global__ __launch_bounds__(kThreads, 2) void paged_kernel(PagedArgs a) {
         __builtin_amdgcn_wave_barrier();
         --left;
         const bool ends = place.t + 1 == place.tiles;
-        if (ends || left == 0) {  // the unit's results, or this wave's part of them
+        if (TEAM == 0 && (ends || left == 0)) {  // the unit's results, or this wave's part of them
             l += __shfl_xor(l, 16);
             l += __shfl_xor(l, 32);
-            const int head = place.unit / a.passes, group0 = (place.unit - head * a.passes) * kQueries;
-            if (column < a.group - group0) {
-                if (begun && ends) {
-                    const float over = l == 0 ? 0.0f : 1.0f / l;
-                    T *to = a.out.template at<T>(place.s, int64_t(head) * a.group + group0 + column);
-                    typedef T T4 __attribute__((ext_vector_type(4)));
+            if (begun && ends) {
+                store_unit<T>(a, place, o, l, column, quarter);
+            } else if (column < a.group - place.unit % a.passes * kQueries) {
+                float *to = a.parts + (number * 2 + begun) * a.rows * (a.dim + 2);
 #pragma unroll
-                    for (int d = 0; d < BLOCKS; ++d) {
-                        T4 y;
-#pragma unroll
-                        for (int e = 0; e < 4; ++e) y[e] = T(o[d][e] * over);
-                        if (d * 16 + quarter * 4 < a.dim) store_any(to + d * 16 + quarter * 4, y);
-                    }
-                } else {
-                    float *to = a.parts + (number * 2 + begun) * a.rows * (a.dim + 2);
-#pragma unroll
-                    for (int d = 0; d < BLOCKS; ++d)
-                        if (d * 16 + quarter * 4 < a.dim) store_any(to + column * a.dim + d * 16 + quarter * 4, o[d]);
-                    if (quarter == 0) store_any(to + a.rows * a.dim + column * 2, make_float2(m, l));
-                }
+                for (int d = 0; d < BLOCKS; ++d)
+                    if (d * 16 + quarter * 4 < a.dim) store_any(to + column * a.dim + d * 16 + quarter * 4, o[d]);
+                if (quarter == 0) store_any(to + a.rows * a.dim + column * 2, make_float2(m, l));
             }
-            if (left == 0) return;
             begun = true;
             load_queries(ahead);
 #pragma unroll
@@ -272,16 +297,49 @@ __global__ __launch_bounds__(kThreads, 2) void paged_kernel(PagedArgs a) {
         place = ahead;
         ahead = second;
     }
+    if constexpr (TEAM > 0) {
+        l += __shfl_xor(l, 16);
+        l += __shfl_xor(l, 32);
+        if constexpr (TEAM == 1) {
+            store_unit<T>(a, place, o, l, column, quarter);
+        } else {
+            if (quarter == 0) stats[wave][column] = make_float2(m, l);
+            f32x4 *mine = reinterpret_cast<f32x4 *>(values[wave]);  // [queries][DP / 4]
+#pragma unroll
+            for (int d = 0; d < BLOCKS; ++d) mine[column * (DP / 4) + d * 4 + quarter] = o[d];
+            __syncthreads();
+            const int head = place.unit / a.passes, group0 = (place.unit - head * a.passes) * kQueries;
+            const int vectors = a.dim / 4, rows = min(kQueries, a.group - group0);
+            for (int i = threadIdx.x; i < rows * vectors; i += TEAM * kWave) {
+                const int r = i / vectors, d = i - r * vectors;
+                float top = kLowest, sum = 0;
+                f32x4 value{0, 0, 0, 0};
+#pragma unroll
+                for (int w = 0; w < TEAM; ++w) top = fmaxf(top, stats[w][r].x);
+#pragma unroll
+                for (int w = 0; w < TEAM; ++w) {
+                    const float f = __builtin_amdgcn_exp2f(stats[w][r].x - top);
+                    const f32x4 x = reinterpret_cast<const f32x4 *>(values[w])[r * (DP / 4) + d];
+                    sum = fmaf(f, stats[w][r].y, sum);
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) value[e] = fmaf(f, x[e], value[e]);
+                }
+                T *to = a.out.template at<T>(place.s, int64_t(head) * a.group + group0 + r) + d * 4;
+#pragma unroll
+                for (int e = 0; e < 4; ++e) to[e] = T(sum == 0 ? 0.0f : value[e] / sum);
+            }
+        }
+    }
 }
 
 // Joins the parts of each unit that more than one wave had, and writes the zeros
 // of sequences without tokens.  A workgroup a unit; where its vectors of 4
 // elements are fewer than threads, groups of threads share the parts.
-template <typename T>
-__global__ __launch_bounds__(kThreads) void paged_join_kernel(PagedArgs a, uint32_t waves) {
-    __shared__ float tops[kQueries][kThreads / kQueries];
-    __shared__ f32x4 shared_value[kThreads];
-    __shared__ float shared_sum[kThreads];
+template <typename T, int THREADS>
+__global__ __launch_bounds__(THREADS) void paged_join_kernel(PagedArgs a, uint32_t waves) {
+    __shared__ float tops[kQueries][THREADS / kQueries];
+    __shared__ f32x4 shared_value[THREADS];
+    __shared__ float shared_sum[THREADS];
     const int units = a.kv_heads * a.passes, s = blockIdx.x / units, unit = blockIdx.x - s * units;
     const int head = unit / a.passes, group0 = (unit - head * a.passes) * kQueries, rows = min(kQueries, a.group - group0);
     const int64_t tiles = a.line[s + 1] - a.line[s], all = a.line[a.sequences] * units;
@@ -303,22 +361,22 @@ __global__ __launch_bounds__(kThreads) void paged_join_kernel(PagedArgs a, uint3
         float top = kLowest;
         if (r < rows) {
 #pragma unroll 4
-            for (int i = j; i < parts; i += kThreads / kQueries) top = fmaxf(top, part(i)[a.rows * a.dim + r * 2]);
+            for (int i = j; i < parts; i += THREADS / kQueries) top = fmaxf(top, part(i)[a.rows * a.dim + r * 2]);
         }
         tops[r][j] = top;
     }
     __syncthreads();
-    const int vectors = rows * (a.dim / 4), groups = max(1, kThreads / vectors);
-    for (int e0 = 0; e0 < vectors; e0 += kThreads) {
-        const int group = threadIdx.x / min(vectors, kThreads), e = e0 + threadIdx.x - group * min(vectors, kThreads);
+    const int vectors = rows * (a.dim / 4), groups = max(1, THREADS / vectors);
+    for (int e0 = 0; e0 < vectors; e0 += THREADS) {
+        const int group = threadIdx.x / min(vectors, THREADS), e = e0 + threadIdx.x - group * min(vectors, THREADS);
         const int r = e / (a.dim / 4), d = (e - r * (a.dim / 4)) * 4;
         f32x4 value{0, 0, 0, 0};
         float sum = 0;
         if (group < groups && e < vectors) {
             float top = tops[r][0];
 #pragma unroll
-            for (int j = 1; j < kThreads / kQueries; ++j) top = fmaxf(top, tops[r][j]);
-#pragma unroll 4
+            for (int j = 1; j < THREADS / kQueries; ++j) top = fmaxf(top, tops[r][j]);
+#pragma unroll 8
             for (int i = group; i < parts; i += groups) {
                 const float *from = part(i);
                 const float2 stat = load_any<float2>(from + a.rows * a.dim + r * 2);
@@ -348,13 +406,17 @@ __global__ __launch_bounds__(kThreads) void paged_join_kernel(PagedArgs a, uint3
     }
 }
 
-// Two workgroups a CU, or a wave a tile where there are fewer.
-int64_t workgroups_of(int64_t sequences, int64_t kv_heads, int64_t passes, int64_t slots) {
-    const int64_t tiles = ceil_div(slots, kTile), most = 512;
-    if (tiles == 0) return 1;
-    return std::max<int64_t>(1, tiles >= most * kWaves
-                                    ? most
-                                    : std::min(most, ceil_div(sequences * kv_heads * passes * tiles, kWaves)));
+// How a call is dealt: waves of a unit's team (0: runs of the line), and workgroups.
+struct Deal {
+    int team;
+    int64_t workgroups;
+};
+Deal deal_of(int64_t sequences, int64_t kv_heads, int64_t passes, int64_t slots) {
+    const int64_t tiles = ceil_div(slots, kTile), units = sequences * kv_heads * passes;
+    const int64_t most = 512;  // two workgroups a CU
+    if (units <= 512 && tiles <= 16) return Deal{8, units};
+    if (tiles <= 2 || (tiles <= 16 && units >= most * kWaves)) return Deal{1, ceil_div(units, kWaves)};
+    return Deal{0, tiles >= most * kWaves ? most : std::min(most, ceil_div(units * tiles, kWaves))};
 }
 
 }  // namespace
@@ -368,8 +430,9 @@ extern "C" int64_t reshard_attention_paged_workspace(int64_t sequences, int64_t 
         pages_a_sequence > 0x7fffffff / page_length)
         return -1;
     const int64_t group = heads / kv_heads, passes = ceil_div(group, kQueries);
-    const int64_t n = workgroups_of(sequences, kv_heads, passes, pages_a_sequence * page_length);
-    return (sequences + 2) / 2 * 16 + n * kWaves * 2 * std::min<int64_t>(group, kQueries) * (dim + 2) * 4;
+    const Deal deal = deal_of(sequences, kv_heads, passes, pages_a_sequence * page_length);
+    if (deal.team > 0) return 0;
+    return (sequences + 2) / 2 * 16 + deal.workgroups * kWaves * 2 * std::min<int64_t>(group, kQueries) * (dim + 2) * 4;
 }
 
 extern "C" reshard_status_t reshard_attention_paged(int64_t sequences, int64_t heads, int64_t kv_heads, int64_t dim,
@@ -404,7 +467,7 @@ extern "C" reshard_status_t reshard_attention_paged(int64_t sequences, int64_t h
         const int64_t need = reshard_attention_paged_workspace(sequences, heads, kv_heads, dim, pages_a_sequence,
                                                                cache->page_length);
         if (sequences == 0) return RESHARD_OK;
-        st = check_workspace("the parts of long sequences need", workspace, workspace_bytes, need);
+        if (need > 0) st = check_workspace("the parts of long sequences need", workspace, workspace_bytes, need);
         if (st != RESHARD_OK) return st;
         a.pages = pages;
         a.lengths = lengths;
@@ -426,16 +489,27 @@ extern "C" reshard_status_t reshard_attention_paged(int64_t sequences, int64_t h
         a.magic = uint32_t((uint64_t(1) << 32) * ((uint64_t(1) << shift) - d) / d + 1);
         a.magic_shift = shift;
         a.scale2 = float(scale) * kLog2e;
-        const unsigned n = unsigned(workgroups_of(sequences, kv_heads, passes, pages_a_sequence * cache->page_length));
+        const Deal deal = deal_of(sequences, kv_heads, passes, pages_a_sequence * cache->page_length);
+        const unsigned n = unsigned(deal.workgroups);
         const hipStream_t s = static_cast<hipStream_t>(stream);
         auto go = [&](auto zero) {
             using T = decltype(zero);
-            auto *kernel = dim <= 32 ? paged_kernel<T, 32> : dim <= 64 ? paged_kernel<T, 64>
-                                   : dim <= 96 ? paged_kernel<T, 96> : paged_kernel<T, 128>;
-            reshard_status_t status = launch("paged attention launch", kernel, dim3(n), kThreads, 0, s, a);
+            auto start = [&](auto team) {
+                constexpr int TEAM = decltype(team)::value;
+                auto *kernel = dim <= 32 ? paged_kernel<T, 32, TEAM> : dim <= 64 ? paged_kernel<T, 64, TEAM>
+                                       : dim <= 96 ? paged_kernel<T, 96, TEAM> : paged_kernel<T, 128, TEAM>;
+                return launch("paged attention launch", kernel, dim3(n), TEAM == 8 ? 512 : kThreads, 0, s, a);
+            };
+            using std::integral_constant;
+            if (deal.team == 8) return start(integral_constant<int, 8>{});
+            if (deal.team == 1) return start(integral_constant<int, 1>{});
+            reshard_status_t status = start(integral_constant<int, 0>{});
             if (status != RESHARD_OK) return status;
-            return launch("paged attention join launch", paged_join_kernel<T>,
-                          dim3(unsigned(sequences * kv_heads * passes)), kThreads, 0, s, a, n * kWaves);
+            // few units have many parts each, many units few
+            const unsigned units = unsigned(sequences * kv_heads * passes), threads = units <= 256 ? 1024 : 64;
+            return launch("paged attention join launch",
+                          threads == 1024 ? paged_join_kernel<T, 1024> : paged_join_kernel<T, 64>, dim3(units), threads, 0, s,
+                          a, n * kWaves);
         };
         return dtype == RESHARD_BF16 ? go(bf16{}) : go(f16{});
     });

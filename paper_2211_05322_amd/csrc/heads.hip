@@ -165,6 +165,7 @@ struct HeadsArgs {
 
 constexpr int kHeadsThreads = 256, kHeadsTurns = 2;
 
+
 // A workgroup takes a run of (token, head)s, 1 << lanes_shift lanes a head and
 // kHeadsTurns heads for each group of lanes, loaded before the angles are
 // computed.
@@ -255,16 +256,17 @@ struct HeadsGradArgs {
 
 // The first workgroups take queries, the others keys, each a contiguous run of
 // (token, head)s, of which every group of lanes holds its columns' sums in
-// registers; no atomics.
+// registers; no atomics.  A step's heads are loaded while the one before is
+// computed, and its angles' positions with them.
 template <typename T, int VP, bool NEIGHBOURS>
-__global__ __launch_bounds__(kHeadsThreads) void heads_grad_kernel(HeadsGradArgs a) {
+__global__ __launch_bounds__(kHeadsThreads, 3) void heads_grad_kernel(HeadsGradArgs a) {
     extern __shared__ float2 turns[];  // [2][span][dim / 2]; at the end a sum for each group and column
     const int k = int(blockIdx.x) >= a.workgroups[0], wg = int(blockIdx.x) - (k ? a.workgroups[0] : 0);
     const int groups = kHeadsThreads >> a.lanes_shift, group = threadIdx.x >> a.lanes_shift;
     const Place<VP, NEIGHBOURS> at(threadIdx.x & ((1 << a.lanes_shift) - 1), a.dim, a.rotary);
-    const int each = a.heads[k];
-    const int64_t total = a.tokens * each, step = groups * kHeadsTurns;
-    const int64_t steps = ceil_div(total, step), n = a.workgroups[k];
+    const int each = a.heads[k], pairs = a.dim / 2, entries = a.span * pairs;
+    const int64_t total = a.tokens * each;
+    const int64_t steps = ceil_div(total, groups), n = a.workgroups[k];
     const int64_t from = steps * wg / n, until = steps * (wg + 1) / n;
     float w0[VP], w1[VP], s0[VP], s1[VP];
 #pragma unroll
@@ -274,49 +276,70 @@ __global__ __launch_bounds__(kHeadsThreads) void heads_grad_kernel(HeadsGradArgs
         w1[i] = weight_at(a.weight[k], a.weight_dtype, e.e1);
         s0[i] = s1[i] = 0;
     }
-    int turn_of = 0;
-    for (int64_t s = from; s < until; ++s, turn_of ^= 1) {
-        const int64_t first = s * step, token0 = first / each;
-        const int rest = int(first - token0 * each);
-        Part<T, VP> px[kHeadsTurns][2], pd[kHeadsTurns][2];
-        int token[kHeadsTurns], head[kHeadsTurns];
-#pragma unroll
-        for (int u = 0; u < kHeadsTurns; ++u) {
-            const int i = rest + u * groups + group;
-            token[u] = i / each;
-            head[u] = i - token[u] * each;
-            const int64_t t = token0 + token[u];
-            if (t >= a.tokens || !at.any) head[u] = -1;
-            if (head[u] < 0) continue;
-            const T *x = a.x[k].template at<const T>(t, head[u]), *d = a.d[k].template at<const T>(t, head[u]);
-            __builtin_memcpy(&px[u][0], x + at.e0, sizeof px[u][0]);
-            __builtin_memcpy(&px[u][1], x + at.e1, sizeof px[u][0]);
-            __builtin_memcpy(&pd[u][0], d + at.e0, sizeof px[u][0]);
-            __builtin_memcpy(&pd[u][1], d + at.e1, sizeof px[u][0]);
+    // the table's first entry of a thread: always the same pair
+    const int my_token = int(threadIdx.x) / pairs, my_pair = int(threadIdx.x) - my_token * pairs;
+    const bool turned = my_pair < a.rotary / 2 && int(threadIdx.x) < entries;
+    const double my_frequency = turned ? a.frequencies[my_pair] : 0.0;
+
+    Part<T, VP> next_x[2], next_d[2];
+    int64_t next_token = from * groups / each, step_token = next_token;  // of the step's first head; of the group's
+    int next_rest = int(from * groups - next_token * each), in_token = 0, head = -1, position = 0;
+    auto load = [&](int64_t s) {
+        const int i = next_rest + group, t = i / each;
+        in_token = t;
+        head = i - t * each;
+        step_token = next_token;
+        if (s >= until || next_token + t >= a.tokens || !at.any) head = -1;
+        if (head >= 0) {
+            const T *x = a.x[k].template at<const T>(next_token + t, head), *d = a.d[k].template at<const T>(next_token + t, head);
+            __builtin_memcpy(&next_x[0], x + at.e0, sizeof next_x[0]);
+            __builtin_memcpy(&next_x[1], x + at.e1, sizeof next_x[0]);
+            __builtin_memcpy(&next_d[0], d + at.e0, sizeof next_x[0]);
+            __builtin_memcpy(&next_d[1], d + at.e1, sizeof next_x[0]);
         }
-        float2 *table = turns + turn_of * a.span * (a.dim / 2);
-        fill_turns<NEIGHBOURS>(table, a.positions, a.frequencies, token0, a.tokens, a.span, a.dim, a.rotary);
-        __syncthreads();  // the other half was read before the barrier ahead of this one
+        if (turned) position = a.positions[min(next_token + my_token, a.tokens - 1)];
+        next_rest += groups;
+        const int whole = next_rest / each;
+        next_token += whole;
+        next_rest -= whole * each;
+    };
+    auto fill = [&](float2 *table) {  // of the step that was loaded last
+        if (int(threadIdx.x) < entries) table[threadIdx.x] = turned ? turn(position, my_frequency) : make_float2(1, 0);
+        for (int i = threadIdx.x + kHeadsThreads; i < entries; i += kHeadsThreads) {
+            const int t = i / pairs, p = i - t * pairs;
+            table[i] = p < a.rotary / 2 ? turn(a.positions[min(step_token + t, a.tokens - 1)], a.frequencies[p])
+                                        : make_float2(1, 0);
+        }
+    };
+    if (from < until) {
+        load(from);
+        fill(turns);
+    }
+    int which = 0;
+    for (int64_t s = from; s < until; ++s, which ^= 1) {
+        __syncthreads();
+        const float2 *table = turns + which * entries;
+        Pairs<T, VP, NEIGHBOURS> x, d;
+        const int h = head, t = in_token;
+        const int64_t token = step_token + t;
+        float sum = 0, along = 0;
+        x.set(next_x[0], next_x[1]);
+        d.set(next_d[0], next_d[1]);
+        load(s + 1);
+        if (h >= 0) {
+            const float2 *c = table + t * pairs + at.pair;
 #pragma unroll
-        for (int u = 0; u < kHeadsTurns; ++u) {
-            Pairs<T, VP, NEIGHBOURS> x, d;
-            float sum = 0, along = 0;
-            if (head[u] >= 0) {
-                x.set(px[u][0], px[u][1]);
-                d.set(pd[u][0], pd[u][1]);
-                const float2 *c = table + token[u] * (a.dim / 2) + at.pair;
-#pragma unroll
-                for (int i = 0; i < VP; ++i) {
-                    sum = fmaf(x.a[i], x.a[i], fmaf(x.b[i], x.b[i], sum));
-                    const float f = d.a[i] * c[i].x + d.b[i] * c[i].y, g = d.b[i] * c[i].x - d.a[i] * c[i].y;
-                    d.a[i] = f;
-                    d.b[i] = g;
-                    along = fmaf(f * w0[i], x.a[i], fmaf(g * w1[i], x.b[i], along));
-                }
+            for (int i = 0; i < VP; ++i) {
+                sum = fmaf(x.a[i], x.a[i], fmaf(x.b[i], x.b[i], sum));
+                const float f = d.a[i] * c[i].x + d.b[i] * c[i].y, g = d.b[i] * c[i].x - d.a[i] * c[i].y;
+                d.a[i] = f;
+                d.b[i] = g;
+                along = fmaf(f * w0[i], x.a[i], fmaf(g * w1[i], x.b[i], along));
             }
-            sum = lanes_sum(sum, a.lanes_shift);
-            along = lanes_sum(along, a.lanes_shift);
-            if (head[u] < 0) continue;
+        }
+        sum = lanes_sum(sum, a.lanes_shift);
+        along = lanes_sum(along, a.lanes_shift);
+        if (h >= 0) {
             const float r = 1.0f / sqrtf(sum / float(a.dim) + a.eps);
             const float mean = along * r / float(a.dim);
 #pragma unroll
@@ -327,8 +350,9 @@ __global__ __launch_bounds__(kHeadsThreads) void heads_grad_kernel(HeadsGradArgs
                 x.a[i] = r * (d.a[i] * w0[i] - h0 * mean);
                 x.b[i] = r * (d.b[i] * w1[i] - h1 * mean);
             }
-            if (a.dx[k].data) x.store(a.dx[k].template at<T>(token0 + token[u], head[u]), at.e0, at.e1);
+            if (a.dx[k].data) x.store(a.dx[k].template at<T>(token, h), at.e0, at.e1);
         }
+        if (s + 1 < until) fill(turns + (which ^ 1) * entries);
     }
     if (!a.partial) return;
     __syncthreads();
@@ -426,7 +450,7 @@ reshard_status_t check_rotation(int64_t tokens, int64_t heads, int64_t kv_heads,
 // Tokens that a run of `items` heads can touch where a token has `each`.
 int span_of(int items, int each) { return (items + each - 2) / each + 1; }
 
-constexpr int kGradWorkgroups = 1024;
+constexpr int kGradWorkgroups = 768;  // three a CU, what registers allow
 
 // Workgroups of the gradients: queries' and keys' share by their heads.
 void split_workgroups(int64_t tokens, int64_t heads, int64_t kv_heads, int *q, int *k) {
@@ -552,7 +576,7 @@ extern "C" reshard_status_t reshard_rotate_heads_backward(
             st = with_heads(dtype, a.dim, a.rotary, interleaved, [&](auto zero, auto vp, auto neighbours) {
                 constexpr int VP = decltype(vp)::value;
                 a.lanes_shift = shift_of(a.dim / 2 / VP);
-                const int groups = kHeadsThreads >> a.lanes_shift, items = groups * kHeadsTurns;
+                const int groups = kHeadsThreads >> a.lanes_shift, items = groups;
                 a.span = span_of(items, int(std::min(heads, kv_heads)));
                 const size_t lds = std::max(size_t(2) * a.span * (a.dim / 2) * 8, size_t(groups) * a.dim * 4);
                 return launch("heads gradient launch", heads_grad_kernel<decltype(zero), VP, decltype(neighbours)::value>,

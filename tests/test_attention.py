@@ -552,6 +552,21 @@ def test_attention_paged_over_many_and_long(gpu_lib):
 
 
 @gpu
+@pytest.mark.parametrize("heads,kv,dim", [(4, 4, 128), (16, 8, 64), (40, 2, 96), (6, 6, 16)])
+@pytest.mark.parametrize("dtype", HALVES, ids=str)
+def test_attention_paged_of_every_length(dtype, heads, kv, dim, gpu_lib):
+    """A batch whose sequences are cut anywhere among the waves, empty ones between them; and short ones, a wave each."""
+    for n, longest in ((70, 900), (200, 250)):
+        g = _seed("every length", dtype, heads, n)
+        lengths = torch.randint(0, longest, (n,), generator=g)
+        lengths[torch.randint(0, n, (n // 8,), generator=g)] = 0
+        lengths = lengths.tolist()
+        caches, table = _paged_case(g, dtype, lengths, kv, dim, 16, -(-longest // 16))
+        q = _randn(g, n, heads, dim).to(dtype).cuda()
+        _check_paged(q, caches, table, lengths, dim ** -0.5, B.reshard_attention_paged(q, *caches, table, _int32(lengths)), n)
+
+
+@gpu
 def test_attention_paged_of_pages_outside_the_cache(gpu_lib):
     """Their tokens do not count; a length past the table is the table's."""
     g = _seed("outside")
