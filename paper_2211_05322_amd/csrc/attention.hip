@@ -30,10 +30,10 @@ struct PromptArgs {
 // keys and values, which is loaded while the one before is used.
 // The maximum only rises when a score passes it by 2^8, so that most tiles
 // leave the sums as they are.
-template <typename T, int DP, int QB, bool ASYNC>
-__global__ __launch_bounds__(kThreads, QB == 1 ? 2 : 1) void attention_kernel(PromptArgs a) {
-    constexpr int STEPS = DP / 16, BLOCKS = DP / 32, ROWS = 32 * QB * kWaves, KEYS = 64, PARTS = KEYS / 32;
-    constexpr int SHIFT = QB == 1 ? 7 : 8, WORDS = KEYS * TileShape<DP>::words;
+template <typename T, int DP, bool ASYNC>
+__global__ __launch_bounds__(kThreads, 2) void attention_kernel(PromptArgs a) {
+    constexpr int STEPS = DP / 16, BLOCKS = DP / 32, ROWS = 32 * kWaves, KEYS = 64, PARTS = KEYS / 32;
+    constexpr int SHIFT = 7, WORDS = KEYS * TileShape<DP>::words;
     // arrays by name: only so does the compiler see that loads into one leave the others alone
     __shared__ uint4 k0[WORDS], v0[WORDS], k1[WORDS], v1[WORDS];
     const Task task = task_of(blockIdx.x, a.blocks, a.heads, a.group);
@@ -41,133 +41,109 @@ __global__ __launch_bounds__(kThreads, QB == 1 ? 2 : 1) void attention_kernel(Pr
     if (!ranked_sequence(a.seq, false, a.causal, a.blocks, task.block, SHIFT, &s)) return;
     const int lane = threadIdx.x % kWave, wave = threadIdx.x / kWave, half = lane / 32;
     const int kv_head = task.head / a.group;
-    const int row0 = s.block * ROWS + wave * 32 * QB;
+    const int row0 = s.block * ROWS + wave * 32, row = row0 + lane % 32, held = min(row, s.lq - 1);
     const T *k = a.k.template at<const T>(s.k0, kv_head), *v = a.v.template at<const T>(s.k0, kv_head);
-
-    Operand8<T> q[QB][STEPS];
-    int last[QB];  // the last key that the lane's query sees
-#pragma unroll
-    for (int b = 0; b < QB; ++b) {
-        const int row = row0 + b * 32 + lane % 32;
-        const T *at = a.q.template at<const T>(s.q0 + min(row, s.lq - 1), task.head);
-#pragma unroll
-        for (int i = 0; i < STEPS; ++i) q[b][i] = global_operand(at, true, i, lane, a.dim);
-        last[b] = a.causal ? min(row, s.lq - 1) + s.lk - s.lq : s.lk - 1;
-    }
     const int to = a.causal ? min(s.lk, min(s.lq, (s.block + 1) * ROWS) + s.lk - s.lq) : s.lk;  // the workgroup's keys
-    const int wave_to = row0 >= s.lq ? 0 : a.causal ? min(s.lk, min(s.lq, row0 + 32 * QB) + s.lk - s.lq) : s.lk;
-    const int all_see = a.causal ? row0 + 1 + s.lk - s.lq : s.lk;  // keys that each of the wave's queries sees
-
-    const LanePlaces places = LanePlaces::of<DP>(lane);
-    f32x16 o[QB][BLOCKS];
-    float m[QB], l[QB];
-#pragma unroll
-    for (int b = 0; b < QB; ++b) {
-        m[b] = -3.402823466e38f;
-        l[b] = 0;
-#pragma unroll
-        for (int d = 0; d < BLOCKS; ++d) o[b][d] = zero16();
-    }
     TileLoader<T, DP, KEYS, kThreads, ASYNC> kl(threadIdx.x, a.dim, a.k.token_pitch), vl(threadIdx.x, a.dim, a.v.token_pitch);
-    // a tile behind the last is asked for too, and is zeros without a read
     const int64_t k_step = KEYS * a.k.token_pitch, v_step = KEYS * a.v.token_pitch;
+    // a tile behind the last is asked for too, and is zeros without a read
     auto load = [&](int key0, auto &k_to, auto &v_to) {
         kl.start(k, s.lk - key0, k_to);
         vl.start(v, s.lk - key0, v_to);
         k += k_step;
         v += v_step;
     };
+    if (to > 0) {
+        load(0, k0, v0);
+        kl.write(k0);
+        vl.write(v0);
+    }
+
+    Operand8<T> q[STEPS];
+#pragma unroll
+    for (int i = 0; i < STEPS; ++i)
+        q[i] = global_operand(a.q.template at<const T>(s.q0 + held, task.head), true, i, lane, a.dim);
+    const int last = a.causal ? held + s.lk - s.lq : s.lk - 1;  // the last key that the lane's query sees
+    const int wave_to = row0 >= s.lq ? 0 : a.causal ? min(s.lk, min(s.lq, row0 + 32) + s.lk - s.lq) : s.lk;
+    const int all_see = a.causal ? row0 + 1 + s.lk - s.lq : s.lk;  // keys that each of the wave's queries sees
+
+    const LanePlaces places = LanePlaces::of<DP>(lane);
+    f32x16 o[BLOCKS];
+    float m = -3.402823466e38f, l = 0;
+#pragma unroll
+    for (int d = 0; d < BLOCKS; ++d) o[d] = zero16();
     auto step = [&](int key0, const auto &kt, const auto &vt, auto &k_next, auto &v_next) {
         if constexpr (ASYNC) loads_done();
         __syncthreads();
         load(key0 + KEYS, k_next, v_next);
         if (key0 < wave_to) {
-            f32x16 x[QB][PARTS];
+            f32x16 x[PARTS];
 #pragma unroll
-            for (int b = 0; b < QB; ++b)
-#pragma unroll
-                for (int n = 0; n < PARTS; ++n) x[b][n] = zero16();
-#pragma unroll
-            for (int i = 0; i < STEPS; ++i)
-#pragma unroll
-                for (int n = 0; n < PARTS; ++n) {
-                    const Operand8<T> kk = row_operand<T, DP>(kt, n * 32, i, places);
-#pragma unroll
-                    for (int b = 0; b < QB; ++b) x[b][n] = mfma(kk, q[b][i], x[b][n]);
-                }
+            for (int n = 0; n < PARTS; ++n) x[n] = zero16();
+            Operand8<T> ahead[2][2];
+            pipelined<STEPS>(
+                [&](auto i) {
+                    ahead[i % 2][0] = row_operand<T, DP>(kt, 0, i, places);
+                    ahead[i % 2][1] = row_operand<T, DP>(kt, 32, i, places);
+                },
+                [&](auto i) {
+                    x[0] = mfma(ahead[i % 2][0], q[i], x[0]);
+                    x[1] = mfma(ahead[i % 2][1], q[i], x[1]);
+                });
             if (key0 + KEYS > all_see || key0 + KEYS > s.lk) {
 #pragma unroll
-                for (int b = 0; b < QB; ++b)
-#pragma unroll
-                    for (int n = 0; n < PARTS; ++n)
-#pragma unroll
-                        for (int r = 0; r < 16; ++r)
-                            if (key0 + n * 32 + result_row(r, half) > last[b]) x[b][n][r] = -INFINITY;
-            }
-            Operand8<T> p[QB][2 * PARTS];
-#pragma unroll
-            for (int b = 0; b < QB; ++b) {
-                float top = x[b][0][0];
-#pragma unroll
                 for (int n = 0; n < PARTS; ++n)
 #pragma unroll
-                    for (int r = 0; r < 16; ++r) top = fmaxf(top, x[b][n][r]);
-                top = halves_max(top) * a.scale2;
-                if (__builtin_amdgcn_ballot_w64(top > m[b] + 8)) {
-                    const float next = fmaxf(m[b], top), shrink = exp2_fast(m[b] - next);
-                    m[b] = next;
-                    l[b] *= shrink;
+                    for (int r = 0; r < 16; ++r)
+                        if (key0 + n * 32 + result_row(r, half) > last) x[n][r] = -INFINITY;
+            }
+            float top = x[0][0];
 #pragma unroll
-                    for (int d = 0; d < BLOCKS; ++d)
+            for (int n = 0; n < PARTS; ++n)
 #pragma unroll
-                        for (int r = 0; r < 16; ++r) o[b][d][r] *= shrink;
+                for (int r = 0; r < 16; ++r) top = fmaxf(top, x[n][r]);
+            top = halves_max(top) * a.scale2;
+            if (__builtin_amdgcn_ballot_w64(top > m + 8)) {
+                const float next = fmaxf(m, top), shrink = exp2_fast(m - next);
+                m = next;
+                l *= shrink;
+#pragma unroll
+                for (int d = 0; d < BLOCKS; ++d)
+#pragma unroll
+                    for (int r = 0; r < 16; ++r) o[d][r] *= shrink;
+            }
+            Operand8<T> p[2 * PARTS];
+            float sum = 0;
+#pragma unroll
+            for (int n = 0; n < PARTS; ++n)
+#pragma unroll
+                for (int r = 0; r < 16; ++r) {
+                    const float e = exp2_fast(fmaf(x[n][r], a.scale2, -m));
+                    sum += e;
+                    p[n * 2 + r / 8].e[r % 8] = T(e);
                 }
-                float sum = 0;
-#pragma unroll
-                for (int n = 0; n < PARTS; ++n)
-#pragma unroll
-                    for (int r = 0; r < 16; ++r) {
-                        const float e = exp2_fast(fmaf(x[b][n][r], a.scale2, -m[b]));
-                        sum += e;
-                        p[b][n * 2 + r / 8].e[r % 8] = T(e);
-                    }
-                l[b] += sum;
-            }
+            l += sum;
 #pragma unroll
             for (int t = 0; t < 2 * PARTS; ++t)
 #pragma unroll
-                for (int d = 0; d < BLOCKS; ++d) {
-                    const Operand8<T> vv = column_operand<T, DP>(vt, t * 16, d, places);
-#pragma unroll
-                    for (int b = 0; b < QB; ++b) o[b][d] = mfma(vv, p[b][t], o[b][d]);
-                }
+                for (int d = 0; d < BLOCKS; ++d) o[d] = mfma(column_operand<T, DP>(vt, t * 16, d, places), p[t], o[d]);
         }
         if constexpr (!ASYNC) {
             kl.write(k_next);
             vl.write(v_next);
         }
     };
-    if (to > 0) {
-        load(0, k0, v0);
-        kl.write(k0);
-        vl.write(v0);
-    }
     for (int key0 = 0; key0 < to; key0 += 2 * KEYS) {
         step(key0, k0, v0, k1, v1);
         if (key0 + KEYS < to) step(key0 + KEYS, k1, v1, k0, v0);
     }
     loads_done();  // none may write into LDS that is another workgroup's by then
+    const float sum = halves_sum(l), over = sum == 0 ? 0.0f : 1.0f / sum;
+    T *to_row = a.out.template at<T>(s.q0 + held, task.head);
 #pragma unroll
-    for (int b = 0; b < QB; ++b) {
-        const int row = row0 + b * 32 + lane % 32;
-        const float sum = halves_sum(l[b]), over = sum == 0 ? 0.0f : 1.0f / sum;
-        T *to_row = a.out.template at<T>(s.q0 + min(row, s.lq - 1), task.head);
-#pragma unroll
-        for (int d = 0; d < BLOCKS; ++d) store_columns(to_row, row < s.lq, o[b][d], over, d, lane, a.dim);
-        if (half == 0 && row < s.lq)
-            a.lse[int64_t(task.head) * a.seq.q_tokens + s.q0 + row] =
-                sum == 0 ? -INFINITY : (m[b] + log2f(sum)) * kLn2;
-    }
+    for (int d = 0; d < BLOCKS; ++d) store_columns(to_row, row < s.lq, o[d], over, d, lane, a.dim);
+    if (half == 0 && row < s.lq)
+        a.lse[int64_t(task.head) * a.seq.q_tokens + s.q0 + row] = sum == 0 ? -INFINITY : (m + log2f(sum)) * kLn2;
 }
 
 }  // namespace
@@ -201,9 +177,9 @@ extern "C" reshard_status_t reshard_attention(int64_t q_tokens, int64_t k_tokens
         return with_dim(dtype, dim, [&](auto zero, auto padded) {
             using T = decltype(zero);
             constexpr int DP = decltype(padded)::value;
-            reshard_status_t status = check_grid(blocks_of(q_tokens, sequences, 7), heads, &a.blocks);
+            reshard_status_t status = check_grid(blocks_of(q_tokens, sequences, 7), heads, kThreads, &a.blocks);
             if (status != RESHARD_OK) return status;
-            return launch("attention launch", async ? attention_kernel<T, DP, 1, true> : attention_kernel<T, DP, 1, false>,
+            return launch("attention launch", async ? attention_kernel<T, DP, true> : attention_kernel<T, DP, false>,
                           dim3(unsigned(a.blocks * heads)), kThreads, 0, static_cast<hipStream_t>(stream), a);
         });
     });

@@ -451,8 +451,10 @@ inline reshard_status_t check_attention(int64_t q_tokens, int64_t k_tokens, int6
     return st;
 }
 
-inline reshard_status_t check_grid(int64_t blocks, int64_t heads, uint32_t *out) {
-    if (blocks * heads > int64_t(1) << 30) return fail(RESHARD_EUNSUPPORTED, "more than 2^30 blocks of rows and heads");
+// A launch has fewer than 2^32 threads.
+inline reshard_status_t check_grid(int64_t blocks, int64_t heads, int64_t threads, uint32_t *out) {
+    if (blocks * heads > 0xffffffff / threads)
+        return fail(RESHARD_EUNSUPPORTED, "more than " + std::to_string(0xffffffff / threads) + " blocks of rows and heads");
     *out = uint32_t(blocks);
     return RESHARD_OK;
 }

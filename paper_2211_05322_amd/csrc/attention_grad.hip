@@ -78,6 +78,17 @@ __global__ __launch_bounds__(kThreads, 2) void attention_dq_kernel(GradArgs a) {
     const int row = row0 + lane % 32, held = min(row, s.lq - 1);
     const T *k = a.k.template at<const T>(s.k0, kv_head), *v = a.v.template at<const T>(s.k0, kv_head);
 
+    const int to = a.causal ? min(s.lk, min(s.lq, (s.block + 1) * kRows) + s.lk - s.lq) : s.lk;
+    TileLoader<T, DP, KEYS, kThreads, ASYNC> kl(threadIdx.x, a.dim, a.k.token_pitch), vl(threadIdx.x, a.dim, a.v.token_pitch);
+    const int64_t k_step = KEYS * a.k.token_pitch, v_step = KEYS * a.v.token_pitch;
+    auto load = [&](int key0, auto &k_to, auto &v_to) {
+        kl.start(k, s.lk - key0, k_to);
+        vl.start(v, s.lk - key0, v_to);
+        k += k_step;
+        v += v_step;
+    };
+    if (to > 0) load(0, k0, v0);  // beside the rows
+
     Operand8<T> q[STEPS], dout[STEPS];
     float delta = 0;
 #pragma unroll
@@ -97,7 +108,6 @@ __global__ __launch_bounds__(kThreads, 2) void attention_dq_kernel(GradArgs a) {
         a.minus_delta[stat] = -delta;
     }
     const int last = a.causal ? held + s.lk - s.lq : s.lk - 1;
-    const int to = a.causal ? min(s.lk, min(s.lq, (s.block + 1) * kRows) + s.lk - s.lq) : s.lk;
     const int wave_to = row0 >= s.lq ? 0 : a.causal ? min(s.lk, min(s.lq, row0 + 32) + s.lk - s.lq) : s.lk;
     const int all_see = a.causal ? row0 + 1 + s.lk - s.lq : s.lk;
 
@@ -108,16 +118,7 @@ __global__ __launch_bounds__(kThreads, 2) void attention_dq_kernel(GradArgs a) {
 #pragma unroll
     for (int d = 0; d < BLOCKS; ++d) dq[d] = zero16();
     float factor = kFirstFactor;
-    TileLoader<T, DP, KEYS, kThreads, ASYNC> kl(threadIdx.x, a.dim, a.k.token_pitch), vl(threadIdx.x, a.dim, a.v.token_pitch);
-    const int64_t k_step = KEYS * a.k.token_pitch, v_step = KEYS * a.v.token_pitch;
-    auto load = [&](int key0, auto &k_to, auto &v_to) {
-        kl.start(k, s.lk - key0, k_to);
-        vl.start(v, s.lk - key0, v_to);
-        k += k_step;
-        v += v_step;
-    };
     if (to > 0) {
-        load(0, k0, v0);
         kl.finish(k0);
         vl.finish(v0);
     }
@@ -274,7 +275,7 @@ __global__ __launch_bounds__(kWave *GROUPS *PARTS, 2) void attention_dkv_kernel(
         if constexpr (VALUES_IN_LDS) {
             TileLoader<T, DP, KEYS, THREADS, ASYNC> vl(threadIdx.x, a.dim, a.v.token_pitch);
             vl.start(a.v.template at<const T>(s.k0 + s.block * KEYS, task.head), s.lk - s.block * KEYS, values);
-            vl.finish(values);
+            vl.write(values);
         }
         load(0, q0, d0, s0);
         write(q0, d0, s0);
@@ -295,12 +296,27 @@ __global__ __launch_bounds__(kWave *GROUPS *PARTS, 2) void attention_dkv_kernel(
                 for (int e = 0; e < 4; ++e) dp[4 * j + e] = delta[e];
             }
             Operand8<T> left[2][2];
-            if constexpr (VALUES_IN_LDS) {  // pipelined, it spills
-#pragma unroll
-                for (int i = 0; i < STEPS; ++i) x = mfma(row_operand<T, DP>(qt, 0, i, places), k[i], x);
-#pragma unroll
-                for (int i = 0; i < STEPS; ++i)
-                    dp = mfma(row_operand<T, DP>(dt, 0, i, places), row_operand<T, DP>(values, 0, i, v_places), dp);
+            if constexpr (VALUES_IN_LDS) {  // first the scores' steps in pairs, then dP's, so that registers hold what is ahead
+                pipelined<STEPS + STEPS / 2>(
+                    [&](auto i_) {
+                        constexpr int i = decltype(i_)::value, at = i % 2, s = i - STEPS / 2;
+                        if constexpr (i < STEPS / 2) {
+                            left[at][0] = row_operand<T, DP>(qt, 0, 2 * i, places);
+                            left[at][1] = row_operand<T, DP>(qt, 0, 2 * i + 1, places);
+                        } else {
+                            left[at][0] = row_operand<T, DP>(dt, 0, s, places);
+                            left[at][1] = row_operand<T, DP>(values, 0, s, v_places);
+                        }
+                    },
+                    [&](auto i_) {
+                        constexpr int i = decltype(i_)::value, at = i % 2, s = i - STEPS / 2;
+                        if constexpr (i < STEPS / 2) {
+                            x = mfma(left[at][0], k[2 * i], x);
+                            x = mfma(left[at][1], k[2 * i + 1], x);
+                        } else {
+                            dp = mfma(left[at][0], left[at][1], dp);
+                        }
+                    });
             } else {
                 pipelined<STEPS>(
                     [&](auto i) {
@@ -339,14 +355,7 @@ __global__ __launch_bounds__(kWave *GROUPS *PARTS, 2) void attention_dkv_kernel(
                 dv[i % BLOCKS] = mfma(left[i % 2][0], p[i / BLOCKS], dv[i % BLOCKS]);
                 dk[i % BLOCKS] = mfma(left[i % 2][1], ds[i / BLOCKS], dk[i % BLOCKS]);
             };
-            if constexpr (VALUES_IN_LDS) {
-                unrolled<2 * BLOCKS>([&](auto i) {
-                    read_columns(i);
-                    add_columns(i);
-                });
-            } else {
-                pipelined<2 * BLOCKS, true>(read_columns, add_columns);
-            }
+            pipelined<2 * BLOCKS, !VALUES_IN_LDS>(read_columns, add_columns);
         }
         row0 += QUERIES;
         if (row0 >= s.lq) row0 = from;
@@ -456,7 +465,7 @@ extern "C" reshard_status_t reshard_attention_backward(
             constexpr int DP = decltype(padded)::value;
             reshard_status_t status = RESHARD_OK;
             if (q_tokens > 0) {
-                status = check_grid(blocks_of(q_tokens, sequences, kShift), heads, &a.blocks);
+                status = check_grid(blocks_of(q_tokens, sequences, kShift), heads, kThreads, &a.blocks);
                 if (status != RESHARD_OK) return status;
                 const bool async = aligned16(a.k, 2) && aligned16(a.v, 2);
                 status = launch("attention gradient launch",
@@ -468,7 +477,7 @@ extern "C" reshard_status_t reshard_attention_backward(
             const bool async = aligned16(a.q, 2) && aligned16(a.dout, 2) && aligned16(a.v, 2);
             auto go = [&](auto groups, auto parts) {
                 constexpr int GROUPS = decltype(groups)::value, PARTS = decltype(parts)::value;
-                reshard_status_t st = check_grid(blocks_of(k_tokens, sequences, GROUPS == 4 ? 7 : 6), kv_heads, &a.blocks);
+                reshard_status_t st = check_grid(blocks_of(k_tokens, sequences, GROUPS == 4 ? 7 : 6), kv_heads, kWave * GROUPS * PARTS, &a.blocks);
                 if (st != RESHARD_OK) return st;
                 return launch("attention gradient launch",
                               async ? attention_dkv_kernel<T, DP, GROUPS, PARTS, true>

@@ -462,8 +462,8 @@ extern "C" reshard_status_t reshard_attention_paged(int64_t sequences, int64_t h
         if (st == RESHARD_OK) st = check_matrix("lengths", lengths, 1, sequences, sequences, 4);
         if (st != RESHARD_OK) return st;
         const int64_t group = heads / kv_heads, passes = ceil_div(group, kQueries);
-        if (pages_a_sequence > 0x7fffffff / cache->page_length || sequences * kv_heads * passes > int64_t(1) << 30)
-            return fail(RESHARD_EUNSUPPORTED, "a sequence's pages hold 2^31 tokens or more, or above 2^30 sequences and heads");
+        if (pages_a_sequence > 0x7fffffff / cache->page_length || sequences * kv_heads * passes > int64_t(1) << 25)
+            return fail(RESHARD_EUNSUPPORTED, "a sequence's pages hold 2^31 tokens or more, or above 2^25 sequences and key heads");
         const int64_t need = reshard_attention_paged_workspace(sequences, heads, kv_heads, dim, pages_a_sequence,
                                                                cache->page_length);
         if (sequences == 0) return RESHARD_OK;

@@ -510,7 +510,8 @@ extern "C" reshard_status_t reshard_rotate_heads(int64_t tokens, int64_t heads, 
             const int items = (kHeadsThreads >> a.lanes_shift) * kHeadsTurns;
             a.span = span_of(items, a.each);
             const int64_t grid = ceil_div(tokens * a.each, items);
-            if (grid > int64_t(1) << 30) return fail(RESHARD_EUNSUPPORTED, "tokens * heads is above 2^30 workgroups");
+            if (grid > 0xffffffff / kHeadsThreads)  // a launch has fewer than 2^32 threads
+                return fail(RESHARD_EUNSUPPORTED, "more than 2^24 - 1 workgroups of heads");
             const size_t lds = size_t(a.span) * (a.dim / 2) * 8 + size_t(a.dim) * 8;
             return launch("heads launch", heads_kernel<decltype(zero), VP, decltype(neighbours)::value>,
                           dim3(unsigned(grid)), kHeadsThreads, lds, static_cast<hipStream_t>(stream), a);

@@ -726,6 +726,7 @@ def test_rotate_heads_refusals():
             (dict(eps=math.nan), EI, "eps"), (dict(f=None), EI, "frequencies"), (dict(pos=None), EI, "positions"), (dict(q=None), EI, "q is"),
             (dict(k=_at(None)), EI, "k is"), (dict(qo=_at(head=63)), EI, "overlap"), (dict(qo=_at(token=511)), EI, "overlap"),
             (dict(ko=_at(P + 1)), EI, "aligned"), (dict(q=_at(token=-1)), EU, "pitch"), (dict(q=_at(token=1 << 60)), EU, "pitch"),
+            (dict(tokens=1 << 28, qo=_at(token=512), ko=_at(token=128)), EU, "workgroups"),
             (dict(v=_at()), EI, "go together"), (dict(cache=cache), EI, "go together"), (dict(v=_at(), cache=cache), EI, "slots"),
             (dict(v=_at(), cache=_cache(P, P, 10, 0, 1, 1, 1), slots=P), EI, "page_length"),
             (dict(v=_at(), cache=_cache(P, None, 10, 16, 2048, 128, 64), slots=P), EI, "values"),
@@ -754,7 +755,7 @@ def test_attention_refusals():
             (dict(dt=4), EI, "dtype"), (dict(scale=0.0), EI, "scale"), (dict(scale=math.nan), EI, "scale"), (dict(scale=math.inf), EI, "scale"),
             (dict(causal=2), EI, "causal"), (dict(q=None), EI, "q is"), (dict(k=_at(None)), EI, "k is"), (dict(qo=None), EI, "q_offsets"),
             (dict(out=_at(token=8)), EI, "overlap"), (dict(lse=None), EI, "lse"), (dict(q=_at(P + 1)), EI, "aligned"),
-            (dict(nq=1 << 30, heads=1 << 16, kv=1, q=_at(token=0, head=0), out=_at(token=1 << 22)), EU, "2^30")):
+            (dict(nq=1 << 30, heads=1 << 16, kv=1, q=_at(token=0, head=0), out=_at(token=1 << 22)), EU, "blocks of rows")):
         _refused(fwd(**call), status, text)
     for call, text in ((dict(d=None), "dout"), (dict(out=_at(None)), "out"), (dict(lse=None), "lse"), (dict(dq=_at(head=0)), "overlap"),
                        (dict(dk=None), "dk"), (dict(work=None), "workspace"), (dict(nbytes=255), "workspace"), (dict(work=P + 8), "workspace"),
@@ -774,8 +775,8 @@ def test_attention_paged_refusals():
             (dict(n=-1), EI, "negative"), (dict(width=-1), EI, "negative"), (dict(heads=9), EI, "multiple"), (dict(dim=36), EU, "multiple of 8"),
             (dict(dt=4), EI, "dtype"), (dict(scale=-1.0), EI, "scale"), (dict(cache=None), EI, "cache"), (dict(q=None), EI, "q is"),
             (dict(out=_at(head=8)), EI, "overlap"), (dict(pages=None), EI, "pages"), (dict(pitch=7), EI, "pitch"), (dict(lengths=None), EI, "lengths"),
-            (dict(work=None), EI, "workspace"), (dict(nbytes=64), EI, "workspace"), (dict(work=P + 8), EI, "workspace"),
-            (dict(width=1 << 28, pitch=1 << 28), EU, "2^31"), (dict(cache=_cache(P + 1, P, 10, 16, 2048, 128, 64)), EI, "aligned")):
+            (dict(width=64, pitch=64, work=None), EI, "workspace"), (dict(width=64, pitch=64, nbytes=64), EI, "workspace"),
+            (dict(width=64, pitch=64, work=P + 8), EI, "workspace"), (dict(width=1 << 28, pitch=1 << 28), EU, "2^31"), (dict(n=1 << 25), EU, "2^25"), (dict(cache=_cache(P + 1, P, 10, 16, 2048, 128, 64)), EI, "aligned")):
         _refused(call(**args), status, text)
     for bad in ((-1, 8, 2, 64, 8, 16), (4, 8, 3, 64, 8, 16), (4, 8, 2, 200, 8, 16), (4, 8, 2, 64, 8, 0), (4, 8, 2, 64, 1 << 30, 16)):
         assert lib.reshard_attention_paged_workspace(*bad) == -1
