@@ -173,7 +173,7 @@ extern "C" reshard_status_t reshard_attention(int64_t q_tokens, int64_t k_tokens
         a.dim = int(dim);
         a.causal = causal;
         a.scale2 = float(scale) * kLog2e;
-        const bool async = aligned16(a.k, 2) && aligned16(a.v, 2);
+        const bool async = loads_itself(a.k, dim) && loads_itself(a.v, dim);
         return with_dim(dtype, dim, [&](auto zero, auto padded) {
             using T = decltype(zero);
             constexpr int DP = decltype(padded)::value;

@@ -412,9 +412,11 @@ __device__ inline Task task_of(uint32_t wg, uint32_t blocks, uint32_t heads, uin
 // exp2 of arguments at or below about 8; far below, zero.
 __device__ inline float exp2_fast(float x) { return __builtin_amdgcn_exp2f(x); }
 
-inline bool aligned16(const Heads &h, int64_t bytes) {
-    return reinterpret_cast<uintptr_t>(h.data) % 16 == 0 && h.token_pitch * bytes % 16 == 0 &&
-           h.head_pitch * bytes % 16 == 0 && h.token_pitch * bytes <= kMaxAsyncPitch;
+// Whether words may go to LDS by themselves.  Rows that overlap (a broadcast
+// gradient's pitch is 0) may not: those past a sequence's end would be in range.
+inline bool loads_itself(const Heads &h, int64_t dim) {
+    return reinterpret_cast<uintptr_t>(h.data) % 16 == 0 && h.token_pitch % 8 == 0 && h.head_pitch % 8 == 0 &&
+           h.token_pitch >= dim && h.token_pitch * 2 <= kMaxAsyncPitch;
 }
 
 // Calls f(zero of the type, elements a head is padded to).

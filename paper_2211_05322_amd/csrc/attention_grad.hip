@@ -467,14 +467,14 @@ extern "C" reshard_status_t reshard_attention_backward(
             if (q_tokens > 0) {
                 status = check_grid(blocks_of(q_tokens, sequences, kShift), heads, kThreads, &a.blocks);
                 if (status != RESHARD_OK) return status;
-                const bool async = aligned16(a.k, 2) && aligned16(a.v, 2);
+                const bool async = loads_itself(a.k, dim) && loads_itself(a.v, dim);
                 status = launch("attention gradient launch",
                                 async ? attention_dq_kernel<T, DP, true> : attention_dq_kernel<T, DP, false>,
                                 dim3(unsigned(a.blocks * heads)), kThreads, 0, stm, a);
                 if (status != RESHARD_OK) return status;
             }
             if (k_tokens == 0) return status;
-            const bool async = aligned16(a.q, 2) && aligned16(a.dout, 2) && aligned16(a.v, 2);
+            const bool async = loads_itself(a.q, dim) && loads_itself(a.dout, dim) && loads_itself(a.v, dim);
             auto go = [&](auto groups, auto parts) {
                 constexpr int GROUPS = decltype(groups)::value, PARTS = decltype(parts)::value;
                 reshard_status_t st = check_grid(blocks_of(k_tokens, sequences, GROUPS == 4 ? 7 : 6), kv_heads, kWave * GROUPS * PARTS, &a.blocks);

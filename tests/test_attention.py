@@ -215,6 +215,30 @@ def test_heads_in_place_without_tokens_and_added_up(gpu_lib):
 
 
 @gpu
+def test_heads_backward_of_what_is_wanted(gpu_lib):
+    """Through the C ABI: any of the gradients may be left out, and the others are the same."""
+    g = _seed("wanted")
+    q, k = _randn(g, 70, 6, 80).bfloat16().cuda(), _randn(g, 70, 2, 80).bfloat16().cuda()
+    dy = [_randn(g, 70, n, 80).bfloat16().cuda() for n in (6, 2)]
+    f, at = torch.rand(20, dtype=torch.float64, device="cuda"), torch.arange(-35, 35, dtype=torch.int32, device="cuda")
+    want = B.reshard_rotate_heads_backward(*dy, q, k, None, None, 1e-6, f, at)
+    heads = [B._heads("x", t, t.shape, t.dtype, 0) for t in (*dy, q, k)]
+    need = gpu_lib.reshard_rotate_heads_backward_workspace(70, 6, 2, 80)
+    work = torch.empty(need, dtype=torch.uint8, device="cuda")
+    for wanted in range(16):
+        got = [torch.full_like(t, 5.0) for t in want]
+        left = [t if wanted >> i & 1 else None for i, t in enumerate(got)]
+        outs = [None if t is None else B._heads("x", t, t.shape, t.dtype, 0) for t in left[:2]]
+        sums = wanted >> 2
+        status = gpu_lib.reshard_rotate_heads_backward(
+            70, 6, 2, 80, 40, 0, 3, *heads, None, None, 3, 1e-6, f.data_ptr(), at.data_ptr(), *outs, B._ptr(left[2]), B._ptr(left[3]),
+            0, work.data_ptr() if sums else None, need if sums else 0, B._stream_handle(None))
+        assert status == B.RESHARD_OK
+        for i, (a, b) in enumerate(zip(got, want)):
+            assert torch.equal(a, b) if wanted >> i & 1 else (a == 5).all(), (wanted, i)
+
+
+@gpu
 def test_heads_backward_against_differences(gpu_lib):
     """The gradients in float32 against central differences of the plain forward pass in 64 bits."""
     g = _seed("differences")
@@ -485,6 +509,60 @@ def test_attention_backward_against_differences(gpu_lib):
             want.view(-1)[i] = (ends[0] - ends[1]) / 2e-5
         # weights, dS and the result rounded to float16, out to float16 in delta: terms of a few units, 10 of them
         _near(grads[which], want, 20 * 2.0 ** -11 * (2 + want.abs()), "qkv"[which])
+
+
+@gpu
+@pytest.mark.parametrize("dtype", HALVES, ids=str)
+def test_attention_of_other_layouts(dtype, gpu_lib):
+    """Heads before tokens, rows that are one row (gradients of a sum), and a given result of another layout: as dense ones."""
+    g = _seed("layouts", dtype)
+    at = [[0, 50, 83, 90], [0, 50, 140, 147]]
+    offsets = [_int32(a) for a in at]
+    for dim in (64, 128):
+        q, k, v = (_randn(g, t, h, dim).to(dtype).cuda() for t, h in ((90, 8), (147, 2), (147, 2)))
+        out, lse = B.reshard_attention(q, k, v, *offsets)
+        _check_attention(q, k, v, at, dim ** -0.5, True, out, lse, "dense")
+        across = [t.transpose(0, 1).contiguous().transpose(0, 1) for t in (q, k, v)]
+        into = torch.empty_like(across[0])
+        got, stats = B.reshard_attention(*across, *offsets, out=into)
+        assert got is into and torch.equal(got, out) and torch.equal(stats, lse)
+        for row in (_randn(g, 1, 8, dim), _randn(g, 90, 1, dim)):
+            dout = row.to(dtype).cuda().expand(90, 8, dim)
+            want = B.reshard_attention_backward(dout.contiguous(), q, k, v, out, lse, *offsets)
+            _check_grads(dout, q, k, v, out, lse, at, dim ** -0.5, True, want, "broadcast")
+            got = B.reshard_attention_backward(dout, *across, out, lse, *offsets)
+            assert all(torch.equal(a, b) for a, b in zip(got, want))
+        one = [t[:1].expand(147, 2, dim) for t in (k, v)]  # every key the same row
+        got = B.reshard_attention(q, *one, *offsets)
+        want = B.reshard_attention(q, *(t.contiguous() for t in one), *offsets)
+        assert all(torch.equal(a, b) for a, b in zip(got, want))
+
+
+@gpu
+def test_attention_of_offsets_outside(gpu_lib):
+    """Offsets past the tensors count as their ends; without queries the keys' gradients are zeros; without sequences nothing
+    is written."""
+    g = _seed("outside")
+    q, k, v = (_randn(g, 40, 2, 64).half().cuda() for _ in range(3))
+    want = B.reshard_attention(q, k, v, _int32([0, 40]), _int32([0, 40]))
+    for bad in ([-5, 41], [-(1 << 31), (1 << 31) - 1]):
+        got = B.reshard_attention(q, k, v, _int32(bad), _int32(bad))
+        assert all(torch.equal(a, b) for a, b in zip(got, want))
+        grads = B.reshard_attention_backward(q, q, k, v, *got, _int32(bad), _int32(bad))
+        for a, b in zip(grads, B.reshard_attention_backward(q, q, k, v, *want, _int32([0, 40]), _int32([0, 40]))):
+            assert torch.equal(a, b)
+    none = q[:0]
+    out, lse = B.reshard_attention(none, k, v, _int32([0, 0]), _int32([0, 40]))
+    assert out.shape == (0, 2, 64) and lse.shape == (2, 0)
+    dq, dk, dv = B.reshard_attention_backward(none, none, k, v, out, lse, _int32([0, 0]), _int32([0, 40]))
+    assert dq.shape == (0, 2, 64) and not dk.any() and not dv.any()
+    out, lse = B.reshard_attention(q, none, none, _int32([0, 40]), _int32([0, 0]))
+    assert not out.any() and (lse == -math.inf).all()
+    dq, _, _ = B.reshard_attention_backward(q, q, none, none, out, lse, _int32([0, 40]), _int32([0, 0]))
+    assert not dq.any()
+    into = torch.full_like(q, 7.0)
+    B.reshard_attention(q, k, v, _int32([0]), _int32([0]), out=into)
+    assert (into == 7).all()
 
 
 # ------------------------------------------------------------------ attention of one token
