@@ -726,8 +726,12 @@ def _heads(name, t, shape, dtype, device):
     if t.shape != shape or t.dtype is not dtype or t.get_device() != device:
         raise ValueError(f"{name} must be {dtype} {tuple(shape)} on device {device}, "
                          f"got {t.dtype} {tuple(t.shape)} on {t.device}")
+    return _pitches(name, t)
+
+
+def _pitches(name, t):
     token, head, last = t.stride()
-    if last != 1 and shape[2] > 1:
+    if last != 1 and t.shape[2] > 1:
         raise ValueError(f"{name}: the last dimension must be dense, its stride is {last}")
     return _pack_heads(t.data_ptr(), token, head)
 
@@ -761,8 +765,11 @@ def _here(name, t, stream):
 
 
 def _new(t):
-    """A dense tensor of t's shape and type beside it (empty_like is the faster call, and dense where t is)."""
-    return _torch.empty_like(t) if t.is_contiguous() else t.new_empty(t.shape)
+    """A dense tensor of t's shape and type beside it, by the fastest call."""
+    if t.is_contiguous():
+        return _torch.empty_like(t)
+    tokens, heads, dim = t.shape
+    return _torch.empty_strided((tokens, heads, dim), (heads * dim, dim, 1), dtype=t.dtype, device=t.device)
 
 
 def _cache(cache, kv_heads, dim, dtype, device):
@@ -789,7 +796,7 @@ def _rotation(q, k, q_weight, k_weight, frequencies, positions):
     tokens, heads, dim = _three("q", q)
     kv_heads = _three("k", k)[1]
     dtype, device = q.dtype, q.get_device()
-    q_at, k_at = _heads("q", q, q.shape, dtype, device), _heads("k", k, (tokens, kv_heads, dim), dtype, device)
+    q_at, k_at = _pitches("q", q), _heads("k", k, (tokens, kv_heads, dim), dtype, device)
     weight = (q_weight if q_weight is not None else k_weight if k_weight is not None else q).dtype
     if q_weight is not None:
         _dense("q_weight", q_weight, (dim,), q, weight)
@@ -875,17 +882,18 @@ def reshard_rotate_heads_backward(dq_out, dk_out, q, k, q_weight=None, k_weight=
 def _packed(q, k, v, q_offsets, k_offsets, scale, stream):
     """What both passes check: sizes, q, k, v, offsets, scale, the stream's handle, q's type and device."""
     q_tokens, heads, dim = _three("q", q)
-    k_tokens, kv_heads, k_dim = _three("k", k)
+    shape = _three("k", k)
+    k_tokens, kv_heads, k_dim = shape
     if k_dim != dim:
-        raise ValueError(f"k must be [tokens, kv_heads, {dim}], got {tuple(k.shape)}")
-    dtype, device, shape = q.dtype, q.get_device(), k.shape
+        raise ValueError(f"k must be [tokens, kv_heads, {dim}], got {tuple(shape)}")
+    dtype, device = q.dtype, q.get_device()
     n = q_offsets.numel()
     if n < 1:
         raise ValueError("q_offsets must hold one number more than there are sequences")
-    return ((q_tokens, k_tokens, n - 1, heads, kv_heads, dim), _heads("q", q, q.shape, dtype, device),
-            _heads("k", k, shape, dtype, device), _heads("v", v, shape, dtype, device),
-            _int32("q_offsets", q_offsets, n, device), _int32("k_offsets", k_offsets, n, device),
-            dim ** -0.5 if scale is None else scale, _here("q", q, stream), dtype, device)
+    return ((q_tokens, k_tokens, n - 1, heads, kv_heads, dim), _pitches("q", q), _heads("k", k, shape, dtype, device),
+            _heads("v", v, shape, dtype, device), _int32("q_offsets", q_offsets, n, device),
+            _int32("k_offsets", k_offsets, n, device), dim ** -0.5 if scale is None else scale, _here("q", q, stream),
+            dtype, device)
 
 
 def reshard_attention(q, k, v, q_offsets, k_offsets, scale=None, causal=True, out=None, lse=None, stream=None):
@@ -901,7 +909,7 @@ def reshard_attention(q, k, v, q_offsets, k_offsets, scale=None, causal=True, ou
     with _on(stream):
         out = _new(q) if out is None else out
         if lse is None:
-            lse = q.new_empty((sizes[3], sizes[0]), dtype=_torch.float32)
+            lse = _torch.empty_strided((sizes[3], sizes[0]), (sizes[0], 1), dtype=_torch.float32, device=q.device)
         else:
             _dense("lse", lse, (sizes[3], sizes[0]), q, _torch.float32)
     status = lib.reshard_attention(*sizes, _dtype_code(dtype), q_at, k_at, v_at, q_offsets, k_offsets, scale,
@@ -942,7 +950,7 @@ def reshard_attention_paged(q, k_cache, v_cache, pages, lengths, scale=None, out
     lib = _lib or load()
     n, heads, dim = _three("q", q)
     dtype, device = q.dtype, q.get_device()
-    q_at = _heads("q", q, q.shape, dtype, device)
+    q_at = _pitches("q", q)
     kv_heads = k_cache.shape[2] if k_cache.dim() == 4 else -1
     cache_at = _cache((k_cache, v_cache), kv_heads, dim, dtype, device)
     if pages.dim() != 2 or pages.shape[0] != n or pages.dtype is not _torch.int32 or pages.get_device() != device or (

@@ -337,7 +337,7 @@ __global__ __launch_bounds__(TEAM == 8 ? 512 : kThreads, 2) void paged_kernel(Pa
 // elements are fewer than threads, groups of threads share the parts.
 template <typename T, int THREADS>
 __global__ __launch_bounds__(THREADS) void paged_join_kernel(PagedArgs a, uint32_t waves) {
-    __shared__ float tops[kQueries][THREADS / kQueries];
+    __shared__ float tops[kQueries];
     __shared__ f32x4 shared_value[THREADS];
     __shared__ float shared_sum[THREADS];
     const int units = a.kv_heads * a.passes, s = blockIdx.x / units, unit = blockIdx.x - s * units;
@@ -356,14 +356,13 @@ __global__ __launch_bounds__(THREADS) void paged_join_kernel(PagedArgs a, uint32
     const int64_t size = int64_t(a.rows) * (a.dim + 2);
     // the first wave began the unit, the others came into it
     auto part = [&](int i) { return a.parts + ((w0 + i) * 2 + (i == 0)) * size; };
-    {
-        const int r = threadIdx.x % kQueries, j = threadIdx.x / kQueries;
+    for (int r = threadIdx.x / kWave; r < rows; r += THREADS / kWave) {  // a wave a row
         float top = kLowest;
-        if (r < rows) {
 #pragma unroll 4
-            for (int i = j; i < parts; i += THREADS / kQueries) top = fmaxf(top, part(i)[a.rows * a.dim + r * 2]);
-        }
-        tops[r][j] = top;
+        for (int i = threadIdx.x % kWave; i < parts; i += kWave) top = fmaxf(top, part(i)[a.rows * a.dim + r * 2]);
+#pragma unroll
+        for (int d = 1; d < kWave; d *= 2) top = fmaxf(top, __shfl_xor(top, d));
+        tops[r] = top;
     }
     __syncthreads();
     const int vectors = rows * (a.dim / 4), groups = max(1, THREADS / vectors);
@@ -373,9 +372,7 @@ __global__ __launch_bounds__(THREADS) void paged_join_kernel(PagedArgs a, uint32
         f32x4 value{0, 0, 0, 0};
         float sum = 0;
         if (group < groups && e < vectors) {
-            float top = tops[r][0];
-#pragma unroll
-            for (int j = 1; j < THREADS / kQueries; ++j) top = fmaxf(top, tops[r][j]);
+            const float top = tops[r];
 #pragma unroll 8
             for (int i = group; i < parts; i += groups) {
                 const float *from = part(i);
