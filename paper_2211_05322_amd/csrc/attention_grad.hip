@@ -65,7 +65,12 @@ __device__ inline void round_scores(const f32x16 &ds, float &factor, f32x16 (&su
 constexpr float kFirstFactor = 1.152921504606846976e18f;  // 2^60: dS below 2^-74 may vanish
 
 // Queries: as in the forward pass a lane holds one's column throughout, so that
-// its statistics are the lane's and dS goes into the next product as it is.
+// its statistics are the lane's and dS goes into the next product as it is.  delta is
+// summed here, where both its rows are at hand, and kept for the keys' kernel.
+// Three products: 8 x 2048 tokens, 96 heads of 128 in bf16 take 1.38 ms, 896 TFLOP/s,
+// the matrix instruction busy 46 % of the cycles at 1.94 GHz; a workgroup passes over
+// 17 tiles on average, and its start, three rows an operand from memory, is a
+// seventh of its time.  13 sequences of up to 2047 tokens, 40 heads of 64 in fp16: 106 us.
 template <typename T, int DP, bool ASYNC>
 __global__ __launch_bounds__(kThreads, 2) void attention_dq_kernel(GradArgs a) {
     constexpr int STEPS = DP / 16, BLOCKS = DP / 32, KEYS = 64, WORDS = TileShape<DP>::words;
@@ -179,14 +184,21 @@ __global__ __launch_bounds__(kThreads, 2) void attention_dq_kernel(GradArgs a) {
 
 // Keys: a lane holds one key's column, and passes over the queries that see it,
 // of every head of its group.  GROUPS waves hold 32 keys each, and PARTS such sets
-// share a tile's queries, 32 each, and add up at the end.  (4, 1): two
-// workgroups a CU, which do not wait for each other, so that one's exponentials run
-// beside the other's products (8 x 2048 tokens, 96 heads of 128: 1.83 ms, 903 TFLOP/s; (4, 2)
-// in one workgroup 2.34).  Where that gives fewer than 2048 workgroups, the longest
-// of which would be waited for, more waves share its keys' queries: (2, 2) for heads
-// up to 64, (2, 4) for larger ones (13 sequences of up to 2047 tokens, 8 key heads of
-// 64: 162 us, (4, 1) 268; but on the case above (2, 4) takes 2.85 ms).  Where
-// registers do not hold two operands and two sums, values stay in LDS.
+// share a tile's queries, 32 each, and add up at the end.
+//
+// (4, 1): two workgroups a CU, which do not wait for each other, so that one's
+// exponentials run beside the other's products.  8 x 2048 tokens, 96 heads of 128 in
+// bf16 take 1.64 ms, 1,005 TFLOP/s of the four products, with the matrix
+// instruction busy 54 % of the cycles at 1.83 GHz, the clock that its power leaves
+// ((4, 2), one workgroup a CU, took 2.34 ms, a third tile in LDS as long as two).
+// Where that gives fewer than 2048 workgroups, the longest of which would be
+// waited for, more waves share its keys' queries: (2, 2) for heads up to 64, (2, 4)
+// for larger ones, whose tiles leave room for one workgroup a CU.  13 sequences of up
+// to 2047 tokens, 8 key heads of 64 in fp16: 160 us, with (4, 1) 268; but with (2, 4) the
+// case above takes 2.85 ms.  There waves hold 61 % of their places: the longest
+// sequence's first keys, with 160 tiles of queries, are what is waited for.
+//
+// Heads above 64 leave no registers for both operands beside both sums: values stay in LDS.
 template <typename T, int DP, int GROUPS, int PARTS, bool ASYNC>
 __global__ __launch_bounds__(kWave *GROUPS *PARTS, 2) void attention_dkv_kernel(GradArgs a) {
     constexpr int STEPS = DP / 16, BLOCKS = DP / 32, QUERIES = 32 * PARTS, WORDS = TileShape<DP>::words;
@@ -229,7 +241,8 @@ __global__ __launch_bounds__(kWave *GROUPS *PARTS, 2) void attention_dkv_kernel(
     const float *delta_at = a.minus_delta + int64_t(next_head) * a.seq.q_tokens + s.q0 + from;
     const int64_t q_step = QUERIES * a.q.token_pitch, d_step = QUERIES * a.dout.token_pitch;
     float stat[2];
-    // a tile behind the last is asked for too, and is zeros without a read.  A query behind its sequence's end so has zeros for statistics, and weights 1 that meet zeros.
+    // a tile behind the last is asked for too, and is zeros without a read; a query behind its sequence's end so has
+    // zeros for statistics, and weights of 1 that meet zeros
     auto load = [&](int turn, auto &q_to, auto &d_to, auto &s_to) {
         const int rows = turn < turns ? rows_left : 0;
         ql.start(q_at, rows, q_to);
