@@ -12,6 +12,7 @@ GPU tests unless marked otherwise; refusals run on the CPU.
 
 import ctypes
 import math
+import threading
 import zlib
 
 import pytest
@@ -657,6 +658,13 @@ def test_attention_paged_of_pages_outside_the_cache(gpu_lib):
     got = B.reshard_attention_paged(q, *caches, bad, _int32([64] * 3))
     few = B.reshard_attention_paged(q, *caches, table, _int32([48, 32, 0]))
     assert torch.equal(got, few) and not got[2].any()
+    # a table without pages, and a cache without any
+    assert not B.reshard_attention_paged(q, *caches, table[:, :0], _int32([64, 1, 0])).any()
+    assert not B.reshard_attention_paged(q, *(c[:0] for c in caches), table, _int32([64, 1, 0])).any()
+    many = torch.randn(700, 4, 64, device="cuda").half()
+    assert not B.reshard_attention_paged(many, *caches, table[:1, :0].expand(700, 0), _int32([9] * 700)).any()
+    none = B.reshard_attention_paged(q[:0], *caches, table[:0], _int32([]))
+    assert none.shape == (0, 4, 64)
 
 
 @gpu
@@ -757,12 +765,51 @@ def test_training_pass_in_a_graph_and_on_another_stream(gpu_lib):
             outs.append(step())
     for turn in range(4):
         qkv.copy_(_randn(g, *qkv.shape).bfloat16())
+        if turn > 1:  # other sequences, lengths and pages: data that the calls read
+            at.copy_(torch.tensor([0, 17 * turn, 333], dtype=torch.int32))
+            lengths.copy_(torch.tensor([3, 60 * turn], dtype=torch.int32))
+            table.copy_(table.flip(1).clone())
         want = [t.clone() for t in step()]
         torch.cuda.synchronize()
         for graph, got in zip(graphs, outs):
             graph.replay()
             torch.cuda.synchronize()
             assert all(torch.equal(a, b) for a, b in zip(got, want)), f"replay {turn}"
+
+
+@gpu
+def test_calls_of_two_threads_at_once(gpu_lib):
+    """Each thread on its own stream, with its own sequences, many times: the results of each are those of it alone."""
+    g = _seed("threads")
+    cases = []
+    for n in (3, 40):
+        lengths = [(20 * n + 7, 20 * n + 7), (5, 50)]
+        (q, k, v), at = _case(g, torch.bfloat16, lengths, 4, 2, 64)
+        caches, table = _paged_case(g, torch.bfloat16, [700 * n, 9], 2, 64, 16, 44 * n)
+        cases.append((q, k, v, [_int32(a) for a in at], caches, table, _int32([700 * n, 9])))
+
+    def step(case, stream=None):
+        q, k, v, at, caches, table, lengths = case
+        out, lse = B.reshard_attention(q, k, v, *at, stream=stream)
+        return [out, lse, *B.reshard_attention_backward(out, q, k, v, out, lse, *at, stream=stream),
+                B.reshard_attention_paged(q[:2], *caches, table, lengths, stream=stream)]
+    want = [step(c) for c in cases]
+    torch.cuda.synchronize()
+    wrong = []
+
+    def work(i):
+        stream = torch.cuda.Stream()
+        for _ in range(20):
+            got = step(cases[i], stream)
+            stream.synchronize()
+            if not all(torch.equal(a, b) for a, b in zip(got, want[i])):
+                wrong.append(i)
+    threads = [threading.Thread(target=work, args=(i,)) for i in range(2)]
+    for t in threads:
+        t.start()
+    for t in threads:
+        t.join()
+    assert not wrong
 
 
 # ------------------------------------------------------------------ refusals (CPU)
