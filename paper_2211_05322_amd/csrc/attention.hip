@@ -13,7 +13,7 @@
 namespace rs {
 namespace {
 
-constexpr int kThreads = 256, kWaves = kThreads / kWave;
+constexpr int kThreads = 256;
 
 struct PromptArgs {
     Heads q, k, v, out;
@@ -40,18 +40,20 @@ struct PromptArgs {
 // workgroup (its place in the batch, its rows, its first tile: about 3 us) counts.
 // Tiles of 32 keys in rings of 3 and 4 were no faster; waves of 64 queries, which read half
 // as much from LDS, leave one a SIMD, and were slower (920 TFLOP/s).
-template <typename T, int DP, bool ASYNC>
+template <typename T, int DP, int GROUPS, int PARTS, bool ASYNC>
 __global__ __launch_bounds__(kThreads, 2) void attention_kernel(PromptArgs a) {
-    constexpr int STEPS = DP / 16, BLOCKS = DP / 32, ROWS = 32 * kWaves, KEYS = 64, PARTS = KEYS / 32;
-    constexpr int SHIFT = 7, WORDS = KEYS * TileShape<DP>::words;
+    static_assert(GROUPS * PARTS * kWave == kThreads, "");
+    constexpr int STEPS = DP / 16, BLOCKS = DP / 32, ROWS = 32 * GROUPS, SHIFT = GROUPS == 4 ? 7 : 6;
+    constexpr int EACH = PARTS == 1 ? 2 : 1, KEYS = 32 * EACH * PARTS, WORDS = KEYS * TileShape<DP>::words;
     // arrays by name: only so does the compiler see that loads into one leave the others alone
     __shared__ uint4 k0[WORDS], v0[WORDS], k1[WORDS], v1[WORDS];
+    __shared__ float2 stats[PARTS > 1 ? PARTS : 1][ROWS];  // maximum and sum
     const Task task = task_of(blockIdx.x, a.blocks, a.heads, a.group);
     Sequence s;
     if (!ranked_sequence(a.seq, false, a.causal, a.blocks, task.block, SHIFT, &s)) return;
-    const int lane = threadIdx.x % kWave, wave = threadIdx.x / kWave, half = lane / 32;
-    const int kv_head = task.head / a.group;
-    const int row0 = s.block * ROWS + wave * 32, row = row0 + lane % 32, held = min(row, s.lq - 1);
+    const int lane = threadIdx.x % kWave, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave), half = lane / 32;
+    const int kv_head = task.head / a.group, part = wave / GROUPS, rows_of = wave % GROUPS, in_tile = part * 32 * EACH;
+    const int row0 = s.block * ROWS + rows_of * 32, row = row0 + lane % 32, held = min(row, s.lq - 1);
     const T *k = a.k.template at<const T>(s.k0, kv_head), *v = a.v.template at<const T>(s.k0, kv_head);
     const int to = a.causal ? min(s.lk, min(s.lq, (s.block + 1) * ROWS) + s.lk - s.lq) : s.lk;  // the workgroup's keys
     TileLoader<T, DP, KEYS, kThreads, ASYNC> kl(threadIdx.x, a.dim, a.k.token_pitch), vl(threadIdx.x, a.dim, a.v.token_pitch);
@@ -77,7 +79,7 @@ __global__ __launch_bounds__(kThreads, 2) void attention_kernel(PromptArgs a) {
     const int wave_to = row0 >= s.lq ? 0 : a.causal ? min(s.lk, min(s.lq, row0 + 32) + s.lk - s.lq) : s.lk;
     const int all_see = a.causal ? row0 + 1 + s.lk - s.lq : s.lk;  // keys that each of the wave's queries sees
 
-    const LanePlaces places = LanePlaces::of<DP>(lane);
+    const LanePlaces places = LanePlaces::of<DP>(lane, in_tile);
     f32x16 o[BLOCKS];
     float m = -3.402823466e38f, l = 0;
 #pragma unroll
@@ -86,30 +88,31 @@ __global__ __launch_bounds__(kThreads, 2) void attention_kernel(PromptArgs a) {
         if constexpr (ASYNC) loads_done();
         __syncthreads();
         load(key0 + KEYS, k_next, v_next);
-        if (key0 < wave_to) {
-            f32x16 x[PARTS];
+        if (key0 + in_tile < wave_to) {
+            f32x16 x[EACH];
 #pragma unroll
-            for (int n = 0; n < PARTS; ++n) x[n] = zero16();
-            Operand8<T> ahead[2][2];
+            for (int n = 0; n < EACH; ++n) x[n] = zero16();
+            Operand8<T> ahead[2][EACH];
             pipelined<STEPS>(
                 [&](auto i) {
-                    ahead[i % 2][0] = row_operand<T, DP>(kt, 0, i, places);
-                    ahead[i % 2][1] = row_operand<T, DP>(kt, 32, i, places);
+#pragma unroll
+                    for (int n = 0; n < EACH; ++n) ahead[i % 2][n] = row_operand<T, DP>(kt, n * 32, i, places);
                 },
                 [&](auto i) {
-                    x[0] = mfma(ahead[i % 2][0], q[i], x[0]);
-                    x[1] = mfma(ahead[i % 2][1], q[i], x[1]);
-                });
-            if (key0 + KEYS > all_see || key0 + KEYS > s.lk) {
 #pragma unroll
-                for (int n = 0; n < PARTS; ++n)
+                    for (int n = 0; n < EACH; ++n) x[n] = mfma(ahead[i % 2][n], q[i], x[n]);
+                });
+            const int key_end = key0 + in_tile + 32 * EACH;
+            if (key_end > all_see || key_end > s.lk) {
+#pragma unroll
+                for (int n = 0; n < EACH; ++n)
 #pragma unroll
                     for (int r = 0; r < 16; ++r)
-                        if (key0 + n * 32 + result_row(r, half) > last) x[n][r] = -INFINITY;
+                        if (key0 + in_tile + n * 32 + result_row(r, half) > last) x[n][r] = -INFINITY;
             }
             float top = x[0][0];
 #pragma unroll
-            for (int n = 0; n < PARTS; ++n)
+            for (int n = 0; n < EACH; ++n)
 #pragma unroll
                 for (int r = 0; r < 16; ++r) top = fmaxf(top, x[n][r]);
             top = halves_max(top) * a.scale2;
@@ -122,10 +125,10 @@ __global__ __launch_bounds__(kThreads, 2) void attention_kernel(PromptArgs a) {
 #pragma unroll
                     for (int r = 0; r < 16; ++r) o[d][r] *= shrink;
             }
-            Operand8<T> p[2 * PARTS];
+            Operand8<T> p[2 * EACH];
             float sum = 0;
 #pragma unroll
-            for (int n = 0; n < PARTS; ++n)
+            for (int n = 0; n < EACH; ++n)
 #pragma unroll
                 for (int r = 0; r < 16; ++r) {
                     const float e = exp2_fast(fmaf(x[n][r], a.scale2, -m));
@@ -134,7 +137,7 @@ __global__ __launch_bounds__(kThreads, 2) void attention_kernel(PromptArgs a) {
                 }
             l += sum;
 #pragma unroll
-            for (int t = 0; t < 2 * PARTS; ++t)
+            for (int t = 0; t < 2 * EACH; ++t)
 #pragma unroll
                 for (int d = 0; d < BLOCKS; ++d) o[d] = mfma(column_operand<T, DP>(vt, t * 16, d, places), p[t], o[d]);
         }
@@ -148,7 +151,27 @@ __global__ __launch_bounds__(kThreads, 2) void attention_kernel(PromptArgs a) {
         if (key0 + KEYS < to) step(key0 + KEYS, k1, v1, k0, v0);
     }
     loads_done();  // none may write into LDS that is another workgroup's by then
-    const float sum = halves_sum(l), over = sum == 0 ? 0.0f : 1.0f / sum;
+    float sum = halves_sum(l);
+    if constexpr (PARTS > 1) {  // the parts' sums to the first, in order, through the tiles' memory
+        if (half == 0) stats[part][rows_of * 32 + lane] = make_float2(m, sum);
+        __syncthreads();
+        float top = m;
+#pragma unroll
+        for (int p = 0; p < PARTS; ++p) top = fmaxf(top, stats[p][rows_of * 32 + lane % 32].x);
+        const float by = exp2_fast(m - top);
+#pragma unroll
+        for (int d = 0; d < BLOCKS; ++d) o[d] *= by;
+        sum = 0;
+#pragma unroll
+        for (int p = 0; p < PARTS; ++p) {
+            const float2 other = stats[p][rows_of * 32 + lane % 32];
+            sum = fmaf(exp2_fast(other.x - top), other.y, sum);
+        }
+        m = top;
+        add_parts<DP, GROUPS, PARTS, WORDS>(o, part, rows_of, lane, k0, v0, k1, v1);
+        if (part > 0) return;
+    }
+    const float over = sum == 0 ? 0.0f : 1.0f / sum;
     T *to_row = a.out.template at<T>(s.q0 + held, task.head);
 #pragma unroll
     for (int d = 0; d < BLOCKS; ++d) store_columns(to_row, row < s.lq, o[d], over, d, lane, a.dim);
@@ -187,10 +210,19 @@ extern "C" reshard_status_t reshard_attention(int64_t q_tokens, int64_t k_tokens
         return with_dim(dtype, dim, [&](auto zero, auto padded) {
             using T = decltype(zero);
             constexpr int DP = decltype(padded)::value;
-            reshard_status_t status = check_grid(blocks_of(q_tokens, sequences, 7), heads, kThreads, &a.blocks);
-            if (status != RESHARD_OK) return status;
-            return launch("attention launch", async ? attention_kernel<T, DP, true> : attention_kernel<T, DP, false>,
-                          dim3(unsigned(a.blocks * heads)), kThreads, 0, static_cast<hipStream_t>(stream), a);
+            auto go = [&](auto groups, auto parts) {
+                constexpr int GROUPS = decltype(groups)::value, PARTS = decltype(parts)::value;
+                const reshard_status_t status =
+                    check_grid(blocks_of(q_tokens, sequences, GROUPS == 4 ? 7 : 6), heads, kThreads, &a.blocks);
+                if (status != RESHARD_OK) return status;
+                return launch("attention launch",
+                              async ? attention_kernel<T, DP, GROUPS, PARTS, true> : attention_kernel<T, DP, GROUPS, PARTS, false>,
+                              dim3(unsigned(a.blocks * heads)), kThreads, 0, static_cast<hipStream_t>(stream), a);
+            };
+            using std::integral_constant;
+            if (blocks_of(q_tokens, sequences, 7) * heads <= 512)
+                return go(integral_constant<int, 2>{}, integral_constant<int, 2>{});
+            return go(integral_constant<int, 4>{}, integral_constant<int, 1>{});
         });
     });
 }

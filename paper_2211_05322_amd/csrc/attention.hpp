@@ -385,6 +385,49 @@ __device__ inline bool ranked_sequence(const Sequences &s, bool by_keys, bool ca
     return true;
 }
 
+// Adds the sums of a workgroup's parts to the first part's, in order, through the
+// tiles' memory (4 arrays of WORDS), which nothing else uses any more.
+template <int DP, int GROUPS, int PARTS, int WORDS>
+__device__ inline void add_parts(f32x16 (&sums)[DP / 32], int part, int group, int lane, uint4 (&t0)[WORDS],
+                                 uint4 (&t1)[WORDS], uint4 (&t2)[WORDS], uint4 (&t3)[WORDS]) {
+    constexpr int SLOT = 32 * DP / 4, EACH = WORDS / SLOT;  // 16-byte words of a part; parts of an array
+    static_assert(EACH * 4 >= (PARTS - 1) * GROUPS, "room for all parts but the first");
+    // f(a lane's first word) of a part's place; a branch for each array, so that its accesses stay LDS's own
+    auto with_slot = [&](int p, auto &&f) {
+        const int n = (p - 1) * GROUPS + group, in = n / EACH, at = (n - in * EACH) * SLOT + lane;
+        if (in == 0) f(reinterpret_cast<f32x4 *>(t0 + at));
+        else if (in == 1) f(reinterpret_cast<f32x4 *>(t1 + at));
+        else if (in == 2) f(reinterpret_cast<f32x4 *>(t2 + at));
+        else f(reinterpret_cast<f32x4 *>(t3 + at));
+    };
+    if (part > 0) {
+        with_slot(part, [&](f32x4 *to) {
+#pragma unroll
+            for (int d = 0; d < DP / 32; ++d)
+#pragma unroll
+                for (int j = 0; j < 4; ++j)
+                    to[(d * 4 + j) * kWave] =
+                        f32x4{sums[d][4 * j], sums[d][4 * j + 1], sums[d][4 * j + 2], sums[d][4 * j + 3]};
+        });
+    }
+    __syncthreads();
+    if (part == 0) {
+#pragma unroll
+        for (int p = 1; p < PARTS; ++p)
+            with_slot(p, [&](const f32x4 *from) {
+#pragma unroll
+                for (int d = 0; d < DP / 32; ++d)
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) {
+                        const f32x4 x = from[(d * 4 + j) * kWave];
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) sums[d][4 * j + e] += x[e];
+                    }
+            });
+    }
+    __syncthreads();
+}
+
 inline int64_t blocks_of(int64_t tokens, int64_t sequences, int shift) { return (tokens >> shift) + sequences; }
 
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;

@@ -191,11 +191,14 @@ __global__ __launch_bounds__(kThreads, 2) void attention_dq_kernel(GradArgs a) {
 // bf16 take 1.64 ms, 1,005 TFLOP/s of the four products, with the matrix
 // instruction busy 54 % of the cycles at 1.83 GHz, the clock that its power leaves
 // ((4, 2), one workgroup a CU, took 2.34 ms, a third tile in LDS as long as two).
-// Where that gives fewer than 2048 workgroups, the longest of which would be
-// waited for, more waves share its keys' queries: (2, 2) for heads up to 64, (2, 4)
-// for larger ones, whose tiles leave room for one workgroup a CU.  13 sequences of up
-// to 2047 tokens, 8 key heads of 64 in fp16: 160 us, with (4, 1) 268; but with (2, 4) the
-// case above takes 2.85 ms.  There waves hold 61 % of their places: the longest
+// Where that gives few workgroups, the longest of which would be waited for, more
+// waves share its keys' queries: (2, 2) for heads up to 64, below 1024 workgroups; (2,
+// 4) for larger ones, whose tiles leave room for one workgroup a CU, below 512.  13
+// sequences of up to 2047 tokens, 8 key heads of 64 in fp16: 160 us, with (4, 1) 268.  Both
+// kernels, without and with it, in us: 2048 tokens, 32 heads of 64 and 8 key heads (136
+// workgroups) 228 and 146; 8192 (520) 1207 and 1015; 16 x 512, 16 heads (1280) 70 and 78; in
+// heads of 128: 2048 (136) 314 and 191; 2 x 4096, 8 heads (528) 288 and 305; 16 x 512 (1280)
+// 119 and 179.  There waves hold 61 % of their places: the longest
 // sequence's first keys, with 160 tiles of queries, are what is waited for.
 //
 // Heads above 64 leave no registers for both operands beside both sums: values stay in LDS.
@@ -381,43 +384,14 @@ __global__ __launch_bounds__(kWave *GROUPS *PARTS, 2) void attention_dkv_kernel(
     loads_done();  // none may write into LDS that is used otherwise, or another workgroup's, by then
     __syncthreads();
     const float down = kNarrow<T> ? 1.0f / 16384 : 1.0f, scale = kNarrow<T> ? a.scale / factor * down : a.scale;
-    if constexpr (PARTS > 1) {  // the parts' sums to the first, in order, through the tiles' memory
-        constexpr int SLOT = 32 * DP / 4, EACH = QUERIES * WORDS / SLOT;  // 16-byte words; slots of an array
-        static_assert(EACH * 4 >= (PARTS - 1) * GROUPS, "");
-        auto slot = [&](int p) {
-            const int n = (p - 1) * GROUPS + keys_of, in = n / EACH;
-            uint4 *tile = in == 0 ? q0 : in == 1 ? d0 : in == 2 ? q1 : d1;
-            return reinterpret_cast<f32x4 *>(tile + (n - in * EACH) * SLOT) + lane;
-        };
-        auto join = [&](f32x16(&sums)[BLOCKS], float by) {
+    if constexpr (PARTS > 1) {
 #pragma unroll
-            for (int d = 0; d < BLOCKS; ++d) sums[d] *= by;
-            if (part > 0) {
-                f32x4 *to = slot(part);
-#pragma unroll
-                for (int d = 0; d < BLOCKS; ++d)
-#pragma unroll
-                    for (int j = 0; j < 4; ++j)
-                        to[(d * 4 + j) * kWave] = f32x4{sums[d][4 * j], sums[d][4 * j + 1], sums[d][4 * j + 2], sums[d][4 * j + 3]};
-            }
-            __syncthreads();
-            if (part == 0) {
-                for (int p = 1; p < PARTS; ++p) {
-                    const f32x4 *from = slot(p);
-#pragma unroll
-                    for (int d = 0; d < BLOCKS; ++d)
-#pragma unroll
-                        for (int j = 0; j < 4; ++j) {
-                            const f32x4 x = from[(d * 4 + j) * kWave];
-#pragma unroll
-                            for (int e = 0; e < 4; ++e) sums[d][4 * j + e] += x[e];
-                        }
-                }
-            }
-            __syncthreads();
-        };
-        join(dk, scale);
-        join(dv, down);
+        for (int d = 0; d < BLOCKS; ++d) {
+            dk[d] *= scale;
+            dv[d] *= down;
+        }
+        add_parts<DP, GROUPS, PARTS, QUERIES * WORDS>(dk, part, keys_of, lane, q0, d0, q1, d1);
+        add_parts<DP, GROUPS, PARTS, QUERIES * WORDS>(dv, part, keys_of, lane, q0, d0, q1, d1);
         if (part > 0) return;
     }
     T *to_dk = a.dk.template at<T>(s.k0 + held, task.head), *to_dv = a.dv.template at<T>(s.k0 + held, task.head);
@@ -498,7 +472,7 @@ extern "C" reshard_status_t reshard_attention_backward(
                               dim3(unsigned(a.blocks * kv_heads)), kWave * GROUPS * PARTS, 0, stm, a);
             };
             using std::integral_constant;
-            if (blocks_of(k_tokens, sequences, 7) * kv_heads < 2048)
+            if (blocks_of(k_tokens, sequences, 7) * kv_heads < (DP <= 64 ? 1024 : 512))
                 return go(integral_constant<int, 2>{}, integral_constant<int, DP <= 64 ? 2 : 4>{});
             return go(integral_constant<int, 4>{}, integral_constant<int, 1>{});
         });
