@@ -19,7 +19,7 @@
 namespace rs {
 namespace {
 
-constexpr int kThreads = 256, kRows = 128, kShift = 7;
+constexpr int kThreads = 256;
 
 struct GradArgs {
     Heads dout, q, k, v, out, dq, dk, dv;
@@ -71,19 +71,25 @@ constexpr float kFirstFactor = 1.152921504606846976e18f;  // 2^60: dS below 2^-7
 // the matrix instruction busy 46 % of the cycles at 1.94 GHz; a workgroup passes over
 // 17 tiles on average, and its start, three rows an operand from memory, is a
 // seventh of its time.  13 sequences of up to 2047 tokens, 40 heads of 64 in fp16: 106 us.
-template <typename T, int DP, bool ASYNC>
+// Teams as in the forward pass: (2, 2) up to 512 workgroups of (4, 1) (both kernels of one
+// sequence of 2048 tokens, 8 heads of 128: 78 us, with (4, 1) 95; of 8192 tokens, 32 heads, 1947
+// and 1869).
+template <typename T, int DP, int GROUPS, int PARTS, bool ASYNC>
 __global__ __launch_bounds__(kThreads, 2) void attention_dq_kernel(GradArgs a) {
+    static_assert(GROUPS * PARTS * kWave == kThreads, "");
     constexpr int STEPS = DP / 16, BLOCKS = DP / 32, KEYS = 64, WORDS = TileShape<DP>::words;
+    constexpr int ROWS = 32 * GROUPS, SHIFT = GROUPS == 4 ? 7 : 6, EACH = 2 / PARTS;
     __shared__ uint4 k0[KEYS * WORDS], v0[KEYS * WORDS], k1[KEYS * WORDS], v1[KEYS * WORDS];
     const Task task = task_of(blockIdx.x, a.blocks, a.heads, a.group);
     Sequence s;
-    if (!ranked_sequence(a.seq, false, a.causal, a.blocks, task.block, kShift, &s)) return;
-    const int lane = threadIdx.x % kWave, wave = threadIdx.x / kWave, half = lane / 32;
-    const int kv_head = task.head / a.group, row0 = s.block * kRows + wave * 32;
+    if (!ranked_sequence(a.seq, false, a.causal, a.blocks, task.block, SHIFT, &s)) return;
+    const int lane = threadIdx.x % kWave, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave), half = lane / 32;
+    const int part = wave / GROUPS, rows_of = wave % GROUPS, in_tile = part * 32 * EACH;
+    const int kv_head = task.head / a.group, row0 = s.block * ROWS + rows_of * 32;
     const int row = row0 + lane % 32, held = min(row, s.lq - 1);
     const T *k = a.k.template at<const T>(s.k0, kv_head), *v = a.v.template at<const T>(s.k0, kv_head);
 
-    const int to = a.causal ? min(s.lk, min(s.lq, (s.block + 1) * kRows) + s.lk - s.lq) : s.lk;
+    const int to = a.causal ? min(s.lk, min(s.lq, (s.block + 1) * ROWS) + s.lk - s.lq) : s.lk;
     TileLoader<T, DP, KEYS, kThreads, ASYNC> kl(threadIdx.x, a.dim, a.k.token_pitch), vl(threadIdx.x, a.dim, a.v.token_pitch);
     const int64_t k_step = KEYS * a.k.token_pitch, v_step = KEYS * a.v.token_pitch;
     auto load = [&](int key0, auto &k_to, auto &v_to) {
@@ -108,7 +114,7 @@ __global__ __launch_bounds__(kThreads, 2) void attention_dq_kernel(GradArgs a) {
     const int64_t stat = int64_t(task.head) * a.seq.q_tokens + s.q0 + held;
     float lse2 = a.lse[stat] * kLog2e;
     if (lse2 == -INFINITY) lse2 = INFINITY;
-    if (half == 0 && row < s.lq) {
+    if (half == 0 && part == 0 && row < s.lq) {
         a.minus_lse[stat] = kRaised<T> - lse2;
         a.minus_delta[stat] = -delta;
     }
@@ -116,7 +122,7 @@ __global__ __launch_bounds__(kThreads, 2) void attention_dq_kernel(GradArgs a) {
     const int wave_to = row0 >= s.lq ? 0 : a.causal ? min(s.lk, min(s.lq, row0 + 32) + s.lk - s.lq) : s.lk;
     const int all_see = a.causal ? row0 + 1 + s.lk - s.lq : s.lk;
 
-    const LanePlaces places = LanePlaces::of<DP>(lane);
+    const LanePlaces places = LanePlaces::of<DP>(lane, in_tile);
     f32x16 dq[BLOCKS], below;  // -delta: what dP - delta is summed from
 #pragma unroll
     for (int r = 0; r < 16; ++r) below[r] = -delta;
@@ -132,8 +138,9 @@ __global__ __launch_bounds__(kThreads, 2) void attention_dq_kernel(GradArgs a) {
         const bool more = key0 + KEYS < to;
         if (more) load(key0 + KEYS, k_next, v_next);
 #pragma unroll
-        for (int n = 0; n < 2; ++n) {
-            if (key0 + n * 32 >= wave_to) continue;
+        for (int n = 0; n < EACH; ++n) {
+            const int first = key0 + in_tile + n * 32;
+            if (first >= wave_to) continue;
             f32x16 x = zero16(), dp = below;
             Operand8<T> left[2][2];
             pipelined<STEPS>(
@@ -151,10 +158,10 @@ __global__ __launch_bounds__(kThreads, 2) void attention_dq_kernel(GradArgs a) {
                 left[i % 2][1] = column_operand<T, DP>(kt, n * 32 + 16, i, places);
             };
             read_columns(std::integral_constant<int, 0>{});
-            if (key0 + n * 32 + 32 > all_see || key0 + n * 32 + 32 > s.lk) {
+            if (first + 32 > all_see || first + 32 > s.lk) {
 #pragma unroll
                 for (int r = 0; r < 16; ++r)
-                    if (key0 + n * 32 + result_row(r, half) > last) x[r] = -INFINITY;
+                    if (first + result_row(r, half) > last) x[r] = -INFINITY;
             }
 #pragma unroll
             for (int r = 0; r < 16; ++r)
@@ -177,7 +184,14 @@ __global__ __launch_bounds__(kThreads, 2) void attention_dq_kernel(GradArgs a) {
         if (key0 + KEYS < to) step(key0 + KEYS, k1, v1, k0, v0);
     }
     T *to_row = a.dq.template at<T>(s.q0 + held, task.head);
-    const float scale = kNarrow<T> ? a.scale / factor : a.scale;
+    float scale = kNarrow<T> ? a.scale / factor : a.scale;
+    if constexpr (PARTS > 1) {
+#pragma unroll
+        for (int d = 0; d < BLOCKS; ++d) dq[d] *= scale;
+        scale = 1;
+        add_parts<DP, GROUPS, PARTS, KEYS * WORDS>(dq, part, rows_of, lane, k0, v0, k1, v1);
+        if (part > 0) return;
+    }
 #pragma unroll
     for (int d = 0; d < BLOCKS; ++d) store_columns(to_row, row < s.lq, dq[d], scale, d, lane, a.dim);
 }
@@ -450,14 +464,23 @@ extern "C" reshard_status_t reshard_attention_backward(
         return with_dim(dtype, dim, [&](auto zero, auto padded) {
             using T = decltype(zero);
             constexpr int DP = decltype(padded)::value;
+            using std::integral_constant;
             reshard_status_t status = RESHARD_OK;
             if (q_tokens > 0) {
-                status = check_grid(blocks_of(q_tokens, sequences, kShift), heads, kThreads, &a.blocks);
-                if (status != RESHARD_OK) return status;
                 const bool async = loads_itself(a.k, dim) && loads_itself(a.v, dim);
-                status = launch("attention gradient launch",
-                                async ? attention_dq_kernel<T, DP, true> : attention_dq_kernel<T, DP, false>,
-                                dim3(unsigned(a.blocks * heads)), kThreads, 0, stm, a);
+                auto go = [&](auto groups, auto parts) {
+                    constexpr int GROUPS = decltype(groups)::value, PARTS = decltype(parts)::value;
+                    reshard_status_t st =
+                        check_grid(blocks_of(q_tokens, sequences, GROUPS == 4 ? 7 : 6), heads, kThreads, &a.blocks);
+                    if (st != RESHARD_OK) return st;
+                    return launch("attention gradient launch",
+                                  async ? attention_dq_kernel<T, DP, GROUPS, PARTS, true>
+                                        : attention_dq_kernel<T, DP, GROUPS, PARTS, false>,
+                                  dim3(unsigned(a.blocks * heads)), kThreads, 0, stm, a);
+                };
+                status = blocks_of(q_tokens, sequences, 7) * heads <= 512
+                             ? go(integral_constant<int, 2>{}, integral_constant<int, 2>{})
+                             : go(integral_constant<int, 4>{}, integral_constant<int, 1>{});
                 if (status != RESHARD_OK) return status;
             }
             if (k_tokens == 0) return status;
@@ -471,7 +494,6 @@ extern "C" reshard_status_t reshard_attention_backward(
                                     : attention_dkv_kernel<T, DP, GROUPS, PARTS, false>,
                               dim3(unsigned(a.blocks * kv_heads)), kWave * GROUPS * PARTS, 0, stm, a);
             };
-            using std::integral_constant;
             if (blocks_of(k_tokens, sequences, 7) * kv_heads < (DP <= 64 ? 1024 : 512))
                 return go(integral_constant<int, 2>{}, integral_constant<int, DP <= 64 ? 2 : 4>{});
             return go(integral_constant<int, 4>{}, integral_constant<int, 1>{});

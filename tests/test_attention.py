@@ -395,6 +395,24 @@ def test_attention_and_its_gradients(dtype, heads, kv, dim, lengths, gpu_lib):
 
 
 @gpu
+@pytest.mark.parametrize("dim", [32, 64, 96, 128])
+@pytest.mark.parametrize("group", [1, 2])
+@pytest.mark.parametrize("dtype", HALVES, ids=str)
+def test_attention_of_many_heads(dtype, group, dim, gpu_lib):
+    """More blocks than CUs hold workgroups: no waves share a block's keys, or its queries."""
+    g = _seed("many heads", dtype, group, dim)
+    lengths = [(190, 190), (33, 170), (70, 40), (0, 9), (129, 129)]
+    for causal, room in ((True, 0), (False, 3)):
+        (q, k, v), at = _case(g, dtype, lengths, 160 * group, 160, dim, room=room)
+        offsets = [_int32(a) for a in at]
+        out, lse = B.reshard_attention(q, k, v, *offsets, 0.2, causal)
+        _check_attention(q, k, v, at, 0.2, causal, out, lse, f"causal {causal}")
+        dout = (0.02 * _randn(g, *q.shape)).to(dtype).cuda()
+        grads = B.reshard_attention_backward(dout, q, k, v, out, lse, *offsets, 0.2, causal)
+        _check_grads(dout, q, k, v, out, lse, at, 0.2, causal, grads, f"causal {causal}")
+
+
+@gpu
 @pytest.mark.parametrize("dtype", HALVES, ids=str)
 def test_attention_of_many_sequences(dtype, gpu_lib):
     """More sequences than a wave has lanes, and more than its square."""
