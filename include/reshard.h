@@ -660,7 +660,8 @@ reshard_status_t reshard_attention(int64_t q_tokens, int64_t k_tokens, int64_t s
  * sequence's stay as they were.  P and dS are rounded to `dtype` for the
  * products that follow, in F16 times powers of two that keep their digits.
  */
-int64_t reshard_attention_backward_workspace(int64_t q_tokens, int64_t heads); /* bytes; -1: bad extents */
+int64_t reshard_attention_backward_workspace(int64_t q_tokens, int64_t k_tokens, int64_t sequences, int64_t heads,
+                                             int64_t kv_heads, int64_t dim); /* bytes; -1: bad extents */
 reshard_status_t reshard_attention_backward(
     int64_t q_tokens, int64_t k_tokens, int64_t sequences, int64_t heads, int64_t kv_heads, int64_t dim,
     reshard_dtype_t dtype, const reshard_heads_t *dout, const reshard_heads_t *q, const reshard_heads_t *k,

@@ -163,7 +163,7 @@ def _declare_operators(lib):
     lib.reshard_rotate_heads_backward.argtypes = [*turned, hp, hp, hp, hp, vp, vp, ci, f64, vp, vp, hp, hp, fp, fp, ci,
                                                   vp, i64, vp]
     lib.reshard_attention.argtypes = [i64] * 6 + [ci, hp, hp, hp, vp, vp, f64, ci, hp, fp, vp]
-    lib.reshard_attention_backward_workspace.argtypes = [i64] * 2
+    lib.reshard_attention_backward_workspace.argtypes = [i64] * 6
     lib.reshard_attention_backward.argtypes = [i64] * 6 + [ci, hp, hp, hp, hp, hp, fp, vp, vp, f64, ci, hp, hp, hp, vp,
                                                            i64, vp]
     lib.reshard_attention_paged_workspace.argtypes = [i64] * 6
@@ -928,7 +928,7 @@ def reshard_attention_backward(dout, q, k, v, out, lse, q_offsets, k_offsets, sc
                                                                                           scale, stream)
     dout_at, out_at = _heads("dout", dout, q.shape, dtype, device), _heads("out", out, q.shape, dtype, device)
     _dense("lse", lse, (sizes[3], sizes[0]), q, _torch.float32)
-    need = lib.reshard_attention_backward_workspace(sizes[0], sizes[3])
+    need = lib.reshard_attention_backward_workspace(*sizes)
     with _on(stream):
         dq = _new(q) if dq is None else dq
         dk = _new(k) if dk is None else dk

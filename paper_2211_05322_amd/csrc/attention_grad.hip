@@ -5,8 +5,8 @@
 //
 // Two kernels: the first holds queries and passes over their keys, the second
 // holds keys and passes over their queries, heads of a group among them.  The
-// scores are made in both, 7 products where 5 would do, and no sum is taken in
-// memory: results do not depend on the order in which workgroups run.
+// scores are made in both, 7 products where 5 would do, and no two workgroups add to the
+// same sum: results do not depend on the order in which they run.
 //
 // In float16, P and dS leave the range in which the type keeps its digits (a
 // weight of 16384 equal ones is 2^-14).  P, at most 1, is multiplied by 2^14.  dS
@@ -25,6 +25,8 @@ struct GradArgs {
     Heads dout, q, k, v, out, dq, dk, dv;
     const float *lse;  // [heads][q_tokens]
     float *minus_lse, *minus_delta;  // [heads][q_tokens]: what the second kernel adds to exponents and to dP
+    float *parts;                    // [splits][dk, dv][k_tokens][kv_heads][dim], where a group's heads are split
+    int splits;
     Sequences seq;
     int heads, group, dim, causal;
     uint32_t blocks;
@@ -225,7 +227,9 @@ __global__ __launch_bounds__(kWave *GROUPS *PARTS, 2) void attention_dkv_kernel(
     __shared__ uint4 q0[QUERIES * WORDS], d0[QUERIES * WORDS], q1[QUERIES * WORDS], d1[QUERIES * WORDS];
     __shared__ __align__(16) float s0[2][STATS], s1[2][STATS];  // -lse, -delta
     __shared__ uint4 values[VALUES_IN_LDS ? KEYS * WORDS : 1];
-    const Task task = task_of(blockIdx.x, a.blocks, a.heads / a.group, 1);
+    Task task = task_of(blockIdx.x, a.blocks, a.heads / a.group * a.splits, a.splits);
+    const int split = task.head % a.splits;
+    task.head /= a.splits;
     Sequence s;
     if (!ranked_sequence(a.seq, true, a.causal, a.blocks, task.block, SHIFT, &s)) return;
     const int lane = threadIdx.x % kWave, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave), half = lane / 32;
@@ -243,7 +247,8 @@ __global__ __launch_bounds__(kWave *GROUPS *PARTS, 2) void attention_dkv_kernel(
     const int first = a.causal ? key - (s.lk - s.lq) : 0;
     const int from = a.causal ? max(0, s.block * KEYS - (s.lk - s.lq)) / QUERIES * QUERIES : 0;
     const int wave_from = a.causal ? key0 - (s.lk - s.lq) : 0, all_see = a.causal ? wave_from + 31 : 0;
-    const int tiles = s.lq > from ? (s.lq - from + QUERIES - 1) / QUERIES : 0, turns = tiles * a.group;
+    const int tiles = s.lq > from ? (s.lq - from + QUERIES - 1) / QUERIES : 0, first_head = split * a.group / a.splits;
+    const int turns = tiles * ((split + 1) * a.group / a.splits - first_head);
 
     const LanePlaces places = LanePlaces::of<DP>(lane, part * 32), v_places = LanePlaces::of<DP>(lane, keys_of * 32);
     f32x16 dk[BLOCKS], dv[BLOCKS];
@@ -252,7 +257,7 @@ __global__ __launch_bounds__(kWave *GROUPS *PARTS, 2) void attention_dkv_kernel(
     float factor = kFirstFactor;
     TileLoader<T, DP, QUERIES, THREADS, ASYNC> ql(threadIdx.x, a.dim, a.q.token_pitch), dl(threadIdx.x, a.dim, a.dout.token_pitch);
     // the tile to be loaded: its head, the rows from it to the sequence's end, and where they are
-    int next_head = task.head * a.group, rows_left = s.lq - from;
+    int next_head = task.head * a.group + first_head, rows_left = s.lq - from;
     const T *q_at = a.q.template at<const T>(s.q0 + from, next_head), *d_at = a.dout.template at<const T>(s.q0 + from, next_head);
     const float *lse_at = a.minus_lse + int64_t(next_head) * a.seq.q_tokens + s.q0 + from;
     const float *delta_at = a.minus_delta + int64_t(next_head) * a.seq.q_tokens + s.q0 + from;
@@ -408,20 +413,87 @@ __global__ __launch_bounds__(kWave *GROUPS *PARTS, 2) void attention_dkv_kernel(
         add_parts<DP, GROUPS, PARTS, QUERIES * WORDS>(dv, part, keys_of, lane, q0, d0, q1, d1);
         if (part > 0) return;
     }
+    const float by_k = PARTS > 1 ? 1.0f : scale, by_v = PARTS > 1 ? 1.0f : down;
+    if (a.splits > 1) {
+        if (key >= s.lk) return;
+        const int64_t each = a.seq.k_tokens * (a.heads / a.group) * a.dim;
+        float *to = a.parts + split * 2 * each + ((s.k0 + key) * (a.heads / a.group) + task.head) * a.dim;
+#pragma unroll
+        for (int b = 0; b < BLOCKS; ++b)
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                const int d = b * 32 + result_row(4 * j, half);
+                if (d >= a.dim) continue;
+                f32x4 x, y;
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    x[e] = dk[b][4 * j + e] * by_k;
+                    y[e] = dv[b][4 * j + e] * by_v;
+                }
+                store_any(to + d, x);
+                store_any(to + each + d, y);
+            }
+        return;
+    }
     T *to_dk = a.dk.template at<T>(s.k0 + held, task.head), *to_dv = a.dv.template at<T>(s.k0 + held, task.head);
 #pragma unroll
     for (int d = 0; d < BLOCKS; ++d) {
-        store_columns(to_dk, key < s.lk, dk[d], PARTS > 1 ? 1.0f : scale, d, lane, a.dim);
-        store_columns(to_dv, key < s.lk, dv[d], PARTS > 1 ? 1.0f : down, d, lane, a.dim);
+        store_columns(to_dk, key < s.lk, dk[d], by_k, d, lane, a.dim);
+        store_columns(to_dv, key < s.lk, dv[d], by_v, d, lane, a.dim);
     }
+}
+
+// Adds up the splits' sums in their order, 4 elements a thread, for the rows that
+// are sequences'.
+template <typename T>
+__global__ __launch_bounds__(kThreads) void attention_join_kernel(GradArgs a) {
+    const int64_t kv_heads = a.heads / a.group, each = a.seq.k_tokens * kv_heads * a.dim;
+    const int64_t at = (int64_t(blockIdx.x) * kThreads + threadIdx.x) * 4;
+    if (at >= each) return;
+    const int64_t row = at / (kv_heads * a.dim);
+    if (row < a.seq.k_offsets[0] || row >= a.seq.k_offsets[a.seq.count]) return;
+    const int rest = int(at - row * kv_heads * a.dim), head = rest / a.dim;
+    f32x4 sum{0, 0, 0, 0};
+    for (int p = 0; p < a.splits; ++p) {
+        const f32x4 x = load_any<f32x4>(a.parts + (p * 2 + int(blockIdx.y)) * each + at);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) sum[e] += x[e];
+    }
+    typedef T T4 __attribute__((ext_vector_type(4)));
+    T4 y;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) y[e] = T(sum[e]);
+    store_any((blockIdx.y ? a.dv : a.dk).template at<T>(row, head) + rest - head * a.dim, y);
+}
+
+// How the keys' kernel is dealt: whether waves share keys (above), and over how many
+// workgroups the heads of a group.  As many as the CUs hold at once, four times that
+// where sequences are of 1024 keys or more, whose first keys have the longest way.  Both
+// kernels without and with it, in us: 8 heads of 128 on one key head, 2048 tokens 258
+// and 87, 8192 tokens 1098 and 570; 32 heads of 64 on 8, 2048 tokens 139 and 105; but 8 x 256
+// tokens, 40 heads of 64 on 8, 39 and with four times as many 61: the sums' way through memory.
+struct KeyDeal {
+    bool few;
+    int64_t splits;
+};
+KeyDeal key_deal(int64_t k_tokens, int64_t sequences, int64_t kv_heads, int64_t group, int64_t dim) {
+    const bool few = blocks_of(k_tokens, sequences, 7) * kv_heads < (dim <= 64 ? 1024 : 512);
+    const int64_t workgroups = std::max<int64_t>(1, blocks_of(k_tokens, sequences, 6) * kv_heads);
+    const int64_t most = (dim <= 64 ? 512 : 256) * (k_tokens >= 1024 * sequences ? 4 : 1);
+    return KeyDeal{few, few ? std::max<int64_t>(1, std::min(group, most / workgroups)) : 1};
 }
 
 }  // namespace
 }  // namespace rs
 
-extern "C" int64_t reshard_attention_backward_workspace(int64_t q_tokens, int64_t heads) {
-    if (q_tokens < 0 || q_tokens > 0x7fffff00 || heads < 1 || heads > rs::kMaxHeads) return -1;
-    return q_tokens * heads * 8;
+extern "C" int64_t reshard_attention_backward_workspace(int64_t q_tokens, int64_t k_tokens, int64_t sequences,
+                                                        int64_t heads, int64_t kv_heads, int64_t dim) {
+    for (int64_t n : {q_tokens, k_tokens, sequences})
+        if (n < 0 || n > 0x7fffff00) return -1;
+    if (heads < 1 || heads > rs::kMaxHeads || kv_heads < 1 || heads % kv_heads || dim < 1 || dim > rs::kMaxDim) return -1;
+    const int64_t splits = rs::key_deal(k_tokens, sequences, kv_heads, heads / kv_heads, dim).splits;
+    const int64_t parts = splits > 1 ? splits * 2 * k_tokens * kv_heads * dim * 4 : 0;
+    return (q_tokens * heads * 8 + 15) / 16 * 16 + parts;
 }
 
 extern "C" reshard_status_t reshard_attention_backward(
@@ -445,14 +517,15 @@ extern "C" reshard_status_t reshard_attention_backward(
         if (st == RESHARD_OK) st = check_heads("dk", dk, k_tokens, kv_heads, dim, 2, true, &a.dk);
         if (st == RESHARD_OK) st = check_heads("dv", dv, k_tokens, kv_heads, dim, 2, true, &a.dv);
         if (st != RESHARD_OK || sequences == 0) return st;
-        if (q_tokens > 0) {
-            st = check_workspace("the queries' statistics need", workspace, workspace_bytes,
-                                 reshard_attention_backward_workspace(q_tokens, heads));
-            if (st != RESHARD_OK) return st;
-        }
+        const int64_t need = reshard_attention_backward_workspace(q_tokens, k_tokens, sequences, heads, kv_heads, dim);
+        if (need > 0) st = check_workspace("the queries' statistics and parts of sums need", workspace, workspace_bytes, need);
+        if (st != RESHARD_OK) return st;
         a.lse = lse;
         a.minus_lse = static_cast<float *>(workspace);
         a.minus_delta = a.minus_lse + q_tokens * heads;
+        const KeyDeal deal = key_deal(k_tokens, sequences, kv_heads, heads / kv_heads, dim);
+        a.splits = int(deal.splits);
+        a.parts = a.minus_lse + (q_tokens * heads * 2 + 3) / 4 * 4;
         a.seq = Sequences{q_offsets, k_offsets, int(sequences), q_tokens, k_tokens};
         a.heads = int(heads);
         a.group = int(heads / kv_heads);
@@ -487,16 +560,20 @@ extern "C" reshard_status_t reshard_attention_backward(
             const bool async = loads_itself(a.q, dim) && loads_itself(a.dout, dim) && loads_itself(a.v, dim);
             auto go = [&](auto groups, auto parts) {
                 constexpr int GROUPS = decltype(groups)::value, PARTS = decltype(parts)::value;
-                reshard_status_t st = check_grid(blocks_of(k_tokens, sequences, GROUPS == 4 ? 7 : 6), kv_heads, kWave * GROUPS * PARTS, &a.blocks);
+                reshard_status_t st = check_grid(blocks_of(k_tokens, sequences, GROUPS == 4 ? 7 : 6),
+                                                 kv_heads * deal.splits, kWave * GROUPS * PARTS, &a.blocks);
                 if (st != RESHARD_OK) return st;
                 return launch("attention gradient launch",
                               async ? attention_dkv_kernel<T, DP, GROUPS, PARTS, true>
                                     : attention_dkv_kernel<T, DP, GROUPS, PARTS, false>,
-                              dim3(unsigned(a.blocks * kv_heads)), kWave * GROUPS * PARTS, 0, stm, a);
+                              dim3(unsigned(a.blocks * kv_heads * deal.splits)), kWave * GROUPS * PARTS, 0, stm, a);
             };
-            if (blocks_of(k_tokens, sequences, 7) * kv_heads < (DP <= 64 ? 1024 : 512))
-                return go(integral_constant<int, 2>{}, integral_constant<int, DP <= 64 ? 2 : 4>{});
-            return go(integral_constant<int, 4>{}, integral_constant<int, 1>{});
+            if (!deal.few) return go(integral_constant<int, 4>{}, integral_constant<int, 1>{});
+            status = go(integral_constant<int, 2>{}, integral_constant<int, DP <= 64 ? 2 : 4>{});
+            if (status != RESHARD_OK || deal.splits == 1) return status;
+            const int64_t vectors = k_tokens * kv_heads * dim / 4;
+            return launch("attention gradient join launch", attention_join_kernel<T>,
+                          dim3(unsigned(ceil_div(vectors, kThreads)), 2), kThreads, 0, stm, a);
         });
     });
 }

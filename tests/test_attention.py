@@ -428,14 +428,10 @@ def test_attention_of_many_sequences(dtype, gpu_lib):
             _check_attention(q, k, v, at, 32 ** -0.5, True, out, lse, n)
             _check_grads(dout, q, k, v, out, lse, at, 32 ** -0.5, True, grads, n)
             continue
-        for i in range(0, n, 97):  # each of a few by itself, bit for bit
-            rows, cols = slice(at[0][i], at[0][i + 1]), slice(at[1][i], at[1][i + 1])
-            alone = [_int32([0, at[j][i + 1] - at[j][i]]) for j in range(2)]
-            o, s = B.reshard_attention(q[rows], k[cols], v[cols], *alone)
-            assert torch.equal(o, out[rows]) and torch.equal(s, lse[:, rows])
-            for a, b, r in zip(B.reshard_attention_backward(dout[rows], q[rows], k[cols], v[cols], o, s.contiguous(), *alone),
-                               grads, (rows, cols, cols)):
-                assert torch.equal(a, b[r])
+        for i in range(0, n, 97):  # a few of them
+            one = [a[i:i + 2] for a in at]
+            _check_attention(q, k, v, one, 32 ** -0.5, True, out, lse, i)
+            _check_grads(dout, q, k, v, out, lse, one, 32 ** -0.5, True, grads, i)
 
 
 @gpu
@@ -904,7 +900,8 @@ def test_attention_refusals():
                        (dict(dk=None), "dk"), (dict(work=None), "workspace"), (dict(nbytes=255), "workspace"), (dict(work=P + 8), "workspace"),
                        (dict(dt=4), "dtype")):
         _refused(bwd(**call), EI, text)
-    assert lib.reshard_attention_backward_workspace(-1, 1) == -1 and lib.reshard_attention_backward_workspace(1, 0) == -1
+    for bad in ((-1, 4, 1, 8, 2, 64), (4, -1, 1, 8, 2, 64), (4, 4, -1, 8, 2, 64), (4, 4, 1, 8, 0, 64), (4, 4, 1, 8, 3, 64), (4, 4, 1, 8, 2, 129)):
+        assert lib.reshard_attention_backward_workspace(*bad) == -1
 
 
 def test_attention_paged_refusals():
