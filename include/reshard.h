@@ -632,9 +632,9 @@ reshard_status_t reshard_rotate_heads_backward(
  * q and out [q_tokens, heads, dim], k and v [k_tokens, kv_heads, dim] are of
  * `dtype` (F16 or BF16); out overlaps none of the others.  lse [heads, q_tokens]
  * floats: the logarithm of the sum of exp(scale q k^T) over the keys that a
- * query sees, which the backward pass reads.  scale > 0.  Sums and statistics
- * are held in 32 bits, weights (each at most 2^8 times the largest) rounded to
- * `dtype` for the second product.
+ * query sees, which the backward pass reads.  scale is between 1e-30 and 1e30.  Sums and
+ * statistics are held in 32 bits, weights (each at most 2^8 times the largest)
+ * rounded to `dtype` for the second product.
  *
  * A key that a query does not see does not count, whatever it holds; an
  * infinite or NaN value may make NaN of any row of its sequence (0 * infinity).
@@ -680,8 +680,8 @@ reshard_status_t reshard_attention_backward(
  * pages_a_sequence * page_length counts as that, one below 1 as 0: the
  * sequence's rows of out are zeros.  Tokens whose page is not in the cache do
  * not count.  What the cache holds behind a sequence's length does not count,
- * whatever it is; a page may be of several sequences.  scale > 0; dim is a
- * multiple of 8 up to 128.
+ * whatever it is; a page may be of several sequences.  scale is between 1e-30
+ * and 1e30; dim is a multiple of 8 up to 128.
  */
 int64_t reshard_attention_paged_workspace(int64_t sequences, int64_t heads, int64_t kv_heads, int64_t dim,
                                           int64_t pages_a_sequence, int64_t page_length); /* bytes; -1: bad extents */

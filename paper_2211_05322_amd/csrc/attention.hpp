@@ -328,9 +328,9 @@ __device__ inline bool ranked_sequence(const Sequences &s, bool by_keys, bool ca
             if (c == 0 || c * kWave < s.count) f(c);
         });
     };
-    auto ceil = [&](int n) { return int((int64_t(n) + (1 << shift) - 1) >> shift); };
-    auto own = [&](int c) { return ceil(by_keys ? lk[c] : lq[c]); };
-    auto other = [&](int c) { return ceil(by_keys ? lq[c] : lk[c]); };
+    auto blocks_in = [&](int n) { return int((int64_t(n) + (1 << shift) - 1) >> shift); };
+    auto own = [&](int c) { return blocks_in(by_keys ? lk[c] : lq[c]); };
+    auto other = [&](int c) { return blocks_in(by_keys ? lq[c] : lk[c]); };
     int highest = 0;
     each([&](auto c) {
         const int i = min(c * kWave + lane, s.count - 1);
@@ -381,8 +381,10 @@ __device__ inline bool ranked_sequence(const Sequences &s, bool by_keys, bool ca
         }
         before += __builtin_amdgcn_readlane(upto, kWave - 1);
     });
+    if (!found) return false;
     if (!by_keys) out->block = ((out->lq - 1) >> shift) - out->block;
-    return true;
+    // counts of offsets that are not ascending may pass 32 bits
+    return out->block >= 0 && out->block < blocks_in(by_keys ? out->lk : out->lq);
 }
 
 // Adds the sums of a workgroup's parts to the first part's, in order, through the
@@ -452,6 +454,9 @@ __device__ inline Task task_of(uint32_t wg, uint32_t blocks, uint32_t heads, uin
     return Task{uint32_t(__builtin_amdgcn_readfirstlane(block)), uint32_t(__builtin_amdgcn_readfirstlane(head))};
 }
 
+// A scale whose product with log2(e) is a normal float32.
+inline bool good_scale(double scale) { return scale > 1e-30 && scale < 1e30; }
+
 // exp2 of arguments at or below about 8; far below, zero.
 __device__ inline float exp2_fast(float x) { return __builtin_amdgcn_exp2f(x); }
 
@@ -489,7 +494,7 @@ inline reshard_status_t check_attention(int64_t q_tokens, int64_t k_tokens, int6
     if (dim % 8 || dim > kMaxDim)
         return fail(RESHARD_EUNSUPPORTED, "dim must be a multiple of 8 up to " + std::to_string(kMaxDim));
     if (dtype != RESHARD_F16 && dtype != RESHARD_BF16) return fail(RESHARD_EINVAL, "dtype must be F16 or BF16");
-    if (!(scale > 0 && scale < 1e30)) return fail(RESHARD_EINVAL, "scale must be positive and finite");
+    if (!good_scale(scale)) return fail(RESHARD_EINVAL, "scale must be between 1e-30 and 1e30");
     if (causal & ~1) return fail(RESHARD_EINVAL, "causal must be 0 or 1");
     st = check_matrix("q_offsets", q_offsets, 1, sequences + 1, sequences + 1, 4);
     if (st == RESHARD_OK) st = check_matrix("k_offsets", k_offsets, 1, sequences + 1, sequences + 1, 4);

@@ -456,7 +456,7 @@ extern "C" reshard_status_t reshard_attention_paged(int64_t sequences, int64_t h
         if (dim % 8 || dim > kMaxDim)
             return fail(RESHARD_EUNSUPPORTED, "dim must be a multiple of 8 up to " + std::to_string(kMaxDim));
         if (dtype != RESHARD_F16 && dtype != RESHARD_BF16) return fail(RESHARD_EINVAL, "dtype must be F16 or BF16");
-        if (!(scale > 0 && scale < 1e30)) return fail(RESHARD_EINVAL, "scale must be positive and finite");
+        if (!good_scale(scale)) return fail(RESHARD_EINVAL, "scale must be between 1e-30 and 1e30");
         if (!cache) return fail(RESHARD_EINVAL, "cache is NULL");
         PagedArgs a{};
         st = check_heads("q", q, sequences, heads, dim, 2, false, &a.q);

@@ -904,6 +904,16 @@ def test_attention_refusals():
         assert lib.reshard_attention_backward_workspace(*bad) == -1
 
 
+@pytest.mark.parametrize("scale", [1e-60, 1e-38, 1e-31, 1e30, -1.0])
+def test_scales_out_of_range(scale):
+    """What float32 holds as 0 or nearly would make NaN of masked scores, -infinity * 0."""
+    lib, cache = B.load(), _cache(P, P, 10, 16, 16 * 128, 128, 64)
+    _refused(lib.reshard_attention(4, 4, 1, 8, 2, 64, 3, _at(), _at(), _at(), P, P, scale, 1, _at(), P, None), EI, "scale")
+    _refused(lib.reshard_attention_backward(4, 4, 1, 8, 2, 64, 3, _at(), _at(), _at(), _at(), _at(), P, P, P, scale, 1, _at(), _at(),
+                                            _at(), P, 1 << 30, None), EI, "scale")
+    _refused(lib.reshard_attention_paged(4, 8, 2, 64, 3, _at(), cache, P, 8, 8, P, scale, _at(), P, 1 << 30, None), EI, "scale")
+
+
 def test_attention_paged_refusals():
     lib = B.load()
     good = _cache(P, P, 10, 16, 16 * 128, 128, 64)
