@@ -413,6 +413,29 @@ def test_attention_of_many_heads(dtype, group, dim, gpu_lib):
 
 
 @gpu
+@pytest.mark.parametrize("lengths,heads,kv,dim", [
+    ([(701, 701), (0, 40), (390, 633), (5, 0), (129, 129)], 21, 3, 64), ([(640, 640), (0, 3), (511, 900)], 21, 3, 128),
+    ([(1100, 1100)], 72, 8, 128), ([(70, 1), (1, 1201)], 300, 1, 32)])
+@pytest.mark.parametrize("dtype", HALVES, ids=str)
+def test_gradients_of_groups_in_parts(dtype, lengths, heads, kv, dim, gpu_lib):
+    """Groups whose heads come to a key in several parts, which they do not always fill alike, of the same bits every time."""
+    g = _seed("parts", dtype, heads, kv, dim, lengths)
+    for causal in (True, False):
+        (q, k, v), at = _case(g, dtype, lengths, heads, kv, dim, 3, 2)
+        offsets = [_int32(a) for a in at]
+        out, lse = B.reshard_attention(q, k, v, *offsets, 0.2, causal)
+        dout = (0.02 * _randn(g, *q.shape)).to(dtype).cuda()
+        runs = []
+        for _ in range(2):
+            runs.append([torch.full(t.shape, 7.0, dtype=dtype, device="cuda") for t in (q, k, v)])
+            B.reshard_attention_backward(dout, q, k, v, out, lse, *offsets, 0.2, causal, *runs[-1])
+        assert all(torch.equal(a, b) for a, b in zip(*runs))
+        _check_grads(dout, q, k, v, out, lse, at, 0.2, causal, runs[0], f"causal {causal}")
+        for t, a in zip(runs[0], (at[0], at[1], at[1])):
+            assert (t[:3] == 7).all() and (t[a[-1]:] == 7).all()
+
+
+@gpu
 @pytest.mark.parametrize("dtype", HALVES, ids=str)
 def test_attention_of_many_sequences(dtype, gpu_lib):
     """More sequences than a wave has lanes, and more than its square."""
