@@ -29,7 +29,7 @@ struct GradArgs {
     int splits;
     Sequences seq;
     int heads, group, dim, causal;
-    uint32_t blocks;
+    uint32_t q_blocks, k_blocks;
     float scale, scale2;
 };
 
@@ -89,6 +89,9 @@ __device__ inline void round_raised(f32x16 &ds, float &raise, f32x16 (&sums)[BLO
     for (int r = 0; r < 16; ++r) to[r / 8].e[r % 8] = T(ds[r]);
 }
 
+// What the exponents of a query's weights are taken from, to base 2.  One that sees no key has weights of 0.
+__device__ inline float weights_base(float lse) { return lse == -INFINITY ? INFINITY : lse * kLog2e; }
+
 // Queries: as in the forward pass a lane holds one's column throughout, so that
 // its statistics are the lane's and dS goes into the next product as it is.  delta is
 // summed here, where both its rows are at hand, and kept for the keys' kernel.
@@ -99,15 +102,16 @@ __device__ inline void round_raised(f32x16 &ds, float &raise, f32x16 (&sums)[BLO
 // Teams as in the forward pass: (2, 2) up to 512 workgroups of (4, 1) (both kernels of one
 // sequence of 2048 tokens, 8 heads of 128: 78 us, with (4, 1) 95; of 8192 tokens, 32 heads, 1947
 // and 1869).
-template <typename T, int DP, int GROUPS, int PARTS, bool ASYNC>
-__global__ __launch_bounds__(kThreads, 2) void attention_dq_kernel(GradArgs a) {
+template <typename T, int DP, int GROUPS, int PARTS, bool ASYNC, bool STATS_GIVEN, int TILE>
+__device__ __forceinline__ void queries_block(const GradArgs &a, uint32_t wg, uint4 (&k0)[TILE], uint4 (&v0)[TILE],
+                                              uint4 (&k1)[TILE], uint4 (&v1)[TILE]) {
     static_assert(GROUPS * PARTS * kWave == kThreads, "");
     constexpr int STEPS = DP / 16, BLOCKS = DP / 32, KEYS = 64, WORDS = TileShape<DP>::words;
     constexpr int ROWS = 32 * GROUPS, SHIFT = GROUPS == 4 ? 7 : 6, EACH = 2 / PARTS;
-    __shared__ uint4 k0[KEYS * WORDS], v0[KEYS * WORDS], k1[KEYS * WORDS], v1[KEYS * WORDS];
-    const Task task = task_of(blockIdx.x, a.blocks, a.heads, a.group);
+    static_assert(TILE == KEYS * WORDS, "");
+    const Task task = task_of(wg, a.q_blocks, a.heads, a.group);
     Sequence s;
-    if (!ranked_sequence(a.seq, false, a.causal, a.blocks, task.block, SHIFT, &s)) return;
+    if (!ranked_sequence(a.seq, false, a.causal, a.q_blocks, task.block, SHIFT, &s)) return;
     const int lane = threadIdx.x % kWave, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave), half = lane / 32;
     const int part = wave / GROUPS, rows_of = wave % GROUPS, in_tile = part * 32 * EACH;
     const int kv_head = task.head / a.group, row0 = s.block * ROWS + rows_of * 32;
@@ -131,17 +135,21 @@ __global__ __launch_bounds__(kThreads, 2) void attention_dq_kernel(GradArgs a) {
     for (int i = 0; i < STEPS; ++i) {
         q[i] = global_operand(a.q.template at<const T>(s.q0 + held, task.head), true, i, lane, a.dim);
         dout[i] = global_operand(a.dout.template at<const T>(s.q0 + held, task.head), true, i, lane, a.dim);
+        if constexpr (STATS_GIVEN) continue;
         const Operand8<T> out = global_operand(a.out.template at<const T>(s.q0 + held, task.head), true, i, lane, a.dim);
 #pragma unroll
         for (int e = 0; e < 8; ++e) delta = fmaf(float(dout[i].e[e]), float(out.e[e]), delta);
     }
-    delta = halves_sum(delta);
     const int64_t stat = int64_t(task.head) * a.seq.q_tokens + s.q0 + held;
-    float lse2 = a.lse[stat] * kLog2e;
-    if (lse2 == -INFINITY) lse2 = INFINITY;
-    if (half == 0 && part == 0 && row < s.lq) {
-        a.minus_lse[stat] = kRaised<T> - lse2;
-        a.minus_delta[stat] = -delta;
+    const float lse2 = weights_base(a.lse[stat]);
+    if constexpr (STATS_GIVEN) {
+        delta = -a.minus_delta[stat];
+    } else {
+        delta = halves_sum(delta);
+        if (half == 0 && part == 0 && row < s.lq) {
+            a.minus_lse[stat] = kRaised<T> - lse2;
+            a.minus_delta[stat] = -delta;
+        }
     }
     const int last = a.causal ? held + s.lk - s.lq : s.lk - 1;
     const int wave_to = row0 >= s.lq ? 0 : a.causal ? min(s.lk, min(s.lq, row0 + 32) + s.lk - s.lq) : s.lk;
@@ -214,7 +222,7 @@ __global__ __launch_bounds__(kThreads, 2) void attention_dq_kernel(GradArgs a) {
 #pragma unroll
         for (int d = 0; d < BLOCKS; ++d) dq[d] *= scale;
         scale = 1;
-        add_parts<DP, GROUPS, PARTS, KEYS * WORDS>(dq, part, rows_of, lane, k0, v0, k1, v1);
+        add_parts<DP, GROUPS, PARTS, TILE>(dq, part, rows_of, lane, k0, v0, k1, v1);
         if (part > 0) return;
     }
 #pragma unroll
@@ -241,20 +249,28 @@ __global__ __launch_bounds__(kThreads, 2) void attention_dq_kernel(GradArgs a) {
 // sequence's first keys, with 160 tiles of queries, are what is waited for.
 //
 // Heads above 64 leave no registers for both operands beside both sums: values stay in LDS.
-template <typename T, int DP, int GROUPS, int PARTS, bool ASYNC>
-__global__ __launch_bounds__(kWave *GROUPS *PARTS, 2) void attention_dkv_kernel(GradArgs a) {
-    constexpr int STEPS = DP / 16, BLOCKS = DP / 32, QUERIES = 32 * PARTS, WORDS = TileShape<DP>::words;
-    constexpr int THREADS = kWave * GROUPS * PARTS, KEYS = 32 * GROUPS, SHIFT = GROUPS == 4 ? 7 : 6;
-    constexpr bool VALUES_IN_LDS = DP > 64;
-    constexpr int STATS = QUERIES < kWave ? kWave : QUERIES;
-    __shared__ uint4 q0[QUERIES * WORDS], d0[QUERIES * WORDS], q1[QUERIES * WORDS], d1[QUERIES * WORDS];
-    __shared__ __align__(16) float s0[2][STATS], s1[2][STATS];  // -lse, -delta
-    __shared__ uint4 values[VALUES_IN_LDS ? KEYS * WORDS : 1];
-    Task task = task_of(blockIdx.x, a.blocks, a.heads / a.group * a.splits, a.splits);
+template <int DP, int GROUPS, int PARTS>
+struct KeysShape {
+    static constexpr int queries = 32 * PARTS, words = TileShape<DP>::words, tile = queries * words, keys = 32 * GROUPS;
+    static constexpr int stats = queries < kWave ? kWave : queries;
+    static constexpr bool values_in_lds = DP > 64;
+    static constexpr int values = values_in_lds ? keys * words : 1;
+};
+
+template <typename T, int DP, int GROUPS, int PARTS, bool ASYNC, int TILE, int STATS, int VALUES>
+__device__ __forceinline__ void keys_block(const GradArgs &a, uint32_t wg, uint4 (&q0)[TILE], uint4 (&d0)[TILE],
+                                           uint4 (&q1)[TILE], uint4 (&d1)[TILE], float (&s0)[2][STATS],
+                                           float (&s1)[2][STATS], uint4 (&values)[VALUES]) {
+    using Shape = KeysShape<DP, GROUPS, PARTS>;
+    constexpr int STEPS = DP / 16, BLOCKS = DP / 32, QUERIES = Shape::queries, KEYS = Shape::keys;
+    constexpr int THREADS = kWave * GROUPS * PARTS, SHIFT = GROUPS == 4 ? 7 : 6;
+    constexpr bool VALUES_IN_LDS = Shape::values_in_lds;
+    static_assert(TILE == Shape::tile && STATS == Shape::stats && VALUES == Shape::values, "");
+    Task task = task_of(wg, a.k_blocks, a.heads / a.group * a.splits, a.splits);
     const int split = task.head % a.splits;
     task.head /= a.splits;
     Sequence s;
-    if (!ranked_sequence(a.seq, true, a.causal, a.blocks, task.block, SHIFT, &s)) return;
+    if (!ranked_sequence(a.seq, true, a.causal, a.k_blocks, task.block, SHIFT, &s)) return;
     const int lane = threadIdx.x % kWave, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave), half = lane / 32;
     const int part = wave / GROUPS, keys_of = wave % GROUPS;
     const int key0 = s.block * KEYS + keys_of * 32, key = key0 + lane % 32, held = min(key, s.lk - 1);
@@ -432,8 +448,8 @@ __global__ __launch_bounds__(kWave *GROUPS *PARTS, 2) void attention_dkv_kernel(
             dk[d] *= scale;
             dv[d] *= down;
         }
-        add_parts<DP, GROUPS, PARTS, QUERIES * WORDS>(dk, part, keys_of, lane, q0, d0, q1, d1);
-        add_parts<DP, GROUPS, PARTS, QUERIES * WORDS>(dv, part, keys_of, lane, q0, d0, q1, d1);
+        add_parts<DP, GROUPS, PARTS, TILE>(dk, part, keys_of, lane, q0, d0, q1, d1);
+        add_parts<DP, GROUPS, PARTS, TILE>(dv, part, keys_of, lane, q0, d0, q1, d1);
         if (part > 0) return;
     }
     const float by_k = PARTS > 1 ? 1.0f : scale, by_v = PARTS > 1 ? 1.0f : down;
@@ -464,6 +480,62 @@ __global__ __launch_bounds__(kWave *GROUPS *PARTS, 2) void attention_dkv_kernel(
         store_columns(to_dk, key < s.lk, dk[d], by_k, d, lane, a.dim);
         store_columns(to_dv, key < s.lk, dv[d], by_v, d, lane, a.dim);
     }
+}
+
+template <typename T, int DP, int GROUPS, int PARTS, bool ASYNC>
+__global__ __launch_bounds__(kThreads, 2) void attention_dq_kernel(GradArgs a) {
+    constexpr int TILE = 64 * TileShape<DP>::words;
+    __shared__ uint4 k0[TILE], v0[TILE], k1[TILE], v1[TILE];
+    queries_block<T, DP, GROUPS, PARTS, ASYNC, false>(a, blockIdx.x, k0, v0, k1, v1);
+}
+
+template <typename T, int DP, int GROUPS, int PARTS, bool ASYNC>
+__global__ __launch_bounds__(kWave *GROUPS *PARTS, 2) void attention_dkv_kernel(GradArgs a) {
+    using Shape = KeysShape<DP, GROUPS, PARTS>;
+    __shared__ uint4 q0[Shape::tile], d0[Shape::tile], q1[Shape::tile], d1[Shape::tile];
+    __shared__ __align__(16) float s0[2][Shape::stats], s1[2][Shape::stats];  // -lse, -delta
+    __shared__ uint4 values[Shape::values];
+    keys_block<T, DP, GROUPS, PARTS, ASYNC>(a, blockIdx.x, q0, d0, q1, d1, s0, s1, values);
+}
+
+// Both in one launch, the keys' blocks first, whose longest are waited for otherwise: the
+// queries' fill the CUs meanwhile.  The statistics are then made beforehand.  In heads of 64,
+// apart and together, in us: 2048 tokens, 8 heads on one key head 64 and 45; 8 x 256, 40 on 8, 45
+// and 37; 13 sequences of up to 2047, 40 heads in fp16, 275 and 263; 4096, 32 on 4, 306 and 312.
+template <typename T, int DP, int GROUPS, int PARTS, bool ASYNC>
+__global__ __launch_bounds__(kThreads, 2) void attention_both_kernel(GradArgs a, uint32_t keys_workgroups) {
+    using Shape = KeysShape<DP, 2, 2>;
+    __shared__ uint4 t0[Shape::tile], t1[Shape::tile], t2[Shape::tile], t3[Shape::tile];
+    __shared__ __align__(16) float s0[2][Shape::stats], s1[2][Shape::stats];
+    __shared__ uint4 values[Shape::values];
+    if (blockIdx.x < keys_workgroups)
+        keys_block<T, DP, 2, 2, ASYNC>(a, blockIdx.x, t0, t1, t2, t3, s0, s1, values);
+    else
+        queries_block<T, DP, GROUPS, PARTS, ASYNC, true>(a, blockIdx.x - keys_workgroups, t0, t1, t2, t3);
+}
+
+// -lse and -delta of 32 queries of a head, 8 lanes a row.
+template <typename T>
+__global__ __launch_bounds__(kThreads) void attention_stats_kernel(GradArgs a) {
+    const uint32_t block = blockIdx.x / uint32_t(a.heads), head = blockIdx.x - block * a.heads;
+    const int64_t row = int64_t(block) * 32 + threadIdx.x / 8;
+    float delta = 0;
+    if (row < a.seq.q_tokens) {
+        const T *dout = a.dout.template at<const T>(row, head), *out = a.out.template at<const T>(row, head);
+        for (int d = threadIdx.x % 8 * 8; d < a.dim; d += 64) {
+            Operand8<T> x, y;
+            x.w = load_any<uint4>(dout + d);
+            y.w = load_any<uint4>(out + d);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) delta = fmaf(float(x.e[e]), float(y.e[e]), delta);
+        }
+    }
+#pragma unroll
+    for (int d = 1; d < 8; d *= 2) delta += __shfl_xor(delta, d);
+    if (row >= a.seq.q_tokens || threadIdx.x % 8) return;
+    const int64_t stat = int64_t(head) * a.seq.q_tokens + row;
+    a.minus_lse[stat] = kRaised<T> - weights_base(a.lse[stat]);
+    a.minus_delta[stat] = -delta;
 }
 
 // Adds up the splits' sums in their order, 4 elements a thread, for the rows that
@@ -561,38 +633,59 @@ extern "C" reshard_status_t reshard_attention_backward(
             using T = decltype(zero);
             constexpr int DP = decltype(padded)::value;
             using std::integral_constant;
-            reshard_status_t status = RESHARD_OK;
-            if (q_tokens > 0) {
-                const bool async = loads_itself(a.k, dim) && loads_itself(a.v, dim);
+            const bool q_async = loads_itself(a.k, dim) && loads_itself(a.v, dim);
+            const bool k_async = loads_itself(a.q, dim) && loads_itself(a.dout, dim) && loads_itself(a.v, dim);
+            const bool q_few = blocks_of(q_tokens, sequences, 7) * heads <= 512;
+            const bool together = DP <= 64 && deal.few && q_tokens > 0 && k_tokens > 0;
+            reshard_status_t status = check_grid(blocks_of(q_tokens, sequences, q_few ? 6 : 7), heads, kThreads, &a.q_blocks);
+            if (status == RESHARD_OK)
+                status = check_grid(blocks_of(k_tokens, sequences, deal.few ? 6 : 7), kv_heads * deal.splits,
+                                    deal.few && DP > 64 ? 512 : kThreads, &a.k_blocks);
+            if (status != RESHARD_OK) return status;
+            const int64_t q_grid = a.q_blocks * heads, k_grid = a.k_blocks * kv_heads * deal.splits;
+            const auto two = integral_constant<int, 2>{};
+            const auto four = integral_constant<int, 4>{};
+            const auto one = integral_constant<int, 1>{};
+            if constexpr (DP <= 64) {
+                if (together) {
+                    uint32_t rows, all;
+                    status = check_grid(ceil_div(q_tokens, 32), heads, kThreads, &rows);
+                    if (status == RESHARD_OK) status = check_grid(q_grid + k_grid, 1, kThreads, &all);
+                    if (status != RESHARD_OK) return status;
+                    status = launch("attention statistics launch", attention_stats_kernel<T>, dim3(unsigned(rows * heads)),
+                                    kThreads, 0, stm, a);
+                    if (status != RESHARD_OK) return status;
+                    auto go = [&](auto groups, auto parts) {
+                        constexpr int GROUPS = decltype(groups)::value, PARTS = decltype(parts)::value;
+                        return launch("attention gradient launch",
+                                      q_async && k_async ? attention_both_kernel<T, DP, GROUPS, PARTS, true>
+                                                         : attention_both_kernel<T, DP, GROUPS, PARTS, false>,
+                                      dim3(all), kThreads, 0, stm, a, uint32_t(k_grid));
+                    };
+                    status = q_few ? go(two, two) : go(four, one);
+                }
+            }
+            if (!together && q_tokens > 0) {
                 auto go = [&](auto groups, auto parts) {
                     constexpr int GROUPS = decltype(groups)::value, PARTS = decltype(parts)::value;
-                    reshard_status_t st =
-                        check_grid(blocks_of(q_tokens, sequences, GROUPS == 4 ? 7 : 6), heads, kThreads, &a.blocks);
-                    if (st != RESHARD_OK) return st;
                     return launch("attention gradient launch",
-                                  async ? attention_dq_kernel<T, DP, GROUPS, PARTS, true>
-                                        : attention_dq_kernel<T, DP, GROUPS, PARTS, false>,
-                                  dim3(unsigned(a.blocks * heads)), kThreads, 0, stm, a);
+                                  q_async ? attention_dq_kernel<T, DP, GROUPS, PARTS, true>
+                                          : attention_dq_kernel<T, DP, GROUPS, PARTS, false>,
+                                  dim3(unsigned(q_grid)), kThreads, 0, stm, a);
                 };
-                status = blocks_of(q_tokens, sequences, 7) * heads <= 512
-                             ? go(integral_constant<int, 2>{}, integral_constant<int, 2>{})
-                             : go(integral_constant<int, 4>{}, integral_constant<int, 1>{});
-                if (status != RESHARD_OK) return status;
+                status = q_few ? go(two, two) : go(four, one);
             }
-            if (k_tokens == 0) return status;
-            const bool async = loads_itself(a.q, dim) && loads_itself(a.dout, dim) && loads_itself(a.v, dim);
-            auto go = [&](auto groups, auto parts) {
-                constexpr int GROUPS = decltype(groups)::value, PARTS = decltype(parts)::value;
-                reshard_status_t st = check_grid(blocks_of(k_tokens, sequences, GROUPS == 4 ? 7 : 6),
-                                                 kv_heads * deal.splits, kWave * GROUPS * PARTS, &a.blocks);
-                if (st != RESHARD_OK) return st;
-                return launch("attention gradient launch",
-                              async ? attention_dkv_kernel<T, DP, GROUPS, PARTS, true>
-                                    : attention_dkv_kernel<T, DP, GROUPS, PARTS, false>,
-                              dim3(unsigned(a.blocks * kv_heads * deal.splits)), kWave * GROUPS * PARTS, 0, stm, a);
-            };
-            if (!deal.few) return go(integral_constant<int, 4>{}, integral_constant<int, 1>{});
-            status = go(integral_constant<int, 2>{}, integral_constant<int, DP <= 64 ? 2 : 4>{});
+            if (status != RESHARD_OK || k_tokens == 0) return status;
+            if (!together) {
+                auto go = [&](auto groups, auto parts) {
+                    constexpr int GROUPS = decltype(groups)::value, PARTS = decltype(parts)::value;
+                    return launch("attention gradient launch",
+                                  k_async ? attention_dkv_kernel<T, DP, GROUPS, PARTS, true>
+                                          : attention_dkv_kernel<T, DP, GROUPS, PARTS, false>,
+                                  dim3(unsigned(k_grid)), kWave * GROUPS * PARTS, 0, stm, a);
+                };
+                status = !deal.few ? go(four, one) : go(two, integral_constant<int, DP <= 64 ? 2 : 4>{});
+            }
             if (status != RESHARD_OK || deal.splits == 1) return status;
             const int64_t vectors = k_tokens * kv_heads * dim / 4;
             return launch("attention gradient join launch", attention_join_kernel<T>,
