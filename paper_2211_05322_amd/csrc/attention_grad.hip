@@ -105,10 +105,9 @@ __device__ inline float weights_base(float lse) { return lse == -INFINITY ? INFI
 template <typename T, int DP, int GROUPS, int PARTS, bool ASYNC, bool STATS_GIVEN, int TILE>
 __device__ __forceinline__ void queries_block(const GradArgs &a, uint32_t wg, uint4 (&k0)[TILE], uint4 (&v0)[TILE],
                                               uint4 (&k1)[TILE], uint4 (&v1)[TILE]) {
-    static_assert(GROUPS * PARTS * kWave == kThreads, "");
-    constexpr int STEPS = DP / 16, BLOCKS = DP / 32, KEYS = 64, WORDS = TileShape<DP>::words;
+    constexpr int STEPS = DP / 16, BLOCKS = DP / 32, KEYS = 64, THREADS = kWave * GROUPS * PARTS;
     constexpr int ROWS = 32 * GROUPS, SHIFT = GROUPS == 4 ? 7 : 6, EACH = 2 / PARTS;
-    static_assert(TILE == KEYS * WORDS, "");
+    static_assert(TILE >= KEYS * TileShape<DP>::words, "");
     const Task task = task_of(wg, a.q_blocks, a.heads, a.group);
     Sequence s;
     if (!ranked_sequence(a.seq, false, a.causal, a.q_blocks, task.block, SHIFT, &s)) return;
@@ -119,7 +118,7 @@ __device__ __forceinline__ void queries_block(const GradArgs &a, uint32_t wg, ui
     const T *k = a.k.template at<const T>(s.k0, kv_head), *v = a.v.template at<const T>(s.k0, kv_head);
 
     const int to = a.causal ? min(s.lk, min(s.lq, (s.block + 1) * ROWS) + s.lk - s.lq) : s.lk;
-    TileLoader<T, DP, KEYS, kThreads, ASYNC> kl(threadIdx.x, a.dim, a.k.token_pitch), vl(threadIdx.x, a.dim, a.v.token_pitch);
+    TileLoader<T, DP, KEYS, THREADS, ASYNC> kl(threadIdx.x, a.dim, a.k.token_pitch), vl(threadIdx.x, a.dim, a.v.token_pitch);
     const int64_t k_step = KEYS * a.k.token_pitch, v_step = KEYS * a.v.token_pitch;
     auto load = [&](int key0, auto &k_to, auto &v_to) {
         kl.start(k, s.lk - key0, k_to);
@@ -502,14 +501,18 @@ __global__ __launch_bounds__(kWave *GROUPS *PARTS, 2) void attention_dkv_kernel(
 // queries' fill the CUs meanwhile.  The statistics are then made beforehand.  In heads of 64,
 // apart and together, in us: 2048 tokens, 8 heads on one key head 64 and 45; 8 x 256, 40 on 8, 45
 // and 37; 13 sequences of up to 2047, 40 heads in fp16, 275 and 263; 4096, 32 on 4, 306 and 312.
+// Of 128, whose workgroups have 8 waves and a CU for themselves, up to 512 workgroups: 2048
+// tokens, 8 heads on one 87 and 73 (400 workgroups), 512 tokens 41 and 30; but 2048, 16 on 2
+// (800) 112 and 121.
 template <typename T, int DP, int GROUPS, int PARTS, bool ASYNC>
-__global__ __launch_bounds__(kThreads, 2) void attention_both_kernel(GradArgs a, uint32_t keys_workgroups) {
-    using Shape = KeysShape<DP, 2, 2>;
+__global__ __launch_bounds__(kWave *GROUPS *PARTS, 2) void attention_both_kernel(GradArgs a, uint32_t keys_workgroups) {
+    constexpr int K_PARTS = GROUPS * PARTS / 2;
+    using Shape = KeysShape<DP, 2, K_PARTS>;
     __shared__ uint4 t0[Shape::tile], t1[Shape::tile], t2[Shape::tile], t3[Shape::tile];
     __shared__ __align__(16) float s0[2][Shape::stats], s1[2][Shape::stats];
     __shared__ uint4 values[Shape::values];
     if (blockIdx.x < keys_workgroups)
-        keys_block<T, DP, 2, 2, ASYNC>(a, blockIdx.x, t0, t1, t2, t3, s0, s1, values);
+        keys_block<T, DP, 2, K_PARTS, ASYNC>(a, blockIdx.x, t0, t1, t2, t3, s0, s1, values);
     else
         queries_block<T, DP, GROUPS, PARTS, ASYNC, true>(a, blockIdx.x - keys_workgroups, t0, t1, t2, t3);
 }
@@ -636,34 +639,37 @@ extern "C" reshard_status_t reshard_attention_backward(
             const bool q_async = loads_itself(a.k, dim) && loads_itself(a.v, dim);
             const bool k_async = loads_itself(a.q, dim) && loads_itself(a.dout, dim) && loads_itself(a.v, dim);
             const bool q_few = blocks_of(q_tokens, sequences, 7) * heads <= 512;
-            const bool together = DP <= 64 && deal.few && q_tokens > 0 && k_tokens > 0;
-            reshard_status_t status = check_grid(blocks_of(q_tokens, sequences, q_few ? 6 : 7), heads, kThreads, &a.q_blocks);
+            const int64_t workgroups = blocks_of(q_tokens, sequences, 7) * heads +
+                                       blocks_of(k_tokens, sequences, 6) * kv_heads * deal.splits;
+            const bool together = deal.few && q_tokens > 0 && k_tokens > 0 && (DP <= 64 || workgroups <= 512);
+            const int k_threads = deal.few && DP > 64 ? 512 : kThreads, q_threads = together ? k_threads : kThreads;
+            reshard_status_t status =
+                check_grid(blocks_of(q_tokens, sequences, q_few && q_threads == kThreads ? 6 : 7), heads, q_threads, &a.q_blocks);
             if (status == RESHARD_OK)
                 status = check_grid(blocks_of(k_tokens, sequences, deal.few ? 6 : 7), kv_heads * deal.splits,
-                                    deal.few && DP > 64 ? 512 : kThreads, &a.k_blocks);
+                                    k_threads, &a.k_blocks);
             if (status != RESHARD_OK) return status;
             const int64_t q_grid = a.q_blocks * heads, k_grid = a.k_blocks * kv_heads * deal.splits;
             const auto two = integral_constant<int, 2>{};
             const auto four = integral_constant<int, 4>{};
             const auto one = integral_constant<int, 1>{};
-            if constexpr (DP <= 64) {
-                if (together) {
-                    uint32_t rows, all;
-                    status = check_grid(ceil_div(q_tokens, 32), heads, kThreads, &rows);
-                    if (status == RESHARD_OK) status = check_grid(q_grid + k_grid, 1, kThreads, &all);
-                    if (status != RESHARD_OK) return status;
-                    status = launch("attention statistics launch", attention_stats_kernel<T>, dim3(unsigned(rows * heads)),
-                                    kThreads, 0, stm, a);
-                    if (status != RESHARD_OK) return status;
-                    auto go = [&](auto groups, auto parts) {
-                        constexpr int GROUPS = decltype(groups)::value, PARTS = decltype(parts)::value;
-                        return launch("attention gradient launch",
-                                      q_async && k_async ? attention_both_kernel<T, DP, GROUPS, PARTS, true>
-                                                         : attention_both_kernel<T, DP, GROUPS, PARTS, false>,
-                                      dim3(all), kThreads, 0, stm, a, uint32_t(k_grid));
-                    };
-                    status = q_few ? go(two, two) : go(four, one);
-                }
+            if (together) {
+                uint32_t rows, all;
+                status = check_grid(ceil_div(q_tokens, 32), heads, kThreads, &rows);
+                if (status == RESHARD_OK) status = check_grid(q_grid + k_grid, 1, k_threads, &all);
+                if (status != RESHARD_OK) return status;
+                status = launch("attention statistics launch", attention_stats_kernel<T>, dim3(unsigned(rows * heads)),
+                                kThreads, 0, stm, a);
+                if (status != RESHARD_OK) return status;
+                auto go = [&](auto groups, auto parts) {
+                    constexpr int GROUPS = decltype(groups)::value, PARTS = decltype(parts)::value;
+                    return launch("attention gradient launch",
+                                  q_async && k_async ? attention_both_kernel<T, DP, GROUPS, PARTS, true>
+                                                     : attention_both_kernel<T, DP, GROUPS, PARTS, false>,
+                                  dim3(all), k_threads, 0, stm, a, uint32_t(k_grid));
+                };
+                if constexpr (DP > 64) status = go(four, two);
+                else status = q_few ? go(two, two) : go(four, one);
             }
             if (!together && q_tokens > 0) {
                 auto go = [&](auto groups, auto parts) {

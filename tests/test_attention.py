@@ -436,6 +436,24 @@ def test_gradients_of_groups_in_parts(dtype, lengths, heads, kv, dim, gpu_lib):
 
 
 @gpu
+@pytest.mark.parametrize("heads,kv", [(16, 16), (64, 64), (64, 32)])
+@pytest.mark.parametrize("dim", [32, 64, 96, 128])
+@pytest.mark.parametrize("dtype", HALVES, ids=str)
+def test_few_queries_over_many_keys(dtype, dim, heads, kv, gpu_lib):
+    """Few blocks of queries beside more blocks of keys than CUs hold workgroups."""
+    g = _seed("few queries", dtype, dim, heads, kv)
+    lengths = [(3, 700), (70, 1500), (1, 0)]
+    for causal, room in ((True, 0), (False, 3)):
+        (q, k, v), at = _case(g, dtype, lengths, heads, kv, dim, room=room)
+        offsets = [_int32(a) for a in at]
+        out, lse = B.reshard_attention(q, k, v, *offsets, 0.2, causal)
+        _check_attention(q, k, v, at, 0.2, causal, out, lse, f"causal {causal}")
+        dout = (0.02 * _randn(g, *q.shape)).to(dtype).cuda()
+        grads = B.reshard_attention_backward(dout, q, k, v, out, lse, *offsets, 0.2, causal)
+        _check_grads(dout, q, k, v, out, lse, at, 0.2, causal, grads, f"causal {causal}")
+
+
+@gpu
 @pytest.mark.parametrize("dtype", HALVES, ids=str)
 def test_attention_of_many_sequences(dtype, gpu_lib):
     """More sequences than a wave has lanes, and more than its square."""
