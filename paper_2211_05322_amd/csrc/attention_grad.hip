@@ -3,7 +3,7 @@
 //   P = exp(scale q k^T - lse)         dP = dout v^T       delta = sum_d dout out
 //   dS = scale P (dP - delta)          dq = dS k           dk = dS^T q      dv = P^T dout
 //
-// Two kernels: the first holds queries and passes over their keys, the second
+// Two passes: the first holds queries and passes over their keys, the second
 // holds keys and passes over their queries, heads of a group among them.  The
 // scores are made in both, 7 products where 5 would do, and no two workgroups add to the
 // same sum: results do not depend on the order in which they run.
@@ -244,8 +244,8 @@ __device__ __forceinline__ void queries_block(const GradArgs &a, uint32_t wg, ui
 // kernels, without and with it, in us: 2048 tokens, 32 heads of 64 and 8 key heads (136
 // workgroups) 228 and 146; 8192 (520) 1207 and 1015; 16 x 512, 16 heads (1280) 70 and 78; in
 // heads of 128: 2048 (136) 314 and 191; 2 x 4096, 8 heads (528) 288 and 305; 16 x 512 (1280)
-// 119 and 179.  There waves hold 61 % of their places: the longest
-// sequence's first keys, with 160 tiles of queries, are what is waited for.
+// 119 and 179.  The 13 sequences' waves hold 61 % of their places: the longest
+// one's first keys, with 160 tiles of queries, are what is waited for.
 //
 // Heads above 64 leave no registers for both operands beside both sums: values stay in LDS.
 template <int DP, int GROUPS, int PARTS>
